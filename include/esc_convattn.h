@@ -302,6 +302,135 @@ esc_status esc_convattn_backward(const void *x, const void *grad_out, esc_dtype 
                                  int accumulate, void *workspace, size_t workspace_bytes, void *stream);
 
 /*
+ * Self-attention over windows of a feature map with a learned relative position bias (the attention of the ESC block in front of
+ * its ConvAttn modules, Sec. 3 and Eq. 3 line 2).  The map is cut into windows of win_h x win_w pixels from its top left corner; windows at
+ * the right and bottom edges are as large as what is left of the map.  In each window, image n and head h, over its pixels i, j:
+ *
+ *   s[i,j] = scale * sum_c q[h,c,i] k[h',c,j] + bias[h, by(y_j - y_i), bx(x_j - x_i)]
+ *   out[h,c,i] = sum_j softmax_j(s[i,.])[j] v[h',c,j]           h' = h / (heads / kv_heads)
+ *
+ *   q            [N, heads * head_dim, H, W] in the storage type: contiguous planes, *_stride ELEMENTS from image to image (ignored where
+ *   k, v         [N, kv_heads * head_dim, H, W]  N is 1), so that all three may be parts of one tensor [N, 3 C, H, W], or the same tensor
+ *   bias         device, fp32 [heads, buckets down, buckets across], or NULL (no bias).  The bucket of an offset o along an axis is
+ *                  n_edges == 0: o + win - 1, each offset its own (2 win - 1 buckets);
+ *                  n_edges  > 0: n_edges + sign(o) * (how many edges are <= |o|), 2 n_edges + 1 buckets, the edges (HOST memory, read
+ *                                during the call) positive and increasing - one by one for near pixels, wider and wider for
+ *                                far ones, as the caller likes.  A bias of -infinity hides what falls into its bucket.
+ *   mask         device, one byte a pixel [N, H, W], or NULL: pixels whose byte is 0 do not exist, as in images padded to a common size:
+ *                they are nobody's key, their own out is 0, and whatever q, k, v hold there (NaN too) is not used
+ *   out          [N, heads * head_dim, H, W], contiguous, rounded once
+ *   saved        what the backward pass needs (the rows' log-sum, and with bf16 storage what rounding took from out), or NULL:
+ *                esc_window_attention_saved_bytes, 256-byte aligned
+ * A pixel with no key left (a bias of -infinity everywhere) has out = 0.  Scores, maxima and sums are fp32.  bf16 storage: products of the stored
+ * values on the matrix cores, the exponentials rounded to bf16 as operands of the second product (their sum is of the unrounded
+ * ones).  fp32 storage: values and exponentials as three bf16 terms each (exact), six products of terms (what is left out lies
+ * below 2^-24 of a product: fp32 accuracy); a value of q, k or v that is not finite makes NaN of what its products reach.
+ * Limits: head_dim <= 64; (2 h - 1)(2 w - 1) <= 16384 offsets, h and w the window's sides or the map's where those are smaller (64 x 64 pixels, or
+ * 1 x 8192); win_h, win_w <= 8192; heads <= 1024; n_edges <= ESC_WINDOW_MAX_EDGES; 2^-20 <= scale <= 64.
+ * One launch; no workspace.  Biases over scale beyond 2^120 count as 2^120.
+ */
+#define ESC_WINDOW_MAX_EDGES 32
+typedef struct esc_window_attn {
+    int N, H, W, heads, kv_heads, head_dim, win_h, win_w;
+    float scale;
+    long q_stride, k_stride, v_stride;
+    const float *bias;
+    int n_edges;
+    const int *edges;
+    const unsigned char *mask;
+} esc_window_attn;
+
+size_t esc_window_attention_saved_bytes(const esc_window_attn *a, esc_dtype dt); /* pointers and strides in *a are ignored; 0 on bad sizes */
+esc_status esc_window_attention_forward(const void *q, const void *k, const void *v, esc_dtype dt, const esc_window_attn *a, void *out,
+                                        void *saved, size_t saved_bytes, void *stream);
+
+/*
+ * Backward of esc_window_attention_forward: given grad_out [N, heads * head_dim, H, W] (contiguous, storage type), the forward's
+ * arguments, its out and its saved,
+ *   g->q, g->k, g->v  in the storage type, shaped like q, k, v with strides of their own (written, every element; those of key and value
+ *                     heads that several heads share are the sums over them; 0 at masked pixels)
+ *   g->bias           fp32, shaped like bias, summed over images, windows and all pairs of a bucket, or NULL;
+ *                     accumulate != 0 adds it to what the buffer holds
+ * The scores are formed again.  Sums are fp32, each in a fixed order: equal calls give equal bits.  With bf16 storage the probabilities
+ * and their gradients are rounded to bf16 as operands of the products that give q's, k's and v's gradients, not in the
+ * bias' gradient.  The workspace (esc_window_attention_backward_workspace_bytes, 256-byte aligned, either storage type) is plain scratch: it needs no
+ * preparation and its contents are undefined after the call.  What is written may not overlap anything else.  Two launches, with
+ * the bias' gradient four.
+ */
+typedef struct esc_window_grads {
+    void *q, *k, *v;
+    long q_stride, k_stride, v_stride;
+    float *bias;
+} esc_window_grads;
+size_t esc_window_attention_backward_workspace_bytes(const esc_window_attn *a); /* as above */
+esc_status esc_window_attention_backward(const void *q, const void *k, const void *v, esc_dtype dt, const esc_window_attn *a, const void *out,
+                                         const void *grad_out, const void *saved, size_t saved_bytes, const esc_window_grads *g,
+                                         int accumulate, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * The AdamW step over all of a network's parameter tensors, in one launch.  For every element, in fp32, each
+ * operation rounded by itself (t counts steps from 1):
+ *
+ *   g' = grad_scale * grad      m = beta1 m + (1 - beta1) g'      v = beta2 v + (1 - beta2) g'^2
+ *   param = param (1 - lr weight_decay) - lr / (1 - beta1^t) * m / ( sqrt(v) / sqrt(1 - beta2^t) + eps )
+ *
+ * param is fp32, as all weights of this library are; the gradients are fp32 or bf16 (grad_dt, the same for all tensors).
+ *   ESC_ADAMW_F32    m and v are fp32 values.
+ *   ESC_ADAMW_EIGHT  m and v are one byte an element, with one fp32 scale for each block of ESC_ADAMW_BLOCK consecutive
+ *                    elements (the last block of a tensor may be shorter): m's element is e4m3(code) * m_scale,
+ *                    v's is (e4m3(code) * v_scale)^2.  A step reads them, computes as above in fp32 (the new m and v go into
+ *                    param before they are rounded) and writes for x = m and for x = sqrt(v): scale = a / 448 with a the largest
+ *                    finite magnitude in the block, code = x * (448 / a) to the nearest e4m3 value (ties to
+ *                    even); a positive sqrt(v) takes the smallest positive code at least; values that are not finite are held as
+ *                    NaN; a block with a < 2^-100 holds zeros, scale 0.  Zeroed bytes and scales are zeroed states.
+ * Every element stands for itself (a NaN gradient makes one parameter NaN), tensors may have any length and lie
+ * at any address that their element type allows (16-byte steps where all of a tensor's buffers are aligned to that
+ * many elements).  Results do not depend on how many tensors there are or in which order.
+ */
+#define ESC_ADAMW_BLOCK 256
+typedef enum { ESC_ADAMW_F32 = 0, ESC_ADAMW_EIGHT = 1, ESC_ADAMW_STATE_INT_RANGE = 0x7fffffff } esc_adamw_state;
+
+typedef struct esc_adamw_tensor {
+    float *param;
+    const void *grad;          /* in the gradients' type                                       */
+    void *m, *v;               /* n floats, or n bytes                                          */
+    float *m_scale, *v_scale;  /* 8-bit states: ceil(n / ESC_ADAMW_BLOCK) floats; else ignored  */
+    long n;                    /* elements; 0 is allowed and touches nothing                    */
+    float weight_decay;        /* >= 0                                                          */
+} esc_adamw_tensor;
+
+/* What esc_adamw_plan_init has laid out: plain data, kept by the caller and handed to every step as it is. */
+typedef struct esc_adamw_plan {
+    void *memory;
+    size_t bytes;
+    int n;
+    long chunks;
+    esc_adamw_state state;
+    esc_dtype grad_dt;
+} esc_adamw_plan;
+
+typedef struct esc_adamw_hyper {
+    double lr, beta1, beta2, eps; /* 0 <= lr, eps < 1e30; 0 <= beta < 1          */
+    double grad_scale;            /* finite; 1 for gradients as they are         */
+    const float *lr_device;       /* device pointer; where not NULL its value is lr: a captured graph's steps can follow a schedule */
+} esc_adamw_hyper;
+
+/* Device memory a plan takes (256-byte aligned).  0 on bad arguments.  `tensors` is HOST memory. */
+size_t esc_adamw_plan_bytes(const esc_adamw_tensor *tensors, int n, esc_adamw_state state);
+
+/*
+ * Lays the plan out: writes the tensors' addresses and sizes into `memory` (a launch for each 32 tensors, on `stream`) and fills *plan
+ * (host).  `step` is how many steps the states have seen (0 for new ones, which are zeros); the count is kept in `memory` and
+ * grows by one with each esc_adamw_step, replayed ones included.  What a step writes may not overlap anything else that the plan names
+ * (ESC_ERR_ALIAS): a tensor appears once.  The tensors' memory has to stay where it is as long as the plan is used.
+ */
+esc_status esc_adamw_plan_init(const esc_adamw_tensor *tensors, int n, esc_adamw_state state, esc_dtype grad_dt, long step, void *memory,
+                               size_t bytes, esc_adamw_plan *plan, void *stream);
+
+/* One step of every tensor of the plan: one launch, nothing allocated.  Steps of one plan must not overlap each other. */
+esc_status esc_adamw_step(const esc_adamw_plan *plan, const esc_adamw_hyper *hyper, void *stream);
+
+/*
  * For callers that cannot allocate or prepare device memory (code under HIP graph
  * capture, tight serving loops, harnesses that forbid hipMalloc): esc_convattn_forward
  * without the workspace arguments.  The mailboxes and counters live in a scratch array

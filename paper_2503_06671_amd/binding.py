@@ -26,8 +26,12 @@ EXPORTS = ("esc_workspace_bytes", "esc_workspace_init", "esc_workspace_errors", 
            "esc_convattn_forward", "esc_convattn_forward_noalloc", "esc_fused_workspace_bytes",
            "esc_convattn_fused_forward", "esc_dense_workspace_bytes", "esc_convattn_dense_forward",
            "esc_backward_workspace_bytes", "esc_convattn_backward", "esc_convffn_workspace_bytes",
-           "esc_convffn_forward", "esc_residual_step_workspace_bytes", "esc_residual_step_forward", "esc_status_string")
+           "esc_convffn_forward", "esc_residual_step_workspace_bytes", "esc_residual_step_forward", "esc_window_attention_saved_bytes",
+           "esc_window_attention_forward", "esc_window_attention_backward_workspace_bytes", "esc_window_attention_backward",
+           "esc_adamw_plan_bytes", "esc_adamw_plan_init", "esc_adamw_step", "esc_status_string")
 NOALLOC_SCRATCH_BYTES = 1 << 20
+ADAMW_BLOCK = 256  # elements that share a scale in the optimiser's 8-bit states
+ADAMW_STATES = {"f32": 0, "8bit": 1}
 
 
 class EscError(RuntimeError):
@@ -45,6 +49,31 @@ class _GenParams(ctypes.Structure):
 class _GenGrads(ctypes.Structure):
     _fields_ = [("w_down", ctypes.c_void_p), ("b_down", ctypes.c_void_p),
                 ("w_up", ctypes.c_void_p), ("b_up", ctypes.c_void_p)]
+
+
+class _WindowAttn(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int) for n in ("N", "H", "W", "heads", "kv_heads", "head_dim", "win_h", "win_w")] + \
+               [("scale", ctypes.c_float), ("q_stride", ctypes.c_long), ("k_stride", ctypes.c_long), ("v_stride", ctypes.c_long),
+                ("bias", ctypes.c_void_p), ("n_edges", ctypes.c_int), ("edges", ctypes.c_void_p), ("mask", ctypes.c_void_p)]
+
+
+class _WindowGrads(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("q_stride", ctypes.c_long),
+                ("k_stride", ctypes.c_long), ("v_stride", ctypes.c_long), ("bias", ctypes.c_void_p)]
+
+
+class _AdamwTensor(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("param", "grad", "m", "v", "m_scale", "v_scale")] + \
+               [("n", ctypes.c_long), ("weight_decay", ctypes.c_float)]
+
+
+class _AdamwPlan(ctypes.Structure):
+    _fields_ = [("memory", ctypes.c_void_p), ("bytes", ctypes.c_size_t), ("n", ctypes.c_int), ("chunks", ctypes.c_long),
+                ("state", ctypes.c_int), ("grad_dt", ctypes.c_int)]
+
+
+class _AdamwHyper(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_double) for n in ("lr", "beta1", "beta2", "eps", "grad_scale")] + [("lr_device", ctypes.c_void_p)]
 
 
 class _NativeModule:
@@ -113,6 +142,21 @@ def load_library():
         lib.esc_residual_step_forward.argtypes = [vp, ci, ci, ci, ci, ci, ci, vp, vp, vp, vp, vp, vp, ci, vp, vp, ci, cl,
                                                   ctypes.POINTER(_GenParams), vp, vp, vp, vp, sz, vp]
         lib.esc_residual_step_forward.restype = ci
+        wa = ctypes.POINTER(_WindowAttn)
+        lib.esc_window_attention_saved_bytes.argtypes = [wa, ci]
+        lib.esc_window_attention_saved_bytes.restype = sz
+        lib.esc_window_attention_forward.argtypes = [vp, vp, vp, ci, wa, vp, vp, sz, vp]
+        lib.esc_window_attention_forward.restype = ci
+        lib.esc_window_attention_backward_workspace_bytes.argtypes = [wa]
+        lib.esc_window_attention_backward_workspace_bytes.restype = sz
+        lib.esc_window_attention_backward.argtypes = [vp, vp, vp, ci, wa, vp, vp, vp, sz, ctypes.POINTER(_WindowGrads), ci, vp, sz, vp]
+        lib.esc_window_attention_backward.restype = ci
+        lib.esc_adamw_plan_bytes.argtypes = [ctypes.POINTER(_AdamwTensor), ci, ci]
+        lib.esc_adamw_plan_bytes.restype = sz
+        lib.esc_adamw_plan_init.argtypes = [ctypes.POINTER(_AdamwTensor), ci, ci, ci, cl, vp, sz, ctypes.POINTER(_AdamwPlan), vp]
+        lib.esc_adamw_plan_init.restype = ci
+        lib.esc_adamw_step.argtypes = [ctypes.POINTER(_AdamwPlan), ctypes.POINTER(_AdamwHyper), vp]
+        lib.esc_adamw_step.restype = ci
         lib.esc_status_string.argtypes = [ci]
         lib.esc_status_string.restype = ctypes.c_char_p
         _lib = lib
@@ -318,3 +362,132 @@ def convattn_backward(x: torch.Tensor, grad_out: torch.Tensor, Ca: int, lk: torc
     estimator, grad_w_up, grad_b_up (and grad_w_down, grad_b_down when hidden > 0).  `grads` may carry
     buffers to write into (required to make sense of accumulate=True)."""
     return _native.convattn_backward(x, grad_out, Ca, lk, workspace, gen, dk_in, accumulate, grads, stream)
+
+
+def _window_sizes(N, heads, head_dim, H, W, window, kv_heads=None):
+    return _WindowAttn(N=N, H=H, W=W, heads=heads, kv_heads=kv_heads or heads, head_dim=head_dim, win_h=window[0], win_w=window[1])
+
+
+def new_window_attention_saved(N: int, heads: int, head_dim: int, H: int, W: int, dtype: torch.dtype, device="cuda") -> torch.Tensor:
+    """Allocate (with torch) what window_attention_forward keeps for the backward pass."""
+    dt = ESC_F32 if dtype == torch.float32 else ESC_BF16
+    nbytes = int(load_library().esc_window_attention_saved_bytes(_window_sizes(N, heads, head_dim, H, W, (1, 1)), dt))
+    if nbytes == 0:
+        raise ValueError("bad shape for window attention")
+    return torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+
+def new_window_attention_backward_workspace(N: int, heads: int, head_dim: int, H: int, W: int, window, device="cuda") -> torch.Tensor:
+    """Allocate (with torch) the scratch workspace of window_attention_backward (needs no preparation)."""
+    nbytes = int(load_library().esc_window_attention_backward_workspace_bytes(_window_sizes(N, heads, head_dim, H, W, window)))
+    if nbytes == 0:
+        raise ValueError("bad shape for window attention")
+    return torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+
+def window_attention_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, heads: int, window,
+                             bias: Optional[torch.Tensor] = None, edges=None, mask: Optional[torch.Tensor] = None,
+                             scale: Optional[float] = None, kv_heads: Optional[int] = None, out: Optional[torch.Tensor] = None,
+                             saved: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """esc_window_attention_forward: self-attention over windows (height, width) of [N, heads * head_dim, H, W] maps.  q, k and v
+    may be slices of one tensor along the channels; k and v have kv_heads * head_dim channels (kv_heads None: heads).  bias
+    [heads, buckets, buckets] is the learned relative position bias, edges (whole numbers, increasing) its buckets' borders, None a bucket for
+    each offset; mask [N, H, W] (uint8 or bool) tells the pixels that exist; scale None is head_dim ** -0.5.  With `saved`
+    (new_window_attention_saved) the backward pass can follow.  Runs on the tensors' device and that device's current stream."""
+    return _native.window_attention_forward(q, k, v, heads, window, bias, edges, mask, scale, kv_heads, out, saved, stream)
+
+
+def window_attention_backward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor, grad_out: torch.Tensor,
+                              saved: torch.Tensor, heads: int, window, workspace: torch.Tensor,
+                              bias: Optional[torch.Tensor] = None, edges=None, mask: Optional[torch.Tensor] = None,
+                              scale: Optional[float] = None, kv_heads: Optional[int] = None, accumulate: bool = False,
+                              grads: Optional[dict] = None, stream=None) -> dict:
+    """esc_window_attention_backward.  Returns a dict of device tensors: grad_q, grad_k, grad_v and, with a bias, grad_bias.  `grads` may
+    carry buffers to write into (slices of one tensor too); accumulate=True adds the bias' gradient to its buffer."""
+    return _native.window_attention_backward(q, k, v, out, grad_out, saved, heads, window, workspace, bias, edges, mask, scale,
+                                             kv_heads, accumulate, grads, stream)
+
+
+class AdamW:
+    """The AdamW step over many tensors in one launch (esc_adamw_plan_init, esc_adamw_step).
+
+    params: contiguous float32 device tensors; grads: their gradients, all float32 or all bfloat16, contiguous, filled anew by the
+    caller before each step.  states "f32": m and v are float32; "8bit": torch.float8_e4m3fn codes with a float32 scale for each
+    ADAMW_BLOCK elements (m_scale, v_scale; v's codes hold sqrt(v)).  States that are not given start as zeros.  weight_decay is one
+    number or one a tensor, `step` how many steps the states have seen.  The object keeps all tensors alive and works on
+    their memory: they have to stay where they are."""
+
+    def __init__(self, params, grads, states: str = "f32", weight_decay=0.0, step: int = 0, m=None, v=None, m_scale=None,
+                 v_scale=None, stream=None):
+        if states not in ADAMW_STATES:
+            raise ValueError(f"states must be one of {sorted(ADAMW_STATES)}, got {states!r}")
+        params, grads = list(params), list(grads)
+        if not params or len(grads) != len(params):
+            raise ValueError(f"{len(params)} parameters with {len(grads)} gradients")
+        device = params[0].device
+        eight = states == "8bit"
+        state_type = torch.float8_e4m3fn if eight else torch.float32
+        grad_type = grads[0].dtype
+        if grad_type not in (torch.float32, torch.bfloat16):
+            raise TypeError(f"gradients must be float32 or bfloat16, got {grad_type}")
+
+        def checked(name, tensors, dtype, sizes):
+            tensors = list(tensors)
+            if len(tensors) != len(params):
+                raise ValueError(f"{len(tensors)} tensors in {name}, {len(params)} parameters")
+            for t, n in zip(tensors, sizes):
+                if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype != dtype or not t.is_contiguous() or t.device != device:
+                    raise TypeError(f"{name} must be contiguous {dtype} tensors on one device")
+                if t.numel() != n:
+                    raise ValueError(f"a tensor of {name} has {t.numel()} elements, {n} are needed")
+            return tensors
+
+        def state(name, given, dtype, sizes):
+            if given is None:
+                return [torch.zeros(n, dtype=torch.uint8, device=device).view(dtype) if eight and dtype is state_type
+                        else torch.zeros(n, dtype=dtype, device=device) for n in sizes]
+            return checked(name, given, dtype, sizes)
+
+        counts = [p.numel() for p in params]
+        self.params, self.grads = checked("params", params, torch.float32, counts), checked("grads", grads, grad_type, counts)
+        self.m, self.v = state("m", m, state_type, counts), state("v", v, state_type, counts)
+        blocks = [-(-n // ADAMW_BLOCK) for n in counts]
+        if eight:
+            self.m_scale, self.v_scale = state("m_scale", m_scale, torch.float32, blocks), state("v_scale", v_scale, torch.float32, blocks)
+        elif m_scale is not None or v_scale is not None:
+            raise ValueError("scales belong to 8-bit states")
+        decays = [float(w) for w in weight_decay] if isinstance(weight_decay, (list, tuple)) else [float(weight_decay)] * len(params)
+        if len(decays) != len(params):
+            raise ValueError(f"{len(decays)} weight decays, {len(params)} parameters")
+        tensors = (_AdamwTensor * len(params))()
+        for i, c in enumerate(tensors):
+            c.param, c.grad, c.m, c.v = (_ptr(t[i]) for t in (self.params, self.grads, self.m, self.v))
+            if eight:
+                c.m_scale, c.v_scale = _ptr(self.m_scale[i]), _ptr(self.v_scale[i])
+            c.n, c.weight_decay = counts[i], decays[i]
+        lib = load_library()
+        nbytes = int(lib.esc_adamw_plan_bytes(tensors, len(params), ADAMW_STATES[states]))
+        if nbytes == 0:
+            raise ValueError("bad sizes for the optimiser")
+        self.device = device
+        self.memory = torch.empty(nbytes, dtype=torch.uint8, device=device)
+        self.plan = _AdamwPlan()
+        with torch.cuda.device(device):
+            _check(lib.esc_adamw_plan_init(tensors, len(params), ADAMW_STATES[states],
+                                           ESC_F32 if grad_type == torch.float32 else ESC_BF16, step, _ptr(self.memory), nbytes,
+                                           ctypes.byref(self.plan), _stream(stream)))
+
+    def step(self, lr, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, grad_scale: float = 1.0, stream=None) -> None:
+        """One step.  lr is a number, or a float32 device tensor of one element that is read on the device (a captured step then follows
+        what is written there)."""
+        lr_device = None
+        if isinstance(lr, torch.Tensor):
+            if not lr.is_cuda or lr.dtype != torch.float32 or lr.numel() != 1 or lr.device != self.device:
+                raise TypeError("lr must be a number or a float32 tensor of one element on the parameters' device")
+            lr_device, lr = lr.data_ptr(), 0.0
+        _native.adamw_step(ctypes.addressof(self.plan), self.device.index, lr, beta1, beta2, eps, grad_scale, lr_device, stream)
+
+    @property
+    def steps(self) -> int:
+        """Steps the states have seen (waits for the device)."""
+        return int(self.memory[:8].view(torch.int64).item())

@@ -11,6 +11,7 @@
 #include "esc_backward.hpp"
 #include "esc_dense.hpp"
 #include "esc_ffn.hpp"
+#include "esc_host.hpp"
 #include "esc_pointwise.hpp"
 
 namespace esc {
@@ -43,8 +44,6 @@ struct WsLayout {
     int ptiles_x, ptiles;
     size_t ctl_off, pool_off, dk_off, g_off, total;
 };
-
-size_t round_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 
 bool ws_layout(int N, int Ca, int H, int W, WsLayout *l)
 {
@@ -88,13 +87,6 @@ esc_status check_common(const void *x, esc_dtype dt, int N, int C, int H, int W,
     const size_t es = dt == ESC_F32 ? 4 : 2;
     if (((uintptr_t)x % es) != 0) return ESC_ERR_SHAPE;
     return ESC_OK;
-}
-
-// do the byte ranges [a, a + na) and [b, b + nb) share a byte?
-bool overlaps(const void *a, size_t na, const void *b, size_t nb)
-{
-    const uintptr_t ua = (uintptr_t)a, ub = (uintptr_t)b;
-    return na > 0 && nb > 0 && ua < ub + nb && ub < ua + na;
 }
 
 esc_status check_gen(const esc_gen_params *gen, int Ca)

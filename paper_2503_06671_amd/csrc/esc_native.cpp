@@ -11,9 +11,11 @@
 
 #include <ATen/ATen.h>
 #include <ATen/core/LegacyTypeDispatch.h>
+#include <c10/core/DeviceGuard.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <cmath>
 #include <string>
 #include <vector>
 
@@ -538,6 +540,246 @@ PyObject *convattn_backward(PyObject *const *a, Py_ssize_t n)
     return r;
 }
 
+// ---- window attention ----
+
+esc_dtype storage_type(const at::Tensor &t, const char *name)
+{
+    if (t.scalar_type() == at::kFloat) return ESC_F32;
+    if (t.scalar_type() == at::kBFloat16) return ESC_BF16;
+    fail(PyExc_TypeError, std::string(name) + " must be float32 or bfloat16, got " + c10::toString(t.scalar_type()));
+}
+
+int fits_int(int64_t v, const char *name)
+{
+    if (v != (int64_t)(int)v) fail(PyExc_ValueError, std::string(name) + " is too large");
+    return (int)v;
+}
+
+// A [N, planes, H, W] device tensor whose images are contiguous; gives the step from image to image.
+long images(const at::Tensor &t, const char *name)
+{
+    bool ok = t.is_cuda() && t.dim() == 4 && t.layout() == at::kStrided;
+    int64_t want = 1;
+    for (int i = 3; ok && i >= 1; --i) {
+        ok = t.size(i) == 1 || t.stride(i) == want;
+        want *= t.size(i);
+    }
+    if (!ok || (t.dim() == 4 && t.size(0) > 1 && t.stride(0) < want))
+        fail(PyExc_TypeError, std::string(name) + " must be a [N,C,H,W] device tensor with contiguous images");
+    return (long)(t.size(0) > 1 ? t.stride(0) : want);
+}
+
+void same_device(const at::Tensor &t, const at::Tensor &as, const char *name)
+{
+    if (t.device() != as.device()) fail(PyExc_ValueError, std::string(name) + " must be on the device of the other tensors");
+}
+
+struct Attention {
+    esc_window_attn a;
+    esc_dtype dt;
+    std::vector<int> edges;
+    const at::Tensor *q, *k, *v, *bias;
+};
+
+// q, k, v, heads, window, bias, edges, mask, scale, kv_heads
+Attention attention_checked(PyObject *qo, PyObject *ko, PyObject *vo, PyObject *heads, PyObject *window, PyObject *bias, PyObject *edges,
+                            PyObject *mask, PyObject *scale, PyObject *kv_heads)
+{
+    Attention at{};
+    esc_window_attn &a = at.a;
+    at.q = &tensor(qo, "q"), at.k = &tensor(ko, "k"), at.v = &tensor(vo, "v");
+    const at::Tensor &q = *at.q, &k = *at.k, &v = *at.v;
+    a.q_stride = images(q, "q"), a.k_stride = images(k, "k"), a.v_stride = images(v, "v");
+    at.dt = storage_type(q, "q");
+    if (k.scalar_type() != q.scalar_type() || v.scalar_type() != q.scalar_type()) fail(PyExc_TypeError, "q, k and v must have one dtype");
+    same_device(k, q, "k");
+    same_device(v, q, "v");
+    a.N = fits_int(q.size(0), "q"), a.H = fits_int(q.size(2), "q"), a.W = fits_int(q.size(3), "q");
+    a.heads = integer(heads);
+    if (a.heads < 1 || q.size(1) % a.heads != 0) fail(PyExc_ValueError, "q must have heads * head_dim channels, heads = " + std::to_string(a.heads));
+    a.head_dim = fits_int(q.size(1) / a.heads, "q");
+    a.kv_heads = given(kv_heads) ? integer(kv_heads) : a.heads;
+    if (k.sizes() != v.sizes() || k.size(0) != q.size(0) || k.size(2) != q.size(2) || k.size(3) != q.size(3) ||
+        k.size(1) != (int64_t)a.kv_heads * a.head_dim)
+        fail(PyExc_ValueError, "k and v must be [N, kv_heads * head_dim, H, W] with q's N, H, W; kv_heads = " + std::to_string(a.kv_heads) +
+                                   ", head_dim = " + std::to_string(a.head_dim));
+    PyObject *w = PySequence_Fast(window, "window must be (height, width)");
+    if (w == nullptr) throw PyError{};
+    const Py_ssize_t wn = PySequence_Fast_GET_SIZE(w);
+    try {
+        if (wn != 2) fail(PyExc_ValueError, "window must be (height, width)");
+        a.win_h = integer(PySequence_Fast_GET_ITEM(w, 0)), a.win_w = integer(PySequence_Fast_GET_ITEM(w, 1));
+    } catch (...) {
+        Py_DECREF(w);
+        throw;
+    }
+    Py_DECREF(w);
+    if (a.win_h < 1 || a.win_w < 1) fail(PyExc_ValueError, "window must be (height, width), both positive");
+    if (given(edges)) {
+        PyObject *e = PySequence_Fast(edges, "edges must be a sequence of whole numbers");
+        if (e == nullptr) throw PyError{};
+        try {
+            for (Py_ssize_t i = 0; i < PySequence_Fast_GET_SIZE(e); ++i) at.edges.push_back(integer(PySequence_Fast_GET_ITEM(e, i)));
+        } catch (...) {
+            Py_DECREF(e);
+            throw;
+        }
+        Py_DECREF(e);
+        if (at.edges.empty()) fail(PyExc_ValueError, "edges must not be empty (None: a bucket for each offset)");
+    }
+    a.n_edges = fits_int((int64_t)at.edges.size(), "edges");
+    at.bias = dev_f32(bias, "bias");
+    if (at.bias != nullptr) {
+        const int64_t nby = a.n_edges > 0 ? 2 * (int64_t)a.n_edges + 1 : 2 * (int64_t)a.win_h - 1, nbx = a.n_edges > 0 ? nby : 2 * (int64_t)a.win_w - 1;
+        if (at.bias->dim() != 3 || at.bias->size(0) != a.heads || at.bias->size(1) != nby || at.bias->size(2) != nbx)
+            fail(PyExc_ValueError, "bias must be [heads, buckets down, buckets across] = [" + std::to_string(a.heads) + ", " + std::to_string(nby) + ", " +
+                                       std::to_string(nbx) + "]");
+        same_device(*at.bias, q, "bias");
+        a.bias = ptr(at.bias);
+    }
+    if (given(mask)) {
+        const at::Tensor &m = tensor(mask, "mask");
+        if (!m.is_cuda() || !m.is_contiguous() || (m.scalar_type() != at::kByte && m.scalar_type() != at::kBool) || m.dim() != 3 || m.size(0) != q.size(0) ||
+            m.size(1) != q.size(2) || m.size(2) != q.size(3))
+            fail(PyExc_TypeError, "mask must be a contiguous uint8 or bool [N,H,W] device tensor");
+        same_device(m, q, "mask");
+        a.mask = static_cast<const unsigned char *>(m.data_ptr());
+    }
+    if (given(scale)) {
+        const double d = PyFloat_AsDouble(scale);
+        if (d == -1.0 && PyErr_Occurred()) throw PyError{};
+        a.scale = (float)d;
+    } else {
+        a.scale = (float)(1.0 / std::sqrt((double)a.head_dim));
+    }
+    return at;
+}
+
+PyObject *window_attention_forward(PyObject *const *a, Py_ssize_t n)
+{
+    want_args(n, 13);  // q, k, v, heads, window, bias, edges, mask, scale, kv_heads, out, saved, stream
+    Attention at = attention_checked(a[0], a[1], a[2], a[3], a[4], a[5], a[6], a[7], a[8], a[9]);
+    at.a.edges = at.edges.data();
+    const at::Tensor &q = *at.q;
+    const c10::DeviceGuard guard(q.device());
+    at::Tensor out;
+    if (given(a[10])) {
+        out = tensor(a[10], "out");
+        if (!like(out, q))
+            fail(PyExc_TypeError, "out must match q in dtype and shape and be contiguous");
+        same_device(out, q, "out");
+    } else {
+        out = at::empty(q.sizes(), q.options());
+    }
+    Ws saved{nullptr, 0};
+    if (given(a[11])) {
+        saved = workspace(a[11]);
+        same_device(tensor(a[11], "saved"), q, "saved");
+    }
+    void *st = stream_of(a[12]);
+    const void *qp = q.data_ptr(), *kp = at.k->data_ptr(), *vp = at.v->data_ptr();
+    void *op = out.data_ptr();
+    check(unlocked([&] { return esc_window_attention_forward(qp, kp, vp, at.dt, &at.a, op, saved.ptr, saved.bytes, st); }));
+    return result(a[10], out);
+}
+
+PyObject *window_attention_backward(PyObject *const *a, Py_ssize_t n)
+{
+    // q, k, v, out, grad_out, saved, heads, window, workspace, bias, edges, mask, scale, kv_heads, accumulate, grads, stream
+    want_args(n, 17);
+    Attention at = attention_checked(a[0], a[1], a[2], a[6], a[7], a[9], a[10], a[11], a[12], a[13]);
+    at.a.edges = at.edges.data();
+    const at::Tensor &q = *at.q, &out = tensor(a[3], "out"), &go = tensor(a[4], "grad_out");
+    const auto whole = [&](const at::Tensor &t, const char *name) {
+        if (!t.is_cuda() || t.scalar_type() != q.scalar_type() || t.sizes() != q.sizes() || !t.is_contiguous())
+            fail(PyExc_TypeError, std::string(name) + " must match q in dtype and shape and be a contiguous device tensor");
+        same_device(t, q, name);
+    };
+    whole(out, "out");
+    whole(go, "grad_out");
+    const Ws saved = workspace(a[5]), ws = workspace(a[8]);
+    same_device(tensor(a[5], "saved"), q, "saved");
+    same_device(tensor(a[8], "workspace"), q, "workspace");
+    const int acc = PyObject_IsTrue(a[14]);
+    if (acc < 0) throw PyError{};
+    const c10::DeviceGuard guard(q.device());
+    struct Dict {
+        PyObject *d;
+        ~Dict() { Py_XDECREF(d); }
+    } grads{nullptr};
+    const int brought_any = given(a[15]) ? PyObject_IsTrue(a[15]) : 0;
+    if (brought_any < 0) throw PyError{};
+    grads.d = brought_any != 0 ? PyObject_CallFunctionObjArgs((PyObject *)&PyDict_Type, a[15], nullptr) : PyDict_New();
+    if (grads.d == nullptr) throw PyError{};
+    auto put = [&](const char *name, const at::Tensor &t) {
+        PyObject *o = wrap(t);
+        const int rc = o != nullptr ? PyDict_SetItemString(grads.d, name, o) : -1;
+        Py_XDECREF(o);
+        if (rc != 0) throw PyError{};
+    };
+    esc_window_grads g{};
+    auto like_input = [&](const char *name, const at::Tensor &x, void **p, long *stride) {
+        if (PyObject *v = item(grads.d, name)) {
+            const at::Tensor &t = tensor(v, name);
+            if (t.scalar_type() != x.scalar_type() || t.sizes() != x.sizes()) fail(PyExc_TypeError, std::string(name) + " must match its input in dtype and shape");
+            *stride = images(t, name);
+            same_device(t, q, name);
+            *p = t.data_ptr();
+        } else {
+            const at::Tensor t = at::empty(x.sizes(), x.options());
+            put(name, t);
+            *stride = (long)(t.size(1) * t.size(2) * t.size(3));
+            *p = t.data_ptr();
+        }
+    };
+    like_input("grad_q", q, &g.q, &g.q_stride);
+    like_input("grad_k", *at.k, &g.k, &g.k_stride);
+    like_input("grad_v", *at.v, &g.v, &g.v_stride);
+    if (at.bias != nullptr) {
+        if (PyObject *v = item(grads.d, "grad_bias")) {
+            const at::Tensor &t = dev_f32_required(v, "grad_bias");
+            if (t.sizes() != at.bias->sizes()) fail(PyExc_TypeError, "grad_bias must match bias in shape");
+            same_device(t, q, "grad_bias");
+            g.bias = static_cast<float *>(t.data_ptr());
+        } else {
+            const at::Tensor t = acc != 0 ? at::zeros(at.bias->sizes(), at.bias->options()) : at::empty(at.bias->sizes(), at.bias->options());
+            put("grad_bias", t);
+            g.bias = static_cast<float *>(t.data_ptr());
+        }
+    }
+    void *st = stream_of(a[16]);
+    const void *qp = q.data_ptr(), *kp = at.k->data_ptr(), *vp = at.v->data_ptr(), *op = out.data_ptr(), *gop = go.data_ptr();
+    check(unlocked([&] {
+        return esc_window_attention_backward(qp, kp, vp, at.dt, &at.a, op, gop, saved.ptr, saved.bytes, &g, acc, ws.ptr, ws.bytes, st);
+    }));
+    PyObject *r = grads.d;
+    grads.d = nullptr;
+    return r;
+}
+
+// ---- AdamW: one step of a plan (laid out once by binding.AdamW) ----
+
+PyObject *adamw_step(PyObject *const *a, Py_ssize_t n)
+{
+    want_args(n, 9);  // address of the plan, device index, lr, beta1, beta2, eps, grad_scale, address of lr_device, stream
+    auto number = [](PyObject *o) {
+        const double d = PyFloat_AsDouble(o);
+        if (d == -1.0 && PyErr_Occurred()) throw PyError{};
+        return d;
+    };
+    const esc_adamw_plan *plan = static_cast<const esc_adamw_plan *>(PyLong_AsVoidPtr(a[0]));
+    if (plan == nullptr) fail(PyExc_ValueError, "no plan");
+    const c10::DeviceGuard guard(c10::Device(c10::DeviceType::CUDA, (c10::DeviceIndex)integer(a[1])));
+    esc_adamw_hyper h{number(a[2]), number(a[3]), number(a[4]), number(a[5]), number(a[6]), nullptr};
+    if (given(a[7])) {
+        h.lr_device = static_cast<const float *>(PyLong_AsVoidPtr(a[7]));
+        if (h.lr_device == nullptr && PyErr_Occurred()) throw PyError{};
+    }
+    void *st = stream_of(a[8]);
+    check(unlocked([&] { return esc_adamw_step(plan, &h, st); }));
+    Py_RETURN_NONE;
+}
+
 // Runs an entry point and turns what it throws into the Python exception.
 template <PyObject *(*F)(PyObject *const *, Py_ssize_t)>
 PyObject *entry(PyObject *, PyObject *const *args, Py_ssize_t n)
@@ -564,7 +806,8 @@ PyObject *entry(PyObject *, PyObject *const *args, Py_ssize_t n)
 #define ESC_ENTRY(name) {#name, (PyCFunction)(void (*)(void))entry<name>, METH_FASTCALL, nullptr}
 PyMethodDef kMethods[] = {ESC_ENTRY(gen_handle),         ESC_ENTRY(dynkernel_gen),    ESC_ENTRY(convattn_forward),
                           ESC_ENTRY(convattn_fused_forward), ESC_ENTRY(convffn_forward), ESC_ENTRY(residual_step_forward),
-                          ESC_ENTRY(convattn_dense_forward), ESC_ENTRY(convattn_backward), {nullptr, nullptr, 0, nullptr}};
+                          ESC_ENTRY(convattn_dense_forward), ESC_ENTRY(convattn_backward),
+                          ESC_ENTRY(window_attention_forward), ESC_ENTRY(window_attention_backward), ESC_ENTRY(adamw_step), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_native", "Argument handling of the binding over the C ABI.", -1, kMethods,
                        nullptr, nullptr, nullptr, nullptr};
 

@@ -1,0 +1,300 @@
+// Host side of window attention (esc_window_attention_* of include/esc_convattn.h): argument checks, geometry, launches.
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "esc_convattn.h"
+#include "esc_host.hpp"
+#include "esc_window.hpp"
+
+namespace {
+
+using namespace esc;
+
+constexpr size_t kAlign = 256;
+constexpr size_t kLdsPerCu = 160 * 1024;
+
+int dim_padded(int d) { return d <= 16 ? 16 : d <= 32 ? 32 : 64; }
+
+// Words of the table of a block of `waves` wavefronts, whatever window of the map it has.
+int table_words(const WindowParams &p, int waves)
+{
+    const int widths[2] = {p.ww, p.W - (p.gx - 1) * p.ww};
+    int most = 0;
+    for (int w : widths) {
+        const int wp = (w + 3) & ~3, tokens = waves * kWinWaveTokens;
+        const int rows = std::min(p.wh - 1, (tokens - 1 + wp - 1) / wp);
+        most = std::max(most, (p.wh - 1 + rows) * p.tw + 2 * wp - 1);
+    }
+    return most;
+}
+
+// The wavefronts a block has: up to four, as many as the longest window fills, fewer where their tables do not fit; two
+// blocks on a compute unit are worth more than two more wavefronts in one.
+template <typename F>
+bool choose_waves(WindowParams &p, F lds)
+{
+    const long tokens = (long)p.wh * ((p.ww + 3) & ~3);
+    const int want = (int)std::min<long>(kWinMaxWaves, (tokens + kWinWaveTokens - 1) / kWinWaveTokens);
+    for (size_t limit : {kLdsPerCu / 2, kLdsPerCu})
+        for (int waves = want; waves >= 1; --waves) {
+            const int len = table_words(p, waves);
+            if (lds(len, waves) <= limit) {
+                p.waves = waves, p.len = len;
+                p.blocks = (int)((tokens + waves * kWinWaveTokens - 1) / (waves * kWinWaveTokens));
+                return true;
+            }
+        }
+    return false;
+}
+
+bool set_units(WindowParams &p, int heads)
+{
+    const __int128 units = (__int128)p.N * p.gy * p.gx * heads * p.blocks;
+    if (units > 0x7fffff00) return false;
+    p.units = (int)units;
+    return true;
+}
+
+esc_status shape(const esc_window_attn *a, WindowParams *p)
+{
+    *p = WindowParams{};
+    if (a->N < 1 || a->H < 1 || a->W < 1 || a->heads < 1 || a->kv_heads < 1 || a->head_dim < 1 || a->win_h < 1 || a->win_w < 1) return ESC_ERR_SHAPE;
+    if (a->heads % a->kv_heads != 0) return ESC_ERR_SHAPE;
+    if (a->head_dim > kWinMaxDim || a->heads > 1024 || a->win_h > 8192 || a->win_w > 8192) return ESC_ERR_UNSUPPORTED;
+    if ((size_t)a->H * (size_t)a->W >= ((size_t)1 << 31)) return ESC_ERR_UNSUPPORTED;
+    if (a->n_edges < 0) return ESC_ERR_SHAPE;
+    if (a->n_edges > kWinMaxEdges) return ESC_ERR_UNSUPPORTED;
+    p->N = a->N, p->H = a->H, p->W = a->W, p->heads = a->heads, p->kv_heads = a->kv_heads, p->d = a->head_dim;
+    p->win_h = a->win_h, p->win_w = a->win_w;
+    p->wh = std::min(a->win_h, a->H), p->ww = std::min(a->win_w, a->W);
+    p->gy = (a->H + p->wh - 1) / p->wh, p->gx = (a->W + p->ww - 1) / p->ww;
+    p->th = 2 * p->wh - 1, p->tw = 2 * p->ww - 1;
+    if ((long)p->th * p->tw > kWinMaxOffsets) return ESC_ERR_UNSUPPORTED;
+    p->n_edges = a->n_edges;
+    p->nby = a->n_edges > 0 ? 2 * a->n_edges + 1 : 2 * a->win_h - 1;
+    p->nbx = a->n_edges > 0 ? 2 * a->n_edges + 1 : 2 * a->win_w - 1;
+    return ESC_OK;
+}
+
+size_t table_bytes(const WindowParams &p) { return (size_t)p.heads * p.nby * p.nbx * 4; }
+
+bool plan_forward(WindowParams &p, bool f32)
+{
+    const int dp = dim_padded(p.d);
+    return choose_waves(p, [&](int len, int) { return window_forward_lds(f32, dp, len); }) && set_units(p, p.heads);
+}
+bool plan_dq(WindowParams &p, bool f32)
+{
+    const int dp = dim_padded(p.d);
+    // (the same plan with and without the table's gradient)
+    if (!choose_waves(p, [&](int len, int waves) { return window_dq_lds(f32, dp, len, waves, true); }) || !set_units(p, p.heads)) return false;
+    p.splits = std::max(1, std::min(32, p.units / p.heads));
+    return true;
+}
+bool plan_dkv(WindowParams &p, bool f32)
+{
+    const int dp = dim_padded(p.d);
+    return choose_waves(p, [&](int len, int) { return window_dkv_lds(f32, dp, len); }) && set_units(p, p.kv_heads);
+}
+
+struct Scratch {
+    size_t delta, part, part2, total;
+};
+Scratch scratch(const WindowParams &p)  // (of plan_dq)
+{
+    Scratch s;
+    s.delta = 0;
+    s.part = round_up((size_t)p.N * p.heads * p.H * p.W * 4, kAlign);
+    s.part2 = s.part + round_up((size_t)p.units * p.len * 4, kAlign);
+    s.total = s.part2 + round_up((size_t)p.splits * p.heads * p.th * p.tw * 4, kAlign);
+    return s;
+}
+
+// two planes of row values, and what rounding took from out
+size_t rows_bytes(const WindowParams &p) { return round_up((size_t)p.N * p.heads * p.H * p.W * 8, kAlign); }
+size_t saved_size(const WindowParams &p, esc_dtype dt)
+{
+    return rows_bytes(p) + (dt == ESC_BF16 ? round_up((size_t)p.N * p.heads * p.d * p.H * p.W * 2, kAlign) : 0);
+}
+
+// Planes of N images, `stride` bytes from image to image.
+struct Images {
+    const void *at;
+    size_t stride, bytes;  // bytes: one image's
+    int N;
+    size_t extent() const { return (size_t)(N - 1) * stride + bytes; }
+};
+
+bool meet(const Images &a, const Images &b)
+{
+    if (!overlaps(a.at, a.extent(), b.at, b.extent())) return false;
+    if (a.stride != b.stride || a.N == 1 || b.N == 1) return true;
+    // the same step from image to image: parts of one tensor may lie between each other
+    const uintptr_t ua = (uintptr_t)a.at, ub = (uintptr_t)b.at;
+    const size_t s = a.stride, from = ub >= ua ? (ub - ua) % s : (s - (ua - ub) % s) % s;
+    return from < a.bytes || from + b.bytes > s;
+}
+bool meets(const Images &a, const void *b, size_t bytes) { return b != nullptr && overlaps(a.at, a.extent(), b, bytes); }
+
+// Checks what both directions take, and fills in the parameters.
+esc_status common(const void *q, const void *k, const void *v, esc_dtype dt, const esc_window_attn *a, WindowParams *p, Images (&in)[3])
+{
+    if (a == nullptr) return ESC_ERR_NULL;
+    if (dt != ESC_F32 && dt != ESC_BF16) return ESC_ERR_DTYPE;
+    const esc_status st = shape(a, p);
+    if (st != ESC_OK) return st;
+    if (q == nullptr || k == nullptr || v == nullptr) return ESC_ERR_NULL;
+    if (a->n_edges > 0) {
+        if (a->edges == nullptr) return ESC_ERR_NULL;
+        for (int i = 0; i < a->n_edges; ++i) {
+            if (a->edges[i] < 1 || (i > 0 && a->edges[i] <= a->edges[i - 1])) return ESC_ERR_SHAPE;
+            p->edges[i] = a->edges[i];
+        }
+    }
+    if (!isfinite(a->scale) || !(a->scale > 0.f)) return ESC_ERR_SHAPE;
+    if (a->scale < 0x1p-20f || a->scale > 64.f) return ESC_ERR_UNSUPPORTED;
+    const size_t es = dt == ESC_F32 ? 4 : 2, plane = (size_t)p->H * p->W;
+    const void *const ptr[3] = {q, k, v};
+    const long stride[3] = {a->q_stride, a->k_stride, a->v_stride};
+    for (int i = 0; i < 3; ++i) {
+        const size_t one = (size_t)(i == 0 ? p->heads : p->kv_heads) * p->d * plane;
+        if ((uintptr_t)ptr[i] % es != 0) return ESC_ERR_SHAPE;
+        if (p->N > 1 && (stride[i] < 0 || (size_t)stride[i] < one || (size_t)stride[i] > ((size_t)1 << 46))) return ESC_ERR_SHAPE;
+        in[i] = Images{ptr[i], p->N > 1 ? (size_t)stride[i] * es : one * es, one * es, p->N};
+    }
+    if ((uintptr_t)a->bias % 4 != 0) return ESC_ERR_SHAPE;
+    p->q = q, p->k = k, p->v = v;
+    p->qs = (long)(in[0].stride / es), p->ks = (long)(in[1].stride / es), p->vs = (long)(in[2].stride / es);
+    p->bias = a->bias, p->mask = a->mask;
+    p->scale = a->scale, p->inv_scale = 1.f / a->scale, p->log2_scale = (float)((double)a->scale * 1.4426950408889634);
+    return ESC_OK;
+}
+
+// Four pixels of a row at a time: rows, windows, images and bases at multiples of four elements.
+bool by_fours(const WindowParams &p, const void *base, long stride, size_t es)
+{
+    return p.W % 4 == 0 && (p.ww % 4 == 0 || p.gx == 1) && stride % 4 == 0 && (uintptr_t)base % (4 * es) == 0;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t esc_window_attention_saved_bytes(const esc_window_attn *a, esc_dtype dt)
+{
+    WindowParams p;
+    if (a == nullptr || (dt != ESC_F32 && dt != ESC_BF16) || shape(a, &p) != ESC_OK) return 0;
+    return saved_size(p, dt);
+}
+
+size_t esc_window_attention_backward_workspace_bytes(const esc_window_attn *a)
+{
+    WindowParams p;
+    size_t most = 0;
+    for (bool f32 : {false, true}) {
+        if (a == nullptr || shape(a, &p) != ESC_OK || !plan_dq(p, f32)) return 0;
+        most = std::max(most, scratch(p).total);
+    }
+    return most;
+}
+
+esc_status esc_window_attention_forward(const void *q, const void *k, const void *v, esc_dtype dt, const esc_window_attn *a, void *out, void *saved,
+                                        size_t saved_bytes, void *stream)
+{
+    WindowParams p;
+    Images in[3];
+    const esc_status st = common(q, k, v, dt, a, &p, in);
+    if (st != ESC_OK) return st;
+    if (out == nullptr) return ESC_ERR_NULL;
+    const size_t es = dt == ESC_F32 ? 4 : 2;
+    if ((uintptr_t)out % es != 0) return ESC_ERR_SHAPE;
+    if (saved != nullptr && ((uintptr_t)saved % kAlign != 0 || saved_bytes < saved_size(p, dt))) return ESC_ERR_WORKSPACE;
+    const Images o{out, in[0].bytes, in[0].bytes, p.N};
+    const size_t mask_bytes = (size_t)p.N * p.H * p.W, sv = saved_size(p, dt);
+    for (const Images &x : in)
+        if (meet(o, x) || meets(x, saved, sv)) return ESC_ERR_ALIAS;
+    if (meets(o, p.mask, mask_bytes) || meets(o, p.bias, table_bytes(p)) || meets(o, saved, sv)) return ESC_ERR_ALIAS;
+    if (saved != nullptr && ((p.mask != nullptr && overlaps(saved, sv, p.mask, mask_bytes)) || (p.bias != nullptr && overlaps(saved, sv, p.bias, table_bytes(p)))))
+        return ESC_ERR_ALIAS;
+    p.out = out;
+    if (saved != nullptr) {
+        p.top = static_cast<float *>(saved);
+        p.log_sum = p.top + (size_t)p.N * p.heads * p.H * p.W;
+        p.rest = dt == ESC_BF16 ? static_cast<char *>(saved) + rows_bytes(p) : nullptr;
+    }
+    p.vec = by_fours(p, k, p.ks, es) && by_fours(p, v, p.vs, es);
+    if (!plan_forward(p, dt == ESC_F32)) return ESC_ERR_UNSUPPORTED;
+    return launch_window_forward(p, dt == ESC_F32, dim_padded(p.d), static_cast<hipStream_t>(stream)) == hipSuccess ? ESC_OK : ESC_ERR_HIP;
+}
+
+esc_status esc_window_attention_backward(const void *q, const void *k, const void *v, esc_dtype dt, const esc_window_attn *a, const void *out,
+                                         const void *grad_out, const void *saved, size_t saved_bytes, const esc_window_grads *g, int accumulate,
+                                         void *workspace, size_t workspace_bytes, void *stream)
+{
+    WindowParams p;
+    Images in[3];
+    const esc_status st = common(q, k, v, dt, a, &p, in);
+    if (st != ESC_OK) return st;
+    if (out == nullptr || grad_out == nullptr || saved == nullptr || g == nullptr || g->q == nullptr || g->k == nullptr || g->v == nullptr) return ESC_ERR_NULL;
+    if (g->bias != nullptr && p.bias == nullptr) return ESC_ERR_NULL;
+    const bool f32 = dt == ESC_F32;
+    const size_t es = f32 ? 4 : 2;
+    if ((uintptr_t)out % es != 0 || (uintptr_t)grad_out % es != 0 || (uintptr_t)g->bias % 4 != 0) return ESC_ERR_SHAPE;
+    const size_t sv = saved_size(p, dt), mask_bytes = (size_t)p.N * p.H * p.W;
+    if ((uintptr_t)saved % kAlign != 0 || saved_bytes < sv) return ESC_ERR_WORKSPACE;
+    void *const gp[3] = {g->q, g->k, g->v};
+    const long gstride[3] = {g->q_stride, g->k_stride, g->v_stride};
+    Images written[3];
+    for (int i = 0; i < 3; ++i) {
+        if ((uintptr_t)gp[i] % es != 0) return ESC_ERR_SHAPE;
+        if (p.N > 1 && (gstride[i] < 0 || (size_t)gstride[i] < in[i].bytes / es || (size_t)gstride[i] > ((size_t)1 << 46))) return ESC_ERR_SHAPE;
+        written[i] = Images{gp[i], p.N > 1 ? (size_t)gstride[i] * es : in[i].bytes, in[i].bytes, p.N};
+    }
+    WindowParams pq = p, pk = p;
+    if (!plan_dq(pq, f32) || !plan_dkv(pk, f32)) return ESC_ERR_UNSUPPORTED;
+    const Scratch sc = scratch(pq);
+    if (workspace == nullptr || (uintptr_t)workspace % kAlign != 0 || workspace_bytes < sc.total) return ESC_ERR_WORKSPACE;
+    const Images o{out, in[0].bytes, in[0].bytes, p.N}, go{grad_out, in[0].bytes, in[0].bytes, p.N};
+    const size_t tb = table_bytes(p);
+    for (int i = 0; i < 3; ++i) {
+        for (const Images &x : in)
+            if (meet(written[i], x)) return ESC_ERR_ALIAS;
+        if (meet(written[i], o) || meet(written[i], go) || meets(written[i], saved, sv) || meets(written[i], workspace, sc.total) ||
+            meets(written[i], p.mask, mask_bytes) || meets(written[i], p.bias, tb) || meets(written[i], g->bias, tb) ||
+            meet(written[i], written[(i + 1) % 3]) || meets(in[i], workspace, sc.total) || meets(in[i], g->bias, tb))
+            return ESC_ERR_ALIAS;
+    }
+    const auto apart = [&](const void *b, size_t n) {  // from what lies in one piece and is read
+        return !(meets(o, b, n) || meets(go, b, n) || overlaps(saved, sv, b, n) || (p.mask != nullptr && overlaps(p.mask, mask_bytes, b, n)) ||
+                 (p.bias != nullptr && overlaps(p.bias, tb, b, n)));
+    };
+    if (!apart(workspace, sc.total)) return ESC_ERR_ALIAS;
+    if (g->bias != nullptr && (!apart(g->bias, tb) || overlaps(workspace, sc.total, g->bias, tb))) return ESC_ERR_ALIAS;
+
+    char *ws = static_cast<char *>(workspace);
+    for (WindowParams *x : {&pq, &pk}) {
+        x->out_in = out, x->go = grad_out;
+        x->top = static_cast<float *>(const_cast<void *>(saved));
+        x->log_sum = x->top + (size_t)p.N * p.heads * p.H * p.W;
+        x->rest = f32 ? nullptr : static_cast<char *>(const_cast<void *>(saved)) + rows_bytes(p);
+        x->gq = g->q, x->gk = g->k, x->gv = g->v;
+        x->gqs = (long)(written[0].stride / es), x->gks = (long)(written[1].stride / es), x->gvs = (long)(written[2].stride / es);
+        x->grad_bias = g->bias;
+        x->accumulate = accumulate;
+        x->delta = reinterpret_cast<float *>(ws + sc.delta);
+        x->part = reinterpret_cast<float *>(ws + sc.part);
+        x->part2 = reinterpret_cast<float *>(ws + sc.part2);
+    }
+    pq.vec = by_fours(p, k, p.ks, es) && by_fours(p, v, p.vs, es);
+    pk.vec = by_fours(p, q, p.qs, es) && by_fours(p, grad_out, (long)(in[0].bytes / es), es);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    const int dp = dim_padded(p.d);
+    if (launch_window_dq(pq, f32, dp, s) != hipSuccess || launch_window_dkv(pk, f32, dp, s) != hipSuccess) return ESC_ERR_HIP;
+    if (g->bias != nullptr && launch_window_bias_grad(pq, s) != hipSuccess) return ESC_ERR_HIP;
+    return ESC_OK;
+}
+
+}  // extern "C"
