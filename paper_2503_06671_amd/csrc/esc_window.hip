@@ -15,38 +15,49 @@ using namespace esc;
 
 constexpr size_t kAlign = 256;
 constexpr size_t kLdsPerCu = 160 * 1024;
+constexpr long kCus = 256, kSimds = 4 * kCus;
 
 int dim_padded(int d) { return d <= 16 ? 16 : d <= 32 ? 32 : 64; }
 
-// Words of the table of a block of `waves` wavefronts, whatever window of the map it has.
-int table_words(const WindowParams &p, int waves)
+// How far the offsets' numbers of `tokens` consecutive tokens lie apart at most, in rows of wp tokens.
+int span(const WindowParams &p, int wp, long tokens)
 {
-    const int widths[2] = {p.ww, p.W - (p.gx - 1) * p.ww};
-    int most = 0;
-    for (int w : widths) {
-        const int wp = (w + 3) & ~3, tokens = waves * kWinWaveTokens;
-        const int rows = std::min(p.wh - 1, (tokens - 1 + wp - 1) / wp);
-        most = std::max(most, (p.wh - 1 + rows) * p.tw + 2 * wp - 1);
-    }
-    return most;
+    const long rows = std::min<long>(p.wh - 1, (tokens - 1 + wp - 1) / wp);
+    if (p.tw < wp) return (int)(rows * p.tw) + wp - 1;
+    return (int)std::min<long>(tokens - 1 + rows * (p.tw - wp), (long)rows * p.tw + wp - 1);
 }
 
-// The wavefronts a block has: up to four, as many as the longest window fills, fewer where their tables do not fit; two
-// blocks on a compute unit are worth more than two more wavefronts in one.
+// The most over the windows' widths (the last one of a row may be narrower) of f(row length).
 template <typename F>
-bool choose_waves(WindowParams &p, F lds)
+int widest(const WindowParams &p, F f)
 {
-    const long tokens = (long)p.wh * ((p.ww + 3) & ~3);
-    const int want = (int)std::min<long>(kWinMaxWaves, (tokens + kWinWaveTokens - 1) / kWinWaveTokens);
+    return std::max(f((p.ww + 3) & ~3), f((p.W - (p.gx - 1) * p.ww + 3) & ~3));
+}
+
+// Words of the table of a block that has `tokens` tokens: their offsets to all tokens of any window of the map.
+int table_words(const WindowParams &p, long tokens)
+{
+    return widest(p, [&](int wp) { return (p.wh - 1) * p.tw + wp - 1 + span(p, wp, tokens) + 1; });
+}
+
+// The backward's wavefronts: as many as leave a block for each compute unit, up to eight; fewer, and one staging buffer instead of two, where LDS
+// does not hold them.  Two blocks on a compute unit are worth more than wavefronts in one.
+template <typename F>
+bool choose_waves(WindowParams &p, int tiles, int heads, F lds)
+{
+    const long tokens = (long)p.wh * ((p.ww + 3) & ~3), windows = (long)p.N * p.gy * p.gx * heads;
+    p.tiles = tiles;
+    const long each = 32 * p.tiles, all = (tokens + each - 1) / each;
+    const int want = (int)std::max<long>(1, std::min({(long)kWinMaxWaves, all, all * windows / kCus}));
     for (size_t limit : {kLdsPerCu / 2, kLdsPerCu})
-        for (int waves = want; waves >= 1; --waves) {
-            const int len = table_words(p, waves);
-            if (lds(len, waves) <= limit) {
-                p.waves = waves, p.len = len;
-                p.blocks = (int)((tokens + waves * kWinWaveTokens - 1) / (waves * kWinWaveTokens));
-                return true;
+        for (int buffers : {2, 1})
+            for (int waves = want; waves >= (limit == kLdsPerCu ? 1 : std::min(want, 4)); --waves) {
+                p.waves = waves, p.buffers = buffers, p.len = table_words(p, waves * each);
+                if (lds(p) <= limit) {
+                    p.blocks = (int)((all + waves - 1) / waves);
+                    return true;
+                }
             }
-        }
     return false;
 }
 
@@ -81,23 +92,50 @@ esc_status shape(const esc_window_attn *a, WindowParams *p)
 
 size_t table_bytes(const WindowParams &p) { return (size_t)p.heads * p.nby * p.nbx * 4; }
 
+// The forward's wavefronts.  A wavefront with two tiles of queries reads keys and values half as often (and is what a chip full of work takes);
+// where that would leave fewer than two wavefronts a SIMD, it takes one.  Where even those are fewer than one a SIMD, up to four
+// wavefronts share a tile's keys.  Blocks are as large as leaves one for each compute unit: they stage a window's keys and values once for all their
+// queries.
 bool plan_forward(WindowParams &p, bool f32)
 {
     const int dp = dim_padded(p.d);
-    return choose_waves(p, [&](int len, int) { return window_forward_lds(f32, dp, len); }) && set_units(p, p.heads);
+    const long tokens = (long)p.wh * ((p.ww + 3) & ~3), each = (tokens + 31) / 32, windows = (long)p.N * p.gy * p.gx * p.heads;
+    const long all = each * windows;
+    p.tiles = !(f32 && dp == 64) && all >= 2 * 2 * kSimds && each > 1 ? 2 : 1;
+    const long waves = (each + p.tiles - 1) / p.tiles;
+    p.ksplit = 1;
+    while (p.tiles == 1 && p.ksplit < 4 && waves * windows * p.ksplit < 2 * kSimds && tokens >= 128 * p.ksplit) p.ksplit *= 2;
+    long queries = std::min<long>(kWinMaxWaves / p.ksplit, waves);
+    queries = std::max<long>(1, std::min(queries, waves * windows / kCus));
+    for (; queries >= 1; --queries) {
+        p.waves = (int)queries * p.ksplit;
+        p.len = table_words(p, (int)queries * p.tiles * 32);
+        if (window_forward_lds(f32, dp, p.len, p.ksplit > 1 ? p.waves : 0) <= kLdsPerCu) {
+            p.blocks = (int)((waves + queries - 1) / queries);
+            return set_units(p, p.heads);
+        }
+    }
+    return false;
 }
 bool plan_dq(WindowParams &p, bool f32)
 {
-    const int dp = dim_padded(p.d);
+    const int dp = dim_padded(p.d), tiles = window_query_tiles(f32, dp);
+    const int reach = widest(p, [&](int wp) { return span(p, wp, 32) + span(p, wp, 32 * tiles) + 1; });
+    for (p.ring = 64; p.ring < reach;) p.ring *= 2;
+    p.part_len = table_words(p, 32 * tiles);
     // (the same plan with and without the table's gradient)
-    if (!choose_waves(p, [&](int len, int waves) { return window_dq_lds(f32, dp, len, waves, true); }) || !set_units(p, p.heads)) return false;
-    p.splits = std::max(1, std::min(32, p.units / p.heads));
+    float *const grad = p.grad_bias;
+    p.grad_bias = reinterpret_cast<float *>(16);
+    const bool fits = choose_waves(p, tiles, p.heads, [&](const WindowParams &x) { return window_dq_lds(x, f32, dp); });
+    p.grad_bias = grad;
+    if (!fits || !set_units(p, p.heads)) return false;
+    p.splits = (int)std::min<long>(32, (long)p.N * p.gy * p.gx);
     return true;
 }
 bool plan_dkv(WindowParams &p, bool f32)
 {
     const int dp = dim_padded(p.d);
-    return choose_waves(p, [&](int len, int) { return window_dkv_lds(f32, dp, len); }) && set_units(p, p.kv_heads);
+    return choose_waves(p, 1, p.kv_heads, [&](const WindowParams &x) { return window_dkv_lds(x, f32, dp); }) && set_units(p, p.kv_heads);
 }
 
 struct Scratch {
@@ -108,7 +146,7 @@ Scratch scratch(const WindowParams &p)  // (of plan_dq)
     Scratch s;
     s.delta = 0;
     s.part = round_up((size_t)p.N * p.heads * p.H * p.W * 4, kAlign);
-    s.part2 = s.part + round_up((size_t)p.units * p.len * 4, kAlign);
+    s.part2 = s.part + round_up((size_t)p.units * p.waves * p.part_len * 4, kAlign);
     s.total = s.part2 + round_up((size_t)p.splits * p.heads * p.th * p.tw * 4, kAlign);
     return s;
 }

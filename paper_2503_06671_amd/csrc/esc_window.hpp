@@ -27,8 +27,7 @@ constexpr float kLargeShift = 0x1p20f;
 constexpr int kWinMaxEdges = 32;
 constexpr int kWinMaxDim = 64;
 constexpr int kWinMaxOffsets = 16384;
-constexpr int kWinMaxWaves = 4;
-constexpr int kWinWaveTokens = 64;  // queries (keys in the gradient of keys and values) of a wavefront
+constexpr int kWinMaxWaves = 8;
 
 struct WindowParams {
     const void *q, *k, *v;
@@ -53,14 +52,17 @@ struct WindowParams {
     int nby, nbx, n_edges;
     int edges[kWinMaxEdges];
     int blocks, units, waves, len;       // blocks a window and head, all blocks, wavefronts a block, words of a block's table
+    int tiles, ksplit;                   // tiles of 32 tokens of a wavefront; forward: wavefronts that share a tile's keys
+    int buffers, ring, part_len;         // backward: staging buffers; words of a wavefront's ring (a power of two) and of its part
     int vec;                             // four pixels at a time
     int splits, accumulate;
     float scale, inv_scale, log2_scale;  // scale * log2(e) last
 };
 
-size_t window_forward_lds(bool f32, int dp, int len);
-size_t window_dq_lds(bool f32, int dp, int len, int waves, bool bias_grad);
-size_t window_dkv_lds(bool f32, int dp, int len);
+size_t window_forward_lds(bool f32, int dp, int len, int joined);  // joined: wavefronts whose sums are joined, or 0
+int window_query_tiles(bool f32, int dp);
+size_t window_dq_lds(const WindowParams &p, bool f32, int dp);  // (buffers, waves, ring, len and grad_bias set)
+size_t window_dkv_lds(const WindowParams &p, bool f32, int dp);
 hipError_t launch_window_forward(const WindowParams &p, bool f32, int dp, hipStream_t s);
 hipError_t launch_window_dq(const WindowParams &p, bool f32, int dp, hipStream_t s);
 hipError_t launch_window_dkv(const WindowParams &p, bool f32, int dp, hipStream_t s);
@@ -84,15 +86,21 @@ struct WinGeom {
     static constexpr int TK = F32 && DP == 64 ? 32 : 64;
     static constexpr int KS = DP / 16;                 // matrix instructions a score takes (of each pair of terms)
     static constexpr int DT = DP <= 32 ? 1 : 2;        // blocks of 32 channels of an output
+#ifndef DQT
+#define DQT 2
+#endif
+    static constexpr int QUERY_TILES = F32 || DP == 64 ? 1 : DQT;  // backward: tiles of 32 own queries of a wavefront (two where the registers hold them); its keys: one
     // rows of tokens: 16-byte pieces of eight channels, [term][channels / 8][token]; four tokens of a group lie SLOT pieces
     // apart, so that 16 lanes' pieces cover all banks once, written and read
     static constexpr int SLOT = TK / 4 + 4;
     static constexpr int RM_TERM = (DP / 8) * 4 * SLOT;
     static constexpr int RM_BYTES = NT * RM_TERM * 16;
     // rows of channels: [term][channel][token], the groups of four in the order 0 2 1 3 of each sixteen (the order in which
-    // a lane of the score's result holds them)
+    // a lane of the score's result holds them).  DP = 16 leaves half of the matrix's rows free: a row of ones there gives sums over
+    // the tokens.
     static constexpr int CM_ROW = TK * 2 + 16;
-    static constexpr int CM_TERM = DP * CM_ROW;
+    static constexpr int CM_ROWS = DP == 16 ? 17 : DP;
+    static constexpr int CM_TERM = CM_ROWS * CM_ROW;
     static constexpr int CM_BYTES = NT * CM_TERM;
 };
 
@@ -122,10 +130,12 @@ __device__ __forceinline__ int unit_of(int units)
 struct TableRange {
     int base, len;
 };
-// `sign`: -1 for queries (offset = key - query), 1 for keys
-__host__ __device__ __forceinline__ TableRange table_range(int t0, int t1, int h, int wp, int tw, int centre, int sign)
+// `sign`: -1 for queries (offset = key - query), 1 for keys.  off() grows with the token, but in windows of one and two columns, whose
+// rows of four overlap: there whole rows count.
+__device__ __forceinline__ TableRange table_range(int t0, int t1, int h, int wp, int tw, int centre, int sign)
 {
-    const int lo = t0 / wp * tw, hi = (t1 - 1) / wp * tw + wp - 1, all = (h - 1) * tw + wp - 1;
+    const int y0 = t0 / wp, y1 = (t1 - 1) / wp, all = (h - 1) * tw + wp - 1;
+    const int lo = y0 * tw + (tw >= wp ? t0 - y0 * wp : 0), hi = y1 * tw + (tw >= wp ? t1 - 1 - y1 * wp : wp - 1);
     return sign < 0 ? TableRange{centre - hi, all + hi - lo + 1} : TableRange{centre + lo - all, all + hi - lo + 1};
 }
 
@@ -185,61 +195,72 @@ __device__ __forceinline__ void stage_tokens(const WindowParams &p, const Win &w
     bits[g] = (uint8_t)b;
 }
 
-// One operand's tokens [t0, t0 + TK) into LDS, by rows of tokens and / or by rows of channels; `plane` is channel 0 of
-// the head's planes of this image.
-template <typename T, int DP, bool RM, bool CM>
-__device__ __forceinline__ void stage(const WindowParams &p, const Win &w, const T *plane, int t0, char *rm, char *cm, int first, int threads)
-{
+// Four tokens of eight channels of one operand on their way from memory into LDS.
+template <typename T, int DP>
+struct Piece {
     using G = WinGeom<T, DP>;
-    const long hw = (long)p.H * p.W;
-    for (int item = first; item < (DP / 8) * (G::TK / 4); item += threads) {
-        const int g = item % (G::TK / 4), d8 = item / (G::TK / 4);
-        const int t = t0 + 4 * g;
-        uint32_t word[G::NT][8][2];  // [term][channel][pair of tokens]
-        bool ok[4] = {};
-        const T *at = plane;
-        if (t < w.L) {
-            const int y = t / w.wp, x = t - y * w.wp;
-            for (int j = 0; j < 4; ++j) ok[j] = seen(p, w, y, x + j);
-            at = plane + (long)(w.y0 + y) * p.W + w.x0 + x;
+    using Four = typename std::conditional<G::F32, wf32x4, wu32x2>::type;
+    Four v[8];
+
+    // tokens t ... t + 3 of the channels from 8 * d8 on; `plane` is channel 0 of the head's planes of this image
+    __device__ __forceinline__ void load(const WindowParams &p, const Win &w, const T *plane, int t, int d8)
+    {
+        const long hw = (long)p.H * p.W;
+        const int y = t / w.wp, x = t - y * w.wp;
+        const bool in = t < w.L;
+        const T *at = plane + (in ? (long)(w.y0 + y) * p.W + w.x0 + x : 0) + (long)(d8 * 8) * hw;
+        bool ok[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) ok[j] = in && x + j < w.w;
+        if (p.vec) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                v[i] = Four{};
+                if (in && d8 * 8 + i < p.d) v[i] = *reinterpret_cast<const Four *>(at + i * hw);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                T e[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) e[j] = ok[j] && d8 * 8 + i < p.d ? at[i * hw + j] : T(0);
+                __builtin_memcpy(&v[i], e, sizeof(Four));
+            }
         }
-        const bool any = ok[0] | ok[1] | ok[2] | ok[3];
+        if (p.mask != nullptr) {
+            const uint8_t *m = p.mask + ((long)w.n * p.H + w.y0 + y) * p.W + w.x0 + x;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) ok[j] = ok[j] && m[j] != 0;
+        }
+        if (!(ok[0] && ok[1] && ok[2] && ok[3])) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                if constexpr (G::F32) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) v[i][j] = ok[j] ? v[i][j] : 0.f;
+                } else {
+                    v[i].x &= (ok[0] ? 0xffffu : 0u) | (ok[1] ? 0xffff0000u : 0u);
+                    v[i].y &= (ok[2] ? 0xffffu : 0u) | (ok[3] ? 0xffff0000u : 0u);
+                }
+            }
+        }
+    }
+
+    // g: the group of four within the staged tokens
+    template <bool RM, bool CM>
+    __device__ __forceinline__ void store(char *rm, char *cm, int g, int d8) const
+    {
+        uint32_t word[G::NT][8][2];  // [term][channel][pair of tokens]
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const int c = d8 * 8 + i;
-            const bool read = any && c < p.d;
-            const T *a = at + c * hw;
             if constexpr (G::F32) {
-                float f[4] = {};
-                if (read) {
-                    if (p.vec) {
-                        const wf32x4 v = *reinterpret_cast<const wf32x4 *>(a);
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) f[j] = ok[j] ? v[j] : 0.f;
-                    } else {
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) f[j] = ok[j] ? a[j] : 0.f;
-                    }
-                }
                 uint32_t t01[3], t23[3];
-                split_bf16(f[0], f[1], t01);
-                split_bf16(f[2], f[3], t23);
+                split_bf16(v[i][0], v[i][1], t01);
+                split_bf16(v[i][2], v[i][3], t23);
 #pragma unroll
                 for (int q = 0; q < 3; ++q) word[q][i][0] = t01[q], word[q][i][1] = t23[q];
             } else {
-                uint32_t u[4] = {};
-                if (read) {
-                    if (p.vec) {
-                        const wu32x2 v = *reinterpret_cast<const wu32x2 *>(a);
-                        u[0] = v.x & 0xffffu, u[1] = v.x >> 16, u[2] = v.y & 0xffffu, u[3] = v.y >> 16;
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) u[j] = ok[j] ? u[j] : 0u;
-                    } else {
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) u[j] = ok[j] ? (uint32_t)a[j] : 0u;
-                    }
-                }
-                word[0][i][0] = u[0] | u[1] << 16, word[0][i][1] = u[2] | u[3] << 16;
+                word[0][i][0] = v[i].x, word[0][i][1] = v[i].y;
             }
         }
 #pragma unroll
@@ -248,11 +269,11 @@ __device__ __forceinline__ void stage(const WindowParams &p, const Win &w, const
                 wu32x4 *to = reinterpret_cast<wu32x4 *>(rm) + q * G::RM_TERM + d8 * 4 * G::SLOT + g;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    wu32x4 v;
+                    wu32x4 r;
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
-                        v[i] = j % 2 == 0 ? low_halves(word[q][2 * i][j / 2], word[q][2 * i + 1][j / 2]) : high_halves(word[q][2 * i][j / 2], word[q][2 * i + 1][j / 2]);
-                    to[j * G::SLOT] = v;
+                        r[i] = j % 2 == 0 ? low_halves(word[q][2 * i][j / 2], word[q][2 * i + 1][j / 2]) : high_halves(word[q][2 * i][j / 2], word[q][2 * i + 1][j / 2]);
+                    to[j * G::SLOT] = r;
                 }
             }
             if constexpr (CM) {
@@ -263,7 +284,62 @@ __device__ __forceinline__ void stage(const WindowParams &p, const Win &w, const
             }
         }
     }
-}
+};
+
+// Two operands staged a chunk of TK tokens at a time into two buffers in turn.  A block's threads fetch the next chunk into registers before
+// they multiply this one (as many pieces as there are threads; where a block has fewer threads, the rest follows behind).
+template <typename T, int DP, bool RM0, bool CM0, bool RM1, bool CM1>
+struct Stager {
+    using G = WinGeom<T, DP>;
+    static constexpr int GROUPS = G::TK / 4;
+    static constexpr int ITEMS = 2 * (DP / 8) * GROUPS;
+    static constexpr int RM0_AT = 0, CM0_AT = RM0_AT + (RM0 ? G::RM_BYTES : 0), RM1_AT = CM0_AT + (CM0 ? G::CM_BYTES : 0),
+                         CM1_AT = RM1_AT + (RM1 ? G::RM_BYTES : 0), OFF_AT = CM1_AT + (CM1 ? G::CM_BYTES : 0), BITS_AT = OFF_AT + GROUPS * 4,
+                         BYTES = (BITS_AT + GROUPS + 15) / 16 * 16;
+    Piece<T, DP> next;
+
+    __device__ __forceinline__ static void place(int item, int *which, int *g, int *d8)
+    {
+        *which = item / (ITEMS / 2);
+        const int i = item % (ITEMS / 2);
+        *g = i % GROUPS, *d8 = i / GROUPS;
+    }
+    __device__ __forceinline__ static void put(const Piece<T, DP> &piece, int item, char *buf)
+    {
+        int which, g, d8;
+        place(item, &which, &g, &d8);
+        if (which == 0) piece.template store<RM0, CM0>(buf + RM0_AT, buf + CM0_AT, g, d8);
+        else piece.template store<RM1, CM1>(buf + RM1_AT, buf + CM1_AT, g, d8);
+    }
+    __device__ __forceinline__ void fetch(const WindowParams &p, const Win &w, const T *op0, const T *op1, int t0)
+    {
+        int which, g, d8;
+        const int item = threadIdx.x;
+        if (item < ITEMS) {
+            place(item, &which, &g, &d8);
+            next.load(p, w, which == 0 ? op0 : op1, t0 + 4 * g, d8);
+        }
+    }
+    __device__ __forceinline__ void write(const WindowParams &p, const Win &w, const T *op0, const T *op1, int t0, char *buf)
+    {
+        if ((int)threadIdx.x < ITEMS) put(next, threadIdx.x, buf);
+        for (int item = threadIdx.x + blockDim.x; item < ITEMS; item += blockDim.x) {
+            int which, g, d8;
+            place(item, &which, &g, &d8);
+            Piece<T, DP> piece;
+            piece.load(p, w, which == 0 ? op0 : op1, t0 + 4 * g, d8);
+            put(piece, item, buf);
+        }
+        stage_tokens<G::TK>(p, w, t0, reinterpret_cast<int *>(buf + OFF_AT), reinterpret_cast<uint8_t *>(buf + BITS_AT));
+    }
+    // the rows of ones (DP = 16), once for each buffer
+    __device__ __forceinline__ static void ones(char *cm)
+    {
+        if constexpr (DP == 16)
+            for (int i = threadIdx.x; i < G::NT * G::CM_ROW / 4; i += blockDim.x)
+                *reinterpret_cast<uint32_t *>(cm + i / (G::CM_ROW / 4) * G::CM_TERM + 16 * G::CM_ROW + i % (G::CM_ROW / 4) * 4) = i < G::CM_ROW / 4 ? 0x3f803f80u : 0u;
+    }
+};
 
 // A wavefront's own tokens as operands kept in registers: lane n = token, eight channels 16 s + 8 (lane / 32) on.
 template <typename T, int DP>
@@ -350,30 +426,38 @@ __device__ __forceinline__ Packed<NT> pack(const wf32x16 &v)
     return o;
 }
 
-// acc += rows of channels x the tile's values (VT terms of them).  DP = 16: the lanes of the matrix's other rows read rows again.
+// acc += rows of channels x the tile's values (VT terms of them), of U tiles of own tokens.  DP = 16: the matrix's rows from 16 on take the row
+// of ones.
 // fp32 storage: the tile's products are summed by themselves first, so that a long sum takes one rounding a tile and not one
 // for each pair of terms (1024 keys: 1.0e-6 off the exact result instead of 3e-7 with the products added one by one).
-template <typename T, int DP, int VT>
-__device__ __forceinline__ void accumulate(const char *cm, int tile, const Packed<VT> &v, wf32x16 (&acc)[WinGeom<T, DP>::DT])
+template <typename T, int DP, int VT, int U>
+__device__ __forceinline__ void accumulate(const char *cm, int tile, const Packed<VT> (&v)[U], wf32x16 (&acc)[U][WinGeom<T, DP>::DT])
 {
     using G = WinGeom<T, DP>;
     const int lane = threadIdx.x & 63, half = lane >> 5;
-    const int row = DP == 16 ? lane & 15 : lane & 31;
+    const int row = DP == 16 ? min(lane & 31, 16) : lane & 31;
     const char *from = cm + row * G::CM_ROW + tile * 64 + half * 16;
 #pragma unroll
     for (int b = 0; b < G::DT; ++b) {
-        wf32x16 sum = G::F32 ? wf32x16{} : acc[b];
+        wf32x16 sum[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) sum[u] = G::F32 ? wf32x16{} : acc[u][b];
 #pragma unroll
         for (int a = 0; a < 2; ++a)
 #pragma unroll
             for (int q = G::NT - 1; q >= 0; --q) {
                 const wu32x4 x = *reinterpret_cast<const wu32x4 *>(from + q * G::CM_TERM + b * 32 * G::CM_ROW + a * 32);
 #pragma unroll
-                for (int r = VT - 1; r >= 0; --r)
-                    if (!G::F32 || r + q < G::NT) sum = mfma(x, v.r[r][a], sum);
+                for (int u = 0; u < U; ++u)
+#pragma unroll
+                    for (int r = VT - 1; r >= 0; --r)
+                        if (!G::F32 || r + q < G::NT) sum[u] = mfma(x, v[u].r[r][a], sum[u]);
             }
-        if constexpr (G::F32) acc[b] += sum;
-        else acc[b] = sum;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if constexpr (G::F32) acc[u][b] += sum[u];
+            else acc[u][b] = sum[u];
+        }
     }
 }
 

@@ -6,45 +6,51 @@
 //   window_dq_kernel: the forward's layout (a lane holds 16 keys of a query); dq^T = K^T ds^T, and the offsets' sums.
 //   window_dkv_kernel: queries down, keys across (a lane holds 16 queries of a key); dv^T = dO^T p, dk^T = Q^T ds, over all
 //     query heads that share the key's.
-// The sums of equal offsets have a fixed order: each wavefront adds to a table of its own in LDS, and no instruction holds two
-// values of one offset (its 64 lanes are 64 queries and one key: permlane32_swap brings the two tiles' halves together).  The
-// wavefronts' tables are added in order, written, and two small kernels add the blocks' tables and the offsets of each bucket.
+//
+// The sums of equal offsets, in a fixed order.  Each wavefront adds to a ring of its own in LDS, in 64 bits: ds_add_f64 takes 8.5 clocks for 64
+// lanes where ds_add_f32 takes 193 (measured).  No instruction holds two values of one offset: its 64 lanes are 64 queries and one key (two
+// tiles of queries: permlane32_swap brings their halves together), or 32 queries and one key (one tile, half after half).  What the ring
+// spans are the offsets between the wavefront's queries and ONE tile of keys; offsets that the next tile no longer reaches are complete and
+// leave for memory.  Two small kernels add the wavefronts' parts and the offsets of each bucket.
 #include "esc_window.hpp"
 
 namespace esc {
 namespace {
 
-__device__ __forceinline__ void lds_add(float *p, float v)
+__device__ __forceinline__ void lds_add(double *p, float v) { __hip_atomic_fetch_add(p, (double)v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP); }
+
+// The offsets of all its window's keys from the tokens [t0, t0 + 32 U) of a wavefront: from the smallest on.
+template <int U>
+__device__ __forceinline__ TableRange wave_range(const WindowParams &p, const Win &w, int t0)
 {
-    __hip_atomic_fetch_add(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+    const int centre = (p.wh - 1) * p.tw + p.ww - 1;
+    return table_range(t0, min(t0 + 32 * U, w.L), w.h, w.wp, p.tw, centre, -1);
 }
 
 template <typename T, int DP>
-__global__ __launch_bounds__(256) void window_dq_kernel(const WindowParams p)
+__global__ __launch_bounds__(512) void window_dq_kernel(const WindowParams p)
 {
     using G = WinGeom<T, DP>;
+    using S = Stager<T, DP, true, true, true, false>;  // keys by tokens and by channels, values by tokens
+    constexpr int U = G::QUERY_TILES;
     extern __shared__ __align__(16) char lds[];
-    char *k_rm = lds, *k_cm = k_rm + G::RM_BYTES, *v_rm = k_cm + G::CM_BYTES;
-    int *off = reinterpret_cast<int *>(v_rm + G::RM_BYTES);
-    uint8_t *bits = reinterpret_cast<uint8_t *>(off + G::TK / 4);
-    float *table = reinterpret_cast<float *>(bits + G::TK / 4);
-    float *sums = table + p.len;  // one table a wavefront
+    double *rings = reinterpret_cast<double *>(lds + p.buffers * S::BYTES);  // one a wavefront
+    float *table = reinterpret_cast<float *>(rings + (p.grad_bias != nullptr ? p.waves * p.ring : 0));
 
     const int unit = unit_of(p.units);
     if (unit < 0) return;
     const int block = unit % p.blocks, head = unit / p.blocks % p.heads, wi = unit / p.blocks / p.heads;
     const Win w = win_of(p, wi / (p.gy * p.gx), wi / p.gx % p.gy, wi % p.gx);
-    const int q0 = block * p.waves * kWinWaveTokens;
+    const int queries = p.waves * 32 * U, q0 = block * queries;
     if (q0 >= w.L) return;
     const int centre = (p.wh - 1) * p.tw + p.ww - 1;
-    const TableRange range = table_range(q0, min(q0 + p.waves * kWinWaveTokens, w.L), w.h, w.wp, p.tw, centre, -1);
-    stage_table(p, table, range, head);
+    const TableRange range = table_range(q0, min(q0 + queries, w.L), w.h, w.wp, p.tw, centre, -1);
     const bool bias_grad = p.grad_bias != nullptr;
-    if (bias_grad)
-        for (int i = threadIdx.x; i < p.waves * p.len; i += blockDim.x) sums[i] = 0.f;
 
     const long hw = (long)p.H * p.W;
-    const int lane = threadIdx.x & 63, half = lane >> 5, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wq0 = q0 + wave * 32 * U;
+    const bool busy = wq0 < w.L;
     const int kvh = head / (p.heads / p.kv_heads);
     const long planes = ((long)w.n * p.heads + head) * p.d * hw, row = ((long)w.n * p.heads + head) * hw;
     const T *q = static_cast<const T *>(p.q) + w.n * p.qs + head * (long)p.d * hw;
@@ -52,26 +58,29 @@ __global__ __launch_bounds__(256) void window_dq_kernel(const WindowParams p)
     const T *v = static_cast<const T *>(p.v) + w.n * p.vs + kvh * (long)p.d * hw;
     const T *go = static_cast<const T *>(p.go) + planes, *out = static_cast<const T *>(p.out_in) + planes;
 
-    Fragment<T, DP> own_q[2], own_go[2];
-    long pixel[2];
-    bool there[2], ok[2], large[2];
-    int place[2];
-    float top[2], shift[2], log_sum[2], delta[2];
-    wf32x16 acc[2][G::DT];
+    S stager;
+    stager.fetch(p, w, k, v, 0);
+    Fragment<T, DP> own_q[U], own_go[U];
+    int pixel[U], place[U];
+    bool there[U], ok[U];
+    float top[U], shift[U], log_sum[U], delta[U];
+    wf32x16 acc[U][G::DT];
+    bool far = false, all = true;
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-        const int t = q0 + wave * kWinWaveTokens + u * 32 + (lane & 31), tc = min(t, w.L - 1);
+    for (int u = 0; u < U; ++u) {
+        const int t = wq0 + u * 32 + (lane & 31), tc = min(t, w.L - 1);
         const int y = tc / w.wp, x = tc - y * w.wp;
         there[u] = t < w.L && x < w.w;
         ok[u] = there[u] && seen(p, w, y, x);
-        pixel[u] = (long)(w.y0 + y) * p.W + w.x0 + x;
+        pixel[u] = (w.y0 + y) * p.W + w.x0 + x;
         place[u] = centre - (y * p.tw + x) - range.base;
         own_q[u] = own_fragment<T, DP>(p, q + pixel[u], ok[u]);
         own_go[u] = own_fragment<T, DP>(p, go + pixel[u], ok[u]);
         top[u] = ok[u] ? p.top[row + pixel[u]] : 0.f;
         log_sum[u] = ok[u] ? p.log_sum[row + pixel[u]] : __builtin_inff();
-        shift[u] = top[u] * p.log2_scale;
-        large[u] = __any(__builtin_fabsf(shift[u]) > kLargeShift);
+        shift[u] = top[u] * p.log2_scale + log_sum[u];
+        far = far || __any(__builtin_fabsf(top[u] * p.log2_scale) > kLargeShift);
+        all = all && __all(ok[u]);
         float sum = 0.f;
         if (ok[u])
             for (int c = half; c < p.d; c += 2) {
@@ -84,43 +93,51 @@ __global__ __launch_bounds__(256) void window_dq_kernel(const WindowParams p)
 #pragma unroll
         for (int b = 0; b < G::DT; ++b) acc[u][b] = wf32x16{};
     }
-    // the table place of the lane's query where the wavefront's 64 lanes are its 64 queries
-    const int place64 = half == 0 ? place[0] : place[1];
-    float *const mine = sums + wave * p.len + place64;
-    const bool busy = q0 + wave * kWinWaveTokens < w.L;
+    stage_table(p, table, range, head);
+    double *const ring = rings + wave * p.ring;
+    const int ring_mask = p.ring - 1;
+    const TableRange mine = wave_range<U>(p, w, min(wq0, w.L - 1));
+    // ring place of the offset to the key with off = 0: of the lane's query where 64 lanes are 64 queries, else of its own
+    const int ring_place = (U == 1 || half == 0 ? place[0] : place[U - 1]) + range.base - mine.base;
+    float *const part = p.part + ((long)unit * p.waves + wave) * p.part_len;
+    int left = 0;  // offsets that have left the ring
+    if (bias_grad)
+        for (int i = lane; i < p.ring; i += 64) ring[i] = 0.0;
+    stager.write(p, w, k, v, 0, lds);
+    __syncthreads();
 
-    for (int t0 = 0; t0 < w.L; t0 += G::TK) {
-        __syncthreads();
-        stage<T, DP, true, true>(p, w, k, t0, k_rm, k_cm, threadIdx.x, blockDim.x);
-        stage<T, DP, true, false>(p, w, v, t0, v_rm, nullptr, threadIdx.x, blockDim.x);
-        stage_tokens<G::TK>(p, w, t0, off, bits);
-        __syncthreads();
-        if (!busy) continue;
-        for (int tile = 0; tile < G::TK / 32 && t0 + tile * 32 < w.L; ++tile) {
-            const wu32x2 nibbles = *reinterpret_cast<const wu32x2 *>(bits + tile * 8);
-            const bool whole = __builtin_amdgcn_readfirstlane((int)((nibbles.x & nibbles.y) == 0x0f0f0f0fu));
-            wf32x16 ds[2];
+    for (int t0 = 0, turn = 0; t0 < w.L; t0 += G::TK) {
+        const bool more = t0 + G::TK < w.L;
+        if (more) stager.fetch(p, w, k, v, t0 + G::TK);
+        const char *buf = lds + turn * S::BYTES;
+        const int *off = reinterpret_cast<const int *>(buf + S::OFF_AT);
+        auto tile_of = [&](int tile, auto large) {
+            const wu32x2 nibbles = *reinterpret_cast<const wu32x2 *>(buf + S::BITS_AT + tile * 8);
+            const bool whole = all && __builtin_amdgcn_readfirstlane((int)(nibbles.x & nibbles.y)) == 0x0f0f0f0f;
+            int key[4];
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
+            for (int a = 0; a < 4; ++a) key[a] = off[tile * 8 + 2 * a + half];
+            wf32x16 ds[U];
+            Packed<G::NT> e[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
                 wf32x16 s;
 #pragma unroll
                 for (int a = 0; a < 4; ++a) {
-                    const float *from = table + place[u] + off[tile * 8 + 2 * a + half];
+                    const float *from = table + place[u] + key[a];
 #pragma unroll
                     for (int j = 0; j < 4; ++j) s[4 * a + j] = from[j];
                 }
-                s = score<T, DP>(k_rm, tile, own_q[u], s);
-                const wf32x16 dp = score<T, DP>(v_rm, tile, own_go[u], wf32x16{});
-                if (__builtin_expect(!large[u], 1)) {
+                s = score<T, DP>(buf + S::RM0_AT, tile, own_q[u], s);
+                const wf32x16 dp = score<T, DP>(buf + S::RM1_AT, tile, own_go[u], wf32x16{});
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) s[i] = __builtin_fmaf(s[i], p.log2_scale, -(shift[u] + log_sum[u]));
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) s[i] = __builtin_fmaf(fminf(s[i] - top[u], 0.f), p.log2_scale, -log_sum[u]);
+                for (int i = 0; i < 16; ++i) {
+                    if constexpr (decltype(large)::value) s[i] = __builtin_fmaf(fminf(s[i] - top[u], 0.f), p.log2_scale, -log_sum[u]);
+                    else s[i] = __builtin_fmaf(s[i], p.log2_scale, -shift[u]);
+                    ds[u][i] = exp2_of(s[i]) * (dp[i] - delta[u]);
                 }
-#pragma unroll
-                for (int i = 0; i < 16; ++i) ds[u][i] = exp2_of(s[i]) * (dp[i] - delta[u]);
-                if (!whole || !ok[u]) {
+                if (!whole) {
+                    asm volatile("; tokens that do not take part");
 #pragma unroll
                     for (int a = 0; a < 4; ++a) {
                         const uint32_t b = (a < 2 ? nibbles.x : nibbles.y) >> (16 * (a & 1) + 8 * half);
@@ -128,170 +145,210 @@ __global__ __launch_bounds__(256) void window_dq_kernel(const WindowParams p)
                         for (int j = 0; j < 4; ++j) ds[u][4 * a + j] = ok[u] && (b >> j & 1) != 0 ? ds[u][4 * a + j] : 0.f;
                     }
                 }
-                accumulate<T, DP>(k_cm, tile, pack<G::NT>(ds[u]), acc[u]);
+                e[u] = pack<G::NT>(ds[u]);
             }
+            accumulate<T, DP>(buf + S::CM0_AT, tile, e, acc);
             if (bias_grad) {
 #pragma unroll
                 for (int a = 0; a < 4; ++a) {
-                    const int lo = off[tile * 8 + 2 * a], hi = off[tile * 8 + 2 * a + 1];
+                    const int lo = ring_place + off[tile * 8 + 2 * a], hi = ring_place + off[tile * 8 + 2 * a + 1];
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(ds[0][4 * a + j]), __float_as_uint(ds[1][4 * a + j]), false, false);
-                        lds_add(mine + lo + j, __uint_as_float(x[0]));
-                        lds_add(mine + hi + j, __uint_as_float(x[1]));
+                        if constexpr (U == 2) {
+                            const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(ds[0][4 * a + j]), __float_as_uint(ds[U - 1][4 * a + j]), false, false);
+                            lds_add(ring + ((lo + j) & ring_mask), __uint_as_float(x[0]));
+                            lds_add(ring + ((hi + j) & ring_mask), __uint_as_float(x[1]));
+                        } else {
+                            if (half == 0) lds_add(ring + ((lo + j) & ring_mask), ds[0][4 * a + j]);
+                            if (half == 1) lds_add(ring + ((hi + j) & ring_mask), ds[0][4 * a + j]);
+                        }
                     }
                 }
-            }
-        }
-    }
-    if (busy) {
-        T *gq = static_cast<T *>(p.gq) + w.n * p.gqs + head * (long)p.d * hw;
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-            for (int b = 0; b < G::DT; ++b)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int c = b * 32 + 8 * (i / 4) + 4 * half + i % 4;
-                    if (there[u] && c < p.d) gq[c * hw + pixel[u]] = narrow<T>(acc[u][b][i] * p.scale);
+                const int t = t0 + tile * 32 + 32;  // the next tile's first key
+                const int done = t < w.L ? t / w.wp * p.tw + t % w.wp : mine.len;
+                for (int i = left + lane; i < done; i += 64) {
+                    part[i] = (float)ring[i & ring_mask];
+                    ring[i & ring_mask] = 0.0;
                 }
-    }
-    if (bias_grad) {
+                left = done;
+            }
+        };
+        if (busy)
+            for (int tile = 0; tile < G::TK / 32 && t0 + tile * 32 < w.L; ++tile) {
+                if (__builtin_expect(far, 0)) tile_of(tile, std::true_type{});
+                else tile_of(tile, std::false_type{});
+            }
+        if (p.buffers == 1) __syncthreads();
+        else turn ^= 1;
+        if (more) stager.write(p, w, k, v, t0 + G::TK, lds + turn * S::BYTES);
         __syncthreads();
-        float *to = p.part + (long)unit * p.len;
-        for (int i = threadIdx.x; i < range.len; i += blockDim.x) {
-            float s = sums[i];
-            for (int j = 1; j < p.waves; ++j) s += sums[j * p.len + i];
-            to[i] = s;
-        }
     }
+    if (!busy) return;
+    T *gq = static_cast<T *>(p.gq) + w.n * p.gqs + head * (long)p.d * hw;
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int b = 0; b < G::DT; ++b)
+#pragma unroll
+            for (int i = 0; i < (DP == 16 ? 8 : 16); ++i) {
+                const int c = b * 32 + 8 * (i / 4) + 4 * half + i % 4;
+                if (there[u] && c < p.d) gq[c * hw + pixel[u]] = narrow<T>(acc[u][b][i] * p.scale);
+            }
 }
 
 template <typename T, int DP>
-__global__ __launch_bounds__(256) void window_dkv_kernel(const WindowParams p)
+__global__ __launch_bounds__(512) void window_dkv_kernel(const WindowParams p)
 {
     using G = WinGeom<T, DP>;
-    extern __shared__ __align__(16) char lds[];
-    char *q_rm = lds, *q_cm = q_rm + G::RM_BYTES, *g_rm = q_cm + G::CM_BYTES, *g_cm = g_rm + G::RM_BYTES;
+    using S = Stager<T, DP, true, true, true, true>;  // queries and the result's gradient, by tokens and by channels
+    constexpr int U = 1;
     // of the staged queries: the exponent's shift (with the sum's logarithm; without it and the largest score, where a shift is large), -delta
-    float *shift = reinterpret_cast<float *>(g_cm + G::CM_BYTES), *top = shift + G::TK, *minus_delta = top + G::TK;
-    int *off = reinterpret_cast<int *>(minus_delta + G::TK);
-    uint8_t *bits = reinterpret_cast<uint8_t *>(off + G::TK / 4);
-    int *large = reinterpret_cast<int *>(bits + G::TK / 4);
-    float *table = reinterpret_cast<float *>(large + 1);
+    constexpr int ROWS_AT = S::BYTES, FAR_AT = ROWS_AT + 3 * G::TK * 4, BYTES = FAR_AT + 16;
+    extern __shared__ __align__(16) char lds[];
+    float *table = reinterpret_cast<float *>(lds + p.buffers * BYTES);
 
     const int unit = unit_of(p.units);
     if (unit < 0) return;
     const int block = unit % p.blocks, kvh = unit / p.blocks % p.kv_heads, wi = unit / p.blocks / p.kv_heads;
     const Win w = win_of(p, wi / (p.gy * p.gx), wi / p.gx % p.gy, wi % p.gx);
-    const int k0 = block * p.waves * kWinWaveTokens;
+    const int keys = p.waves * 32 * U, k0 = block * keys;
     if (k0 >= w.L) return;
     const int centre = (p.wh - 1) * p.tw + p.ww - 1;
-    const TableRange range = table_range(k0, min(k0 + p.waves * kWinWaveTokens, w.L), w.h, w.wp, p.tw, centre, 1);
+    const TableRange range = table_range(k0, min(k0 + keys, w.L), w.h, w.wp, p.tw, centre, 1);
 
     const long hw = (long)p.H * p.W;
-    const int lane = threadIdx.x & 63, half = lane >> 5, wave = threadIdx.x >> 6;
-    const int group = p.heads / p.kv_heads;
+    const int lane = threadIdx.x & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int group = p.heads / p.kv_heads, chunks = (w.L + G::TK - 1) / G::TK;
+    const int wk0 = k0 + wave * 32 * U;
+    const bool busy = wk0 < w.L;
     const T *k = static_cast<const T *>(p.k) + w.n * p.ks + kvh * (long)p.d * hw;
     const T *v = static_cast<const T *>(p.v) + w.n * p.vs + kvh * (long)p.d * hw;
+    const T *q = static_cast<const T *>(p.q) + w.n * p.qs, *go = static_cast<const T *>(p.go) + (long)w.n * p.heads * p.d * hw;
 
-    Fragment<T, DP> own_k[2], own_v[2];
-    long pixel[2];
-    bool there[2], ok[2];
-    int place[2];
-    wf32x16 dk[2][G::DT], dv[2][G::DT];
+    // a chunk's number counts through the group's heads
+    S stager;
+    float from, log_sum, minus;  // of this thread's query of the next chunk
+    auto fetch = [&](int c) {
+        const int head = kvh * group + c / chunks, t0 = c % chunks * G::TK;
+        stager.fetch(p, w, q + head * (long)p.d * hw, go + head * (long)p.d * hw, t0);
+        from = 0.f, log_sum = __builtin_inff(), minus = 0.f;
+        if (threadIdx.x < G::TK) {
+            const int t = t0 + threadIdx.x, y = t / w.wp, x = t - y * w.wp;
+            if (t < w.L && seen(p, w, y, x)) {
+                const long pix = ((long)w.n * p.heads + head) * hw + (long)(w.y0 + y) * p.W + w.x0 + x;
+                from = p.top[pix], log_sum = p.log_sum[pix], minus = -p.delta[pix];
+            }
+        }
+    };
+    auto write = [&](int c, char *buf) {
+        const int head = kvh * group + c / chunks, t0 = c % chunks * G::TK;
+        stager.write(p, w, q + head * (long)p.d * hw, go + head * (long)p.d * hw, t0, buf);
+        if (threadIdx.x < G::TK) {  // (threads of one wavefront)
+            float *rows = reinterpret_cast<float *>(buf + ROWS_AT) + threadIdx.x;
+            const bool far = __any(__builtin_fabsf(from * p.log2_scale) > kLargeShift);
+            rows[0] = far ? log_sum : from * p.log2_scale + log_sum;
+            rows[G::TK] = from, rows[2 * G::TK] = minus;
+            if (threadIdx.x == 0) *reinterpret_cast<int *>(buf + FAR_AT) = far;
+        }
+    };
+    fetch(0);
+    Fragment<T, DP> own_k[U], own_v[U];
+    int pixel[U], place[U];
+    bool there[U], ok[U];
+    wf32x16 dk[U][G::DT], dv[U][G::DT];
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-        const int t = k0 + wave * kWinWaveTokens + u * 32 + (lane & 31), tc = min(t, w.L - 1);
+    for (int u = 0; u < U; ++u) {
+        const int t = wk0 + u * 32 + (lane & 31), tc = min(t, w.L - 1);
         const int y = tc / w.wp, x = tc - y * w.wp;
         there[u] = t < w.L && x < w.w;
         ok[u] = there[u] && seen(p, w, y, x);
-        pixel[u] = (long)(w.y0 + y) * p.W + w.x0 + x;
+        pixel[u] = (w.y0 + y) * p.W + w.x0 + x;
         place[u] = centre + (y * p.tw + x) - range.base;
         own_k[u] = own_fragment<T, DP>(p, k + pixel[u], ok[u]);
         own_v[u] = own_fragment<T, DP>(p, v + pixel[u], ok[u]);
 #pragma unroll
         for (int b = 0; b < G::DT; ++b) dk[u][b] = wf32x16{}, dv[u][b] = wf32x16{};
     }
-    const bool busy = k0 + wave * kWinWaveTokens < w.L;
+    stage_table(p, table, range, kvh * group);
+    write(0, lds);
+    __syncthreads();
 
-    for (int head = kvh * group; head < (kvh + 1) * group; ++head) {
-        const long planes = ((long)w.n * p.heads + head) * p.d * hw, row = ((long)w.n * p.heads + head) * hw;
-        const T *q = static_cast<const T *>(p.q) + w.n * p.qs + head * (long)p.d * hw;
-        const T *go = static_cast<const T *>(p.go) + planes;
-        __syncthreads();
-        stage_table(p, table, range, head);
-        for (int t0 = 0; t0 < w.L; t0 += G::TK) {
-            __syncthreads();
-            stage<T, DP, true, true>(p, w, q, t0, q_rm, q_cm, threadIdx.x, blockDim.x);
-            stage<T, DP, true, true>(p, w, go, t0, g_rm, g_cm, threadIdx.x, blockDim.x);
-            stage_tokens<G::TK>(p, w, t0, off, bits);
-            bool far = false;
-            if (threadIdx.x < G::TK) {
-                const int t = t0 + threadIdx.x;
-                float from = 0.f, log_sum = __builtin_inff(), d = 0.f;
-                if (t < w.L) {
-                    const int y = t / w.wp, x = t - y * w.wp;
-                    if (seen(p, w, y, x)) {
-                        const long pix = row + (long)(w.y0 + y) * p.W + w.x0 + x;
-                        from = p.top[pix], log_sum = p.log_sum[pix], d = -p.delta[pix];
+    for (int c = 0, turn = 0; c < chunks * group; ++c) {
+        const bool more = c + 1 < chunks * group;
+        const int t0 = c % chunks * G::TK;
+        if (more) fetch(c + 1);
+        const char *buf = lds + turn * BYTES;
+        const int *off = reinterpret_cast<const int *>(buf + S::OFF_AT);
+        const float *rows = reinterpret_cast<const float *>(buf + ROWS_AT);
+        const bool far = __builtin_amdgcn_readfirstlane(*reinterpret_cast<const int *>(buf + FAR_AT)) != 0;
+        auto tile_of = [&](int tile, auto large) {
+            const wu32x2 nibbles = *reinterpret_cast<const wu32x2 *>(buf + S::BITS_AT + tile * 8);
+            const bool whole = __builtin_amdgcn_readfirstlane((int)(nibbles.x & nibbles.y)) == 0x0f0f0f0f;
+            Packed<G::NT> ep[U], es[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                wf32x16 s, dp;
+#pragma unroll
+                for (int a = 0; a < 4; ++a) {
+                    const float *at = table + place[u] - off[tile * 8 + 2 * a + half];
+                    const wf32x4 d = *reinterpret_cast<const wf32x4 *>(rows + 2 * G::TK + tile * 32 + 8 * a + 4 * half);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) s[4 * a + j] = at[-j], dp[4 * a + j] = d[j];
+                }
+                s = score<T, DP, true>(buf + S::RM0_AT, tile, own_k[u], s);
+                dp = score<T, DP>(buf + S::RM1_AT, tile, own_v[u], dp);
+#pragma unroll
+                for (int a = 0; a < 4; ++a) {
+                    const wf32x4 l = *reinterpret_cast<const wf32x4 *>(rows + tile * 32 + 8 * a + 4 * half);
+                    wf32x4 m;
+                    if constexpr (decltype(large)::value) m = *reinterpret_cast<const wf32x4 *>(rows + G::TK + tile * 32 + 8 * a + 4 * half);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        float x = s[4 * a + j];
+                        if constexpr (decltype(large)::value) x = fminf(x - m[j], 0.f);
+                        s[4 * a + j] = exp2_of(__builtin_fmaf(x, p.log2_scale, -l[j]));
                     }
                 }
-                far = __any(__builtin_fabsf(from * p.log2_scale) > kLargeShift);  // (a wavefront's threads: TK is at most 64)
-                shift[threadIdx.x] = far ? log_sum : from * p.log2_scale + log_sum;
-                top[threadIdx.x] = from, minus_delta[threadIdx.x] = d;
-                if (threadIdx.x == 0) *large = far;
-            }
-            __syncthreads();
-            if (!busy) continue;
-            far = __builtin_amdgcn_readfirstlane(*large) != 0;
-            for (int tile = 0; tile < G::TK / 32 && t0 + tile * 32 < w.L; ++tile) {
-                const wu32x2 nibbles = *reinterpret_cast<const wu32x2 *>(bits + tile * 8);
-                const bool whole = __builtin_amdgcn_readfirstlane((int)((nibbles.x & nibbles.y) == 0x0f0f0f0fu));
-#pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    wf32x16 s, dp;
+                if (!whole) {
+                    asm volatile("; queries that do not take part");
 #pragma unroll
                     for (int a = 0; a < 4; ++a) {
-                        const float *from = table + place[u] - off[tile * 8 + 2 * a + half];
-                        const wf32x4 d = *reinterpret_cast<const wf32x4 *>(minus_delta + tile * 32 + 8 * a + 4 * half);
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) s[4 * a + j] = from[-j], dp[4 * a + j] = d[j];
-                    }
-                    s = score<T, DP, true>(q_rm, tile, own_k[u], s);
-                    dp = score<T, DP>(g_rm, tile, own_v[u], dp);
-#pragma unroll
-                    for (int a = 0; a < 4; ++a) {
-                        const wf32x4 l = *reinterpret_cast<const wf32x4 *>(shift + tile * 32 + 8 * a + 4 * half);
-                        if (__builtin_expect(far, 0)) {
-                            const wf32x4 m = *reinterpret_cast<const wf32x4 *>(top + tile * 32 + 8 * a + 4 * half);
-#pragma unroll
-                            for (int j = 0; j < 4; ++j) s[4 * a + j] = fminf(s[4 * a + j] - m[j], 0.f);
-                        }
                         const uint32_t b = (a < 2 ? nibbles.x : nibbles.y) >> (16 * (a & 1) + 8 * half);
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            const float e = exp2_of(__builtin_fmaf(s[4 * a + j], p.log2_scale, -l[j]));
-                            s[4 * a + j] = whole || (b >> j & 1) != 0 ? e : 0.f;
-                        }
+                        for (int j = 0; j < 4; ++j) s[4 * a + j] = (b >> j & 1) != 0 ? s[4 * a + j] : 0.f;
                     }
-                    accumulate<T, DP>(g_cm, tile, pack<G::NT>(s), dv[u]);
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) s[i] *= dp[i];
-                    accumulate<T, DP>(q_cm, tile, pack<G::NT>(s), dk[u]);
                 }
+                ep[u] = pack<G::NT>(s);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[i] *= dp[i];
+                es[u] = pack<G::NT>(s);
             }
+            accumulate<T, DP>(buf + S::CM1_AT, tile, ep, dv);
+            accumulate<T, DP>(buf + S::CM0_AT, tile, es, dk);
+        };
+        if (busy)
+            for (int tile = 0; tile < G::TK / 32 && t0 + tile * 32 < w.L; ++tile) {
+                if (__builtin_expect(far, 0)) tile_of(tile, std::true_type{});
+                else tile_of(tile, std::false_type{});
+            }
+        if (p.buffers == 1) __syncthreads();
+        else turn ^= 1;
+        if (more) write(c + 1, lds + turn * BYTES);
+        if (more && (c + 1) % chunks == 0) {  // (uniform) another head's biases: nobody may still read the last one's
+            if (p.buffers != 1) __syncthreads();
+            stage_table(p, table, range, kvh * group + (c + 1) / chunks);
         }
+        __syncthreads();
     }
     if (!busy) return;
     T *gk = static_cast<T *>(p.gk) + w.n * p.gks + kvh * (long)p.d * hw;
     T *gv = static_cast<T *>(p.gv) + w.n * p.gvs + kvh * (long)p.d * hw;
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
+    for (int u = 0; u < U; ++u)
 #pragma unroll
         for (int b = 0; b < G::DT; ++b)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
+            for (int i = 0; i < (DP == 16 ? 8 : 16); ++i) {
                 const int c = b * 32 + 8 * (i / 4) + 4 * half + i % 4;
                 if (there[u] && c < p.d) {
                     gk[c * hw + pixel[u]] = narrow<T>(ok[u] ? dk[u][b][i] * p.scale : 0.f);
@@ -300,21 +357,21 @@ __global__ __launch_bounds__(256) void window_dkv_kernel(const WindowParams p)
             }
 }
 
-// Sums of equal offsets over every `splits`-th block's table, in order.
+// Sums of equal offsets over the wavefronts' parts, every `splits`-th window's, in order.
 __global__ __launch_bounds__(256) void window_offsets_kernel(const WindowParams p)
 {
     const int at = blockIdx.x * 256 + threadIdx.x, head = blockIdx.y;
     if (at >= p.th * p.tw) return;
-    const int centre = (p.wh - 1) * p.tw + p.ww - 1;
+    const int centre = (p.wh - 1) * p.tw + p.ww - 1, tokens = 32 * p.tiles, windows = p.N * p.gy * p.gx;
     float sum = 0.f;
-    for (int i = blockIdx.z; i < p.units / p.heads; i += p.splits) {
-        const int block = i % p.blocks, wi = i / p.blocks;
+    for (int wi = blockIdx.z; wi < windows; wi += p.splits) {
         const Win w = win_of(p, wi / (p.gy * p.gx), wi / p.gx % p.gy, wi % p.gx);
-        const int q0 = block * p.waves * kWinWaveTokens;
-        if (q0 >= w.L) continue;
-        const TableRange r = table_range(q0, min(q0 + p.waves * kWinWaveTokens, w.L), w.h, w.wp, p.tw, centre, -1);
-        const int in = at - r.base;
-        if (in >= 0 && in < r.len) sum += p.part[((long)(wi * p.heads + head) * p.blocks + block) * p.len + in];
+        const float *part = p.part + (long)(wi * p.heads + head) * p.blocks * p.waves * p.part_len;
+        for (int t0 = 0; t0 < w.L; t0 += tokens, part += p.part_len) {
+            const TableRange r = table_range(t0, min(t0 + tokens, w.L), w.h, w.wp, p.tw, centre, -1);
+            const int in = at - r.base;
+            if (in >= 0 && in < r.len) sum += part[in];
+        }
     }
     p.part2[((long)blockIdx.z * p.heads + head) * p.th * p.tw + at] = sum;
 }
@@ -357,16 +414,14 @@ __global__ __launch_bounds__(256) void window_buckets_kernel(const WindowParams 
 }
 
 template <typename T, int DP>
-size_t dq_lds(int len, int tables)
+size_t dq_lds(const WindowParams &p)
 {
-    using G = WinGeom<T, DP>;
-    return 2 * G::RM_BYTES + G::CM_BYTES + (G::TK / 4) * 5 + (size_t)len * 4 * (1 + tables);
+    return p.buffers * (size_t)Stager<T, DP, true, true, true, false>::BYTES + (p.grad_bias != nullptr ? (size_t)p.waves * p.ring * 8 : 0) + (size_t)p.len * 4;
 }
 template <typename T, int DP>
-size_t dkv_lds(int len)
+size_t dkv_lds(const WindowParams &p)
 {
-    using G = WinGeom<T, DP>;
-    return 2 * (G::RM_BYTES + G::CM_BYTES) + G::TK * 12 + (G::TK / 4) * 5 + 4 + (size_t)len * 4;
+    return p.buffers * (size_t)(Stager<T, DP, true, true, true, true>::BYTES + 3 * WinGeom<T, DP>::TK * 4 + 16) + (size_t)p.len * 4;
 }
 
 hipError_t allow(const void *kernel, size_t lds)
@@ -377,7 +432,7 @@ hipError_t allow(const void *kernel, size_t lds)
 template <typename T, int DP>
 hipError_t launch_dq(const WindowParams &p, hipStream_t s)
 {
-    const size_t lds = dq_lds<T, DP>(p.len, p.grad_bias != nullptr ? p.waves : 0);
+    const size_t lds = dq_lds<T, DP>(p);
     const hipError_t e = allow(reinterpret_cast<const void *>(&window_dq_kernel<T, DP>), lds);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL((window_dq_kernel<T, DP>), dim3((unsigned)((p.units + 7) / 8 * 8)), dim3(64 * p.waves), lds, s, p);
@@ -386,7 +441,7 @@ hipError_t launch_dq(const WindowParams &p, hipStream_t s)
 template <typename T, int DP>
 hipError_t launch_dkv(const WindowParams &p, hipStream_t s)
 {
-    const size_t lds = dkv_lds<T, DP>(p.len);
+    const size_t lds = dkv_lds<T, DP>(p);
     const hipError_t e = allow(reinterpret_cast<const void *>(&window_dkv_kernel<T, DP>), lds);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL((window_dkv_kernel<T, DP>), dim3((unsigned)((p.units + 7) / 8 * 8)), dim3(64 * p.waves), lds, s, p);
@@ -395,17 +450,22 @@ hipError_t launch_dkv(const WindowParams &p, hipStream_t s)
 
 }  // namespace
 
-size_t window_dq_lds(bool f32, int dp, int len, int waves, bool bias_grad)
+int window_query_tiles(bool f32, int dp)
 {
-    const int tables = bias_grad ? waves : 0;
-    if (f32) return dp == 16 ? dq_lds<float, 16>(len, tables) : dp == 32 ? dq_lds<float, 32>(len, tables) : dq_lds<float, 64>(len, tables);
-    return dp == 16 ? dq_lds<uint16_t, 16>(len, tables) : dp == 32 ? dq_lds<uint16_t, 32>(len, tables) : dq_lds<uint16_t, 64>(len, tables);
+    if (f32) return dp == 16 ? WinGeom<float, 16>::QUERY_TILES : dp == 32 ? WinGeom<float, 32>::QUERY_TILES : WinGeom<float, 64>::QUERY_TILES;
+    return dp == 16 ? WinGeom<uint16_t, 16>::QUERY_TILES : dp == 32 ? WinGeom<uint16_t, 32>::QUERY_TILES : WinGeom<uint16_t, 64>::QUERY_TILES;
 }
 
-size_t window_dkv_lds(bool f32, int dp, int len)
+size_t window_dq_lds(const WindowParams &p, bool f32, int dp)
 {
-    if (f32) return dp == 16 ? dkv_lds<float, 16>(len) : dp == 32 ? dkv_lds<float, 32>(len) : dkv_lds<float, 64>(len);
-    return dp == 16 ? dkv_lds<uint16_t, 16>(len) : dp == 32 ? dkv_lds<uint16_t, 32>(len) : dkv_lds<uint16_t, 64>(len);
+    if (f32) return dp == 16 ? dq_lds<float, 16>(p) : dp == 32 ? dq_lds<float, 32>(p) : dq_lds<float, 64>(p);
+    return dp == 16 ? dq_lds<uint16_t, 16>(p) : dp == 32 ? dq_lds<uint16_t, 32>(p) : dq_lds<uint16_t, 64>(p);
+}
+
+size_t window_dkv_lds(const WindowParams &p, bool f32, int dp)
+{
+    if (f32) return dp == 16 ? dkv_lds<float, 16>(p) : dp == 32 ? dkv_lds<float, 32>(p) : dkv_lds<float, 64>(p);
+    return dp == 16 ? dkv_lds<uint16_t, 16>(p) : dp == 32 ? dkv_lds<uint16_t, 32>(p) : dkv_lds<uint16_t, 64>(p);
 }
 
 hipError_t launch_window_dq(const WindowParams &p, bool f32, int dp, hipStream_t s)

@@ -1,185 +1,245 @@
 // Window attention, forward: out = softmax(scale q.k + bias) v over the keys of a window, in one pass over the keys with a running
 // maximum and sum.
 //
-// A wavefront has 64 queries (two tiles of 32), a block up to four wavefronts, and goes through the window's keys TK at a time,
-// staged in LDS.  Scores are formed transposed (keys down, queries across: S^T = K Q^T), so that a lane holds 16 keys of ONE query:
+// A wavefront has one or two tiles of 32 queries, a block up to eight wavefronts, and goes through the window's keys TK at a time,
+// staged in LDS in two buffers.  Scores are formed transposed (keys down, queries across: S^T = K Q^T), so that a lane holds 16 keys of ONE query:
 // maximum and sum need no exchange but between the two halves of the wavefront, and the exponentials are, as they lie in registers,
-// the right operand of the next product O^T = V^T P^T.  The bias is the product's starting value.
+// the right operand of the next product O^T = V^T P^T.  The bias is the product's starting value.  The running maximum is followed only
+// where a score exceeds it by more than kSlack: the exponentials then reach 2^kSlack, and most tiles rescale nothing.
+//
+// Calls with fewer tiles than the chip has room for take one tile a wavefront and let up to four wavefronts share a tile's keys; their sums are
+// joined in LDS at the end.
 #include "esc_window.hpp"
 
 namespace esc {
 namespace {
 
+constexpr float kSlack = 8.f;
+
 // SAVE: the backward pass follows.  Its delta = sum over the channels of out * dout stands for sum over the keys of p * dp, and what it is off goes into every
 // term of the bias' gradient, an fp32 result: with bf16 storage the exponentials are then two bf16 terms (with one the bias' gradient
 // was 9e-5 off, with two 4e-7).
-template <typename T, int DP, bool SAVE>
-__global__ __launch_bounds__(256) void window_forward_kernel(const WindowParams p)
+template <typename T, int DP, int U, bool SAVE>
+__global__ __launch_bounds__(512) void window_forward_kernel(const WindowParams p)
 {
     using G = WinGeom<T, DP>;
+    using S = Stager<T, DP, true, false, false, true>;  // keys by tokens, values by channels
+    constexpr bool SUM_ROW = DP == 16;                  // the exponentials' sum is row 16 of the product
+    constexpr int VT = G::F32 ? 3 : SAVE ? 2 : 1;
     extern __shared__ __align__(16) char lds[];
-    char *rm = lds, *cm = rm + G::RM_BYTES;
-    int *off = reinterpret_cast<int *>(cm + G::CM_BYTES);
-    uint8_t *bits = reinterpret_cast<uint8_t *>(off + G::TK / 4);
-    float *table = reinterpret_cast<float *>(bits + G::TK / 4);
+    float *table = reinterpret_cast<float *>(lds + 2 * S::BYTES);
 
     const int unit = unit_of(p.units);
     if (unit < 0) return;
     const int block = unit % p.blocks, head = unit / p.blocks % p.heads, wi = unit / p.blocks / p.heads;
     const Win w = win_of(p, wi / (p.gy * p.gx), wi / p.gx % p.gy, wi % p.gx);
-    const int q0 = block * p.waves * kWinWaveTokens;
+    const int queries = p.waves / p.ksplit * (U * 32), q0 = block * queries;
     if (q0 >= w.L) return;
     const int centre = (p.wh - 1) * p.tw + p.ww - 1;
-    const TableRange range = table_range(q0, min(q0 + p.waves * kWinWaveTokens, w.L), w.h, w.wp, p.tw, centre, -1);
-    stage_table(p, table, range, head);
+    const TableRange range = table_range(q0, min(q0 + queries, w.L), w.h, w.wp, p.tw, centre, -1);
 
     const long hw = (long)p.H * p.W;
-    const int lane = threadIdx.x & 63, half = lane >> 5, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int share = wave % p.ksplit, wq0 = q0 + wave / p.ksplit * (U * 32);
     const int kvh = head / (p.heads / p.kv_heads);
     const T *q = static_cast<const T *>(p.q) + w.n * p.qs + head * (long)p.d * hw;
     const T *k = static_cast<const T *>(p.k) + w.n * p.ks + kvh * (long)p.d * hw;
     const T *v = static_cast<const T *>(p.v) + w.n * p.vs + kvh * (long)p.d * hw;
 
-    Fragment<T, DP> own[2];
-    long pixel[2];
-    bool ok[2], there[2];
-    int place[2];  // in the table, of the offset to the key that has off = 0
-    float top[2], sum[2];
-    wf32x16 acc[2][G::DT];
+    S stager;
+    stager.fetch(p, w, k, v, 0);
+    Fragment<T, DP> own[U];
+    int pixel[U], place[U];  // place: in the table, of the offset to the key that has off = 0
+    bool ok[U], there[U];
+    float top[U], sum[U];
+    wf32x16 acc[U][G::DT];
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-        const int t = q0 + wave * kWinWaveTokens + u * 32 + (lane & 31), tc = min(t, w.L - 1);
+    for (int u = 0; u < U; ++u) {
+        const int t = wq0 + u * 32 + (lane & 31), tc = min(t, w.L - 1);
         const int y = tc / w.wp, x = tc - y * w.wp;
         there[u] = t < w.L && x < w.w;
         ok[u] = there[u] && seen(p, w, y, x);
-        pixel[u] = (long)(w.y0 + y) * p.W + w.x0 + x;
+        pixel[u] = (w.y0 + y) * p.W + w.x0 + x;
         place[u] = centre - (y * p.tw + x) - range.base;
         own[u] = own_fragment<T, DP>(p, q + pixel[u], ok[u]);
         top[u] = -__builtin_inff(), sum[u] = 0.f;
 #pragma unroll
         for (int b = 0; b < G::DT; ++b) acc[u][b] = wf32x16{};
     }
-    const bool busy = q0 + wave * kWinWaveTokens < w.L;  // (the same for the wavefront)
+    stage_table(p, table, range, head);
+    S::ones(lds + S::CM1_AT);
+    S::ones(lds + S::BYTES + S::CM1_AT);
+    stager.write(p, w, k, v, 0, lds);
+    __syncthreads();
+    const float slack = kSlack / p.log2_scale;
+    const bool busy = wq0 < w.L;
 
-    for (int t0 = 0; t0 < w.L; t0 += G::TK) {
-        __syncthreads();
-        stage<T, DP, true, false>(p, w, k, t0, rm, nullptr, threadIdx.x, blockDim.x);
-        stage<T, DP, false, true>(p, w, v, t0, nullptr, cm, threadIdx.x, blockDim.x);
-        stage_tokens<G::TK>(p, w, t0, off, bits);
-        __syncthreads();
-        if (!busy) continue;
-        for (int tile = 0; tile < G::TK / 32 && t0 + tile * 32 < w.L; ++tile) {
-            const wu32x2 nibbles = *reinterpret_cast<const wu32x2 *>(bits + tile * 8);
-            const bool whole = __builtin_amdgcn_readfirstlane((int)((nibbles.x & nibbles.y) == 0x0f0f0f0fu));
+    for (int t0 = 0, turn = 0; t0 < w.L; t0 += G::TK, turn ^= 1) {
+        const bool more = t0 + G::TK < w.L;
+        if (more) stager.fetch(p, w, k, v, t0 + G::TK);
+        const char *buf = lds + turn * S::BYTES;
+        const int *off = reinterpret_cast<const int *>(buf + S::OFF_AT);
+        if (busy)
+            for (int tile = share; tile < G::TK / 32 && t0 + tile * 32 < w.L; tile += p.ksplit) {
+                const wu32x2 nibbles = *reinterpret_cast<const wu32x2 *>(buf + S::BITS_AT + tile * 8);
+                const bool whole = __builtin_amdgcn_readfirstlane((int)(nibbles.x & nibbles.y)) == 0x0f0f0f0f;
+                int key[4];
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                wf32x16 s;
+                for (int a = 0; a < 4; ++a) key[a] = off[tile * 8 + 2 * a + half];
+                Packed<VT> e[U];
 #pragma unroll
-                for (int a = 0; a < 4; ++a) {
-                    const float *from = table + place[u] + off[tile * 8 + 2 * a + half];
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) s[4 * a + j] = from[j];
-                }
-                s = score<T, DP>(rm, tile, own[u], s);
-                if (!whole) {
+                for (int u = 0; u < U; ++u) {
+                    wf32x16 s;
 #pragma unroll
                     for (int a = 0; a < 4; ++a) {
-                        const uint32_t b = (a < 2 ? nibbles.x : nibbles.y) >> (16 * (a & 1) + 8 * half);
+                        const float *from = table + place[u] + key[a];
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) s[4 * a + j] = (b >> j & 1) != 0 ? s[4 * a + j] : -__builtin_inff();
+                        for (int j = 0; j < 4; ++j) s[4 * a + j] = from[j];
                     }
+                    s = score<T, DP>(buf + S::RM0_AT, tile, own[u], s);
+                    if (!whole) {
+                        asm volatile("; keys that do not take part");  // (keeps the selection out of the way of whole tiles)
+#pragma unroll
+                        for (int a = 0; a < 4; ++a) {
+                            const uint32_t b = (a < 2 ? nibbles.x : nibbles.y) >> (16 * (a & 1) + 8 * half);
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) s[4 * a + j] = (b >> j & 1) != 0 ? s[4 * a + j] : -__builtin_inff();
+                        }
+                    }
+                    float m = fmaxf(s[0], s[1]);
+#pragma unroll
+                    for (int i = 2; i < 16; i += 2) m = fmaxf(fmaxf(m, s[i]), s[i + 1]);
+                    m = fmaxf(m, other_half(m));
+                    if (__any(m > top[u] + slack)) {
+                        const float old = top[u], next = fmaxf(old, m);
+                        // (a row that has seen no key yet has nothing to shrink)
+                        const float shrink = old == -__builtin_inff() ? 0.f : exp2_of((old - next) * p.log2_scale);
+                        top[u] = next;
+                        sum[u] *= shrink;
+#pragma unroll
+                        for (int b = 0; b < G::DT; ++b)
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) acc[u][b][i] *= shrink;
+                    }
+                    const float from = top[u] == -__builtin_inff() ? 0.f : top[u], shift = from * p.log2_scale;
+                    if (__builtin_expect(!__any(__builtin_fabsf(shift) > kLargeShift), 1)) {
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) s[i] = __builtin_fmaf(s[i], p.log2_scale, -shift);
+                    } else {
+                        asm volatile("; large scores");
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) s[i] = (s[i] - from) * p.log2_scale;
+                    }
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) s[i] = exp2_of(s[i]);
+                    if constexpr (!SUM_ROW) {
+                        float add = 0.f;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) add += s[i];
+                        sum[u] += add;
+                    }
+                    e[u] = pack<VT>(s);
                 }
-                float m = s[0];
-#pragma unroll
-                for (int i = 1; i < 16; ++i) m = fmaxf(m, s[i]);
-                m = fmaxf(m, other_half(m));
-                const float old = top[u], next = fmaxf(old, m), from = next == -__builtin_inff() ? 0.f : next;
-                const float shift = from * p.log2_scale;
-                float shrink;
-                if (__builtin_expect(!__any(__builtin_fabsf(shift) > kLargeShift), 1)) {
-                    shrink = old == -__builtin_inff() ? 0.f : exp2_of(old * p.log2_scale - shift);
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) s[i] = __builtin_fmaf(s[i], p.log2_scale, -shift);
-                } else {
-                    shrink = exp2_of((old - from) * p.log2_scale);
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) s[i] = (s[i] - from) * p.log2_scale;
-                }
-                top[u] = next;
-                float add = 0.f;
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    s[i] = exp2_of(s[i]);
-                    add += s[i];
-                }
-                sum[u] = __builtin_fmaf(sum[u], shrink, add);
-#pragma unroll
-                for (int b = 0; b < G::DT; ++b)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) acc[u][b][i] *= shrink;
-                accumulate<T, DP>(cm, tile, pack<G::F32 ? 3 : SAVE ? 2 : 1>(s), acc[u]);
+                accumulate<T, DP>(buf + S::CM1_AT, tile, e, acc);
             }
+        if (more) stager.write(p, w, k, v, t0 + G::TK, lds + (turn ^ 1) * S::BYTES);
+        __syncthreads();
+    }
+
+    if (p.ksplit > 1) {  // (uniform) one tile a wavefront then
+        constexpr int WORDS = 64 * (2 + G::DT * 16);
+        float *room = reinterpret_cast<float *>(lds);
+        if (share != 0) {
+            float *to = room + wave * WORDS + lane;
+            to[0] = top[0], to[64] = sum[0];
+#pragma unroll
+            for (int b = 0; b < G::DT; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) to[(2 + b * 16 + i) * 64] = acc[0][b][i];
+        }
+        __syncthreads();
+        if (share != 0) return;
+        for (int other = 1; other < p.ksplit; ++other) {
+            const float *from = room + (wave + other) * WORDS + lane;
+            const float mine = top[0], theirs = from[0], next = fmaxf(mine, theirs);
+            const float fm = mine == -__builtin_inff() ? 0.f : exp2_of((mine - next) * p.log2_scale);
+            const float ft = theirs == -__builtin_inff() ? 0.f : exp2_of((theirs - next) * p.log2_scale);
+            top[0] = next;
+            sum[0] = sum[0] * fm + from[64] * ft;
+#pragma unroll
+            for (int b = 0; b < G::DT; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) acc[0][b][i] = acc[0][b][i] * fm + from[(2 + b * 16 + i) * 64] * ft;
         }
     }
     if (!busy) return;
-    T *out = static_cast<T *>(p.out) + ((long)w.n * p.heads + head) * p.d * hw;
+    const long planes = ((long)w.n * p.heads + head) * p.d * hw, row = ((long)w.n * p.heads + head) * hw;
+    T *out = static_cast<T *>(p.out) + planes;
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-        const float all = sum[u] + other_half(sum[u]);
+    for (int u = 0; u < U; ++u) {
+        float all;
+        if constexpr (SUM_ROW) {  // (row 16 lies with the lower half)
+            const float low = other_half(acc[u][0][8]);
+            all = half == 0 ? acc[u][0][8] : low;
+        } else {
+            all = sum[u] + other_half(sum[u]);
+        }
         if (!there[u]) continue;
         const bool some = ok[u] && !(all == 0.f);
         const float over = some ? 1.f / all : 0.f;
-        const long pix = ((long)w.n * p.heads + head) * hw + pixel[u];
         if (SAVE && half == 0) {
-            p.top[pix] = some && top[u] != -__builtin_inff() ? top[u] : 0.f;
-            p.log_sum[pix] = some ? __builtin_log2f(all) : __builtin_inff();
+            p.top[row + pixel[u]] = some && top[u] != -__builtin_inff() ? top[u] : 0.f;
+            p.log_sum[row + pixel[u]] = some ? __builtin_log2f(all) : __builtin_inff();
         }
 #pragma unroll
         for (int b = 0; b < G::DT; ++b)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
+            for (int i = 0; i < (DP == 16 ? 8 : 16); ++i) {
                 const int c = b * 32 + 8 * (i / 4) + 4 * half + i % 4;
                 if (c < p.d) {
                     const float o = some ? acc[u][b][i] * over : 0.f;
                     const T r = narrow<T>(o);
                     out[c * hw + pixel[u]] = r;
-                    if constexpr (SAVE && !G::F32) static_cast<T *>(p.rest)[((long)w.n * p.heads + head) * p.d * hw + c * hw + pixel[u]] = to_bf16(o - widen(r));
+                    if constexpr (SAVE && !G::F32) static_cast<T *>(p.rest)[planes + c * hw + pixel[u]] = to_bf16(o - widen(r));
                 }
             }
     }
 }
 
 template <typename T, int DP>
-size_t lds_of(int len)
+size_t lds_of(int len, int waves)
 {
     using G = WinGeom<T, DP>;
-    return G::RM_BYTES + G::CM_BYTES + (G::TK / 4) * 5 + (size_t)len * 4;
+    const size_t staged = 2 * Stager<T, DP, true, false, false, true>::BYTES + (size_t)len * 4, joined = (size_t)waves * 256 * (2 + G::DT * 16);
+    return staged > joined ? staged : joined;
 }
 
-template <typename T, int DP, bool SAVE>
+template <typename T, int DP, int U, bool SAVE>
 hipError_t launch_one(const WindowParams &p, hipStream_t s)
 {
-    const size_t lds = lds_of<T, DP>(p.len);
+    const size_t lds = lds_of<T, DP>(p.len, p.ksplit > 1 ? p.waves : 0);
     if (lds > 64 * 1024) {
-        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&window_forward_kernel<T, DP, SAVE>), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&window_forward_kernel<T, DP, U, SAVE>), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
         if (e != hipSuccess) return e;
     }
-    hipLaunchKernelGGL((window_forward_kernel<T, DP, SAVE>), dim3((unsigned)((p.units + 7) / 8 * 8)), dim3(64 * p.waves), lds, s, p);
+    hipLaunchKernelGGL((window_forward_kernel<T, DP, U, SAVE>), dim3((unsigned)((p.units + 7) / 8 * 8)), dim3(64 * p.waves), lds, s, p);
     return hipGetLastError();
 }
 
 template <typename T, int DP>
 hipError_t launch(const WindowParams &p, hipStream_t s)
 {
-    return p.top != nullptr ? launch_one<T, DP, true>(p, s) : launch_one<T, DP, false>(p, s);
+    if (p.tiles == 1) return p.top != nullptr ? launch_one<T, DP, 1, true>(p, s) : launch_one<T, DP, 1, false>(p, s);
+    if constexpr (std::is_same<T, float>::value && DP == 64) return hipErrorInvalidValue;  // (two tiles would not fit the registers)
+    else return p.top != nullptr ? launch_one<T, DP, 2, true>(p, s) : launch_one<T, DP, 2, false>(p, s);
 }
 
 }  // namespace
 
-size_t window_forward_lds(bool f32, int dp, int len)
+size_t window_forward_lds(bool f32, int dp, int len, int joined)
 {
-    if (f32) return dp == 16 ? lds_of<float, 16>(len) : dp == 32 ? lds_of<float, 32>(len) : lds_of<float, 64>(len);
-    return dp == 16 ? lds_of<uint16_t, 16>(len) : dp == 32 ? lds_of<uint16_t, 32>(len) : lds_of<uint16_t, 64>(len);
+    if (f32) return dp == 16 ? lds_of<float, 16>(len, joined) : dp == 32 ? lds_of<float, 32>(len, joined) : lds_of<float, 64>(len, joined);
+    return dp == 16 ? lds_of<uint16_t, 16>(len, joined) : dp == 32 ? lds_of<uint16_t, 32>(len, joined) : lds_of<uint16_t, 64>(len, joined);
 }
 
 hipError_t launch_window_forward(const WindowParams &p, bool f32, int dp, hipStream_t s)
