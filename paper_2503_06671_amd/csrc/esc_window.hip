@@ -82,6 +82,7 @@ esc_status shape(const esc_window_attn *a, WindowParams *p)
     p->win_h = a->win_h, p->win_w = a->win_w;
     p->wh = std::min(a->win_h, a->H), p->ww = std::min(a->win_w, a->W);
     p->gy = (a->H + p->wh - 1) / p->wh, p->gx = (a->W + p->ww - 1) / p->ww;
+    p->pairs = a->H > 1 || a->W > 1;
     p->th = 2 * p->wh - 1, p->tw = 2 * p->ww - 1;
     if ((long)p->th * p->tw > kWinMaxOffsets) return ESC_ERR_UNSUPPORTED;
     p->n_edges = a->n_edges;
@@ -207,14 +208,10 @@ esc_status common(const void *q, const void *k, const void *v, esc_dtype dt, con
     p->q = q, p->k = k, p->v = v;
     p->qs = (long)(in[0].stride / es), p->ks = (long)(in[1].stride / es), p->vs = (long)(in[2].stride / es);
     p->bias = a->bias, p->mask = a->mask;
+    // (without a mask, the first image of k: more bytes than a plane has pixels)
+    p->mask_read = a->mask != nullptr ? a->mask : static_cast<const uint8_t *>(k), p->mask_step = a->mask != nullptr ? (long)plane : 0;
     p->scale = a->scale, p->inv_scale = 1.f / a->scale, p->log2_scale = (float)((double)a->scale * 1.4426950408889634);
     return ESC_OK;
-}
-
-// Four pixels of a row at a time: rows, windows, images and bases at multiples of four elements.
-bool by_fours(const WindowParams &p, const void *base, long stride, size_t es)
-{
-    return p.W % 4 == 0 && (p.ww % 4 == 0 || p.gx == 1) && stride % 4 == 0 && (uintptr_t)base % (4 * es) == 0;
 }
 
 }  // namespace
@@ -263,7 +260,6 @@ esc_status esc_window_attention_forward(const void *q, const void *k, const void
         p.log_sum = p.top + (size_t)p.N * p.heads * p.H * p.W;
         p.rest = dt == ESC_BF16 ? static_cast<char *>(saved) + rows_bytes(p) : nullptr;
     }
-    p.vec = by_fours(p, k, p.ks, es) && by_fours(p, v, p.vs, es);
     if (!plan_forward(p, dt == ESC_F32)) return ESC_ERR_UNSUPPORTED;
     return launch_window_forward(p, dt == ESC_F32, dim_padded(p.d), static_cast<hipStream_t>(stream)) == hipSuccess ? ESC_OK : ESC_ERR_HIP;
 }
@@ -326,8 +322,6 @@ esc_status esc_window_attention_backward(const void *q, const void *k, const voi
         x->part = reinterpret_cast<float *>(ws + sc.part);
         x->part2 = reinterpret_cast<float *>(ws + sc.part2);
     }
-    pq.vec = by_fours(p, k, p.ks, es) && by_fours(p, v, p.vs, es);
-    pk.vec = by_fours(p, q, p.qs, es) && by_fours(p, grad_out, (long)(in[0].bytes / es), es);
     hipStream_t s = static_cast<hipStream_t>(stream);
     const int dp = dim_padded(p.d);
     if (launch_window_dq(pq, f32, dp, s) != hipSuccess || launch_window_dkv(pk, f32, dp, s) != hipSuccess) return ESC_ERR_HIP;

@@ -44,6 +44,8 @@ struct WindowParams {
     float *grad_bias;
     const float *bias;                   // [heads, nby, nbx] or nullptr
     const uint8_t *mask;                 // [N, H, W] or nullptr
+    const uint8_t *mask_read;            // what is read in its place where there is none (and not used), so that the loads need no condition
+    long mask_step;
     int N, H, W, heads, kv_heads, d;
     int win_h, win_w;                    // as the table has them
     int wh, ww;                          // cut to the map
@@ -54,7 +56,7 @@ struct WindowParams {
     int blocks, units, waves, len;       // blocks a window and head, all blocks, wavefronts a block, words of a block's table
     int tiles, ksplit;                   // tiles of 32 tokens of a wavefront; forward: wavefronts that share a tile's keys
     int buffers, ring, part_len;         // backward: staging buffers; words of a wavefront's ring (a power of two) and of its part
-    int vec;                             // four pixels at a time
+    int pairs;                           // planes have two pixels at least
     int splits, accumulate;
     float scale, inv_scale, log2_scale;  // scale * log2(e) last
 };
@@ -83,7 +85,7 @@ template <typename T, int DP>
 struct WinGeom {
     static constexpr bool F32 = std::is_same<T, float>::value;
     static constexpr int NT = F32 ? 3 : 1;
-    static constexpr int TK = F32 && DP == 64 ? 32 : 64;
+    static constexpr int TK = F32 ? (DP == 64 ? 32 : 64) : (DP == 16 ? 128 : 64);
     static constexpr int KS = DP / 16;                 // matrix instructions a score takes (of each pair of terms)
     static constexpr int DT = DP <= 32 ? 1 : 2;        // blocks of 32 channels of an output
 #ifndef DQT
@@ -178,159 +180,151 @@ __device__ __forceinline__ bool seen(const WindowParams &p, const Win &w, int y,
 __device__ __forceinline__ uint32_t low_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); }
 __device__ __forceinline__ uint32_t high_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
 
-// Offsets (of groups of four tokens) and the bits of those that take part.
-template <int TK>
-__device__ __forceinline__ void stage_tokens(const WindowParams &p, const Win &w, int t0, int *off, uint8_t *bits)
-{
-    const int g = threadIdx.x;
-    if (g >= TK / 4) return;
-    const int t = t0 + 4 * g;
-    int o = 0, b = 0;
-    if (t < w.L) {
+// Where a group of tokens t ... lies in its image's planes: `at`, which `near` brings so far from the plane's end that `n` elements can be read
+// from there, and how many of them to skip then; which of the n tokens exist (but for the mask).
+struct Spot {
+    int at, skip;
+    uint32_t bits;
+    __device__ __forceinline__ Spot(const WindowParams &p, const Win &w, int t, int n)
+    {
         const int y = t / w.wp, x = t - y * w.wp;
-        o = y * p.tw + x;
-        for (int j = 0; j < 4; ++j) b |= seen(p, w, y, x + j) ? 1 << j : 0;
+        const bool in = t < w.L;
+        const int pos = in ? (w.y0 + y) * p.W + w.x0 + x : 0;
+        at = max(min(pos, p.H * p.W - n), 0), skip = pos - at;
+        bits = in ? (1u << max(min(w.w - x, n), 0)) - 1 : 0u;
     }
-    off[g] = o;
-    bits[g] = (uint8_t)b;
+};
+
+// Offsets of groups of four tokens.
+template <int TK>
+__device__ __forceinline__ void stage_offsets(const WindowParams &p, const Win &w, int t0, int *off)
+{
+    if (threadIdx.x >= TK / 4) return;
+    const int t = t0 + 4 * threadIdx.x, y = t / w.wp, x = t - y * w.wp;
+    off[threadIdx.x] = t < w.L ? y * p.tw + x : 0;
 }
 
-// Four tokens of eight channels of one operand on their way from memory into LDS.
+// A lane's 16 tokens of a staged tile, of which those whose pair's bit is not set get `none`.  bits: a byte for each pair of tokens.
+__device__ __forceinline__ bool all_take_part(wu32x4 bits)
+{
+    return __builtin_amdgcn_readfirstlane((int)(bits.x & bits.y & bits.z & bits.w)) == 0x03030303;
+}
+__device__ __forceinline__ void leave_out(wu32x4 bits, float none, wf32x16 &s)
+{
+    const int half = (threadIdx.x >> 5) & 1;
+#pragma unroll
+    for (int a = 0; a < 4; ++a) {
+        const uint32_t b = bits[a] >> 16 * half;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s[4 * a + j] = (b >> (8 * (j / 2) + j % 2) & 1) != 0 ? s[4 * a + j] : none;
+    }
+}
+
+// Two tokens of four channels of one operand on their way from memory into LDS: as they come (fetch asks for nothing under a condition, so that
+// nothing waits for an answer before `store`), and cleaned and laid out.  Reads need no alignment beyond the element's.
 template <typename T, int DP>
 struct Piece {
     using G = WinGeom<T, DP>;
-    using Four = typename std::conditional<G::F32, wf32x4, wu32x2>::type;
-    Four v[8];
+    using Two = typename std::conditional<G::F32, wf32x2, uint32_t>::type;
+    Two v[4];
+    uint16_t mask;  // (two bytes)
 
-    // tokens t ... t + 3 of the channels from 8 * d8 on; `plane` is channel 0 of the head's planes of this image
-    __device__ __forceinline__ void load(const WindowParams &p, const Win &w, const T *plane, int t, int d8)
+    __device__ __forceinline__ void fetch(const WindowParams &p, const Win &w, const T *plane, int t, int c4)
     {
         const long hw = (long)p.H * p.W;
-        const int y = t / w.wp, x = t - y * w.wp;
-        const bool in = t < w.L;
-        const T *at = plane + (in ? (long)(w.y0 + y) * p.W + w.x0 + x : 0) + (long)(d8 * 8) * hw;
-        bool ok[4];
+        const Spot s(p, w, t, 2);
+        const T *a[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) ok[j] = in && x + j < w.w;
-        if (p.vec) {
+        for (int i = 0; i < 4; ++i) a[i] = plane + min(c4 * 4 + i, p.d - 1) * hw + s.at;
+        const uint8_t *m = p.mask_read + w.n * p.mask_step + s.at;
+        if (p.pairs) {  // (uniform: not where a plane is one pixel)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                v[i] = Four{};
-                if (in && d8 * 8 + i < p.d) v[i] = *reinterpret_cast<const Four *>(at + i * hw);
-            }
+            for (int i = 0; i < 4; ++i) __builtin_memcpy(&v[i], a[i], sizeof(Two));
+            __builtin_memcpy(&mask, m, 2);
         } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                T e[4];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) e[j] = ok[j] && d8 * 8 + i < p.d ? at[i * hw + j] : T(0);
-                __builtin_memcpy(&v[i], e, sizeof(Four));
+            for (int i = 0; i < 4; ++i) {
+                const T e[2] = {a[i][0], T(0)};
+                __builtin_memcpy(&v[i], e, sizeof(Two));
             }
-        }
-        if (p.mask != nullptr) {
-            const uint8_t *m = p.mask + ((long)w.n * p.H + w.y0 + y) * p.W + w.x0 + x;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) ok[j] = ok[j] && m[j] != 0;
-        }
-        if (!(ok[0] && ok[1] && ok[2] && ok[3])) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                if constexpr (G::F32) {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) v[i][j] = ok[j] ? v[i][j] : 0.f;
-                } else {
-                    v[i].x &= (ok[0] ? 0xffffu : 0u) | (ok[1] ? 0xffff0000u : 0u);
-                    v[i].y &= (ok[2] ? 0xffffu : 0u) | (ok[3] ? 0xffff0000u : 0u);
-                }
-            }
+            mask = m[0];
         }
     }
 
-    // g: the group of four within the staged tokens
+    // g2: the pair within the staged tokens
     template <bool RM, bool CM>
-    __device__ __forceinline__ void store(char *rm, char *cm, int g, int d8) const
+    __device__ __forceinline__ void store(const WindowParams &p, const Win &w, int t, char *rm, char *cm, uint8_t *bits, int g2, int c4) const
     {
-        uint32_t word[G::NT][8][2];  // [term][channel][pair of tokens]
+        const Spot s(p, w, t, 2);
+        const uint32_t m = p.mask != nullptr ? mask >> 8 * s.skip : 0x101u;
+        const bool ok0 = (s.bits & 1) != 0 && (m & 0xff) != 0, ok1 = (s.bits & 2) != 0 && (m & 0xff00) != 0;
+        if (bits != nullptr && c4 == 0) bits[g2] = (uint8_t)((ok0 ? 1 : 0) | (ok1 ? 2 : 0));
+        uint32_t word[G::NT][4];  // [term][channel]: both tokens
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < 4; ++i) {
+            const bool c = c4 * 4 + i < p.d;
             if constexpr (G::F32) {
-                uint32_t t01[3], t23[3];
-                split_bf16(v[i][0], v[i][1], t01);
-                split_bf16(v[i][2], v[i][3], t23);
+                uint32_t q[3];
+                split_bf16(c && ok0 ? (s.skip != 0 ? v[i].y : v[i].x) : 0.f, c && ok1 ? v[i].y : 0.f, q);
 #pragma unroll
-                for (int q = 0; q < 3; ++q) word[q][i][0] = t01[q], word[q][i][1] = t23[q];
+                for (int k = 0; k < 3; ++k) word[k][i] = q[k];
             } else {
-                word[0][i][0] = v[i].x, word[0][i][1] = v[i].y;
+                const uint32_t x = s.skip != 0 ? v[i] >> 16 : v[i];
+                word[0][i] = c ? x & ((ok0 ? 0xffffu : 0u) | (ok1 ? 0xffff0000u : 0u)) : 0u;
             }
         }
+        const int g = g2 / 2, odd = g2 & 1;
 #pragma unroll
-        for (int q = 0; q < G::NT; ++q) {
+        for (int k = 0; k < G::NT; ++k) {
             if constexpr (RM) {
-                wu32x4 *to = reinterpret_cast<wu32x4 *>(rm) + q * G::RM_TERM + d8 * 4 * G::SLOT + g;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    wu32x4 r;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        r[i] = j % 2 == 0 ? low_halves(word[q][2 * i][j / 2], word[q][2 * i + 1][j / 2]) : high_halves(word[q][2 * i][j / 2], word[q][2 * i + 1][j / 2]);
-                    to[j * G::SLOT] = r;
-                }
+                char *to = rm + ((k * G::RM_TERM + (c4 >> 1) * 4 * G::SLOT + odd * 2 * G::SLOT + g) * 16 + (c4 & 1) * 8);
+                *reinterpret_cast<wu32x2 *>(to) = wu32x2{low_halves(word[k][0], word[k][1]), low_halves(word[k][2], word[k][3])};
+                *reinterpret_cast<wu32x2 *>(to + G::SLOT * 16) = wu32x2{high_halves(word[k][0], word[k][1]), high_halves(word[k][2], word[k][3])};
             }
             if constexpr (CM) {
                 const int place = (g & ~3) | ((g & 1) << 1) | ((g & 2) >> 1);
-                char *to = cm + q * G::CM_TERM + d8 * 8 * G::CM_ROW + place * 8;
+                char *to = cm + k * G::CM_TERM + c4 * 4 * G::CM_ROW + place * 8 + odd * 4;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) *reinterpret_cast<wu32x2 *>(to + i * G::CM_ROW) = wu32x2{word[q][i][0], word[q][i][1]};
+                for (int i = 0; i < 4; ++i) *reinterpret_cast<uint32_t *>(to + i * G::CM_ROW) = word[k][i];
             }
         }
     }
 };
 
 // Two operands staged a chunk of TK tokens at a time into two buffers in turn.  A block's threads fetch the next chunk into registers before
-// they multiply this one (as many pieces as there are threads; where a block has fewer threads, the rest follows behind).
+// they multiply this one (a piece each; where a block has so few threads that there are more pieces, the rest follows behind).
 template <typename T, int DP, bool RM0, bool CM0, bool RM1, bool CM1>
 struct Stager {
     using G = WinGeom<T, DP>;
-    static constexpr int GROUPS = G::TK / 4;
-    static constexpr int ITEMS = 2 * (DP / 8) * GROUPS;
+    static constexpr int GROUPS = G::TK / 4, PAIRS = G::TK / 2;
+    static constexpr int HALF = DP / 4 * PAIRS, ITEMS = 2 * HALF;
     static constexpr int RM0_AT = 0, CM0_AT = RM0_AT + (RM0 ? G::RM_BYTES : 0), RM1_AT = CM0_AT + (CM0 ? G::CM_BYTES : 0),
-                         CM1_AT = RM1_AT + (RM1 ? G::RM_BYTES : 0), OFF_AT = CM1_AT + (CM1 ? G::CM_BYTES : 0), BITS_AT = OFF_AT + GROUPS * 4,
-                         BYTES = (BITS_AT + GROUPS + 15) / 16 * 16;
+                         CM1_AT = RM1_AT + (RM1 ? G::RM_BYTES : 0), BITS_AT = CM1_AT + (CM1 ? G::CM_BYTES : 0), OFF_AT = BITS_AT + PAIRS,
+                         BYTES = (OFF_AT + GROUPS * 4 + 15) / 16 * 16;
     Piece<T, DP> next;
 
-    __device__ __forceinline__ static void place(int item, int *which, int *g, int *d8)
+    __device__ __forceinline__ static int pair_of(int item) { return item % PAIRS; }
+    __device__ __forceinline__ static int channels_of(int item) { return item % HALF / PAIRS; }
+    __device__ __forceinline__ static void put(const Piece<T, DP> &piece, const WindowParams &p, const Win &w, int t0, int item, char *buf)
     {
-        *which = item / (ITEMS / 2);
-        const int i = item % (ITEMS / 2);
-        *g = i % GROUPS, *d8 = i / GROUPS;
-    }
-    __device__ __forceinline__ static void put(const Piece<T, DP> &piece, int item, char *buf)
-    {
-        int which, g, d8;
-        place(item, &which, &g, &d8);
-        if (which == 0) piece.template store<RM0, CM0>(buf + RM0_AT, buf + CM0_AT, g, d8);
-        else piece.template store<RM1, CM1>(buf + RM1_AT, buf + CM1_AT, g, d8);
+        const int g2 = pair_of(item), c4 = channels_of(item);
+        if (item < HALF) piece.template store<RM0, CM0>(p, w, t0 + 2 * g2, buf + RM0_AT, buf + CM0_AT, reinterpret_cast<uint8_t *>(buf + BITS_AT), g2, c4);
+        else piece.template store<RM1, CM1>(p, w, t0 + 2 * g2, buf + RM1_AT, buf + CM1_AT, nullptr, g2, c4);
     }
     __device__ __forceinline__ void fetch(const WindowParams &p, const Win &w, const T *op0, const T *op1, int t0)
     {
-        int which, g, d8;
-        const int item = threadIdx.x;
-        if (item < ITEMS) {
-            place(item, &which, &g, &d8);
-            next.load(p, w, which == 0 ? op0 : op1, t0 + 4 * g, d8);
-        }
+        const int item = min((int)threadIdx.x, ITEMS - 1);
+        next.fetch(p, w, item < HALF ? op0 : op1, t0 + 2 * pair_of(item), channels_of(item));
     }
     __device__ __forceinline__ void write(const WindowParams &p, const Win &w, const T *op0, const T *op1, int t0, char *buf)
     {
-        if ((int)threadIdx.x < ITEMS) put(next, threadIdx.x, buf);
+        if ((int)threadIdx.x < ITEMS) put(next, p, w, t0, threadIdx.x, buf);
         for (int item = threadIdx.x + blockDim.x; item < ITEMS; item += blockDim.x) {
-            int which, g, d8;
-            place(item, &which, &g, &d8);
             Piece<T, DP> piece;
-            piece.load(p, w, which == 0 ? op0 : op1, t0 + 4 * g, d8);
-            put(piece, item, buf);
+            piece.fetch(p, w, item < HALF ? op0 : op1, t0 + 2 * pair_of(item), channels_of(item));
+            put(piece, p, w, t0, item, buf);
         }
-        stage_tokens<G::TK>(p, w, t0, reinterpret_cast<int *>(buf + OFF_AT), reinterpret_cast<uint8_t *>(buf + BITS_AT));
+        stage_offsets<G::TK>(p, w, t0, reinterpret_cast<int *>(buf + OFF_AT));
     }
     // the rows of ones (DP = 16), once for each buffer
     __device__ __forceinline__ static void ones(char *cm)

@@ -112,8 +112,8 @@ __global__ __launch_bounds__(512) void window_dq_kernel(const WindowParams p)
         const char *buf = lds + turn * S::BYTES;
         const int *off = reinterpret_cast<const int *>(buf + S::OFF_AT);
         auto tile_of = [&](int tile, auto large) {
-            const wu32x2 nibbles = *reinterpret_cast<const wu32x2 *>(buf + S::BITS_AT + tile * 8);
-            const bool whole = all && __builtin_amdgcn_readfirstlane((int)(nibbles.x & nibbles.y)) == 0x0f0f0f0f;
+            const wu32x4 bits = *reinterpret_cast<const wu32x4 *>(buf + S::BITS_AT + tile * 16);
+            const bool whole = all && all_take_part(bits);
             int key[4];
 #pragma unroll
             for (int a = 0; a < 4; ++a) key[a] = off[tile * 8 + 2 * a + half];
@@ -138,12 +138,9 @@ __global__ __launch_bounds__(512) void window_dq_kernel(const WindowParams p)
                 }
                 if (!whole) {
                     asm volatile("; tokens that do not take part");
+                    leave_out(bits, 0.f, ds[u]);
 #pragma unroll
-                    for (int a = 0; a < 4; ++a) {
-                        const uint32_t b = (a < 2 ? nibbles.x : nibbles.y) >> (16 * (a & 1) + 8 * half);
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) ds[u][4 * a + j] = ok[u] && (b >> j & 1) != 0 ? ds[u][4 * a + j] : 0.f;
-                    }
+                    for (int i = 0; i < 16; ++i) ds[u][i] = ok[u] ? ds[u][i] : 0.f;
                 }
                 e[u] = pack<G::NT>(ds[u]);
             }
@@ -202,8 +199,9 @@ __global__ __launch_bounds__(512) void window_dkv_kernel(const WindowParams p)
     using G = WinGeom<T, DP>;
     using S = Stager<T, DP, true, true, true, true>;  // queries and the result's gradient, by tokens and by channels
     constexpr int U = 1;
-    // of the staged queries: the exponent's shift (with the sum's logarithm; without it and the largest score, where a shift is large), -delta
-    constexpr int ROWS_AT = S::BYTES, FAR_AT = ROWS_AT + 3 * G::TK * 4, BYTES = FAR_AT + 16;
+    // of the staged queries: the exponent's shift with the sum's logarithm, -delta; for large shifts the largest score and the logarithm
+    // by themselves; a flag of each wavefront that has seen such a shift
+    constexpr int ROWS_AT = S::BYTES, FAR_AT = ROWS_AT + 4 * G::TK * 4, BYTES = FAR_AT + 4 * kWinMaxWaves;
     extern __shared__ __align__(16) char lds[];
     float *table = reinterpret_cast<float *>(lds + p.buffers * BYTES);
 
@@ -227,29 +225,33 @@ __global__ __launch_bounds__(512) void window_dkv_kernel(const WindowParams p)
 
     // a chunk's number counts through the group's heads
     S stager;
-    float from, log_sum, minus;  // of this thread's query of the next chunk
+    float from, log_sum, delta;  // of this thread's query of the next chunk, as they come
+    auto fetch_row = [&](int head, int t) {
+        const long pix = ((long)w.n * p.heads + head) * hw + Spot(p, w, t, 1).at;
+        from = p.top[pix], log_sum = p.log_sum[pix], delta = p.delta[pix];
+    };
     auto fetch = [&](int c) {
         const int head = kvh * group + c / chunks, t0 = c % chunks * G::TK;
         stager.fetch(p, w, q + head * (long)p.d * hw, go + head * (long)p.d * hw, t0);
-        from = 0.f, log_sum = __builtin_inff(), minus = 0.f;
-        if (threadIdx.x < G::TK) {
-            const int t = t0 + threadIdx.x, y = t / w.wp, x = t - y * w.wp;
-            if (t < w.L && seen(p, w, y, x)) {
-                const long pix = ((long)w.n * p.heads + head) * hw + (long)(w.y0 + y) * p.W + w.x0 + x;
-                from = p.top[pix], log_sum = p.log_sum[pix], minus = -p.delta[pix];
-            }
-        }
+        fetch_row(head, t0 + min((int)threadIdx.x, G::TK - 1));
     };
     auto write = [&](int c, char *buf) {
         const int head = kvh * group + c / chunks, t0 = c % chunks * G::TK;
         stager.write(p, w, q + head * (long)p.d * hw, go + head * (long)p.d * hw, t0, buf);
-        if (threadIdx.x < G::TK) {  // (threads of one wavefront)
-            float *rows = reinterpret_cast<float *>(buf + ROWS_AT) + threadIdx.x;
-            const bool far = __any(__builtin_fabsf(from * p.log2_scale) > kLargeShift);
-            rows[0] = far ? log_sum : from * p.log2_scale + log_sum;
-            rows[G::TK] = from, rows[2 * G::TK] = minus;
-            if (threadIdx.x == 0) *reinterpret_cast<int *>(buf + FAR_AT) = far;
+        bool large = false;
+        for (int r = threadIdx.x; r < G::TK; r += blockDim.x) {
+            if (r != (int)threadIdx.x) fetch_row(head, t0 + r);
+            // (masked pixels have a sum of +infinity and a delta of 0; those beyond the window get them here)
+            const bool in = Spot(p, w, t0 + r, 1).bits != 0;
+            float *rows = reinterpret_cast<float *>(buf + ROWS_AT) + r;
+            const float shift = in ? from * p.log2_scale : 0.f, l = in ? log_sum : __builtin_inff();
+            large = large || __builtin_fabsf(shift) > kLargeShift;
+            rows[0] = shift + l, rows[G::TK] = in ? -delta : 0.f, rows[2 * G::TK] = from, rows[3 * G::TK] = l;
         }
+        int *flags = reinterpret_cast<int *>(buf + FAR_AT);
+        const bool any = __any(large);
+        if (lane == 0) flags[wave] = any;
+        if ((int)threadIdx.x >= p.waves && threadIdx.x < kWinMaxWaves) flags[threadIdx.x] = 0;
     };
     fetch(0);
     Fragment<T, DP> own_k[U], own_v[U];
@@ -280,10 +282,11 @@ __global__ __launch_bounds__(512) void window_dkv_kernel(const WindowParams p)
         const char *buf = lds + turn * BYTES;
         const int *off = reinterpret_cast<const int *>(buf + S::OFF_AT);
         const float *rows = reinterpret_cast<const float *>(buf + ROWS_AT);
-        const bool far = __builtin_amdgcn_readfirstlane(*reinterpret_cast<const int *>(buf + FAR_AT)) != 0;
+        const wu32x4 flags = *reinterpret_cast<const wu32x4 *>(buf + FAR_AT) | *reinterpret_cast<const wu32x4 *>(buf + FAR_AT + 16);
+        const bool far = __builtin_amdgcn_readfirstlane((int)(flags.x | flags.y | flags.z | flags.w)) != 0;
         auto tile_of = [&](int tile, auto large) {
-            const wu32x2 nibbles = *reinterpret_cast<const wu32x2 *>(buf + S::BITS_AT + tile * 8);
-            const bool whole = __builtin_amdgcn_readfirstlane((int)(nibbles.x & nibbles.y)) == 0x0f0f0f0f;
+            const wu32x4 bits = *reinterpret_cast<const wu32x4 *>(buf + S::BITS_AT + tile * 16);
+            const bool whole = all_take_part(bits);
             Packed<G::NT> ep[U], es[U];
 #pragma unroll
             for (int u = 0; u < U; ++u) {
@@ -291,7 +294,7 @@ __global__ __launch_bounds__(512) void window_dkv_kernel(const WindowParams p)
 #pragma unroll
                 for (int a = 0; a < 4; ++a) {
                     const float *at = table + place[u] - off[tile * 8 + 2 * a + half];
-                    const wf32x4 d = *reinterpret_cast<const wf32x4 *>(rows + 2 * G::TK + tile * 32 + 8 * a + 4 * half);
+                    const wf32x4 d = *reinterpret_cast<const wf32x4 *>(rows + G::TK + tile * 32 + 8 * a + 4 * half);
 #pragma unroll
                     for (int j = 0; j < 4; ++j) s[4 * a + j] = at[-j], dp[4 * a + j] = d[j];
                 }
@@ -299,9 +302,10 @@ __global__ __launch_bounds__(512) void window_dkv_kernel(const WindowParams p)
                 dp = score<T, DP>(buf + S::RM1_AT, tile, own_v[u], dp);
 #pragma unroll
                 for (int a = 0; a < 4; ++a) {
-                    const wf32x4 l = *reinterpret_cast<const wf32x4 *>(rows + tile * 32 + 8 * a + 4 * half);
+                    const float *at = rows + (decltype(large)::value ? 3 * G::TK : 0) + tile * 32 + 8 * a + 4 * half;
+                    const wf32x4 l = *reinterpret_cast<const wf32x4 *>(at);
                     wf32x4 m;
-                    if constexpr (decltype(large)::value) m = *reinterpret_cast<const wf32x4 *>(rows + G::TK + tile * 32 + 8 * a + 4 * half);
+                    if constexpr (decltype(large)::value) m = *reinterpret_cast<const wf32x4 *>(at - G::TK);
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         float x = s[4 * a + j];
@@ -311,12 +315,7 @@ __global__ __launch_bounds__(512) void window_dkv_kernel(const WindowParams p)
                 }
                 if (!whole) {
                     asm volatile("; queries that do not take part");
-#pragma unroll
-                    for (int a = 0; a < 4; ++a) {
-                        const uint32_t b = (a < 2 ? nibbles.x : nibbles.y) >> (16 * (a & 1) + 8 * half);
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) s[4 * a + j] = (b >> j & 1) != 0 ? s[4 * a + j] : 0.f;
-                    }
+                    leave_out(bits, 0.f, s);
                 }
                 ep[u] = pack<G::NT>(s);
 #pragma unroll
@@ -421,7 +420,7 @@ size_t dq_lds(const WindowParams &p)
 template <typename T, int DP>
 size_t dkv_lds(const WindowParams &p)
 {
-    return p.buffers * (size_t)(Stager<T, DP, true, true, true, true>::BYTES + 3 * WinGeom<T, DP>::TK * 4 + 16) + (size_t)p.len * 4;
+    return p.buffers * (size_t)(Stager<T, DP, true, true, true, true>::BYTES + 4 * WinGeom<T, DP>::TK * 4 + 4 * kWinMaxWaves) + (size_t)p.len * 4;
 }
 
 hipError_t allow(const void *kernel, size_t lds)

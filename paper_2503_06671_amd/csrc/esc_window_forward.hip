@@ -80,9 +80,11 @@ __global__ __launch_bounds__(512) void window_forward_kernel(const WindowParams 
         const char *buf = lds + turn * S::BYTES;
         const int *off = reinterpret_cast<const int *>(buf + S::OFF_AT);
         if (busy)
-            for (int tile = share; tile < G::TK / 32 && t0 + tile * 32 < w.L; tile += p.ksplit) {
-                const wu32x2 nibbles = *reinterpret_cast<const wu32x2 *>(buf + S::BITS_AT + tile * 8);
-                const bool whole = __builtin_amdgcn_readfirstlane((int)(nibbles.x & nibbles.y)) == 0x0f0f0f0f;
+#pragma unroll  // (in a loop the compiler waits for the next chunk's loads first)
+            for (int tile = 0; tile < G::TK / 32; ++tile) {
+                if (t0 + tile * 32 >= w.L || (tile & (p.ksplit - 1)) != share) continue;
+                const wu32x4 bits = *reinterpret_cast<const wu32x4 *>(buf + S::BITS_AT + tile * 16);
+                const bool whole = all_take_part(bits);
                 int key[4];
 #pragma unroll
                 for (int a = 0; a < 4; ++a) key[a] = off[tile * 8 + 2 * a + half];
@@ -99,12 +101,7 @@ __global__ __launch_bounds__(512) void window_forward_kernel(const WindowParams 
                     s = score<T, DP>(buf + S::RM0_AT, tile, own[u], s);
                     if (!whole) {
                         asm volatile("; keys that do not take part");  // (keeps the selection out of the way of whole tiles)
-#pragma unroll
-                        for (int a = 0; a < 4; ++a) {
-                            const uint32_t b = (a < 2 ? nibbles.x : nibbles.y) >> (16 * (a & 1) + 8 * half);
-#pragma unroll
-                            for (int j = 0; j < 4; ++j) s[4 * a + j] = (b >> j & 1) != 0 ? s[4 * a + j] : -__builtin_inff();
-                        }
+                        leave_out(bits, -__builtin_inff(), s);
                     }
                     float m = fmaxf(s[0], s[1]);
 #pragma unroll
