@@ -379,9 +379,9 @@ esc_status esc_window_attention_backward(const void *q, const void *k, const voi
  *   ESC_ADAMW_EIGHT  m and v are one byte an element, with one fp32 scale for each block of ESC_ADAMW_BLOCK consecutive
  *                    elements (the last block of a tensor may be shorter): m's element is e4m3(code) * m_scale,
  *                    v's is (e4m3(code) * v_scale)^2.  A step reads them, computes as above in fp32 (the new m and v go into
- *                    param before they are rounded) and writes for x = m and for x = sqrt(v): scale = a / 448 with a the largest
- *                    finite magnitude in the block, code = x * (448 / a) to the nearest e4m3 value (ties to
- *                    even); a positive sqrt(v) takes the smallest positive code at least; values that are not finite are held as
+ *                    param before they are rounded) and writes for x = m and for x = sqrt(v): scale = a * (1 / 448) with a the largest
+ *                    finite magnitude in the block, code = x * (448 * (1 / a)) to the nearest e4m3 value (ties to
+ *                    even; 1 / 448 and 1 / a rounded to fp32); a positive sqrt(v) takes the smallest positive code at least; values that are not finite are held as
  *                    NaN; a block with a < 2^-100 holds zeros, scale 0.  Zeroed bytes and scales are zeroed states.
  * Every element stands for itself (a NaN gradient makes one parameter NaN), tensors may have any length and lie
  * at any address that their element type allows (16-byte steps where all of a tensor's buffers are aligned to that

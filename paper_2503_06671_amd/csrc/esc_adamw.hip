@@ -7,8 +7,8 @@
 //   p  = p (1 - lr wd) - lr / (1 - beta1^t) * ( m / (r / sqrt(1 - beta2^t) + eps) )
 // (the factors in front are made in 64 bits and rounded once; r is multiplied by the rounded 1 / sqrt(1 - beta2^t)).
 //
-// In 8 bits a state is the code e4m3(x * (448 / a)) of x = m, or of x = r (not v: half the exponent range), and a fp32
-// scale a / 448 for each block of 256 consecutive elements of a tensor, a the block's largest finite magnitude; blocks
+// In 8 bits a state is the code e4m3(x * (448 * (1 / a))) of x = m, or of x = r (not v: half the exponent range), and a fp32
+// scale a * (1 / 448) for each block of 256 consecutive elements of a tensor, a the block's largest finite magnitude; blocks
 // whose magnitudes all lie below 2^-100 hold zeros.  A positive r never becomes zero (it takes the smallest code): the next
 // step would divide what is left of m by eps.
 //
@@ -111,21 +111,21 @@ __device__ double power(double b, long n)
     return r;
 }
 
-// Four neighbouring elements at once where `vec`, else those below n.
-template <typename V, typename E>
-__device__ __forceinline__ V load4(const E *a, long i, long n, bool vec)
+// Four neighbouring elements: at once where the chunk is WHOLE (and its buffers aligned), else those below n.
+template <bool WHOLE, typename V, typename E>
+__device__ __forceinline__ V load4(const E *a, long i, long n)
 {
     static_assert(sizeof(V) == 4 * sizeof(E), "");
-    if (vec && i + 4 <= n) return *reinterpret_cast<const V *>(a + i);
+    if constexpr (WHOLE) return *reinterpret_cast<const V *>(a + i);
     E e[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) e[j] = i + j < n ? a[i + j] : E(0);
     return __builtin_bit_cast(V, e);
 }
-template <typename V, typename E>
-__device__ __forceinline__ void store4(E *a, long i, long n, bool vec, V v)
+template <bool WHOLE, typename V, typename E>
+__device__ __forceinline__ void store4(E *a, long i, long n, V v)
 {
-    if (vec && i + 4 <= n) {
+    if constexpr (WHOLE) {
         *reinterpret_cast<V *>(a + i) = v;
         return;
     }
@@ -157,8 +157,8 @@ __device__ __forceinline__ uint32_t encode(f32x4 x, float *scale)
     }
     const float a = __uint_as_float((unsigned)__builtin_amdgcn_readlane((int)wave_max(top), 63));
     const bool full = a >= kTiny;
-    *scale = full ? a / kCodeMax : 0.f;
-    const float inverse = full ? kCodeMax / a : 0.f;
+    *scale = full ? a * (1.f / kCodeMax) : 0.f;
+    const float inverse = full ? kCodeMax * (1.f / a) : 0.f;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         float y = x[j] * inverse;
@@ -171,82 +171,93 @@ __device__ __forceinline__ uint32_t encode(f32x4 x, float *scale)
     return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x[2], x[3], c, true);
 }
 
-template <bool EIGHT, bool BF16>
-__global__ __launch_bounds__(kThreads) void adamw_kernel(const StepArgs a)
+// What a step has in common.
+struct Factors {
+    float beta1, rest1, beta2, rest2, eps, grad_scale, size, correct;
+};
+
+// A wavefront's part of a chunk: kUnits units of 256 elements, all of whose loads are on their way before the first is waited for.
+template <bool EIGHT, bool BF16, bool WHOLE>
+__device__ __forceinline__ void part_of_chunk(const Record &r, const Factors &f, float keep, long base)
 {
     using G = typename std::conditional<BF16, uint16_t, float>::type;
     typedef G g4 __attribute__((ext_vector_type(4)));
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    typedef uint8_t u8x4 __attribute__((ext_vector_type(4)));
+    const int lane = threadIdx.x & 63;
+    f32x4 p[kUnits], m[kUnits], v[kUnits];
+    g4 g[kUnits];
+    u8x4 mc[kUnits], vc[kUnits];
+    float ms[kUnits], vs[kUnits];
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u) {
+        const long i = base + u * kUnit + lane * 4, unit = base / kUnit + u;
+        p[u] = load4<WHOLE, f32x4>(r.p, i, r.n);
+        g[u] = load4<WHOLE, g4>(static_cast<const G *>(r.g), i, r.n);
+        if constexpr (EIGHT) {
+            mc[u] = load4<WHOLE, u8x4>(static_cast<const uint8_t *>(r.m), i, r.n), vc[u] = load4<WHOLE, u8x4>(static_cast<const uint8_t *>(r.v), i, r.n);
+            const bool any = WHOLE || unit * kUnit < r.n;
+            ms[u] = any ? r.m_scale[unit] : 0.f, vs[u] = any ? r.v_scale[unit] : 0.f;
+        } else {
+            m[u] = load4<WHOLE, f32x4>(static_cast<const float *>(r.m), i, r.n);
+            v[u] = load4<WHOLE, f32x4>(static_cast<const float *>(r.v), i, r.n);
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u) {
+        const long i = base + u * kUnit + lane * 4, unit = base / kUnit + u;
+        if (!WHOLE && unit * kUnit >= r.n) break;  // (the same for the wavefront)
+        if constexpr (EIGHT) {
+            m[u] = decode(__builtin_bit_cast(uint32_t, mc[u]));
+            v[u] = decode(__builtin_bit_cast(uint32_t, vc[u]));
+        }
+        f32x4 root;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if constexpr (EIGHT) {
+                m[u][j] = m[u][j] * ms[u];
+                const float held = v[u][j] * vs[u];
+                v[u][j] = held * held;
+            }
+            float gs;
+            if constexpr (BF16) gs = __uint_as_float((uint32_t)g[u][j] << 16);
+            else gs = g[u][j];
+            gs *= f.grad_scale;
+            m[u][j] = f.beta1 * m[u][j] + f.rest1 * gs;
+            v[u][j] = f.beta2 * v[u][j] + f.rest2 * (gs * gs);
+            root[j] = sqrtf(v[u][j]);
+            p[u][j] = p[u][j] * keep - f.size * (m[u][j] / (root[j] * f.correct + f.eps));
+        }
+        store4<WHOLE>(r.p, i, r.n, p[u]);
+        if constexpr (EIGHT) {
+            float ns, nr;
+            // (lanes beyond the tensor's end have loaded zeros: their states stay zero and below any maximum)
+            const uint32_t nm = encode<false>(m[u], &ns), nv = encode<true>(root, &nr);
+            store4<WHOLE>(static_cast<uint8_t *>(r.m), i, r.n, __builtin_bit_cast(u8x4, nm));
+            store4<WHOLE>(static_cast<uint8_t *>(r.v), i, r.n, __builtin_bit_cast(u8x4, nv));
+            if (lane == 0) r.m_scale[unit] = ns, r.v_scale[unit] = nr;
+        } else {
+            store4<WHOLE>(static_cast<float *>(r.m), i, r.n, m[u]);
+            store4<WHOLE>(static_cast<float *>(r.v), i, r.n, v[u]);
+        }
+    }
+}
+
+template <bool EIGHT, bool BF16>
+__global__ __launch_bounds__(kThreads) void adamw_kernel(const StepArgs a)
+{
+    constexpr uintptr_t kGradMask = BF16 ? 7 : 15, kStateMask = EIGHT ? 3 : 15;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const long step = a.control->step + 1;
     const double lr = a.lr_device != nullptr ? (double)*a.lr_device : a.lr;
-    const float beta1 = (float)a.beta1, rest1 = (float)(1.0 - a.beta1), beta2 = (float)a.beta2, rest2 = (float)(1.0 - a.beta2);
-    const float eps = (float)a.eps, grad_scale = (float)a.grad_scale;
-    const float size = (float)(lr / (1.0 - power(a.beta1, step)));
-    const float correct = (float)(1.0 / sqrt(1.0 - power(a.beta2, step)));
-
+    const Factors f{(float)a.beta1, (float)(1.0 - a.beta1), (float)a.beta2, (float)(1.0 - a.beta2), (float)a.eps, (float)a.grad_scale,
+                    (float)(lr / (1.0 - power(a.beta1, step))), (float)(1.0 / sqrt(1.0 - power(a.beta2, step)))};
     for (int c = blockIdx.x; c < a.chunks; c += gridDim.x) {
         const Record r = a.records[a.map[c]];
-        const long base = (long)(c - r.first_chunk) * kChunk + wave * (kUnit * kUnits) + lane * 4;
-        const bool vec = (((uintptr_t)r.p | (EIGHT ? 0 : (uintptr_t)r.m | (uintptr_t)r.v)) & 15) == 0 && ((uintptr_t)r.g & (4 * sizeof(G) - 1)) == 0 &&
-                         (!EIGHT || (((uintptr_t)r.m | (uintptr_t)r.v) & 3) == 0);
+        const long base = (long)(c - r.first_chunk) * kChunk + wave * (kUnit * kUnits);
+        const bool aligned = (((uintptr_t)r.p & 15) | ((uintptr_t)r.g & kGradMask) | (((uintptr_t)r.m | (uintptr_t)r.v) & kStateMask)) == 0;
         const float keep = (float)(1.0 - lr * (double)r.weight_decay);
-        f32x4 p[kUnits], g[kUnits], m[kUnits], v[kUnits];
-#pragma unroll
-        for (int u = 0; u < kUnits; ++u) {
-            const long i = base + u * kUnit;
-            p[u] = load4<f32x4>(r.p, i, r.n, vec);
-            const g4 raw = load4<g4>(static_cast<const G *>(r.g), i, r.n, vec);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                if constexpr (BF16) g[u][j] = __uint_as_float((uint32_t)raw[j] << 16);
-                else g[u][j] = raw[j];
-            }
-            if constexpr (EIGHT) {
-                typedef uint8_t u8x4 __attribute__((ext_vector_type(4)));
-                const u8x4 mc = load4<u8x4>(static_cast<const uint8_t *>(r.m), i, r.n, vec), vc = load4<u8x4>(static_cast<const uint8_t *>(r.v), i, r.n, vec);
-                const long unit = (i - lane * 4) / kUnit;
-                const bool any = unit * kUnit < r.n;
-                const float ms = any ? r.m_scale[unit] : 0.f, vs = any ? r.v_scale[unit] : 0.f;
-                m[u] = decode(__builtin_bit_cast(uint32_t, mc));
-                v[u] = decode(__builtin_bit_cast(uint32_t, vc));
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    m[u][j] = m[u][j] * ms;
-                    const float root = v[u][j] * vs;
-                    v[u][j] = root * root;
-                }
-            } else {
-                m[u] = load4<f32x4>(static_cast<const float *>(r.m), i, r.n, vec);
-                v[u] = load4<f32x4>(static_cast<const float *>(r.v), i, r.n, vec);
-            }
-        }
-#pragma unroll
-        for (int u = 0; u < kUnits; ++u) {
-            const long i = base + u * kUnit;
-            if (i - lane * 4 >= r.n) break;  // (the same for the wavefront)
-            f32x4 root;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float gs = g[u][j] * grad_scale;
-                m[u][j] = beta1 * m[u][j] + rest1 * gs;
-                v[u][j] = beta2 * v[u][j] + rest2 * (gs * gs);
-                root[j] = sqrtf(v[u][j]);
-                p[u][j] = p[u][j] * keep - size * (m[u][j] / (root[j] * correct + eps));
-            }
-            store4(r.p, i, r.n, vec, p[u]);
-            if constexpr (EIGHT) {
-                const long unit = (i - lane * 4) / kUnit;
-                float ms, vs;
-                // (lanes beyond the tensor's end have loaded zeros: their states stay zero and below any maximum)
-                const uint32_t mc = encode<false>(m[u], &ms), vc = encode<true>(root, &vs);
-                store4(static_cast<uint8_t *>(r.m), i, r.n, vec, mc);
-                store4(static_cast<uint8_t *>(r.v), i, r.n, vec, vc);
-                if (lane == 0) r.m_scale[unit] = ms, r.v_scale[unit] = vs;
-            } else {
-                store4(static_cast<float *>(r.m), i, r.n, vec, m[u]);
-                store4(static_cast<float *>(r.v), i, r.n, vec, v[u]);
-            }
-        }
+        if (aligned && base + kUnit * kUnits <= r.n) part_of_chunk<EIGHT, BF16, true>(r, f, keep, base);
+        else if (base < r.n) part_of_chunk<EIGHT, BF16, false>(r, f, keep, base);
     }
     // The last block to leave counts the step.  Two levels, so that no word sees more than kMaxGrid / kLeaves or kLeaves atomics.
     if (threadIdx.x == 0) {

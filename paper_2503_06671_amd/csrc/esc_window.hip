@@ -52,7 +52,7 @@ bool choose_waves(WindowParams &p, int tiles, int heads, F lds)
     for (size_t limit : {kLdsPerCu / 2, kLdsPerCu})
         for (int buffers : {2, 1})
             for (int waves = want; waves >= (limit == kLdsPerCu ? 1 : std::min(want, 4)); --waves) {
-                p.waves = waves, p.buffers = buffers, p.len = table_words(p, waves * each);
+                p.waves = waves, p.buffers = buffers, p.len = (table_words(p, waves * each) + 3) & ~3;
                 if (lds(p) <= limit) {
                     p.blocks = (int)((all + waves - 1) / waves);
                     return true;
@@ -93,8 +93,10 @@ esc_status shape(const esc_window_attn *a, WindowParams *p)
 
 size_t table_bytes(const WindowParams &p) { return (size_t)p.heads * p.nby * p.nbx * 4; }
 
-// The forward's wavefronts.  A wavefront with two tiles of queries reads keys and values half as often (and is what a chip full of work takes);
-// where that would leave fewer than two wavefronts a SIMD, it takes one.  Where even those are fewer than one a SIMD, up to four
+// The forward's wavefronts.  A wavefront with two tiles of queries reads keys and values half as often, with one it takes so few registers that
+// four of a SIMD hide each other's waits.  Two: fp32 storage, whose three terms make the reads dear (180x320, windows of 32: 155 us, with one
+// 183), and bf16 storage in windows of fewer than 16 tiles, where a block's beginning weighs (3 x 339 x 511, windows of 13: 440 us, with one 573; windows of
+// 48: 361, with one 276) - where that leaves two wavefronts a SIMD.  Where even those are fewer than one a SIMD, up to four
 // wavefronts share a tile's keys.  Blocks are as large as leaves one for each compute unit: they stage a window's keys and values once for all their
 // queries.
 bool plan_forward(WindowParams &p, bool f32)
@@ -102,7 +104,7 @@ bool plan_forward(WindowParams &p, bool f32)
     const int dp = dim_padded(p.d);
     const long tokens = (long)p.wh * ((p.ww + 3) & ~3), each = (tokens + 31) / 32, windows = (long)p.N * p.gy * p.gx * p.heads;
     const long all = each * windows;
-    p.tiles = !(f32 && dp == 64) && all >= 2 * 2 * kSimds && each > 1 ? 2 : 1;
+    p.tiles = (f32 ? dp < 64 : each < 16) && all >= 2 * 2 * kSimds && each > 1 ? 2 : 1;
     const long waves = (each + p.tiles - 1) / p.tiles;
     p.ksplit = 1;
     while (p.tiles == 1 && p.ksplit < 4 && waves * windows * p.ksplit < 2 * kSimds && tokens >= 128 * p.ksplit) p.ksplit *= 2;
@@ -110,7 +112,7 @@ bool plan_forward(WindowParams &p, bool f32)
     queries = std::max<long>(1, std::min(queries, waves * windows / kCus));
     for (; queries >= 1; --queries) {
         p.waves = (int)queries * p.ksplit;
-        p.len = table_words(p, (int)queries * p.tiles * 32);
+        p.len = (table_words(p, (int)queries * p.tiles * 32) + 3) & ~3;
         if (window_forward_lds(f32, dp, p.len, p.ksplit > 1 ? p.waves : 0) <= kLdsPerCu) {
             p.blocks = (int)((waves + queries - 1) / queries);
             return set_units(p, p.heads);
@@ -210,6 +212,7 @@ esc_status common(const void *q, const void *k, const void *v, esc_dtype dt, con
     p->bias = a->bias, p->mask = a->mask;
     // (without a mask, the first image of k: more bytes than a plane has pixels)
     p->mask_read = a->mask != nullptr ? a->mask : static_cast<const uint8_t *>(k), p->mask_step = a->mask != nullptr ? (long)plane : 0;
+    p->mask_set = a->mask != nullptr ? 0 : 0xffff;
     p->scale = a->scale, p->inv_scale = 1.f / a->scale, p->log2_scale = (float)((double)a->scale * 1.4426950408889634);
     return ESC_OK;
 }

@@ -46,6 +46,7 @@ struct WindowParams {
     const uint8_t *mask;                 // [N, H, W] or nullptr
     const uint8_t *mask_read;            // what is read in its place where there is none (and not used), so that the loads need no condition
     long mask_step;
+    uint32_t mask_set;                   // no mask: all bits
     int N, H, W, heads, kv_heads, d;
     int win_h, win_w;                    // as the table has them
     int wh, ww;                          // cut to the map
@@ -91,6 +92,10 @@ struct WinGeom {
 #ifndef DQT
 #define DQT 2
 #endif
+#ifndef KT
+#define KT 1
+#endif
+    static constexpr int KEY_TILES = F32 || DP == 64 ? 1 : KT;
     static constexpr int QUERY_TILES = F32 || DP == 64 ? 1 : DQT;  // backward: tiles of 32 own queries of a wavefront (two where the registers hold them); its keys: one
     // rows of tokens: 16-byte pieces of eight channels, [term][channels / 8][token]; four tokens of a group lie SLOT pieces
     // apart, so that 16 lanes' pieces cover all banks once, written and read
@@ -108,6 +113,10 @@ struct WinGeom {
 
 struct Win {
     int n, y0, x0, h, w, wp, L;
+    float inv;
+    // the row of a token: a quotient that is at least 0.5 / wp away from whole numbers, which the product's error (2^-22 of it) does not reach
+    // below two million tokens
+    __device__ __forceinline__ int row(int t) const { return (int)(((float)t + 0.5f) * inv); }
 };
 
 __device__ __forceinline__ Win win_of(const WindowParams &p, int n, int wy, int wx)
@@ -117,6 +126,7 @@ __device__ __forceinline__ Win win_of(const WindowParams &p, int n, int wy, int 
     w.h = min(p.wh, p.H - w.y0), w.w = min(p.ww, p.W - w.x0);
     w.wp = (w.w + 3) & ~3;
     w.L = w.h * w.wp;
+    w.inv = __builtin_amdgcn_rcpf((float)w.wp);
     return w;
 }
 
@@ -134,9 +144,9 @@ struct TableRange {
 };
 // `sign`: -1 for queries (offset = key - query), 1 for keys.  off() grows with the token, but in windows of one and two columns, whose
 // rows of four overlap: there whole rows count.
-__device__ __forceinline__ TableRange table_range(int t0, int t1, int h, int wp, int tw, int centre, int sign)
+__device__ __forceinline__ TableRange table_range(const Win &w, int t0, int t1, int tw, int centre, int sign)
 {
-    const int y0 = t0 / wp, y1 = (t1 - 1) / wp, all = (h - 1) * tw + wp - 1;
+    const int wp = w.wp, y0 = w.row(t0), y1 = w.row(t1 - 1), all = (w.h - 1) * tw + wp - 1;
     const int lo = y0 * tw + (tw >= wp ? t0 - y0 * wp : 0), hi = y1 * tw + (tw >= wp ? t1 - 1 - y1 * wp : wp - 1);
     return sign < 0 ? TableRange{centre - hi, all + hi - lo + 1} : TableRange{centre + lo - all, all + hi - lo + 1};
 }
@@ -155,26 +165,30 @@ __device__ __forceinline__ int bucket_of(const WindowParams &p, int o, int full)
 }
 
 // The range of the head's table, over the scale (scores are kept unscaled; the largest magnitudes are cut to 2^120, an
-// infinity stays one).
+// infinity stays one).  REVERSED: last first, for lanes that hold a key and go through queries.  Four loads on their way at a time.
+template <bool REVERSED>
 __device__ __forceinline__ void stage_table(const WindowParams &p, float *table, TableRange r, int head)
 {
-    for (int i = threadIdx.x; i < r.len; i += blockDim.x) {
-        const int at = r.base + i;
-        float b = 0.f;
-        if (p.bias != nullptr && at >= 0 && at < p.th * p.tw) {
-            const int y = at / p.tw, x = at - y * p.tw;
+    const float *bias = p.bias + (long)head * p.nby * p.nbx, inv_tw = __builtin_amdgcn_rcpf((float)p.tw);
+    for (int i0 = threadIdx.x; i0 < r.len; i0 += 4 * blockDim.x) {
+        float b[4];
+        bool in[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int at = r.base + i0 + k * blockDim.x;
+            in[k] = at >= 0 && at < p.th * p.tw;
+            const int c = in[k] ? at : 0, y = (int)(((float)c + 0.5f) * inv_tw), x = c - y * p.tw;  // (as Win::row)
             const int by = bucket_of(p, y - (p.wh - 1), p.win_h), bx = bucket_of(p, x - (p.ww - 1), p.win_w);
-            b = p.bias[((long)head * p.nby + by) * p.nbx + bx];
-            if (__builtin_isfinite(b)) b = fminf(fmaxf(b * p.inv_scale, -0x1p120f), 0x1p120f);
+            b[k] = p.bias != nullptr ? bias[(long)by * p.nbx + bx] : 0.f;
         }
-        table[i] = b;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int i = i0 + k * blockDim.x;
+            float v = in[k] ? b[k] : 0.f;
+            if (__builtin_isfinite(v)) v = fminf(fmaxf(v * p.inv_scale, -0x1p120f), 0x1p120f);
+            if (i < r.len) table[REVERSED ? r.len - 1 - i : i] = v;
+        }
     }
-}
-
-// Does the pixel exist and take part?
-__device__ __forceinline__ bool seen(const WindowParams &p, const Win &w, int y, int x)
-{
-    return y < w.h && x < w.w && (p.mask == nullptr || p.mask[((long)w.n * p.H + w.y0 + y) * p.W + w.x0 + x] != 0);
 }
 
 __device__ __forceinline__ uint32_t low_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); }
@@ -185,9 +199,10 @@ __device__ __forceinline__ uint32_t high_halves(uint32_t a, uint32_t b) { return
 struct Spot {
     int at, skip;
     uint32_t bits;
+    Spot() = default;
     __device__ __forceinline__ Spot(const WindowParams &p, const Win &w, int t, int n)
     {
-        const int y = t / w.wp, x = t - y * w.wp;
+        const int y = w.row(t), x = t - y * w.wp;
         const bool in = t < w.L;
         const int pos = in ? (w.y0 + y) * p.W + w.x0 + x : 0;
         at = max(min(pos, p.H * p.W - n), 0), skip = pos - at;
@@ -195,13 +210,13 @@ struct Spot {
     }
 };
 
-// Offsets of groups of four tokens.
+// Offsets of groups of four tokens, in bytes of a table of floats.
 template <int TK>
 __device__ __forceinline__ void stage_offsets(const WindowParams &p, const Win &w, int t0, int *off)
 {
     if (threadIdx.x >= TK / 4) return;
-    const int t = t0 + 4 * threadIdx.x, y = t / w.wp, x = t - y * w.wp;
-    off[threadIdx.x] = t < w.L ? y * p.tw + x : 0;
+    const int t = t0 + 4 * threadIdx.x, y = w.row(t), x = t - y * w.wp;
+    off[threadIdx.x] = t < w.L ? 4 * (y * p.tw + x) : 0;
 }
 
 // A lane's 16 tokens of a staged tile, of which those whose pair's bit is not set get `none`.  bits: a byte for each pair of tokens.
@@ -211,6 +226,8 @@ __device__ __forceinline__ bool all_take_part(wu32x4 bits)
 }
 __device__ __forceinline__ void leave_out(wu32x4 bits, float none, wf32x16 &s)
 {
+    // (called where a tile is not whole: the compiler would work out the sixteen conditions for every tile)
+    asm volatile("; tokens that do not take part" : "+v"(bits));
     const int half = (threadIdx.x >> 5) & 1;
 #pragma unroll
     for (int a = 0; a < 4; ++a) {
@@ -228,11 +245,12 @@ struct Piece {
     using Two = typename std::conditional<G::F32, wf32x2, uint32_t>::type;
     Two v[4];
     uint16_t mask;  // (two bytes)
+    Spot spot;
 
     __device__ __forceinline__ void fetch(const WindowParams &p, const Win &w, const T *plane, int t, int c4)
     {
         const long hw = (long)p.H * p.W;
-        const Spot s(p, w, t, 2);
+        const Spot s = spot = Spot(p, w, t, 2);
         const T *a[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) a[i] = plane + min(c4 * 4 + i, p.d - 1) * hw + s.at;
@@ -253,10 +271,10 @@ struct Piece {
 
     // g2: the pair within the staged tokens
     template <bool RM, bool CM>
-    __device__ __forceinline__ void store(const WindowParams &p, const Win &w, int t, char *rm, char *cm, uint8_t *bits, int g2, int c4) const
+    __device__ __forceinline__ void store(const WindowParams &p, char *rm, char *cm, uint8_t *bits, int g2, int c4) const
     {
-        const Spot s(p, w, t, 2);
-        const uint32_t m = p.mask != nullptr ? mask >> 8 * s.skip : 0x101u;
+        const Spot s = spot;
+        const uint32_t m = (mask | p.mask_set) >> 8 * s.skip;  // (used in any case: a load whose answer is not used is waited for where its register is next)
         const bool ok0 = (s.bits & 1) != 0 && (m & 0xff) != 0, ok1 = (s.bits & 2) != 0 && (m & 0xff00) != 0;
         if (bits != nullptr && c4 == 0) bits[g2] = (uint8_t)((ok0 ? 1 : 0) | (ok1 ? 2 : 0));
         uint32_t word[G::NT][4];  // [term][channel]: both tokens
@@ -305,11 +323,11 @@ struct Stager {
 
     __device__ __forceinline__ static int pair_of(int item) { return item % PAIRS; }
     __device__ __forceinline__ static int channels_of(int item) { return item % HALF / PAIRS; }
-    __device__ __forceinline__ static void put(const Piece<T, DP> &piece, const WindowParams &p, const Win &w, int t0, int item, char *buf)
+    __device__ __forceinline__ static void put(const Piece<T, DP> &piece, const WindowParams &p, int item, char *buf)
     {
         const int g2 = pair_of(item), c4 = channels_of(item);
-        if (item < HALF) piece.template store<RM0, CM0>(p, w, t0 + 2 * g2, buf + RM0_AT, buf + CM0_AT, reinterpret_cast<uint8_t *>(buf + BITS_AT), g2, c4);
-        else piece.template store<RM1, CM1>(p, w, t0 + 2 * g2, buf + RM1_AT, buf + CM1_AT, nullptr, g2, c4);
+        if (item < HALF) piece.template store<RM0, CM0>(p, buf + RM0_AT, buf + CM0_AT, reinterpret_cast<uint8_t *>(buf + BITS_AT), g2, c4);
+        else piece.template store<RM1, CM1>(p, buf + RM1_AT, buf + CM1_AT, nullptr, g2, c4);
     }
     __device__ __forceinline__ void fetch(const WindowParams &p, const Win &w, const T *op0, const T *op1, int t0)
     {
@@ -318,11 +336,12 @@ struct Stager {
     }
     __device__ __forceinline__ void write(const WindowParams &p, const Win &w, const T *op0, const T *op1, int t0, char *buf)
     {
-        if ((int)threadIdx.x < ITEMS) put(next, p, w, t0, threadIdx.x, buf);
+        if ((int)threadIdx.x < ITEMS) put(next, p, threadIdx.x, buf);
         for (int item = threadIdx.x + blockDim.x; item < ITEMS; item += blockDim.x) {
             Piece<T, DP> piece;
             piece.fetch(p, w, item < HALF ? op0 : op1, t0 + 2 * pair_of(item), channels_of(item));
-            put(piece, p, w, t0, item, buf);
+            put(piece, p, item, buf);
+            __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): all have come, but the compiler sees paths on which nobody waited
         }
         stage_offsets<G::TK>(p, w, t0, reinterpret_cast<int *>(buf + OFF_AT));
     }
@@ -335,24 +354,60 @@ struct Stager {
     }
 };
 
-// A wavefront's own tokens as operands kept in registers: lane n = token, eight channels 16 s + 8 (lane / 32) on.
+// A wavefront's own token: where it lies, whether it exists and takes part, its offset.  The loads need no condition (the place is one of the
+// window's in any case), so that they can all be on their way before the first is waited for.
+struct OwnToken {
+    int pixel, off;
+    bool there;
+    uint8_t mask;
+    __device__ __forceinline__ OwnToken(const WindowParams &p, const Win &w, int t)
+    {
+        const int tc = min(t, w.L - 1), y = w.row(tc), x = tc - y * w.wp;
+        there = t < w.L && x < w.w;
+        off = y * p.tw + x;
+        pixel = (w.y0 + y) * p.W + w.x0 + min(x, w.w - 1);
+        mask = p.mask_read[w.n * p.mask_step + pixel];
+    }
+    __device__ __forceinline__ bool ok(const WindowParams &p) const { return there && (mask | p.mask_set) != 0; }
+};
+
+// Eight channels 16 s + 8 (lane / 32) on of an own token, as they come ...
+template <typename T, int DP>
+struct OwnValues {
+    T v[WinGeom<T, DP>::KS][8];
+    __device__ __forceinline__ void fetch(const WindowParams &p, const T *plane, int pixel)
+    {
+        const long hw = (long)p.H * p.W;
+        const int half = (threadIdx.x >> 5) & 1;
+#pragma unroll
+        for (int s = 0; s < WinGeom<T, DP>::KS; ++s)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[s][j] = plane[min(16 * s + 8 * half + j, p.d - 1) * hw + pixel];
+    }
+    __device__ __forceinline__ void clean(const WindowParams &p, bool ok)
+    {
+        const int half = (threadIdx.x >> 5) & 1;
+#pragma unroll
+        for (int s = 0; s < WinGeom<T, DP>::KS; ++s)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[s][j] = ok && 16 * s + 8 * half + j < p.d ? v[s][j] : T(0);
+    }
+};
+// ... and as an operand that stays in registers.
 template <typename T, int DP>
 struct Fragment {
     wu32x4 r[WinGeom<T, DP>::NT][WinGeom<T, DP>::KS];
 };
 template <typename T, int DP>
-__device__ __forceinline__ Fragment<T, DP> own_fragment(const WindowParams &p, const T *pixel, bool ok)
+__device__ __forceinline__ Fragment<T, DP> fragment_of(const OwnValues<T, DP> &o)
 {
     using G = WinGeom<T, DP>;
     Fragment<T, DP> f;
-    const long hw = (long)p.H * p.W;
-    const int half = (threadIdx.x >> 5) & 1;
 #pragma unroll
     for (int s = 0; s < G::KS; ++s)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int c = 16 * s + 8 * half + 2 * i;
-            const T a = ok && c < p.d ? pixel[c * hw] : T(0), b = ok && c + 1 < p.d ? pixel[(c + 1) * hw] : T(0);
+            const T a = o.v[s][2 * i], b = o.v[s][2 * i + 1];
             if constexpr (G::F32) {
                 uint32_t t[3];
                 split_bf16(a, b, t);
@@ -455,11 +510,16 @@ __device__ __forceinline__ void accumulate(const char *cm, int tile, const Packe
     }
 }
 
-// (lanes l and l + 32 hold halves of a token's values)
-__device__ __forceinline__ float other_half(float v)
+// lanes l and l + 32 hold halves of a token's values: of both halves together
+__device__ __forceinline__ float max_of_halves(float v)
 {
     const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    return __uint_as_float((threadIdx.x & 32) != 0 ? s[0] : s[1]);
+    return fmaxf(__uint_as_float(s[0]), __uint_as_float(s[1]));
+}
+__device__ __forceinline__ float sum_of_halves(float v)
+{
+    const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(s[0]) + __uint_as_float(s[1]);
 }
 
 __device__ __forceinline__ float exp2_of(float v) { return __builtin_amdgcn_exp2f(v); }

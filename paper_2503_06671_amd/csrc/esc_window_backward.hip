@@ -24,18 +24,19 @@ template <int U>
 __device__ __forceinline__ TableRange wave_range(const WindowParams &p, const Win &w, int t0)
 {
     const int centre = (p.wh - 1) * p.tw + p.ww - 1;
-    return table_range(t0, min(t0 + 32 * U, w.L), w.h, w.wp, p.tw, centre, -1);
+    return table_range(w, t0, min(t0 + 32 * U, w.L), p.tw, centre, -1);
 }
 
 template <typename T, int DP>
-__global__ __launch_bounds__(512) void window_dq_kernel(const WindowParams p)
+__global__ __launch_bounds__(512, (WinGeom<T, DP>::F32 || DP == 64 || DQT == 2) ? 2 : 4) void window_dq_kernel(const WindowParams p)
 {
     using G = WinGeom<T, DP>;
     using S = Stager<T, DP, true, true, true, false>;  // keys by tokens and by channels, values by tokens
     constexpr int U = G::QUERY_TILES;
     extern __shared__ __align__(16) char lds[];
-    double *rings = reinterpret_cast<double *>(lds + p.buffers * S::BYTES);  // one a wavefront
-    float *table = reinterpret_cast<float *>(rings + (p.grad_bias != nullptr ? p.waves * p.ring : 0));
+    float *table = reinterpret_cast<float *>(lds);  // (first: its reads' addresses are then sums of two terms and a constant)
+    double *rings = reinterpret_cast<double *>(lds + (size_t)p.len * 4);  // one a wavefront
+    char *const staged = reinterpret_cast<char *>(rings + (p.grad_bias != nullptr ? p.waves * (p.ring + 4) : 0));
 
     const int unit = unit_of(p.units);
     if (unit < 0) return;
@@ -44,7 +45,7 @@ __global__ __launch_bounds__(512) void window_dq_kernel(const WindowParams p)
     const int queries = p.waves * 32 * U, q0 = block * queries;
     if (q0 >= w.L) return;
     const int centre = (p.wh - 1) * p.tw + p.ww - 1;
-    const TableRange range = table_range(q0, min(q0 + queries, w.L), w.h, w.wp, p.tw, centre, -1);
+    const TableRange range = table_range(w, q0, min(q0 + queries, w.L), p.tw, centre, -1);
     const bool bias_grad = p.grad_bias != nullptr;
 
     const long hw = (long)p.H * p.W;
@@ -66,50 +67,65 @@ __global__ __launch_bounds__(512) void window_dq_kernel(const WindowParams p)
     float top[U], shift[U], log_sum[U], delta[U];
     wf32x16 acc[U][G::DT];
     bool far = false, all = true;
+    {
+        OwnValues<T, DP> vq[U], vgo[U], vout[U], vrest[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-        const int t = wq0 + u * 32 + (lane & 31), tc = min(t, w.L - 1);
-        const int y = tc / w.wp, x = tc - y * w.wp;
-        there[u] = t < w.L && x < w.w;
-        ok[u] = there[u] && seen(p, w, y, x);
-        pixel[u] = (w.y0 + y) * p.W + w.x0 + x;
-        place[u] = centre - (y * p.tw + x) - range.base;
-        own_q[u] = own_fragment<T, DP>(p, q + pixel[u], ok[u]);
-        own_go[u] = own_fragment<T, DP>(p, go + pixel[u], ok[u]);
-        top[u] = ok[u] ? p.top[row + pixel[u]] : 0.f;
-        log_sum[u] = ok[u] ? p.log_sum[row + pixel[u]] : __builtin_inff();
-        shift[u] = top[u] * p.log2_scale + log_sum[u];
-        far = far || __any(__builtin_fabsf(top[u] * p.log2_scale) > kLargeShift);
-        all = all && __all(ok[u]);
-        float sum = 0.f;
-        if (ok[u])
-            for (int c = half; c < p.d; c += 2) {
-                float o = widen(out[c * hw + pixel[u]]);
-                if constexpr (!G::F32) o += widen(static_cast<const T *>(p.rest)[planes + c * hw + pixel[u]]);
-                sum = __builtin_fmaf(o, widen(go[c * hw + pixel[u]]), sum);
-            }
-        delta[u] = sum + other_half(sum);
-        if (there[u] && half == 0) p.delta[row + pixel[u]] = delta[u];
+        for (int u = 0; u < U; ++u) {
+            const OwnToken own_token(p, w, wq0 + u * 32 + (lane & 31));
+            there[u] = own_token.there, pixel[u] = own_token.pixel, ok[u] = own_token.ok(p);
+            place[u] = 4 * (centre - own_token.off - range.base);
+            vq[u].fetch(p, q, pixel[u]);
+            vgo[u].fetch(p, go, pixel[u]);
+            vout[u].fetch(p, out, pixel[u]);
+            if constexpr (!G::F32) vrest[u].fetch(p, static_cast<const T *>(p.rest) + planes, pixel[u]);
+            top[u] = p.top[row + pixel[u]], log_sum[u] = p.log_sum[row + pixel[u]];
+        }
+        stage_table<false>(p, table, range, head);
 #pragma unroll
-        for (int b = 0; b < G::DT; ++b) acc[u][b] = wf32x16{};
+        for (int u = 0; u < U; ++u) {
+            vq[u].clean(p, ok[u]);
+            vgo[u].clean(p, ok[u]);
+            vout[u].clean(p, ok[u]);
+            own_q[u] = fragment_of(vq[u]);
+            own_go[u] = fragment_of(vgo[u]);
+            float sum = 0.f;
+#pragma unroll
+            for (int s = 0; s < G::KS; ++s)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    float o = widen(vout[u].v[s][j]);
+                    if constexpr (!G::F32) {
+                        vrest[u].clean(p, ok[u]);
+                        o += widen(vrest[u].v[s][j]);
+                    }
+                    sum = __builtin_fmaf(o, widen(vgo[u].v[s][j]), sum);
+                }
+            delta[u] = sum_of_halves(sum);
+            if (there[u] && half == 0) p.delta[row + pixel[u]] = delta[u];
+            if (!ok[u]) top[u] = 0.f, log_sum[u] = __builtin_inff();
+            shift[u] = top[u] * p.log2_scale + log_sum[u];
+            far = far || __any(__builtin_fabsf(top[u] * p.log2_scale) > kLargeShift);
+            all = all && __all(ok[u]);
+#pragma unroll
+            for (int b = 0; b < G::DT; ++b) acc[u][b] = wf32x16{};
+        }
     }
-    stage_table(p, table, range, head);
-    double *const ring = rings + wave * p.ring;
+    double *const ring = rings + wave * (p.ring + 4);  // (four places more: a group of four that runs over the end stays together)
     const int ring_mask = p.ring - 1;
     const TableRange mine = wave_range<U>(p, w, min(wq0, w.L - 1));
     // ring place of the offset to the key with off = 0: of the lane's query where 64 lanes are 64 queries, else of its own
-    const int ring_place = (U == 1 || half == 0 ? place[0] : place[U - 1]) + range.base - mine.base;
+    const int ring_place = (U == 1 || half == 0 ? place[0] : place[U - 1]) / 4 + range.base - mine.base;
     float *const part = p.part + ((long)unit * p.waves + wave) * p.part_len;
     int left = 0;  // offsets that have left the ring
     if (bias_grad)
-        for (int i = lane; i < p.ring; i += 64) ring[i] = 0.0;
-    stager.write(p, w, k, v, 0, lds);
+        for (int i = lane; i < p.ring + 4; i += 64) ring[i] = 0.0;
+    stager.write(p, w, k, v, 0, staged);
     __syncthreads();
 
     for (int t0 = 0, turn = 0; t0 < w.L; t0 += G::TK) {
         const bool more = t0 + G::TK < w.L;
         if (more) stager.fetch(p, w, k, v, t0 + G::TK);
-        const char *buf = lds + turn * S::BYTES;
+        const char *buf = staged + turn * S::BYTES;
         const int *off = reinterpret_cast<const int *>(buf + S::OFF_AT);
         auto tile_of = [&](int tile, auto large) {
             const wu32x4 bits = *reinterpret_cast<const wu32x4 *>(buf + S::BITS_AT + tile * 16);
@@ -124,7 +140,7 @@ __global__ __launch_bounds__(512) void window_dq_kernel(const WindowParams p)
                 wf32x16 s;
 #pragma unroll
                 for (int a = 0; a < 4; ++a) {
-                    const float *from = table + place[u] + key[a];
+                    const float *from = reinterpret_cast<const float *>(reinterpret_cast<const char *>(table) + (place[u] + key[a]));
 #pragma unroll
                     for (int j = 0; j < 4; ++j) s[4 * a + j] = from[j];
                 }
@@ -137,8 +153,7 @@ __global__ __launch_bounds__(512) void window_dq_kernel(const WindowParams p)
                     ds[u][i] = exp2_of(s[i]) * (dp[i] - delta[u]);
                 }
                 if (!whole) {
-                    asm volatile("; tokens that do not take part");
-                    leave_out(bits, 0.f, ds[u]);
+                                        leave_out(bits, 0.f, ds[u]);
 #pragma unroll
                     for (int i = 0; i < 16; ++i) ds[u][i] = ok[u] ? ds[u][i] : 0.f;
                 }
@@ -148,36 +163,45 @@ __global__ __launch_bounds__(512) void window_dq_kernel(const WindowParams p)
             if (bias_grad) {
 #pragma unroll
                 for (int a = 0; a < 4; ++a) {
-                    const int lo = ring_place + off[tile * 8 + 2 * a], hi = ring_place + off[tile * 8 + 2 * a + 1];
+                    double *const lo = ring + ((ring_place + off[tile * 8 + 2 * a] / 4) & ring_mask);
+                    double *const hi = ring + ((ring_place + off[tile * 8 + 2 * a + 1] / 4) & ring_mask);
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         if constexpr (U == 2) {
                             const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(ds[0][4 * a + j]), __float_as_uint(ds[U - 1][4 * a + j]), false, false);
-                            lds_add(ring + ((lo + j) & ring_mask), __uint_as_float(x[0]));
-                            lds_add(ring + ((hi + j) & ring_mask), __uint_as_float(x[1]));
+                            lds_add(lo + j, __uint_as_float(x[0]));
+                            lds_add(hi + j, __uint_as_float(x[1]));
                         } else {
-                            if (half == 0) lds_add(ring + ((lo + j) & ring_mask), ds[0][4 * a + j]);
-                            if (half == 1) lds_add(ring + ((hi + j) & ring_mask), ds[0][4 * a + j]);
+                            if (half == 0) lds_add(lo + j, ds[0][4 * a + j]);
+                            if (half == 1) lds_add(hi + j, ds[0][4 * a + j]);
                         }
                     }
                 }
                 const int t = t0 + tile * 32 + 32;  // the next tile's first key
-                const int done = t < w.L ? t / w.wp * p.tw + t % w.wp : mine.len;
+                const int y = w.row(t), done = t < w.L ? y * p.tw + t - y * w.wp : mine.len;
                 for (int i = left + lane; i < done; i += 64) {
-                    part[i] = (float)ring[i & ring_mask];
-                    ring[i & ring_mask] = 0.0;
+                    const int at = i & ring_mask;
+                    double sum = ring[at];
+                    ring[at] = 0.0;
+                    if (at < 4) sum += ring[p.ring + at], ring[p.ring + at] = 0.0;
+                    part[i] = (float)sum;
                 }
                 left = done;
             }
         };
-        if (busy)
-            for (int tile = 0; tile < G::TK / 32 && t0 + tile * 32 < w.L; ++tile) {
-                if (__builtin_expect(far, 0)) tile_of(tile, std::true_type{});
-                else tile_of(tile, std::false_type{});
+        if (busy) {
+            if (__builtin_expect(!far, 1)) {
+#pragma unroll
+                for (int tile = 0; tile < G::TK / 32; ++tile)
+                    if (t0 + tile * 32 < w.L) tile_of(tile, std::false_type{});
+            } else {
+#pragma unroll 1
+                for (int tile = 0; tile < G::TK / 32 && t0 + tile * 32 < w.L; ++tile) tile_of(tile, std::true_type{});
             }
+        }
         if (p.buffers == 1) __syncthreads();
         else turn ^= 1;
-        if (more) stager.write(p, w, k, v, t0 + G::TK, lds + turn * S::BYTES);
+        if (more) stager.write(p, w, k, v, t0 + G::TK, staged + turn * S::BYTES);
         __syncthreads();
     }
     if (!busy) return;
@@ -194,16 +218,17 @@ __global__ __launch_bounds__(512) void window_dq_kernel(const WindowParams p)
 }
 
 template <typename T, int DP>
-__global__ __launch_bounds__(512) void window_dkv_kernel(const WindowParams p)
+__global__ __launch_bounds__(512, (WinGeom<T, DP>::F32 || DP == 64) ? 2 : KVB) void window_dkv_kernel(const WindowParams p)
 {
     using G = WinGeom<T, DP>;
     using S = Stager<T, DP, true, true, true, true>;  // queries and the result's gradient, by tokens and by channels
-    constexpr int U = 1;
+    constexpr int U = G::KEY_TILES;
     // of the staged queries: the exponent's shift with the sum's logarithm, -delta; for large shifts the largest score and the logarithm
     // by themselves; a flag of each wavefront that has seen such a shift
     constexpr int ROWS_AT = S::BYTES, FAR_AT = ROWS_AT + 4 * G::TK * 4, BYTES = FAR_AT + 4 * kWinMaxWaves;
     extern __shared__ __align__(16) char lds[];
-    float *table = reinterpret_cast<float *>(lds + p.buffers * BYTES);
+    float *table = reinterpret_cast<float *>(lds);
+    char *const staged = lds + (size_t)p.len * 4;
 
     const int unit = unit_of(p.units);
     if (unit < 0) return;
@@ -212,37 +237,37 @@ __global__ __launch_bounds__(512) void window_dkv_kernel(const WindowParams p)
     const int keys = p.waves * 32 * U, k0 = block * keys;
     if (k0 >= w.L) return;
     const int centre = (p.wh - 1) * p.tw + p.ww - 1;
-    const TableRange range = table_range(k0, min(k0 + keys, w.L), w.h, w.wp, p.tw, centre, 1);
+    const TableRange range = table_range(w, k0, min(k0 + keys, w.L), p.tw, centre, 1);
 
     const long hw = (long)p.H * p.W;
     const int lane = threadIdx.x & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int group = p.heads / p.kv_heads, chunks = (w.L + G::TK - 1) / G::TK;
+    const int group = p.heads / p.kv_heads;
     const int wk0 = k0 + wave * 32 * U;
     const bool busy = wk0 < w.L;
     const T *k = static_cast<const T *>(p.k) + w.n * p.ks + kvh * (long)p.d * hw;
     const T *v = static_cast<const T *>(p.v) + w.n * p.vs + kvh * (long)p.d * hw;
     const T *q = static_cast<const T *>(p.q) + w.n * p.qs, *go = static_cast<const T *>(p.go) + (long)w.n * p.heads * p.d * hw;
 
-    // a chunk's number counts through the group's heads
+    // chunks of queries of one head after the other of the group
     S stager;
     float from, log_sum, delta;  // of this thread's query of the next chunk, as they come
+    bool in;
     auto fetch_row = [&](int head, int t) {
-        const long pix = ((long)w.n * p.heads + head) * hw + Spot(p, w, t, 1).at;
+        const Spot spot(p, w, t, 1);
+        const long pix = ((long)w.n * p.heads + head) * hw + spot.at;
         from = p.top[pix], log_sum = p.log_sum[pix], delta = p.delta[pix];
+        in = spot.bits != 0;
     };
-    auto fetch = [&](int c) {
-        const int head = kvh * group + c / chunks, t0 = c % chunks * G::TK;
+    auto fetch = [&](int head, int t0) {
         stager.fetch(p, w, q + head * (long)p.d * hw, go + head * (long)p.d * hw, t0);
         fetch_row(head, t0 + min((int)threadIdx.x, G::TK - 1));
     };
-    auto write = [&](int c, char *buf) {
-        const int head = kvh * group + c / chunks, t0 = c % chunks * G::TK;
+    auto write = [&](int head, int t0, char *buf) {
         stager.write(p, w, q + head * (long)p.d * hw, go + head * (long)p.d * hw, t0, buf);
         bool large = false;
         for (int r = threadIdx.x; r < G::TK; r += blockDim.x) {
             if (r != (int)threadIdx.x) fetch_row(head, t0 + r);
             // (masked pixels have a sum of +infinity and a delta of 0; those beyond the window get them here)
-            const bool in = Spot(p, w, t0 + r, 1).bits != 0;
             float *rows = reinterpret_cast<float *>(buf + ROWS_AT) + r;
             const float shift = in ? from * p.log2_scale : 0.f, l = in ? log_sum : __builtin_inff();
             large = large || __builtin_fabsf(shift) > kLargeShift;
@@ -253,33 +278,41 @@ __global__ __launch_bounds__(512) void window_dkv_kernel(const WindowParams p)
         if (lane == 0) flags[wave] = any;
         if ((int)threadIdx.x >= p.waves && threadIdx.x < kWinMaxWaves) flags[threadIdx.x] = 0;
     };
-    fetch(0);
+    int head = kvh * group;
+    fetch(head, 0);
     Fragment<T, DP> own_k[U], own_v[U];
     int pixel[U], place[U];
     bool there[U], ok[U];
     wf32x16 dk[U][G::DT], dv[U][G::DT];
+    {
+        OwnValues<T, DP> vk[U], vv[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-        const int t = wk0 + u * 32 + (lane & 31), tc = min(t, w.L - 1);
-        const int y = tc / w.wp, x = tc - y * w.wp;
-        there[u] = t < w.L && x < w.w;
-        ok[u] = there[u] && seen(p, w, y, x);
-        pixel[u] = (w.y0 + y) * p.W + w.x0 + x;
-        place[u] = centre + (y * p.tw + x) - range.base;
-        own_k[u] = own_fragment<T, DP>(p, k + pixel[u], ok[u]);
-        own_v[u] = own_fragment<T, DP>(p, v + pixel[u], ok[u]);
+        for (int u = 0; u < U; ++u) {
+            const OwnToken own_token(p, w, wk0 + u * 32 + (lane & 31));
+            there[u] = own_token.there, pixel[u] = own_token.pixel, ok[u] = own_token.ok(p);
+            place[u] = 4 * (range.len - 1 - (centre + own_token.off - range.base));
+            vk[u].fetch(p, k, pixel[u]);
+            vv[u].fetch(p, v, pixel[u]);
+        }
+        stage_table<true>(p, table, range, kvh * group);
 #pragma unroll
-        for (int b = 0; b < G::DT; ++b) dk[u][b] = wf32x16{}, dv[u][b] = wf32x16{};
+        for (int u = 0; u < U; ++u) {
+            vk[u].clean(p, ok[u]);
+            vv[u].clean(p, ok[u]);
+            own_k[u] = fragment_of(vk[u]);
+            own_v[u] = fragment_of(vv[u]);
+#pragma unroll
+            for (int b = 0; b < G::DT; ++b) dk[u][b] = wf32x16{}, dv[u][b] = wf32x16{};
+        }
     }
-    stage_table(p, table, range, kvh * group);
-    write(0, lds);
+    write(head, 0, staged);
     __syncthreads();
 
-    for (int c = 0, turn = 0; c < chunks * group; ++c) {
-        const bool more = c + 1 < chunks * group;
-        const int t0 = c % chunks * G::TK;
-        if (more) fetch(c + 1);
-        const char *buf = lds + turn * BYTES;
+    for (int t0 = 0, turn = 0;;) {
+        const bool last = t0 + G::TK >= w.L, more = !last || head + 1 < (kvh + 1) * group;
+        const int next_t0 = last ? 0 : t0 + G::TK, next_head = last ? head + 1 : head;
+        if (more) fetch(next_head, next_t0);
+        const char *buf = staged + turn * BYTES;
         const int *off = reinterpret_cast<const int *>(buf + S::OFF_AT);
         const float *rows = reinterpret_cast<const float *>(buf + ROWS_AT);
         const wu32x4 flags = *reinterpret_cast<const wu32x4 *>(buf + FAR_AT) | *reinterpret_cast<const wu32x4 *>(buf + FAR_AT + 16);
@@ -293,10 +326,10 @@ __global__ __launch_bounds__(512) void window_dkv_kernel(const WindowParams p)
                 wf32x16 s, dp;
 #pragma unroll
                 for (int a = 0; a < 4; ++a) {
-                    const float *at = table + place[u] - off[tile * 8 + 2 * a + half];
+                    const float *at = reinterpret_cast<const float *>(reinterpret_cast<const char *>(table) + (place[u] + off[tile * 8 + 2 * a + half]));
                     const wf32x4 d = *reinterpret_cast<const wf32x4 *>(rows + G::TK + tile * 32 + 8 * a + 4 * half);
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) s[4 * a + j] = at[-j], dp[4 * a + j] = d[j];
+                    for (int j = 0; j < 4; ++j) s[4 * a + j] = at[j], dp[4 * a + j] = d[j];
                 }
                 s = score<T, DP, true>(buf + S::RM0_AT, tile, own_k[u], s);
                 dp = score<T, DP>(buf + S::RM1_AT, tile, own_v[u], dp);
@@ -314,8 +347,7 @@ __global__ __launch_bounds__(512) void window_dkv_kernel(const WindowParams p)
                     }
                 }
                 if (!whole) {
-                    asm volatile("; queries that do not take part");
-                    leave_out(bits, 0.f, s);
+                                        leave_out(bits, 0.f, s);
                 }
                 ep[u] = pack<G::NT>(s);
 #pragma unroll
@@ -325,19 +357,26 @@ __global__ __launch_bounds__(512) void window_dkv_kernel(const WindowParams p)
             accumulate<T, DP>(buf + S::CM1_AT, tile, ep, dv);
             accumulate<T, DP>(buf + S::CM0_AT, tile, es, dk);
         };
-        if (busy)
-            for (int tile = 0; tile < G::TK / 32 && t0 + tile * 32 < w.L; ++tile) {
-                if (__builtin_expect(far, 0)) tile_of(tile, std::true_type{});
-                else tile_of(tile, std::false_type{});
+        if (busy) {
+            if (__builtin_expect(!far, 1)) {
+#pragma unroll
+                for (int tile = 0; tile < G::TK / 32; ++tile)
+                    if (t0 + tile * 32 < w.L) tile_of(tile, std::false_type{});
+            } else {
+#pragma unroll 1
+                for (int tile = 0; tile < G::TK / 32 && t0 + tile * 32 < w.L; ++tile) tile_of(tile, std::true_type{});
             }
+        }
         if (p.buffers == 1) __syncthreads();
         else turn ^= 1;
-        if (more) write(c + 1, lds + turn * BYTES);
-        if (more && (c + 1) % chunks == 0) {  // (uniform) another head's biases: nobody may still read the last one's
+        if (!more) break;
+        write(next_head, next_t0, staged + turn * BYTES);
+        if (last) {  // (uniform) another head's biases: nobody may still read the last one's
             if (p.buffers != 1) __syncthreads();
-            stage_table(p, table, range, kvh * group + (c + 1) / chunks);
+            stage_table<true>(p, table, range, next_head);
         }
         __syncthreads();
+        t0 = next_t0, head = next_head;
     }
     if (!busy) return;
     T *gk = static_cast<T *>(p.gk) + w.n * p.gks + kvh * (long)p.d * hw;
@@ -356,23 +395,30 @@ __global__ __launch_bounds__(512) void window_dkv_kernel(const WindowParams p)
             }
 }
 
-// Sums of equal offsets over the wavefronts' parts, every `splits`-th window's, in order.
+// Sums of equal offsets over the wavefronts' parts, every `splits`-th window's, in order.  Parts of one window are read eight at a time.
 __global__ __launch_bounds__(256) void window_offsets_kernel(const WindowParams p)
 {
     const int at = blockIdx.x * 256 + threadIdx.x, head = blockIdx.y;
-    if (at >= p.th * p.tw) return;
     const int centre = (p.wh - 1) * p.tw + p.ww - 1, tokens = 32 * p.tiles, windows = p.N * p.gy * p.gx;
     float sum = 0.f;
     for (int wi = blockIdx.z; wi < windows; wi += p.splits) {
         const Win w = win_of(p, wi / (p.gy * p.gx), wi / p.gx % p.gy, wi % p.gx);
         const float *part = p.part + (long)(wi * p.heads + head) * p.blocks * p.waves * p.part_len;
-        for (int t0 = 0; t0 < w.L; t0 += tokens, part += p.part_len) {
-            const TableRange r = table_range(t0, min(t0 + tokens, w.L), w.h, w.wp, p.tw, centre, -1);
-            const int in = at - r.base;
-            if (in >= 0 && in < r.len) sum += part[in];
+        for (int t0 = 0; t0 < w.L; t0 += 8 * tokens) {
+            float v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int t = t0 + i * tokens;
+                const TableRange r = table_range(w, t, min(t + tokens, w.L), p.tw, centre, -1);
+                const int in = at - r.base;
+                v[i] = t < w.L && in >= 0 && in < r.len ? part[in] : 0.f;
+                part += p.part_len;
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum += v[i];
         }
     }
-    p.part2[((long)blockIdx.z * p.heads + head) * p.th * p.tw + at] = sum;
+    if (at < p.th * p.tw) p.part2[((long)blockIdx.z * p.heads + head) * p.th * p.tw + at] = sum;
 }
 
 // The offsets (inclusive) along one axis that a bucket holds, cut to those that exist.
@@ -415,7 +461,7 @@ __global__ __launch_bounds__(256) void window_buckets_kernel(const WindowParams 
 template <typename T, int DP>
 size_t dq_lds(const WindowParams &p)
 {
-    return p.buffers * (size_t)Stager<T, DP, true, true, true, false>::BYTES + (p.grad_bias != nullptr ? (size_t)p.waves * p.ring * 8 : 0) + (size_t)p.len * 4;
+    return p.buffers * (size_t)Stager<T, DP, true, true, true, false>::BYTES + (p.grad_bias != nullptr ? (size_t)p.waves * (p.ring + 4) * 8 : 0) + (size_t)p.len * 4;
 }
 template <typename T, int DP>
 size_t dkv_lds(const WindowParams &p)

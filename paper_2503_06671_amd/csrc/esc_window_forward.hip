@@ -27,7 +27,8 @@ __global__ __launch_bounds__(512) void window_forward_kernel(const WindowParams 
     constexpr bool SUM_ROW = DP == 16;                  // the exponentials' sum is row 16 of the product
     constexpr int VT = G::F32 ? 3 : SAVE ? 2 : 1;
     extern __shared__ __align__(16) char lds[];
-    float *table = reinterpret_cast<float *>(lds + 2 * S::BYTES);
+    float *table = reinterpret_cast<float *>(lds);  // (first: its reads' addresses are then sums of two terms and a constant)
+    char *const staged = lds + (size_t)p.len * 4;
 
     const int unit = unit_of(p.units);
     if (unit < 0) return;
@@ -36,7 +37,7 @@ __global__ __launch_bounds__(512) void window_forward_kernel(const WindowParams 
     const int queries = p.waves / p.ksplit * (U * 32), q0 = block * queries;
     if (q0 >= w.L) return;
     const int centre = (p.wh - 1) * p.tw + p.ww - 1;
-    const TableRange range = table_range(q0, min(q0 + queries, w.L), w.h, w.wp, p.tw, centre, -1);
+    const TableRange range = table_range(w, q0, min(q0 + queries, w.L), p.tw, centre, -1);
 
     const long hw = (long)p.H * p.W;
     const int lane = threadIdx.x & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -49,27 +50,33 @@ __global__ __launch_bounds__(512) void window_forward_kernel(const WindowParams 
     S stager;
     stager.fetch(p, w, k, v, 0);
     Fragment<T, DP> own[U];
-    int pixel[U], place[U];  // place: in the table, of the offset to the key that has off = 0
+    int pixel[U], place[U];  // place: in the table, in bytes, of the offset to the key that has off = 0
     bool ok[U], there[U];
-    float top[U], sum[U];
+    float top[U], limit[U], shift[U], sum[U];
+    bool far = false;  // (uniform) a shift is large
     wf32x16 acc[U][G::DT];
+    {
+        OwnValues<T, DP> values[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-        const int t = wq0 + u * 32 + (lane & 31), tc = min(t, w.L - 1);
-        const int y = tc / w.wp, x = tc - y * w.wp;
-        there[u] = t < w.L && x < w.w;
-        ok[u] = there[u] && seen(p, w, y, x);
-        pixel[u] = (w.y0 + y) * p.W + w.x0 + x;
-        place[u] = centre - (y * p.tw + x) - range.base;
-        own[u] = own_fragment<T, DP>(p, q + pixel[u], ok[u]);
-        top[u] = -__builtin_inff(), sum[u] = 0.f;
+        for (int u = 0; u < U; ++u) {
+            const OwnToken own_token(p, w, wq0 + u * 32 + (lane & 31));
+            there[u] = own_token.there, pixel[u] = own_token.pixel, ok[u] = own_token.ok(p);
+            place[u] = 4 * (centre - own_token.off - range.base);
+            values[u].fetch(p, q, pixel[u]);
+        }
+        stage_table<false>(p, table, range, head);
 #pragma unroll
-        for (int b = 0; b < G::DT; ++b) acc[u][b] = wf32x16{};
+        for (int u = 0; u < U; ++u) {
+            values[u].clean(p, ok[u]);
+            own[u] = fragment_of(values[u]);
+            top[u] = limit[u] = -__builtin_inff(), shift[u] = sum[u] = 0.f;
+#pragma unroll
+            for (int b = 0; b < G::DT; ++b) acc[u][b] = wf32x16{};
+        }
     }
-    stage_table(p, table, range, head);
-    S::ones(lds + S::CM1_AT);
-    S::ones(lds + S::BYTES + S::CM1_AT);
-    stager.write(p, w, k, v, 0, lds);
+    S::ones(staged + S::CM1_AT);
+    S::ones(staged + S::BYTES + S::CM1_AT);
+    stager.write(p, w, k, v, 0, staged);
     __syncthreads();
     const float slack = kSlack / p.log2_scale;
     const bool busy = wq0 < w.L;
@@ -77,7 +84,7 @@ __global__ __launch_bounds__(512) void window_forward_kernel(const WindowParams 
     for (int t0 = 0, turn = 0; t0 < w.L; t0 += G::TK, turn ^= 1) {
         const bool more = t0 + G::TK < w.L;
         if (more) stager.fetch(p, w, k, v, t0 + G::TK);
-        const char *buf = lds + turn * S::BYTES;
+        const char *buf = staged + turn * S::BYTES;
         const int *off = reinterpret_cast<const int *>(buf + S::OFF_AT);
         if (busy)
 #pragma unroll  // (in a loop the compiler waits for the next chunk's loads first)
@@ -88,58 +95,78 @@ __global__ __launch_bounds__(512) void window_forward_kernel(const WindowParams 
                 int key[4];
 #pragma unroll
                 for (int a = 0; a < 4; ++a) key[a] = off[tile * 8 + 2 * a + half];
-                Packed<VT> e[U];
+                wf32x16 s[U];
+                float m[U];
+                bool over = false;
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
-                    wf32x16 s;
 #pragma unroll
                     for (int a = 0; a < 4; ++a) {
-                        const float *from = table + place[u] + key[a];
+                        const float *from = reinterpret_cast<const float *>(reinterpret_cast<const char *>(table) + (place[u] + key[a]));
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) s[4 * a + j] = from[j];
+                        for (int j = 0; j < 4; ++j) s[u][4 * a + j] = from[j];
                     }
-                    s = score<T, DP>(buf + S::RM0_AT, tile, own[u], s);
-                    if (!whole) {
-                        asm volatile("; keys that do not take part");  // (keeps the selection out of the way of whole tiles)
-                        leave_out(bits, -__builtin_inff(), s);
-                    }
-                    float m = fmaxf(s[0], s[1]);
+                    s[u] = score<T, DP>(buf + S::RM0_AT, tile, own[u], s[u]);
+                }
+                if (!whole) {
 #pragma unroll
-                    for (int i = 2; i < 16; i += 2) m = fmaxf(fmaxf(m, s[i]), s[i + 1]);
-                    m = fmaxf(m, other_half(m));
-                    if (__any(m > top[u] + slack)) {
-                        const float old = top[u], next = fmaxf(old, m);
+                    for (int u = 0; u < U; ++u) leave_out(bits, -__builtin_inff(), s[u]);
+                }
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    m[u] = fmaxf(s[u][0], s[u][1]);
+#pragma unroll
+                    for (int i = 2; i < 16; i += 2) m[u] = fmaxf(fmaxf(m[u], s[u][i]), s[u][i + 1]);
+                    m[u] = max_of_halves(m[u]);
+                    over = over || m[u] > limit[u];
+                }
+                if (__any(over)) {
+                    far = false;
+#pragma unroll
+                    for (int u = 0; u < U; ++u) {
+                        const float old = top[u], next = fmaxf(old, m[u]);
                         // (a row that has seen no key yet has nothing to shrink)
                         const float shrink = old == -__builtin_inff() ? 0.f : exp2_of((old - next) * p.log2_scale);
-                        top[u] = next;
+                        top[u] = next, limit[u] = next + slack;
+                        shift[u] = next == -__builtin_inff() ? 0.f : next * p.log2_scale;
+                        far = far || __any(__builtin_fabsf(shift[u]) > kLargeShift);
                         sum[u] *= shrink;
 #pragma unroll
                         for (int b = 0; b < G::DT; ++b)
 #pragma unroll
                             for (int i = 0; i < 16; ++i) acc[u][b][i] *= shrink;
                     }
-                    const float from = top[u] == -__builtin_inff() ? 0.f : top[u], shift = from * p.log2_scale;
-                    if (__builtin_expect(!__any(__builtin_fabsf(shift) > kLargeShift), 1)) {
+                }
+                if (__builtin_expect(!far, 1)) {
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) s[i] = __builtin_fmaf(s[i], p.log2_scale, -shift);
-                    } else {
-                        asm volatile("; large scores");
+                    for (int u = 0; u < U; ++u)
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) s[i] = (s[i] - from) * p.log2_scale;
+                        for (int i = 0; i < 16; ++i) s[u][i] = __builtin_fmaf(s[u][i], p.log2_scale, -shift[u]);
+                } else {
+                    asm volatile("; large scores");
+#pragma unroll
+                    for (int u = 0; u < U; ++u) {
+                        const float from = top[u] == -__builtin_inff() ? 0.f : top[u];
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) s[u][i] = (s[u][i] - from) * p.log2_scale;
                     }
+                }
+                Packed<VT> e[U];
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) s[i] = exp2_of(s[i]);
+                for (int u = 0; u < U; ++u) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) s[u][i] = exp2_of(s[u][i]);
                     if constexpr (!SUM_ROW) {
                         float add = 0.f;
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) add += s[i];
+                        for (int i = 0; i < 16; ++i) add += s[u][i];
                         sum[u] += add;
                     }
-                    e[u] = pack<VT>(s);
+                    e[u] = pack<VT>(s[u]);
                 }
                 accumulate<T, DP>(buf + S::CM1_AT, tile, e, acc);
             }
-        if (more) stager.write(p, w, k, v, t0 + G::TK, lds + (turn ^ 1) * S::BYTES);
+        if (more) stager.write(p, w, k, v, t0 + G::TK, staged + (turn ^ 1) * S::BYTES);
         __syncthreads();
     }
 
@@ -176,10 +203,9 @@ __global__ __launch_bounds__(512) void window_forward_kernel(const WindowParams 
     for (int u = 0; u < U; ++u) {
         float all;
         if constexpr (SUM_ROW) {  // (row 16 lies with the lower half)
-            const float low = other_half(acc[u][0][8]);
-            all = half == 0 ? acc[u][0][8] : low;
+            all = sum_of_halves(half == 0 ? acc[u][0][8] : 0.f);
         } else {
-            all = sum[u] + other_half(sum[u]);
+            all = sum_of_halves(sum[u]);
         }
         if (!there[u]) continue;
         const bool some = ok[u] && !(all == 0.f);

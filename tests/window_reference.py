@@ -149,9 +149,8 @@ def held(x, up):
     size = torch.where(torch.isfinite(x), x.abs(), torch.zeros(()))
     top = torch.nn.functional.pad(size, (0, blocks * BLOCK - n)).reshape(blocks, BLOCK).amax(1)
     full = top >= TINY
-    most = torch.full_like(top, CODE_MAX)  # (a tensor: with a number torch multiplies by a reciprocal)
-    scale = torch.where(full, top / most, torch.zeros(()))
-    y = x * torch.where(full, most / top, torch.zeros(())).repeat_interleave(BLOCK)[:n]
+    scale = torch.where(full, top * f32(1 / CODE_MAX), torch.zeros(()))
+    y = x * torch.where(full, CODE_MAX * (torch.ones(()) / top), torch.zeros(())).repeat_interleave(BLOCK)[:n]
     y = torch.where(torch.isfinite(y), y, torch.full((), math.nan))
     if up:
         y = torch.where((y > 0) & (y < 2.0 ** -9), torch.full((), 2.0 ** -9), y)
