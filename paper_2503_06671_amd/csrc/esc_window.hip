@@ -43,16 +43,15 @@ int table_words(const WindowParams &p, long tokens)
 // The backward's wavefronts: as many as leave a block for each compute unit, up to eight; fewer, and one staging buffer instead of two, where LDS
 // does not hold them.  Two blocks on a compute unit are worth more than wavefronts in one.
 template <typename F>
-bool choose_waves(WindowParams &p, int tiles, int heads, F lds)
+bool choose_waves(WindowParams &p, int heads, F lds)
 {
     const long tokens = (long)p.wh * ((p.ww + 3) & ~3), windows = (long)p.N * p.gy * p.gx * heads;
-    p.tiles = tiles;
-    const long each = 32 * p.tiles, all = (tokens + each - 1) / each;
+    const long all = (tokens + 31) / 32;
     const int want = (int)std::max<long>(1, std::min({(long)kWinMaxWaves, all, all * windows / kCus}));
     for (size_t limit : {kLdsPerCu / 2, kLdsPerCu})
         for (int buffers : {2, 1})
             for (int waves = want; waves >= (limit == kLdsPerCu ? 1 : std::min(want, 4)); --waves) {
-                p.waves = waves, p.buffers = buffers, p.len = (table_words(p, waves * each) + 3) & ~3;
+                p.waves = waves, p.buffers = buffers, p.len = (table_words(p, waves * 32) + 3) & ~3;
                 if (lds(p) <= limit) {
                     p.blocks = (int)((all + waves - 1) / waves);
                     return true;
@@ -122,14 +121,14 @@ bool plan_forward(WindowParams &p, bool f32)
 }
 bool plan_dq(WindowParams &p, bool f32)
 {
-    const int dp = dim_padded(p.d), tiles = window_query_tiles(f32, dp);
-    const int reach = widest(p, [&](int wp) { return span(p, wp, 32) + span(p, wp, 32 * tiles) + 1; });
+    const int dp = dim_padded(p.d);
+    const int reach = widest(p, [&](int wp) { return 2 * span(p, wp, 32) + 1; });
     for (p.ring = 64; p.ring < reach;) p.ring *= 2;
-    p.part_len = table_words(p, 32 * tiles);
+    p.part_len = table_words(p, 32);
     // (the same plan with and without the table's gradient)
     float *const grad = p.grad_bias;
     p.grad_bias = reinterpret_cast<float *>(16);
-    const bool fits = choose_waves(p, tiles, p.heads, [&](const WindowParams &x) { return window_dq_lds(x, f32, dp); });
+    const bool fits = choose_waves(p, p.heads, [&](const WindowParams &x) { return window_dq_lds(x, f32, dp); });
     p.grad_bias = grad;
     if (!fits || !set_units(p, p.heads)) return false;
     p.splits = (int)std::min<long>(32, (long)p.N * p.gy * p.gx);
@@ -138,7 +137,7 @@ bool plan_dq(WindowParams &p, bool f32)
 bool plan_dkv(WindowParams &p, bool f32)
 {
     const int dp = dim_padded(p.d);
-    return choose_waves(p, 1, p.kv_heads, [&](const WindowParams &x) { return window_dkv_lds(x, f32, dp); }) && set_units(p, p.kv_heads);
+    return choose_waves(p, p.kv_heads, [&](const WindowParams &x) { return window_dkv_lds(x, f32, dp); }) && set_units(p, p.kv_heads);
 }
 
 struct Scratch {

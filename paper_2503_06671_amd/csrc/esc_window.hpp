@@ -63,7 +63,6 @@ struct WindowParams {
 };
 
 size_t window_forward_lds(bool f32, int dp, int len, int joined);  // joined: wavefronts whose sums are joined, or 0
-int window_query_tiles(bool f32, int dp);
 size_t window_dq_lds(const WindowParams &p, bool f32, int dp);  // (buffers, waves, ring, len and grad_bias set)
 size_t window_dkv_lds(const WindowParams &p, bool f32, int dp);
 hipError_t launch_window_forward(const WindowParams &p, bool f32, int dp, hipStream_t s);
@@ -89,14 +88,6 @@ struct WinGeom {
     static constexpr int TK = F32 ? (DP == 64 ? 32 : 64) : (DP == 16 ? 128 : 64);
     static constexpr int KS = DP / 16;                 // matrix instructions a score takes (of each pair of terms)
     static constexpr int DT = DP <= 32 ? 1 : 2;        // blocks of 32 channels of an output
-#ifndef DQT
-#define DQT 2
-#endif
-#ifndef KT
-#define KT 1
-#endif
-    static constexpr int KEY_TILES = F32 || DP == 64 ? 1 : KT;
-    static constexpr int QUERY_TILES = F32 || DP == 64 ? 1 : DQT;  // backward: tiles of 32 own queries of a wavefront (two where the registers hold them); its keys: one
     // rows of tokens: 16-byte pieces of eight channels, [term][channels / 8][token]; four tokens of a group lie SLOT pieces
     // apart, so that 16 lanes' pieces cover all banks once, written and read
     static constexpr int SLOT = TK / 4 + 4;
@@ -191,6 +182,16 @@ __device__ __forceinline__ void stage_table(const WindowParams &p, float *table,
     }
 }
 
+// split_bf16's three terms of two values, in eleven instructions: the halves are taken from the values as they are.
+__device__ __forceinline__ void three_terms(float v0, float v1, uint32_t (&t)[3])
+{
+#pragma unroll
+    for (int q = 0; q < 3; ++q) {
+        const uint32_t a = __float_as_uint(v0), b = __float_as_uint(v1);
+        t[q] = __builtin_amdgcn_perm(b, a, 0x07060302u);
+        if (q < 2) v0 -= __uint_as_float(a & 0xffff0000u), v1 -= __uint_as_float(b & 0xffff0000u);
+    }
+}
 __device__ __forceinline__ uint32_t low_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); }
 __device__ __forceinline__ uint32_t high_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
 
@@ -283,7 +284,7 @@ struct Piece {
             const bool c = c4 * 4 + i < p.d;
             if constexpr (G::F32) {
                 uint32_t q[3];
-                split_bf16(c && ok0 ? (s.skip != 0 ? v[i].y : v[i].x) : 0.f, c && ok1 ? v[i].y : 0.f, q);
+                three_terms(c && ok0 ? (s.skip != 0 ? v[i].y : v[i].x) : 0.f, c && ok1 ? v[i].y : 0.f, q);
 #pragma unroll
                 for (int k = 0; k < 3; ++k) word[k][i] = q[k];
             } else {
@@ -410,7 +411,7 @@ __device__ __forceinline__ Fragment<T, DP> fragment_of(const OwnValues<T, DP> &o
             const T a = o.v[s][2 * i], b = o.v[s][2 * i + 1];
             if constexpr (G::F32) {
                 uint32_t t[3];
-                split_bf16(a, b, t);
+                three_terms(a, b, t);
 #pragma unroll
                 for (int q = 0; q < 3; ++q) f.r[q][s][i] = t[q];
             } else {
@@ -467,7 +468,7 @@ __device__ __forceinline__ Packed<NT> pack(const wf32x16 &v)
                     uint32_t, __builtin_convertvector(wf32x2{a - __uint_as_float(h << 16), b - __uint_as_float(h & 0xffff0000u)}, wbf16x2));
         } else {
             uint32_t t[3];
-            split_bf16(v[2 * i], v[2 * i + 1], t);
+            three_terms(v[2 * i], v[2 * i + 1], t);
 #pragma unroll
             for (int q = 0; q < 3; ++q) o.r[q][i / 4][i % 4] = t[q];
         }

@@ -8,8 +8,8 @@
 //     query heads that share the key's.
 //
 // The sums of equal offsets, in a fixed order.  Each wavefront adds to a ring of its own in LDS, in 64 bits: ds_add_f64 takes 8.5 clocks for 64
-// lanes where ds_add_f32 takes 193 (measured).  No instruction holds two values of one offset: its 64 lanes are 64 queries and one key (two
-// tiles of queries: permlane32_swap brings their halves together), or 32 queries and one key (one tile, half after half).  What the ring
+// lanes where ds_add_f32 takes 193 (measured).  No instruction holds two values of one offset: its lanes are 32 queries and one
+// key, one half of the wavefront after the other.  What the ring
 // spans are the offsets between the wavefront's queries and ONE tile of keys; offsets that the next tile no longer reaches are complete and
 // leave for memory.  Two small kernels add the wavefronts' parts and the offsets of each bucket.
 #include "esc_window.hpp"
@@ -19,20 +19,19 @@ namespace {
 
 __device__ __forceinline__ void lds_add(double *p, float v) { __hip_atomic_fetch_add(p, (double)v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP); }
 
-// The offsets of all its window's keys from the tokens [t0, t0 + 32 U) of a wavefront: from the smallest on.
-template <int U>
+// The offsets of all its window's keys from the 32 tokens from t0 on: from the smallest on.
 __device__ __forceinline__ TableRange wave_range(const WindowParams &p, const Win &w, int t0)
 {
     const int centre = (p.wh - 1) * p.tw + p.ww - 1;
-    return table_range(w, t0, min(t0 + 32 * U, w.L), p.tw, centre, -1);
+    return table_range(w, t0, min(t0 + 32, w.L), p.tw, centre, -1);
 }
 
 template <typename T, int DP>
-__global__ __launch_bounds__(512, (WinGeom<T, DP>::F32 || DP == 64 || DQT == 2) ? 2 : 4) void window_dq_kernel(const WindowParams p)
+__global__ __launch_bounds__(512, (WinGeom<T, DP>::F32 || DP == 64) ? 2 : 4) void window_dq_kernel(const WindowParams p)
 {
     using G = WinGeom<T, DP>;
     using S = Stager<T, DP, true, true, true, false>;  // keys by tokens and by channels, values by tokens
-    constexpr int U = G::QUERY_TILES;
+    constexpr int U = 1;
     extern __shared__ __align__(16) char lds[];
     float *table = reinterpret_cast<float *>(lds);  // (first: its reads' addresses are then sums of two terms and a constant)
     double *rings = reinterpret_cast<double *>(lds + (size_t)p.len * 4);  // one a wavefront
@@ -111,10 +110,9 @@ __global__ __launch_bounds__(512, (WinGeom<T, DP>::F32 || DP == 64 || DQT == 2) 
         }
     }
     double *const ring = rings + wave * (p.ring + 4);  // (four places more: a group of four that runs over the end stays together)
-    const int ring_mask = p.ring - 1;
-    const TableRange mine = wave_range<U>(p, w, min(wq0, w.L - 1));
-    // ring place of the offset to the key with off = 0: of the lane's query where 64 lanes are 64 queries, else of its own
-    const int ring_place = (U == 1 || half == 0 ? place[0] : place[U - 1]) / 4 + range.base - mine.base;
+    const int ring_mask = 8 * p.ring - 8;  // (in bytes)
+    const TableRange mine = wave_range(p, w, min(wq0, w.L - 1));
+    const int ring_place = 2 * place[0] + 8 * (range.base - mine.base);  // in the ring, in bytes, of the offset to the key that has off = 0
     float *const part = p.part + ((long)unit * p.waves + wave) * p.part_len;
     int left = 0;  // offsets that have left the ring
     if (bias_grad)
@@ -161,26 +159,22 @@ __global__ __launch_bounds__(512, (WinGeom<T, DP>::F32 || DP == 64 || DQT == 2) 
             }
             accumulate<T, DP>(buf + S::CM0_AT, tile, e, acc);
             if (bias_grad) {
+                // (both halves of a query's lanes; the second after the first: keys four tokens apart see equal offsets of queries four apart)
+                double *to[4];
 #pragma unroll
-                for (int a = 0; a < 4; ++a) {
-                    double *const lo = ring + ((ring_place + off[tile * 8 + 2 * a] / 4) & ring_mask);
-                    double *const hi = ring + ((ring_place + off[tile * 8 + 2 * a + 1] / 4) & ring_mask);
+                for (int a = 0; a < 4; ++a) to[a] = reinterpret_cast<double *>(reinterpret_cast<char *>(ring) + ((ring_place + 2 * key[a]) & ring_mask));
+                if (half == 0) {
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        if constexpr (U == 2) {
-                            const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(ds[0][4 * a + j]), __float_as_uint(ds[U - 1][4 * a + j]), false, false);
-                            lds_add(lo + j, __uint_as_float(x[0]));
-                            lds_add(hi + j, __uint_as_float(x[1]));
-                        } else {
-                            if (half == 0) lds_add(lo + j, ds[0][4 * a + j]);
-                            if (half == 1) lds_add(hi + j, ds[0][4 * a + j]);
-                        }
-                    }
+                    for (int i = 0; i < 16; ++i) lds_add(to[i / 4] + i % 4, ds[0][i]);
+                }
+                if (half == 1) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) lds_add(to[i / 4] + i % 4, ds[0][i]);
                 }
                 const int t = t0 + tile * 32 + 32;  // the next tile's first key
                 const int y = w.row(t), done = t < w.L ? y * p.tw + t - y * w.wp : mine.len;
                 for (int i = left + lane; i < done; i += 64) {
-                    const int at = i & ring_mask;
+                    const int at = i & (p.ring - 1);
                     double sum = ring[at];
                     ring[at] = 0.0;
                     if (at < 4) sum += ring[p.ring + at], ring[p.ring + at] = 0.0;
@@ -218,11 +212,11 @@ __global__ __launch_bounds__(512, (WinGeom<T, DP>::F32 || DP == 64 || DQT == 2) 
 }
 
 template <typename T, int DP>
-__global__ __launch_bounds__(512, (WinGeom<T, DP>::F32 || DP == 64) ? 2 : KVB) void window_dkv_kernel(const WindowParams p)
+__global__ __launch_bounds__(512, (WinGeom<T, DP>::F32 || DP == 64) ? 2 : 3) void window_dkv_kernel(const WindowParams p)
 {
     using G = WinGeom<T, DP>;
     using S = Stager<T, DP, true, true, true, true>;  // queries and the result's gradient, by tokens and by channels
-    constexpr int U = G::KEY_TILES;
+    constexpr int U = 1;
     // of the staged queries: the exponent's shift with the sum's logarithm, -delta; for large shifts the largest score and the logarithm
     // by themselves; a flag of each wavefront that has seen such a shift
     constexpr int ROWS_AT = S::BYTES, FAR_AT = ROWS_AT + 4 * G::TK * 4, BYTES = FAR_AT + 4 * kWinMaxWaves;
@@ -399,7 +393,7 @@ __global__ __launch_bounds__(512, (WinGeom<T, DP>::F32 || DP == 64) ? 2 : KVB) v
 __global__ __launch_bounds__(256) void window_offsets_kernel(const WindowParams p)
 {
     const int at = blockIdx.x * 256 + threadIdx.x, head = blockIdx.y;
-    const int centre = (p.wh - 1) * p.tw + p.ww - 1, tokens = 32 * p.tiles, windows = p.N * p.gy * p.gx;
+    const int centre = (p.wh - 1) * p.tw + p.ww - 1, tokens = 32, windows = p.N * p.gy * p.gx;
     float sum = 0.f;
     for (int wi = blockIdx.z; wi < windows; wi += p.splits) {
         const Win w = win_of(p, wi / (p.gy * p.gx), wi / p.gx % p.gy, wi % p.gx);
@@ -494,12 +488,6 @@ hipError_t launch_dkv(const WindowParams &p, hipStream_t s)
 }
 
 }  // namespace
-
-int window_query_tiles(bool f32, int dp)
-{
-    if (f32) return dp == 16 ? WinGeom<float, 16>::QUERY_TILES : dp == 32 ? WinGeom<float, 32>::QUERY_TILES : WinGeom<float, 64>::QUERY_TILES;
-    return dp == 16 ? WinGeom<uint16_t, 16>::QUERY_TILES : dp == 32 ? WinGeom<uint16_t, 32>::QUERY_TILES : WinGeom<uint16_t, 64>::QUERY_TILES;
-}
 
 size_t window_dq_lds(const WindowParams &p, bool f32, int dp)
 {
