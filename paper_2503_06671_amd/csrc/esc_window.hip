@@ -41,14 +41,15 @@ int table_words(const WindowParams &p, long tokens)
 }
 
 // The backward's wavefronts: as many as leave a block for each compute unit, up to eight; fewer, and one staging buffer instead of two, where LDS
-// does not hold them.  Two blocks on a compute unit are worth more than wavefronts in one.
+// does not hold them.  Two blocks on a compute unit are worth more than wavefronts in one, where their registers fit (not with fp32 storage, nor with
+// heads wider than 32).
 template <typename F>
-bool choose_waves(WindowParams &p, int heads, F lds)
+bool choose_waves(WindowParams &p, int heads, bool alone, F lds)
 {
     const long tokens = (long)p.wh * ((p.ww + 3) & ~3), windows = (long)p.N * p.gy * p.gx * heads;
     const long all = (tokens + 31) / 32;
     const int want = (int)std::max<long>(1, std::min({(long)kWinMaxWaves, all, all * windows / kCus}));
-    for (size_t limit : {kLdsPerCu / 2, kLdsPerCu})
+    for (size_t limit : {alone ? kLdsPerCu : kLdsPerCu / 2, kLdsPerCu})
         for (int buffers : {2, 1})
             for (int waves = want; waves >= (limit == kLdsPerCu ? 1 : std::min(want, 4)); --waves) {
                 p.waves = waves, p.buffers = buffers, p.len = (table_words(p, waves * 32) + 3) & ~3;
@@ -128,16 +129,16 @@ bool plan_dq(WindowParams &p, bool f32)
     // (the same plan with and without the table's gradient)
     float *const grad = p.grad_bias;
     p.grad_bias = reinterpret_cast<float *>(16);
-    const bool fits = choose_waves(p, p.heads, [&](const WindowParams &x) { return window_dq_lds(x, f32, dp); });
+    const bool fits = choose_waves(p, p.heads, f32 || dp == 64, [&](const WindowParams &x) { return window_dq_lds(x, f32, dp); });
     p.grad_bias = grad;
     if (!fits || !set_units(p, p.heads)) return false;
-    p.splits = (int)std::min<long>(32, (long)p.N * p.gy * p.gx);
+    p.splits = (int)std::min<long>(64, (long)p.N * p.gy * p.gx);
     return true;
 }
 bool plan_dkv(WindowParams &p, bool f32)
 {
     const int dp = dim_padded(p.d);
-    return choose_waves(p, p.kv_heads, [&](const WindowParams &x) { return window_dkv_lds(x, f32, dp); }) && set_units(p, p.kv_heads);
+    return choose_waves(p, p.kv_heads, f32 || dp == 64, [&](const WindowParams &x) { return window_dkv_lds(x, f32, dp); }) && set_units(p, p.kv_heads);
 }
 
 struct Scratch {

@@ -316,37 +316,44 @@ template <typename T, int DP, bool RM0, bool CM0, bool RM1, bool CM1>
 struct Stager {
     using G = WinGeom<T, DP>;
     static constexpr int GROUPS = G::TK / 4, PAIRS = G::TK / 2;
-    static constexpr int HALF = DP / 4 * PAIRS, ITEMS = 2 * HALF;
     static constexpr int RM0_AT = 0, CM0_AT = RM0_AT + (RM0 ? G::RM_BYTES : 0), RM1_AT = CM0_AT + (CM0 ? G::CM_BYTES : 0),
                          CM1_AT = RM1_AT + (RM1 ? G::RM_BYTES : 0), BITS_AT = CM1_AT + (CM1 ? G::CM_BYTES : 0), OFF_AT = BITS_AT + PAIRS,
                          BYTES = (OFF_AT + GROUPS * 4 + 15) / 16 * 16;
     Piece<T, DP> next;
 
+    // pieces of one operand: of the channels that exist (the others' place is cleared once)
+    __device__ __forceinline__ static int half(const WindowParams &p) { return (p.d + 3) / 4 * PAIRS; }
     __device__ __forceinline__ static int pair_of(int item) { return item % PAIRS; }
-    __device__ __forceinline__ static int channels_of(int item) { return item % HALF / PAIRS; }
+    __device__ __forceinline__ static int channels_of(int item, int half) { return (item < half ? item : item - half) / PAIRS; }
     __device__ __forceinline__ static void put(const Piece<T, DP> &piece, const WindowParams &p, int item, char *buf)
     {
-        const int g2 = pair_of(item), c4 = channels_of(item);
-        if (item < HALF) piece.template store<RM0, CM0>(p, buf + RM0_AT, buf + CM0_AT, reinterpret_cast<uint8_t *>(buf + BITS_AT), g2, c4);
+        const int h = half(p), g2 = pair_of(item), c4 = channels_of(item, h);
+        if (item < h) piece.template store<RM0, CM0>(p, buf + RM0_AT, buf + CM0_AT, reinterpret_cast<uint8_t *>(buf + BITS_AT), g2, c4);
         else piece.template store<RM1, CM1>(p, buf + RM1_AT, buf + CM1_AT, nullptr, g2, c4);
     }
     __device__ __forceinline__ void fetch(const WindowParams &p, const Win &w, const T *op0, const T *op1, int t0)
     {
-        const int item = min((int)threadIdx.x, ITEMS - 1);
-        next.fetch(p, w, item < HALF ? op0 : op1, t0 + 2 * pair_of(item), channels_of(item));
+        const int h = half(p), item = min((int)threadIdx.x, 2 * h - 1);
+        next.fetch(p, w, item < h ? op0 : op1, t0 + 2 * pair_of(item), channels_of(item, h));
     }
     __device__ __forceinline__ void write(const WindowParams &p, const Win &w, const T *op0, const T *op1, int t0, char *buf)
     {
-        if ((int)threadIdx.x < ITEMS) put(next, p, threadIdx.x, buf);
-        for (int item = threadIdx.x + blockDim.x; item < ITEMS; item += blockDim.x) {
+        const int h = half(p);
+        if ((int)threadIdx.x < 2 * h) put(next, p, threadIdx.x, buf);
+        for (int item = threadIdx.x + blockDim.x; item < 2 * h; item += blockDim.x) {
             Piece<T, DP> piece;
-            piece.fetch(p, w, item < HALF ? op0 : op1, t0 + 2 * pair_of(item), channels_of(item));
+            piece.fetch(p, w, item < h ? op0 : op1, t0 + 2 * pair_of(item), channels_of(item, h));
             put(piece, p, item, buf);
             __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): all have come, but the compiler sees paths on which nobody waited
         }
         stage_offsets<G::TK>(p, w, t0, reinterpret_cast<int *>(buf + OFF_AT));
     }
-    // the rows of ones (DP = 16), once for each buffer
+    // What no piece writes, once for each buffer and in front of a barrier: zeros for the channels that do not exist, rows of ones (DP = 16).
+    __device__ __forceinline__ static void clear(const WindowParams &p, char *buf)
+    {
+        if ((p.d + 3) / 4 * 4 < DP)
+            for (int i = threadIdx.x; i < BITS_AT / 16; i += blockDim.x) reinterpret_cast<wu32x4 *>(buf)[i] = wu32x4{};
+    }
     __device__ __forceinline__ static void ones(char *cm)
     {
         if constexpr (DP == 16)

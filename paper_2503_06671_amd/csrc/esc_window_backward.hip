@@ -117,6 +117,9 @@ __global__ __launch_bounds__(512, (WinGeom<T, DP>::F32 || DP == 64) ? 2 : 4) voi
     int left = 0;  // offsets that have left the ring
     if (bias_grad)
         for (int i = lane; i < p.ring + 4; i += 64) ring[i] = 0.0;
+    S::clear(p, staged);
+    if (p.buffers == 2) S::clear(p, staged + S::BYTES);
+    __syncthreads();
     stager.write(p, w, k, v, 0, staged);
     __syncthreads();
 
@@ -299,6 +302,9 @@ __global__ __launch_bounds__(512, (WinGeom<T, DP>::F32 || DP == 64) ? 2 : 3) voi
             for (int b = 0; b < G::DT; ++b) dk[u][b] = wf32x16{}, dv[u][b] = wf32x16{};
         }
     }
+    S::clear(p, staged);
+    if (p.buffers == 2) S::clear(p, staged + BYTES);
+    __syncthreads();
     write(head, 0, staged);
     __syncthreads();
 
@@ -389,30 +395,39 @@ __global__ __launch_bounds__(512, (WinGeom<T, DP>::F32 || DP == 64) ? 2 : 3) voi
             }
 }
 
-// Sums of equal offsets over the wavefronts' parts, every `splits`-th window's, in order.  Parts of one window are read eight at a time.
+// Sums of equal offsets over the wavefronts' parts, every `splits`-th window's, in order.  A thread has four offsets (the parts' ranges are worked
+// out once for them), and reads four parts at a time.
 __global__ __launch_bounds__(256) void window_offsets_kernel(const WindowParams p)
 {
-    const int at = blockIdx.x * 256 + threadIdx.x, head = blockIdx.y;
-    const int centre = (p.wh - 1) * p.tw + p.ww - 1, tokens = 32, windows = p.N * p.gy * p.gx;
-    float sum = 0.f;
+    constexpr int EACH = 4, AHEAD = 4;
+    const int at0 = blockIdx.x * (256 * EACH) + threadIdx.x, head = blockIdx.y;
+    const int centre = (p.wh - 1) * p.tw + p.ww - 1, windows = p.N * p.gy * p.gx;
+    float sum[EACH] = {};
     for (int wi = blockIdx.z; wi < windows; wi += p.splits) {
         const Win w = win_of(p, wi / (p.gy * p.gx), wi / p.gx % p.gy, wi % p.gx);
         const float *part = p.part + (long)(wi * p.heads + head) * p.blocks * p.waves * p.part_len;
-        for (int t0 = 0; t0 < w.L; t0 += 8 * tokens) {
-            float v[8];
+        for (int t0 = 0; t0 < w.L; t0 += 32 * AHEAD) {
+            float v[AHEAD][EACH];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int t = t0 + i * tokens;
-                const TableRange r = table_range(w, t, min(t + tokens, w.L), p.tw, centre, -1);
-                const int in = at - r.base;
-                v[i] = t < w.L && in >= 0 && in < r.len ? part[in] : 0.f;
+            for (int i = 0; i < AHEAD; ++i) {
+                const int t = t0 + 32 * i;
+                const TableRange r = table_range(w, t, min(t + 32, w.L), p.tw, centre, -1);
+#pragma unroll
+                for (int e = 0; e < EACH; ++e) {
+                    const int in = at0 + 256 * e - r.base;
+                    v[i][e] = t < w.L && in >= 0 && in < r.len ? part[in] : 0.f;
+                }
                 part += p.part_len;
             }
 #pragma unroll
-            for (int i = 0; i < 8; ++i) sum += v[i];
+            for (int i = 0; i < AHEAD; ++i)
+#pragma unroll
+                for (int e = 0; e < EACH; ++e) sum[e] += v[i][e];
         }
     }
-    if (at < p.th * p.tw) p.part2[((long)blockIdx.z * p.heads + head) * p.th * p.tw + at] = sum;
+#pragma unroll
+    for (int e = 0; e < EACH; ++e)
+        if (at0 + 256 * e < p.th * p.tw) p.part2[((long)blockIdx.z * p.heads + head) * p.th * p.tw + at0 + 256 * e] = sum[e];
 }
 
 // The offsets (inclusive) along one axis that a bucket holds, cut to those that exist.
@@ -430,23 +445,33 @@ __device__ __forceinline__ void bucket_range(const WindowParams &p, int b, int f
     *hi = min(*hi, n - 1);
 }
 
-// A wavefront for each bucket: the sums of its offsets.
+// The sums of each bucket's offsets: a wavefront for each where every offset has its own, a block where buckets hold many.
 __global__ __launch_bounds__(256) void window_buckets_kernel(const WindowParams p)
 {
-    const int b = blockIdx.x * 4 + (threadIdx.x >> 6), head = blockIdx.y, lane = threadIdx.x & 63;
-    if (b >= p.nby * p.nbx) return;
-    int y0, y1, x0, x1;
-    bucket_range(p, b / p.nbx, p.win_h, p.wh, &y0, &y1);
-    bucket_range(p, b % p.nbx, p.win_w, p.ww, &x0, &x1);
-    const int cols = x1 - x0 + 1, count = y1 >= y0 && cols > 0 ? (y1 - y0 + 1) * cols * p.splits : 0;
+    __shared__ float part[4];
+    const int wave = threadIdx.x >> 6, head = blockIdx.y, lane = threadIdx.x & 63;
+    const bool whole = p.n_edges > 0;
+    const int b = whole ? blockIdx.x : blockIdx.x * 4 + wave, threads = whole ? 256 : 64;
     float sum = 0.f;
-    for (int i = lane; i < count; i += 64) {
-        const int split = i % p.splits, o = i / p.splits, y = y0 + o / cols, x = x0 + o % cols;
-        sum += p.part2[((long)split * p.heads + head) * p.th * p.tw + (y + p.wh - 1) * p.tw + x + p.ww - 1];
+    if (b < p.nby * p.nbx) {
+        int y0, y1, x0, x1;
+        bucket_range(p, b / p.nbx, p.win_h, p.wh, &y0, &y1);
+        bucket_range(p, b % p.nbx, p.win_w, p.ww, &x0, &x1);
+        const int cols = x1 - x0 + 1, count = y1 >= y0 && cols > 0 ? (y1 - y0 + 1) * cols * p.splits : 0;
+#pragma unroll 4
+        for (int i = whole ? threadIdx.x : lane; i < count; i += threads) {
+            const int split = i % p.splits, o = i / p.splits, y = y0 + o / cols, x = x0 + o % cols;
+            sum += p.part2[((long)split * p.heads + head) * p.th * p.tw + (y + p.wh - 1) * p.tw + x + p.ww - 1];
+        }
     }
 #pragma unroll
     for (int m = 32; m >= 1; m >>= 1) sum += __shfl_xor(sum, m);
-    if (lane == 0) {
+    if (whole) {
+        if (lane == 0) part[wave] = sum;
+        __syncthreads();
+        sum = part[0] + part[1] + part[2] + part[3];
+    }
+    if ((whole ? threadIdx.x == 0 : lane == 0) && b < p.nby * p.nbx) {
         float *to = p.grad_bias + (long)head * p.nby * p.nbx + b;
         *to = p.accumulate != 0 ? *to + sum : sum;
     }
@@ -515,10 +540,10 @@ hipError_t launch_window_dkv(const WindowParams &p, bool f32, int dp, hipStream_
 
 hipError_t launch_window_bias_grad(const WindowParams &p, hipStream_t s)
 {
-    hipLaunchKernelGGL(window_offsets_kernel, dim3((unsigned)((p.th * p.tw + 255) / 256), (unsigned)p.heads, (unsigned)p.splits), dim3(256), 0, s, p);
+    hipLaunchKernelGGL(window_offsets_kernel, dim3((unsigned)((p.th * p.tw + 1023) / 1024), (unsigned)p.heads, (unsigned)p.splits), dim3(256), 0, s, p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(window_buckets_kernel, dim3((unsigned)((p.nby * p.nbx + 3) / 4), (unsigned)p.heads), dim3(256), 0, s, p);
+    hipLaunchKernelGGL(window_buckets_kernel, dim3((unsigned)(p.n_edges > 0 ? p.nby * p.nbx : (p.nby * p.nbx + 3) / 4), (unsigned)p.heads), dim3(256), 0, s, p);
     return hipGetLastError();
 }
 

@@ -74,6 +74,9 @@ __global__ __launch_bounds__(512) void window_forward_kernel(const WindowParams 
             for (int b = 0; b < G::DT; ++b) acc[u][b] = wf32x16{};
         }
     }
+    S::clear(p, staged);
+    S::clear(p, staged + S::BYTES);
+    __syncthreads();
     S::ones(staged + S::CM1_AT);
     S::ones(staged + S::BYTES + S::CM1_AT);
     stager.write(p, w, k, v, 0, staged);
