@@ -35,7 +35,7 @@ struct WindowParams {
     const void *out_in, *go;             // backward: the forward's result and its gradient
     void *out;
     float *top, *log_sum;                // [N, heads, H, W]: a row's largest score (unscaled), log2 of its sum of exponentials, +inf without keys
-    void *rest;                          // bf16 storage: what rounding took from out
+    void *rest;                          // bf16 storage: what rounding took from out (16 bits each)
     void *gq, *gk, *gv;
     long gqs, gks, gvs;
     float *delta;                        // [N, heads, H, W]: sum over d of out * grad_out
@@ -539,6 +539,13 @@ __device__ __forceinline__ uint16_t to_bf16(float v)
     typedef __bf16 one;
     return __builtin_bit_cast(uint16_t, (one)v);
 }
+// What rounding v to r took from it, so that the two give v again: v's bits less those of r, 16 of them.  (v halfway between two, rounded down: 2^15 does
+// not fit, one less does, 2^-24 off.)
+__device__ __forceinline__ uint16_t taken_by_rounding(float v, uint16_t r)
+{
+    return (uint16_t)min((int)(__float_as_uint(v) - ((uint32_t)r << 16)), 0x7fff);
+}
+__device__ __forceinline__ float unrounded(uint16_t r, uint16_t taken) { return __uint_as_float(((uint32_t)r << 16) + (uint32_t)(int)(int16_t)taken); }
 template <typename T>
 __device__ __forceinline__ T narrow(float v)
 {

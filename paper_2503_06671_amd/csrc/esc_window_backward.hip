@@ -17,6 +17,12 @@
 namespace esc {
 namespace {
 
+// ds in the products with keys and queries, with bf16 storage: two terms.  Its sum over a query's keys is 0, so what one rounding of each term takes
+// weighs more in the sums than it does in those of p: dq and dk were 0.0025 off with one term and are 0.0017, which is the rounding of the
+// results alone, for 50 us more of 571 (dq) and 77 of 589 (dkv) for 64 maps of 64 x 64.  p in dv's sums has one: 0.0023, and 135 us more with two.
+template <typename T>
+constexpr int kDsTerms = std::is_same<T, float>::value ? 3 : 2;
+
 __device__ __forceinline__ void lds_add(double *p, float v) { __hip_atomic_fetch_add(p, (double)v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP); }
 
 // The offsets of all its window's keys from the 32 tokens from t0 on: from the smallest on.
@@ -85,6 +91,7 @@ __global__ __launch_bounds__(512, (WinGeom<T, DP>::F32 || DP == 64) ? 2 : 4) voi
             vq[u].clean(p, ok[u]);
             vgo[u].clean(p, ok[u]);
             vout[u].clean(p, ok[u]);
+            if constexpr (!G::F32) vrest[u].clean(p, ok[u]);
             own_q[u] = fragment_of(vq[u]);
             own_go[u] = fragment_of(vgo[u]);
             float sum = 0.f;
@@ -92,11 +99,9 @@ __global__ __launch_bounds__(512, (WinGeom<T, DP>::F32 || DP == 64) ? 2 : 4) voi
             for (int s = 0; s < G::KS; ++s)
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    float o = widen(vout[u].v[s][j]);
-                    if constexpr (!G::F32) {
-                        vrest[u].clean(p, ok[u]);
-                        o += widen(vrest[u].v[s][j]);
-                    }
+                    float o;
+                    if constexpr (G::F32) o = vout[u].v[s][j];
+                    else o = unrounded(vout[u].v[s][j], vrest[u].v[s][j]);
                     sum = __builtin_fmaf(o, widen(vgo[u].v[s][j]), sum);
                 }
             delta[u] = sum_of_halves(sum);
@@ -135,7 +140,7 @@ __global__ __launch_bounds__(512, (WinGeom<T, DP>::F32 || DP == 64) ? 2 : 4) voi
 #pragma unroll
             for (int a = 0; a < 4; ++a) key[a] = off[tile * 8 + 2 * a + half];
             wf32x16 ds[U];
-            Packed<G::NT> e[U];
+            Packed<kDsTerms<T>> e[U];
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 wf32x16 s;
@@ -158,7 +163,7 @@ __global__ __launch_bounds__(512, (WinGeom<T, DP>::F32 || DP == 64) ? 2 : 4) voi
 #pragma unroll
                     for (int i = 0; i < 16; ++i) ds[u][i] = ok[u] ? ds[u][i] : 0.f;
                 }
-                e[u] = pack<G::NT>(ds[u]);
+                e[u] = pack<kDsTerms<T>>(ds[u]);
             }
             accumulate<T, DP>(buf + S::CM0_AT, tile, e, acc);
             if (bias_grad) {
@@ -320,7 +325,8 @@ __global__ __launch_bounds__(512, (WinGeom<T, DP>::F32 || DP == 64) ? 2 : 3) voi
         auto tile_of = [&](int tile, auto large) {
             const wu32x4 bits = *reinterpret_cast<const wu32x4 *>(buf + S::BITS_AT + tile * 16);
             const bool whole = all_take_part(bits);
-            Packed<G::NT> ep[U], es[U];
+            Packed<G::NT> ep[U];
+            Packed<kDsTerms<T>> es[U];
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 wf32x16 s, dp;
@@ -352,7 +358,7 @@ __global__ __launch_bounds__(512, (WinGeom<T, DP>::F32 || DP == 64) ? 2 : 3) voi
                 ep[u] = pack<G::NT>(s);
 #pragma unroll
                 for (int i = 0; i < 16; ++i) s[i] *= dp[i];
-                es[u] = pack<G::NT>(s);
+                es[u] = pack<kDsTerms<T>>(s);
             }
             accumulate<T, DP>(buf + S::CM1_AT, tile, ep, dv);
             accumulate<T, DP>(buf + S::CM0_AT, tile, es, dk);
