@@ -33,8 +33,8 @@
  *     Ks >= 19, give NaN/Inf exactly where the definition does.
  *   - All arguments are validated on the host before the first launch; a call
  *     that returns an error has enqueued nothing.
- *   - Every compute call needs a workspace (work queue and the mailboxes blocks
- *     use to hand over the GAP sums and DK).  It must have been prepared once with
+ *   - Every call of the ConvAttn module needs a workspace (work queue and the mailboxes
+ *     blocks use to hand over the GAP sums and DK).  It must have been prepared once with
  *     esc_workspace_init on a stream ordered before its first use; calls leave it
  *     ready for the next call, whatever its shape, so it carries state from call
  *     to call and must not be cleared or reused for anything else in between.
@@ -52,6 +52,9 @@
  *     expire, the values that never came are taken as NaN - the affected outputs
  *     are NaN, never silently wrong numbers - and the workspace's error word is
  *     raised; esc_workspace_errors reads it.
+ *   - Window attention and the AdamW step wait for no other block and take no prepared
+ *     workspace: on different streams, each with its own outputs and scratch, they may run
+ *     at once.
  *   - Limits: 0 <= C_a <= min(C, 256); estimator hidden width <= 256; Ks odd,
  *     1 <= Ks <= 31; H*W < 2^31; N, C, H, W >= 1.  No lower bound on H or W
  *     relative to Ks.
@@ -319,14 +322,16 @@ esc_status esc_convattn_backward(const void *x, const void *grad_out, esc_dtype 
  *   mask         device, one byte a pixel [N, H, W], or NULL: pixels whose byte is 0 do not exist, as in images padded to a common size:
  *                they are nobody's key, their own out is 0, and whatever q, k, v hold there (NaN too) is not used
  *   out          [N, heads * head_dim, H, W], contiguous, rounded once
- *   saved        what the backward pass needs (the rows' log-sum, and with bf16 storage what rounding took from out), or NULL:
- *                esc_window_attention_saved_bytes, 256-byte aligned
+ *   saved        what the backward pass needs (the rows' largest scores and logarithms of their sums, with bf16 storage also what rounding
+ *                took from out), or NULL: esc_window_attention_saved_bytes, 256-byte aligned
  * A pixel with no key left (a bias of -infinity everywhere) has out = 0.  Scores, maxima and sums are fp32.  bf16 storage: products of the stored
- * values on the matrix cores, the exponentials rounded to bf16 as operands of the second product (their sum is of the unrounded
- * ones).  fp32 storage: values and exponentials as three bf16 terms each (exact), six products of terms (what is left out lies
- * below 2^-24 of a product: fp32 accuracy); a value of q, k or v that is not finite makes NaN of what its products reach.
+ * values on the matrix cores, the exponentials rounded to bf16 as operands of the second product (2^-9 of each term at most; where
+ * `saved` is given they are three bf16 terms, exact, since the bias' gradient, an fp32 result, comes of the same sums: the two may round
+ * an element of out differently).  fp32 storage: values and exponentials as three bf16 terms each (exact), six products of terms (what is left out
+ * lies below 2^-21 of a product, 2^-24 on average); a value of q, k or v that is not finite makes NaN of what its products reach.
  * Limits: head_dim <= 64; (2 h - 1)(2 w - 1) <= 16384 offsets, h and w the window's sides or the map's where those are smaller (64 x 64 pixels, or
- * 1 x 8192); win_h, win_w <= 8192; heads <= 1024; n_edges <= ESC_WINDOW_MAX_EDGES; 2^-20 <= scale <= 64.
+ * 1 x 8192); win_h, win_w <= 8192; heads <= 1024; n_edges <= ESC_WINDOW_MAX_EDGES; 2^-20 <= scale <= 64;
+ * windows x heads x wavefronts (one for 32 or 64 of a window's pixels, one at least) <= 2^26; ESC_ERR_UNSUPPORTED beyond.
  * One launch; no workspace.  Biases over scale beyond 2^120 count as 2^120.
  */
 #define ESC_WINDOW_MAX_EDGES 32
@@ -351,11 +356,11 @@ esc_status esc_window_attention_forward(const void *q, const void *k, const void
  *                     heads that several heads share are the sums over them; 0 at masked pixels)
  *   g->bias           fp32, shaped like bias, summed over images, windows and all pairs of a bucket, or NULL;
  *                     accumulate != 0 adds it to what the buffer holds
- * The scores are formed again.  Sums are fp32, each in a fixed order: equal calls give equal bits.  With bf16 storage the probabilities
- * and their gradients are rounded to bf16 as operands of the products that give q's, k's and v's gradients, not in the
- * bias' gradient.  The workspace (esc_window_attention_backward_workspace_bytes, 256-byte aligned, either storage type) is plain scratch: it needs no
- * preparation and its contents are undefined after the call.  What is written may not overlap anything else.  Two launches, with
- * the bias' gradient four.
+ * The scores are formed again.  Sums are fp32 (those of a bucket begin in 64 bits), each in a fixed order: equal calls give equal bits.  With bf16
+ * storage, as operands of the products that give q's, k's and v's gradients, the probabilities are rounded to bf16 and the scores'
+ * gradients to two bf16 terms; the bias' gradient takes them unrounded.  The workspace (esc_window_attention_backward_workspace_bytes, 256-byte
+ * aligned, either storage type) is plain scratch: it needs no preparation and its contents are undefined after the call.  What is
+ * written may not overlap anything else.  Two launches, with the bias' gradient four.
  */
 typedef struct esc_window_grads {
     void *q, *k, *v;

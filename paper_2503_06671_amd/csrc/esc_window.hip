@@ -19,53 +19,71 @@ constexpr long kCus = 256, kSimds = 4 * kCus;
 
 int dim_padded(int d) { return d <= 16 ? 16 : d <= 32 ? 32 : 64; }
 
-// How far the offsets' numbers of `tokens` consecutive tokens lie apart at most, in rows of wp tokens.
-int span(const WindowParams &p, int wp, long tokens)
+// How far the offsets' numbers of `tokens` consecutive tokens of a window lie apart at most.
+int span(const WindowParams &p, int width, long tokens)
 {
+    const int wp = in_pairs(width), tw = 2 * width - 1;
     const long rows = std::min<long>(p.wh - 1, (tokens - 1 + wp - 1) / wp);
-    if (p.tw < wp) return (int)(rows * p.tw) + wp - 1;
-    return (int)std::min<long>(tokens - 1 + rows * (p.tw - wp), (long)rows * p.tw + wp - 1);
+    if (tw < wp) return (int)(rows * tw) + wp - 1;
+    return (int)std::min<long>(tokens - 1 + rows * (tw - wp), (long)rows * tw + wp - 1);
 }
 
-// The most over the windows' widths (the last one of a row may be narrower) of f(row length).
+// The most over the windows' widths (the last one of a row may be narrower) of f(width).
 template <typename F>
 int widest(const WindowParams &p, F f)
 {
-    return std::max(f((p.ww + 3) & ~3), f((p.W - (p.gx - 1) * p.ww + 3) & ~3));
+    return std::max(f(p.ww), f(p.W - (p.gx - 1) * p.ww));
 }
 
 // Words of the table of a block that has `tokens` tokens: their offsets to all tokens of any window of the map.
 int table_words(const WindowParams &p, long tokens)
 {
-    return widest(p, [&](int wp) { return (p.wh - 1) * p.tw + wp - 1 + span(p, wp, tokens) + 1; });
+    return widest(p, [&](int width) { return (p.wh - 1) * (2 * width - 1) + in_pairs(width) + span(p, width, tokens); });
 }
 
 // The backward's wavefronts: as many as leave a block for each compute unit, up to eight; fewer, and one staging buffer instead of two, where LDS
 // does not hold them.  Two blocks on a compute unit are worth more than wavefronts in one, where their registers fit (not with fp32 storage, nor with
-// heads wider than 32).
+// heads wider than 32).  Blocks of fewer than four wavefronts (small windows): what leaves most of them on a compute unit, up to what its registers
+// hold; and one buffer where a window is one chunk (6 heads of 33 channels, fp32, windows of 6 x 6, gradients: 935 us, with two buffers 1449; 3 x 5,
+// 32 channels, forward: 127 and 281).
 template <typename F>
-bool choose_waves(WindowParams &p, int heads, bool alone, F lds)
+bool choose_waves(WindowParams &p, int heads, bool f32, int dp, F lds)
 {
-    const long tokens = (long)p.wh * ((p.ww + 3) & ~3), windows = (long)p.N * p.gy * p.gx * heads;
+    const long tokens = (long)p.wh * in_pairs(p.ww), windows = (long)p.N * p.gy * p.gx * heads;
     const long all = (tokens + 31) / 32;
     const int want = (int)std::max<long>(1, std::min({(long)kWinMaxWaves, all, all * windows / kCus}));
-    for (size_t limit : {alone ? kLdsPerCu : kLdsPerCu / 2, kLdsPerCu})
-        for (int buffers : {2, 1})
-            for (int waves = want; waves >= (limit == kLdsPerCu ? 1 : std::min(want, 4)); --waves) {
-                p.waves = waves, p.buffers = buffers, p.len = (table_words(p, waves * 32) + 3) & ~3;
-                if (lds(p) <= limit) {
-                    p.blocks = (int)((all + waves - 1) / waves);
-                    return true;
+    const int most = tokens <= win_chunk(f32, dp) ? 1 : 2;
+    const bool alone = f32 || dp == 64;
+    auto take = [&](int owners, int buffers, size_t limit) {
+        p.owners = owners, p.buffers = buffers, p.len = (table_words(p, owners * 32) + 3) & ~3;
+        p.blocks = (int)((all + owners - 1) / owners);
+        return lds(p) <= limit;
+    };
+    if (want < 4) {
+        int best = 0, best_owners = 0, best_buffers = 0;
+        for (int buffers = most; buffers >= 1; --buffers)
+            for (int owners = want; owners >= 1; --owners)
+                if (take(owners, buffers, kLdsPerCu)) {
+                    const int resident = (int)std::min<size_t>(alone ? 8 : 16, kLdsPerCu / lds(p) * owners);
+                    if (resident > best) best = resident, best_owners = owners, best_buffers = buffers;
                 }
-            }
+        return best > 0 && take(best_owners, best_buffers, kLdsPerCu);
+    }
+    for (size_t limit : {alone ? kLdsPerCu : kLdsPerCu / 2, kLdsPerCu})
+        for (int buffers = most; buffers >= 1; --buffers)
+            for (int owners = want; owners >= (limit == kLdsPerCu ? 1 : 4); --owners)
+                if (take(owners, buffers, limit)) return true;
     return false;
 }
 
+// All blocks.  Where there are few, of few wavefronts, up to four help staging (6 heads of 48 channels that share one key, 8 sequences of 969 in
+// windows of 600, bf16, gradients: 386 us, without 742; with many blocks they only take room: 3 x 339 x 511, windows of 13: 351, without 307).
 bool set_units(WindowParams &p, int heads)
 {
     const __int128 units = (__int128)p.N * p.gy * p.gx * heads * p.blocks;
-    if (units > 0x7fffff00) return false;
+    if (units * p.owners * 64 > 0xffff0000u) return false;  // (a launch has fewer than 2^32 lanes)
     p.units = (int)units;
+    for (p.waves = p.owners; p.waves < 4 && (long)p.units * p.waves < 2 * kSimds;) p.waves *= 2;
     return true;
 }
 
@@ -76,6 +94,7 @@ esc_status shape(const esc_window_attn *a, WindowParams *p)
     if (a->heads % a->kv_heads != 0) return ESC_ERR_SHAPE;
     if (a->head_dim > kWinMaxDim || a->heads > 1024 || a->win_h > 8192 || a->win_w > 8192) return ESC_ERR_UNSUPPORTED;
     if ((size_t)a->H * (size_t)a->W >= ((size_t)1 << 31)) return ESC_ERR_UNSUPPORTED;
+    if ((__int128)a->N * a->heads * a->head_dim * a->H * a->W > (__int128)1 << 46) return ESC_ERR_UNSUPPORTED;  // (sizes in bytes stay far from 64 bits)
     if (a->n_edges < 0) return ESC_ERR_SHAPE;
     if (a->n_edges > kWinMaxEdges) return ESC_ERR_UNSUPPORTED;
     p->N = a->N, p->H = a->H, p->W = a->W, p->heads = a->heads, p->kv_heads = a->kv_heads, p->d = a->head_dim;
@@ -102,7 +121,7 @@ size_t table_bytes(const WindowParams &p) { return (size_t)p.heads * p.nby * p.n
 bool plan_forward(WindowParams &p, bool f32)
 {
     const int dp = dim_padded(p.d);
-    const long tokens = (long)p.wh * ((p.ww + 3) & ~3), each = (tokens + 31) / 32, windows = (long)p.N * p.gy * p.gx * p.heads;
+    const long tokens = (long)p.wh * in_pairs(p.ww), each = (tokens + 31) / 32, windows = (long)p.N * p.gy * p.gx * p.heads;
     const long all = each * windows;
     p.tiles = (f32 ? dp < 64 : each < 16) && all >= 2 * 2 * kSimds && each > 1 ? 2 : 1;
     const long waves = (each + p.tiles - 1) / p.tiles;
@@ -110,10 +129,11 @@ bool plan_forward(WindowParams &p, bool f32)
     while (p.tiles == 1 && p.ksplit < 4 && waves * windows * p.ksplit < 2 * kSimds && tokens >= 128 * p.ksplit) p.ksplit *= 2;
     long queries = std::min<long>(kWinMaxWaves / p.ksplit, waves);
     queries = std::max<long>(1, std::min(queries, waves * windows / kCus));
+    p.buffers = tokens <= win_chunk(f32, dp) ? 1 : 2;
     for (; queries >= 1; --queries) {
-        p.waves = (int)queries * p.ksplit;
+        p.owners = (int)queries * p.ksplit;
         p.len = (table_words(p, (int)queries * p.tiles * 32) + 3) & ~3;
-        if (window_forward_lds(f32, dp, p.len, p.ksplit > 1 ? p.waves : 0) <= kLdsPerCu) {
+        if (window_forward_lds(p, f32, dp) <= kLdsPerCu) {
             p.blocks = (int)((waves + queries - 1) / queries);
             return set_units(p, p.heads);
         }
@@ -123,13 +143,13 @@ bool plan_forward(WindowParams &p, bool f32)
 bool plan_dq(WindowParams &p, bool f32)
 {
     const int dp = dim_padded(p.d);
-    const int reach = widest(p, [&](int wp) { return 2 * span(p, wp, 32) + 1; });
+    const int reach = widest(p, [&](int width) { return 2 * span(p, width, 32) + 1; });
     for (p.ring = 64; p.ring < reach;) p.ring *= 2;
     p.part_len = table_words(p, 32);
     // (the same plan with and without the table's gradient)
     float *const grad = p.grad_bias;
     p.grad_bias = reinterpret_cast<float *>(16);
-    const bool fits = choose_waves(p, p.heads, f32 || dp == 64, [&](const WindowParams &x) { return window_dq_lds(x, f32, dp); });
+    const bool fits = choose_waves(p, p.heads, f32, dp, [&](const WindowParams &x) { return window_dq_lds(x, f32, dp); });
     p.grad_bias = grad;
     if (!fits || !set_units(p, p.heads)) return false;
     p.splits = (int)std::min<long>(64, (long)p.N * p.gy * p.gx);
@@ -138,7 +158,7 @@ bool plan_dq(WindowParams &p, bool f32)
 bool plan_dkv(WindowParams &p, bool f32)
 {
     const int dp = dim_padded(p.d);
-    return choose_waves(p, p.kv_heads, f32 || dp == 64, [&](const WindowParams &x) { return window_dkv_lds(x, f32, dp); }) && set_units(p, p.kv_heads);
+    return choose_waves(p, p.kv_heads, f32, dp, [&](const WindowParams &x) { return window_dkv_lds(x, f32, dp); }) && set_units(p, p.kv_heads);
 }
 
 struct Scratch {
@@ -149,7 +169,7 @@ Scratch scratch(const WindowParams &p)  // (of plan_dq)
     Scratch s;
     s.delta = 0;
     s.part = round_up((size_t)p.N * p.heads * p.H * p.W * 4, kAlign);
-    s.part2 = s.part + round_up((size_t)p.units * p.waves * p.part_len * 4, kAlign);
+    s.part2 = s.part + round_up((size_t)p.units * p.owners * p.part_len * 4, kAlign);
     s.total = s.part2 + round_up((size_t)p.splits * p.heads * p.th * p.tw * 4, kAlign);
     return s;
 }

@@ -10,7 +10,7 @@
 // place that is linear in both tokens.  A block's queries see only the offsets of a range; that range alone is kept.
 //
 // Matrix instructions: v_mfma_f32_32x32x16_bf16.  bf16 storage as it is; fp32 values as three bf16 terms by truncation (exact),
-// the six products of terms whose orders add up to two at most (what is left out lies below 2^-24 of a product).
+// the six products of terms whose orders add up to two at most (what is left out: below 2^-21 of a product, 2^-24 on average).
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -51,19 +51,20 @@ struct WindowParams {
     int win_h, win_w;                    // as the table has them
     int wh, ww;                          // cut to the map
     int gy, gx;                          // windows down and across
-    int tw, th;                          // offsets across and down: 2 ww - 1, 2 wh - 1
+    int tw, th;                          // offsets across and down of a whole window: 2 ww - 1, 2 wh - 1
     int nby, nbx, n_edges;
     int edges[kWinMaxEdges];
     int blocks, units, waves, len;       // blocks a window and head, all blocks, wavefronts a block, words of a block's table
+    int owners;                          // so many of a block's wavefronts have tokens of their own (the others help staging)
     int tiles, ksplit;                   // tiles of 32 tokens of a wavefront; forward: wavefronts that share a tile's keys
-    int buffers, ring, part_len;         // backward: staging buffers; words of a wavefront's ring (a power of two) and of its part
+    int buffers, ring, part_len;         // staging buffers; backward: words of a wavefront's ring (a power of two) and of its part
     int pairs;                           // planes have two pixels at least
     int splits, accumulate;
     float scale, inv_scale, log2_scale;  // scale * log2(e) last
 };
 
-size_t window_forward_lds(bool f32, int dp, int len, int joined);  // joined: wavefronts whose sums are joined, or 0
-size_t window_dq_lds(const WindowParams &p, bool f32, int dp);  // (buffers, waves, ring, len and grad_bias set)
+size_t window_forward_lds(const WindowParams &p, bool f32, int dp);  // (buffers, waves, ksplit and len set)
+size_t window_dq_lds(const WindowParams &p, bool f32, int dp);  // (buffers, owners, ring, len and grad_bias set)
 size_t window_dkv_lds(const WindowParams &p, bool f32, int dp);
 hipError_t launch_window_forward(const WindowParams &p, bool f32, int dp, hipStream_t s);
 hipError_t launch_window_dq(const WindowParams &p, bool f32, int dp, hipStream_t s);
@@ -79,13 +80,17 @@ typedef float wf32x4 __attribute__((ext_vector_type(4)));
 typedef float wf32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t wu32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t wu32x2 __attribute__((ext_vector_type(2)));
+typedef int wi32x2 __attribute__((ext_vector_type(2)));
 
-// The operands' shape: DP is the head's dimension rounded up to 16, 32 or 64; TK tokens are staged at a time.
+// Tokens staged at a time.
+constexpr int win_chunk(bool f32, int dp) { return f32 ? (dp == 64 ? 32 : 64) : (dp == 16 ? 128 : 64); }
+
+// The operands' shape: DP is the head's dimension rounded up to 16, 32 or 64.
 template <typename T, int DP>
 struct WinGeom {
     static constexpr bool F32 = std::is_same<T, float>::value;
     static constexpr int NT = F32 ? 3 : 1;
-    static constexpr int TK = F32 ? (DP == 64 ? 32 : 64) : (DP == 16 ? 128 : 64);
+    static constexpr int TK = win_chunk(F32, DP);
     static constexpr int KS = DP / 16;                 // matrix instructions a score takes (of each pair of terms)
     static constexpr int DT = DP <= 32 ? 1 : 2;        // blocks of 32 channels of an output
     // rows of tokens: 16-byte pieces of eight channels, [term][channels / 8][token]; four tokens of a group lie SLOT pieces
@@ -102,8 +107,12 @@ struct WinGeom {
     static constexpr int CM_BYTES = NT * CM_TERM;
 };
 
+// A window's row in tokens: whole pairs, which share the address of a bias (pairs, not fours: windows of 13 x 13 are 6 tiles and not 7, 307 us and not 391 for
+// 3 x 339 x 511 bf16; the additions cost windows of 32 and 48 2 %).
+__host__ __device__ __forceinline__ int in_pairs(int width) { return (width + 1) & ~1; }
+
 struct Win {
-    int n, y0, x0, h, w, wp, L;
+    int n, y0, x0, h, w, wp, L, tw, centre;
     float inv;
     // the row of a token: a quotient that is at least 0.5 / wp away from whole numbers, which the product's error (2^-22 of it) does not reach
     // below two million tokens
@@ -115,8 +124,9 @@ __device__ __forceinline__ Win win_of(const WindowParams &p, int n, int wy, int 
     Win w;
     w.n = n, w.y0 = wy * p.wh, w.x0 = wx * p.ww;
     w.h = min(p.wh, p.H - w.y0), w.w = min(p.ww, p.W - w.x0);
-    w.wp = (w.w + 3) & ~3;
+    w.wp = in_pairs(w.w);
     w.L = w.h * w.wp;
+    w.tw = 2 * w.w - 1, w.centre = (p.wh - 1) * w.tw + w.w - 1;
     w.inv = __builtin_amdgcn_rcpf((float)w.wp);
     return w;
 }
@@ -133,11 +143,11 @@ __device__ __forceinline__ int unit_of(int units)
 struct TableRange {
     int base, len;
 };
-// `sign`: -1 for queries (offset = key - query), 1 for keys.  off() grows with the token, but in windows of one and two columns, whose
-// rows of four overlap: there whole rows count.
-__device__ __forceinline__ TableRange table_range(const Win &w, int t0, int t1, int tw, int centre, int sign)
+// `sign`: -1 for queries (offset = key - query), 1 for keys.  off() grows with the token, but in windows of one column, whose
+// rows of two overlap: there whole rows count.
+__device__ __forceinline__ TableRange table_range(const Win &w, int t0, int t1, int sign)
 {
-    const int wp = w.wp, y0 = w.row(t0), y1 = w.row(t1 - 1), all = (w.h - 1) * tw + wp - 1;
+    const int wp = w.wp, tw = w.tw, centre = w.centre, y0 = w.row(t0), y1 = w.row(t1 - 1), all = (w.h - 1) * tw + wp - 1;
     const int lo = y0 * tw + (tw >= wp ? t0 - y0 * wp : 0), hi = y1 * tw + (tw >= wp ? t1 - 1 - y1 * wp : wp - 1);
     return sign < 0 ? TableRange{centre - hi, all + hi - lo + 1} : TableRange{centre + lo - all, all + hi - lo + 1};
 }
@@ -158,18 +168,18 @@ __device__ __forceinline__ int bucket_of(const WindowParams &p, int o, int full)
 // The range of the head's table, over the scale (scores are kept unscaled; the largest magnitudes are cut to 2^120, an
 // infinity stays one).  REVERSED: last first, for lanes that hold a key and go through queries.  Four loads on their way at a time.
 template <bool REVERSED>
-__device__ __forceinline__ void stage_table(const WindowParams &p, float *table, TableRange r, int head)
+__device__ __forceinline__ void stage_table(const WindowParams &p, const Win &w, float *table, TableRange r, int head)
 {
-    const float *bias = p.bias + (long)head * p.nby * p.nbx, inv_tw = __builtin_amdgcn_rcpf((float)p.tw);
+    const float *bias = p.bias + (long)head * p.nby * p.nbx, inv_tw = __builtin_amdgcn_rcpf((float)w.tw);
     for (int i0 = threadIdx.x; i0 < r.len; i0 += 4 * blockDim.x) {
         float b[4];
         bool in[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             const int at = r.base + i0 + k * blockDim.x;
-            in[k] = at >= 0 && at < p.th * p.tw;
-            const int c = in[k] ? at : 0, y = (int)(((float)c + 0.5f) * inv_tw), x = c - y * p.tw;  // (as Win::row)
-            const int by = bucket_of(p, y - (p.wh - 1), p.win_h), bx = bucket_of(p, x - (p.ww - 1), p.win_w);
+            in[k] = at >= 0 && at < p.th * w.tw;
+            const int c = in[k] ? at : 0, y = (int)(((float)c + 0.5f) * inv_tw), x = c - y * w.tw;  // (as Win::row)
+            const int by = bucket_of(p, y - (p.wh - 1), p.win_h), bx = bucket_of(p, x - (w.w - 1), p.win_w);
             b[k] = p.bias != nullptr ? bias[(long)by * p.nbx + bx] : 0.f;
         }
 #pragma unroll
@@ -211,13 +221,13 @@ struct Spot {
     }
 };
 
-// Offsets of groups of four tokens, in bytes of a table of floats.
+// Offsets of pairs of tokens, in bytes of a table of floats.
 template <int TK>
 __device__ __forceinline__ void stage_offsets(const WindowParams &p, const Win &w, int t0, int *off)
 {
-    if (threadIdx.x >= TK / 4) return;
-    const int t = t0 + 4 * threadIdx.x, y = w.row(t), x = t - y * w.wp;
-    off[threadIdx.x] = t < w.L ? 4 * (y * p.tw + x) : 0;
+    if (threadIdx.x >= TK / 2) return;
+    const int t = t0 + 2 * threadIdx.x, y = w.row(t), x = t - y * w.wp;
+    off[threadIdx.x] = t < w.L ? 4 * (y * w.tw + x) : 0;
 }
 
 // A lane's 16 tokens of a staged tile, of which those whose pair's bit is not set get `none`.  bits: a byte for each pair of tokens.
@@ -315,10 +325,10 @@ struct Piece {
 template <typename T, int DP, bool RM0, bool CM0, bool RM1, bool CM1>
 struct Stager {
     using G = WinGeom<T, DP>;
-    static constexpr int GROUPS = G::TK / 4, PAIRS = G::TK / 2;
+    static constexpr int PAIRS = G::TK / 2;
     static constexpr int RM0_AT = 0, CM0_AT = RM0_AT + (RM0 ? G::RM_BYTES : 0), RM1_AT = CM0_AT + (CM0 ? G::CM_BYTES : 0),
                          CM1_AT = RM1_AT + (RM1 ? G::RM_BYTES : 0), BITS_AT = CM1_AT + (CM1 ? G::CM_BYTES : 0), OFF_AT = BITS_AT + PAIRS,
-                         BYTES = (OFF_AT + GROUPS * 4 + 15) / 16 * 16;
+                         BYTES = (OFF_AT + PAIRS * 4 + 15) / 16 * 16;
     Piece<T, DP> next;
 
     // pieces of one operand: of the channels that exist (the others' place is cleared once)
@@ -372,7 +382,7 @@ struct OwnToken {
     {
         const int tc = min(t, w.L - 1), y = w.row(tc), x = tc - y * w.wp;
         there = t < w.L && x < w.w;
-        off = y * p.tw + x;
+        off = y * w.tw + x;
         pixel = (w.y0 + y) * p.W + w.x0 + min(x, w.w - 1);
         mask = p.mask_read[w.n * p.mask_step + pixel];
     }

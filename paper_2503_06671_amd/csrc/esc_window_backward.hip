@@ -17,6 +17,9 @@
 namespace esc {
 namespace {
 
+// A ring's places behind its end: a pair of offsets that runs over it stays together (two: an even number keeps what follows aligned).
+constexpr int kRingMore = 2;
+
 // ds in the products with keys and queries, with bf16 storage: two terms.  Its sum over a query's keys is 0, so what one rounding of each term takes
 // weighs more in the sums than it does in those of p: dq and dk were 0.0025 off with one term and are 0.0017, which is the rounding of the
 // results alone, for 50 us more of 571 (dq) and 77 of 589 (dkv) for 64 maps of 64 x 64.  p in dv's sums has one: 0.0023, and 135 us more with two.
@@ -26,10 +29,9 @@ constexpr int kDsTerms = std::is_same<T, float>::value ? 3 : 2;
 __device__ __forceinline__ void lds_add(double *p, float v) { __hip_atomic_fetch_add(p, (double)v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP); }
 
 // The offsets of all its window's keys from the 32 tokens from t0 on: from the smallest on.
-__device__ __forceinline__ TableRange wave_range(const WindowParams &p, const Win &w, int t0)
+__device__ __forceinline__ TableRange wave_range(const Win &w, int t0)
 {
-    const int centre = (p.wh - 1) * p.tw + p.ww - 1;
-    return table_range(w, t0, min(t0 + 32, w.L), p.tw, centre, -1);
+    return table_range(w, t0, min(t0 + 32, w.L), -1);
 }
 
 template <typename T, int DP>
@@ -41,22 +43,21 @@ __global__ __launch_bounds__(512, (WinGeom<T, DP>::F32 || DP == 64) ? 2 : 4) voi
     extern __shared__ __align__(16) char lds[];
     float *table = reinterpret_cast<float *>(lds);  // (first: its reads' addresses are then sums of two terms and a constant)
     double *rings = reinterpret_cast<double *>(lds + (size_t)p.len * 4);  // one a wavefront
-    char *const staged = reinterpret_cast<char *>(rings + (p.grad_bias != nullptr ? p.waves * (p.ring + 4) : 0));
+    char *const staged = reinterpret_cast<char *>(rings + (p.grad_bias != nullptr ? p.owners * (p.ring + kRingMore) : 0));
 
     const int unit = unit_of(p.units);
     if (unit < 0) return;
     const int block = unit % p.blocks, head = unit / p.blocks % p.heads, wi = unit / p.blocks / p.heads;
     const Win w = win_of(p, wi / (p.gy * p.gx), wi / p.gx % p.gy, wi % p.gx);
-    const int queries = p.waves * 32 * U, q0 = block * queries;
+    const int queries = p.owners * 32 * U, q0 = block * queries;
     if (q0 >= w.L) return;
-    const int centre = (p.wh - 1) * p.tw + p.ww - 1;
-    const TableRange range = table_range(w, q0, min(q0 + queries, w.L), p.tw, centre, -1);
+    const TableRange range = table_range(w, q0, min(q0 + queries, w.L), -1);
     const bool bias_grad = p.grad_bias != nullptr;
 
     const long hw = (long)p.H * p.W;
     const int lane = threadIdx.x & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wq0 = q0 + wave * 32 * U;
-    const bool busy = wq0 < w.L;
+    const bool busy = wave < p.owners && wq0 < w.L;
     const int kvh = head / (p.heads / p.kv_heads);
     const long planes = ((long)w.n * p.heads + head) * p.d * hw, row = ((long)w.n * p.heads + head) * hw;
     const T *q = static_cast<const T *>(p.q) + w.n * p.qs + head * (long)p.d * hw;
@@ -78,14 +79,14 @@ __global__ __launch_bounds__(512, (WinGeom<T, DP>::F32 || DP == 64) ? 2 : 4) voi
         for (int u = 0; u < U; ++u) {
             const OwnToken own_token(p, w, wq0 + u * 32 + (lane & 31));
             there[u] = own_token.there, pixel[u] = own_token.pixel, ok[u] = own_token.ok(p);
-            place[u] = 4 * (centre - own_token.off - range.base);
+            place[u] = 4 * (w.centre - own_token.off - range.base);
             vq[u].fetch(p, q, pixel[u]);
             vgo[u].fetch(p, go, pixel[u]);
             vout[u].fetch(p, out, pixel[u]);
             if constexpr (!G::F32) vrest[u].fetch(p, static_cast<const T *>(p.rest) + planes, pixel[u]);
             top[u] = p.top[row + pixel[u]], log_sum[u] = p.log_sum[row + pixel[u]];
         }
-        stage_table<false>(p, table, range, head);
+        stage_table<false>(p, w, table, range, head);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             vq[u].clean(p, ok[u]);
@@ -114,14 +115,14 @@ __global__ __launch_bounds__(512, (WinGeom<T, DP>::F32 || DP == 64) ? 2 : 4) voi
             for (int b = 0; b < G::DT; ++b) acc[u][b] = wf32x16{};
         }
     }
-    double *const ring = rings + wave * (p.ring + 4);  // (four places more: a group of four that runs over the end stays together)
+    double *const ring = rings + wave * (p.ring + kRingMore);
     const int ring_mask = 8 * p.ring - 8;  // (in bytes)
-    const TableRange mine = wave_range(p, w, min(wq0, w.L - 1));
+    const TableRange mine = wave_range(w, min(wq0, w.L - 1));
     const int ring_place = 2 * place[0] + 8 * (range.base - mine.base);  // in the ring, in bytes, of the offset to the key that has off = 0
-    float *const part = p.part + ((long)unit * p.waves + wave) * p.part_len;
+    float *const part = p.part + ((long)unit * p.owners + wave) * p.part_len;
     int left = 0;  // offsets that have left the ring
-    if (bias_grad)
-        for (int i = lane; i < p.ring + 4; i += 64) ring[i] = 0.0;
+    if (bias_grad && busy)
+        for (int i = lane; i < p.ring + kRingMore; i += 64) ring[i] = 0.0;
     S::clear(p, staged);
     if (p.buffers == 2) S::clear(p, staged + S::BYTES);
     __syncthreads();
@@ -136,9 +137,9 @@ __global__ __launch_bounds__(512, (WinGeom<T, DP>::F32 || DP == 64) ? 2 : 4) voi
         auto tile_of = [&](int tile, auto large) {
             const wu32x4 bits = *reinterpret_cast<const wu32x4 *>(buf + S::BITS_AT + tile * 16);
             const bool whole = all && all_take_part(bits);
-            int key[4];
+            wi32x2 key[4];
 #pragma unroll
-            for (int a = 0; a < 4; ++a) key[a] = off[tile * 8 + 2 * a + half];
+            for (int a = 0; a < 4; ++a) key[a] = *reinterpret_cast<const wi32x2 *>(off + tile * 16 + 4 * a + 2 * half);
             wf32x16 ds[U];
             Packed<kDsTerms<T>> e[U];
 #pragma unroll
@@ -146,9 +147,11 @@ __global__ __launch_bounds__(512, (WinGeom<T, DP>::F32 || DP == 64) ? 2 : 4) voi
                 wf32x16 s;
 #pragma unroll
                 for (int a = 0; a < 4; ++a) {
-                    const float *from = reinterpret_cast<const float *>(reinterpret_cast<const char *>(table) + (place[u] + key[a]));
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) s[4 * a + j] = from[j];
+                    for (int j = 0; j < 2; ++j) {
+                        const float *from = reinterpret_cast<const float *>(reinterpret_cast<const char *>(table) + (place[u] + key[a][j]));
+                        s[4 * a + 2 * j] = from[0], s[4 * a + 2 * j + 1] = from[1];
+                    }
                 }
                 s = score<T, DP>(buf + S::RM0_AT, tile, own_q[u], s);
                 const wf32x16 dp = score<T, DP>(buf + S::RM1_AT, tile, own_go[u], wf32x16{});
@@ -168,24 +171,24 @@ __global__ __launch_bounds__(512, (WinGeom<T, DP>::F32 || DP == 64) ? 2 : 4) voi
             accumulate<T, DP>(buf + S::CM0_AT, tile, e, acc);
             if (bias_grad) {
                 // (both halves of a query's lanes; the second after the first: keys four tokens apart see equal offsets of queries four apart)
-                double *to[4];
+                double *to[8];
 #pragma unroll
-                for (int a = 0; a < 4; ++a) to[a] = reinterpret_cast<double *>(reinterpret_cast<char *>(ring) + ((ring_place + 2 * key[a]) & ring_mask));
+                for (int a = 0; a < 8; ++a) to[a] = reinterpret_cast<double *>(reinterpret_cast<char *>(ring) + ((ring_place + 2 * key[a / 2][a % 2]) & ring_mask));
                 if (half == 0) {
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) lds_add(to[i / 4] + i % 4, ds[0][i]);
+                    for (int i = 0; i < 16; ++i) lds_add(to[i / 2] + i % 2, ds[0][i]);
                 }
                 if (half == 1) {
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) lds_add(to[i / 4] + i % 4, ds[0][i]);
+                    for (int i = 0; i < 16; ++i) lds_add(to[i / 2] + i % 2, ds[0][i]);
                 }
                 const int t = t0 + tile * 32 + 32;  // the next tile's first key
-                const int y = w.row(t), done = t < w.L ? y * p.tw + t - y * w.wp : mine.len;
+                const int y = w.row(t), done = t < w.L ? y * w.tw + t - y * w.wp : mine.len;
                 for (int i = left + lane; i < done; i += 64) {
                     const int at = i & (p.ring - 1);
                     double sum = ring[at];
                     ring[at] = 0.0;
-                    if (at < 4) sum += ring[p.ring + at], ring[p.ring + at] = 0.0;
+                    if (at == 0) sum += ring[p.ring + at], ring[p.ring + at] = 0.0;
                     part[i] = (float)sum;
                 }
                 left = done;
@@ -236,16 +239,15 @@ __global__ __launch_bounds__(512, (WinGeom<T, DP>::F32 || DP == 64) ? 2 : 3) voi
     if (unit < 0) return;
     const int block = unit % p.blocks, kvh = unit / p.blocks % p.kv_heads, wi = unit / p.blocks / p.kv_heads;
     const Win w = win_of(p, wi / (p.gy * p.gx), wi / p.gx % p.gy, wi % p.gx);
-    const int keys = p.waves * 32 * U, k0 = block * keys;
+    const int keys = p.owners * 32 * U, k0 = block * keys;
     if (k0 >= w.L) return;
-    const int centre = (p.wh - 1) * p.tw + p.ww - 1;
-    const TableRange range = table_range(w, k0, min(k0 + keys, w.L), p.tw, centre, 1);
+    const TableRange range = table_range(w, k0, min(k0 + keys, w.L), 1);
 
     const long hw = (long)p.H * p.W;
     const int lane = threadIdx.x & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int group = p.heads / p.kv_heads;
     const int wk0 = k0 + wave * 32 * U;
-    const bool busy = wk0 < w.L;
+    const bool busy = wave < p.owners && wk0 < w.L;
     const T *k = static_cast<const T *>(p.k) + w.n * p.ks + kvh * (long)p.d * hw;
     const T *v = static_cast<const T *>(p.v) + w.n * p.vs + kvh * (long)p.d * hw;
     const T *q = static_cast<const T *>(p.q) + w.n * p.qs, *go = static_cast<const T *>(p.go) + (long)w.n * p.heads * p.d * hw;
@@ -292,11 +294,11 @@ __global__ __launch_bounds__(512, (WinGeom<T, DP>::F32 || DP == 64) ? 2 : 3) voi
         for (int u = 0; u < U; ++u) {
             const OwnToken own_token(p, w, wk0 + u * 32 + (lane & 31));
             there[u] = own_token.there, pixel[u] = own_token.pixel, ok[u] = own_token.ok(p);
-            place[u] = 4 * (range.len - 1 - (centre + own_token.off - range.base));
+            place[u] = 4 * (range.len - 1 - (w.centre + own_token.off - range.base));
             vk[u].fetch(p, k, pixel[u]);
             vv[u].fetch(p, v, pixel[u]);
         }
-        stage_table<true>(p, table, range, kvh * group);
+        stage_table<true>(p, w, table, range, kvh * group);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             vk[u].clean(p, ok[u]);
@@ -332,10 +334,13 @@ __global__ __launch_bounds__(512, (WinGeom<T, DP>::F32 || DP == 64) ? 2 : 3) voi
                 wf32x16 s, dp;
 #pragma unroll
                 for (int a = 0; a < 4; ++a) {
-                    const float *at = reinterpret_cast<const float *>(reinterpret_cast<const char *>(table) + (place[u] + off[tile * 8 + 2 * a + half]));
+                    const wi32x2 query = *reinterpret_cast<const wi32x2 *>(off + tile * 16 + 4 * a + 2 * half);
                     const wf32x4 d = *reinterpret_cast<const wf32x4 *>(rows + G::TK + tile * 32 + 8 * a + 4 * half);
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) s[4 * a + j] = at[j], dp[4 * a + j] = d[j];
+                    for (int j = 0; j < 4; ++j) {
+                        const float *at = reinterpret_cast<const float *>(reinterpret_cast<const char *>(table) + (place[u] + query[j / 2]));
+                        s[4 * a + j] = at[j % 2], dp[4 * a + j] = d[j];
+                    }
                 }
                 s = score<T, DP, true>(buf + S::RM0_AT, tile, own_k[u], s);
                 dp = score<T, DP>(buf + S::RM1_AT, tile, own_v[u], dp);
@@ -379,7 +384,7 @@ __global__ __launch_bounds__(512, (WinGeom<T, DP>::F32 || DP == 64) ? 2 : 3) voi
         write(next_head, next_t0, staged + turn * BYTES);
         if (last) {  // (uniform) another head's biases: nobody may still read the last one's
             if (p.buffers != 1) __syncthreads();
-            stage_table<true>(p, table, range, next_head);
+            stage_table<true>(p, w, table, range, next_head);
         }
         __syncthreads();
         t0 = next_t0, head = next_head;
@@ -407,21 +412,27 @@ __global__ __launch_bounds__(256) void window_offsets_kernel(const WindowParams 
 {
     constexpr int EACH = 4, AHEAD = 4;
     const int at0 = blockIdx.x * (256 * EACH) + threadIdx.x, head = blockIdx.y;
-    const int centre = (p.wh - 1) * p.tw + p.ww - 1, windows = p.N * p.gy * p.gx;
+    const int windows = p.N * p.gy * p.gx;
     float sum[EACH] = {};
+    int oy[EACH], ox[EACH];
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) oy[e] = (at0 + 256 * e) / p.tw, ox[e] = (at0 + 256 * e) % p.tw - (p.ww - 1);
     for (int wi = blockIdx.z; wi < windows; wi += p.splits) {
         const Win w = win_of(p, wi / (p.gy * p.gx), wi / p.gx % p.gy, wi % p.gx);
-        const float *part = p.part + (long)(wi * p.heads + head) * p.blocks * p.waves * p.part_len;
+        const float *part = p.part + (long)(wi * p.heads + head) * p.blocks * p.owners * p.part_len;
+        int at[EACH];  // the offset's number in this window
+#pragma unroll
+        for (int e = 0; e < EACH; ++e) at[e] = abs(ox[e]) < w.w ? oy[e] * w.tw + ox[e] + w.w - 1 : -1;
         for (int t0 = 0; t0 < w.L; t0 += 32 * AHEAD) {
             float v[AHEAD][EACH];
 #pragma unroll
             for (int i = 0; i < AHEAD; ++i) {
                 const int t = t0 + 32 * i;
-                const TableRange r = table_range(w, t, min(t + 32, w.L), p.tw, centre, -1);
+                const TableRange r = wave_range(w, t);
 #pragma unroll
                 for (int e = 0; e < EACH; ++e) {
-                    const int in = at0 + 256 * e - r.base;
-                    v[i][e] = t < w.L && in >= 0 && in < r.len ? part[in] : 0.f;
+                    const int in = at[e] - r.base;
+                    v[i][e] = t < w.L && at[e] >= 0 && in >= 0 && in < r.len ? part[in] : 0.f;
                 }
                 part += p.part_len;
             }
@@ -486,7 +497,7 @@ __global__ __launch_bounds__(256) void window_buckets_kernel(const WindowParams 
 template <typename T, int DP>
 size_t dq_lds(const WindowParams &p)
 {
-    return p.buffers * (size_t)Stager<T, DP, true, true, true, false>::BYTES + (p.grad_bias != nullptr ? (size_t)p.waves * (p.ring + 4) * 8 : 0) + (size_t)p.len * 4;
+    return p.buffers * (size_t)Stager<T, DP, true, true, true, false>::BYTES + (p.grad_bias != nullptr ? (size_t)p.owners * (p.ring + kRingMore) * 8 : 0) + (size_t)p.len * 4;
 }
 template <typename T, int DP>
 size_t dkv_lds(const WindowParams &p)

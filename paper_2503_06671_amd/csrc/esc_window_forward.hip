@@ -35,10 +35,9 @@ __global__ __launch_bounds__(512) void window_forward_kernel(const WindowParams 
     if (unit < 0) return;
     const int block = unit % p.blocks, head = unit / p.blocks % p.heads, wi = unit / p.blocks / p.heads;
     const Win w = win_of(p, wi / (p.gy * p.gx), wi / p.gx % p.gy, wi % p.gx);
-    const int queries = p.waves / p.ksplit * (U * 32), q0 = block * queries;
+    const int queries = p.owners / p.ksplit * (U * 32), q0 = block * queries;
     if (q0 >= w.L) return;
-    const int centre = (p.wh - 1) * p.tw + p.ww - 1;
-    const TableRange range = table_range(w, q0, min(q0 + queries, w.L), p.tw, centre, -1);
+    const TableRange range = table_range(w, q0, min(q0 + queries, w.L), -1);
 
     const long hw = (long)p.H * p.W;
     const int lane = threadIdx.x & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -62,10 +61,10 @@ __global__ __launch_bounds__(512) void window_forward_kernel(const WindowParams 
         for (int u = 0; u < U; ++u) {
             const OwnToken own_token(p, w, wq0 + u * 32 + (lane & 31));
             there[u] = own_token.there, pixel[u] = own_token.pixel, ok[u] = own_token.ok(p);
-            place[u] = 4 * (centre - own_token.off - range.base);
+            place[u] = 4 * (w.centre - own_token.off - range.base);
             values[u].fetch(p, q, pixel[u]);
         }
-        stage_table<false>(p, table, range, head);
+        stage_table<false>(p, w, table, range, head);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             values[u].clean(p, ok[u]);
@@ -76,14 +75,14 @@ __global__ __launch_bounds__(512) void window_forward_kernel(const WindowParams 
         }
     }
     S::clear(p, staged);
-    S::clear(p, staged + S::BYTES);
+    if (p.buffers == 2) S::clear(p, staged + S::BYTES);
     __syncthreads();
     S::ones(staged + S::CM1_AT);
-    S::ones(staged + S::BYTES + S::CM1_AT);
+    if (p.buffers == 2) S::ones(staged + S::BYTES + S::CM1_AT);
     stager.write(p, w, k, v, 0, staged);
     __syncthreads();
     const float slack = kSlack / p.log2_scale;
-    const bool busy = wq0 < w.L;
+    const bool busy = wave < p.owners && wq0 < w.L;
 
     for (int t0 = 0, turn = 0; t0 < w.L; t0 += G::TK, turn ^= 1) {
         const bool more = t0 + G::TK < w.L;
@@ -96,9 +95,9 @@ __global__ __launch_bounds__(512) void window_forward_kernel(const WindowParams 
                 if (t0 + tile * 32 >= w.L || (tile & (p.ksplit - 1)) != share) continue;
                 const wu32x4 bits = *reinterpret_cast<const wu32x4 *>(buf + S::BITS_AT + tile * 16);
                 const bool whole = all_take_part(bits);
-                int key[4];
+                wi32x2 key[4];
 #pragma unroll
-                for (int a = 0; a < 4; ++a) key[a] = off[tile * 8 + 2 * a + half];
+                for (int a = 0; a < 4; ++a) key[a] = *reinterpret_cast<const wi32x2 *>(off + tile * 16 + 4 * a + 2 * half);
                 wf32x16 s[U];
                 float m[U];
                 bool over = false;
@@ -106,9 +105,11 @@ __global__ __launch_bounds__(512) void window_forward_kernel(const WindowParams 
                 for (int u = 0; u < U; ++u) {
 #pragma unroll
                     for (int a = 0; a < 4; ++a) {
-                        const float *from = reinterpret_cast<const float *>(reinterpret_cast<const char *>(table) + (place[u] + key[a]));
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) s[u][4 * a + j] = from[j];
+                        for (int j = 0; j < 2; ++j) {
+                            const float *from = reinterpret_cast<const float *>(reinterpret_cast<const char *>(table) + (place[u] + key[a][j]));
+                            s[u][4 * a + 2 * j] = from[0], s[u][4 * a + 2 * j + 1] = from[1];
+                        }
                     }
                     s[u] = score<T, DP>(buf + S::RM0_AT, tile, own[u], s[u]);
                 }
@@ -177,7 +178,7 @@ __global__ __launch_bounds__(512) void window_forward_kernel(const WindowParams 
     if (p.ksplit > 1) {  // (uniform) one tile a wavefront then
         constexpr int WORDS = 64 * (2 + G::DT * 16);
         float *room = reinterpret_cast<float *>(lds);
-        if (share != 0) {
+        if (share != 0 && wave < p.owners) {
             float *to = room + wave * WORDS + lane;
             to[0] = top[0], to[64] = sum[0];
 #pragma unroll
@@ -186,7 +187,7 @@ __global__ __launch_bounds__(512) void window_forward_kernel(const WindowParams 
                 for (int i = 0; i < 16; ++i) to[(2 + b * 16 + i) * 64] = acc[0][b][i];
         }
         __syncthreads();
-        if (share != 0) return;
+        if (share != 0 || wave >= p.owners) return;
         for (int other = 1; other < p.ksplit; ++other) {
             const float *from = room + (wave + other) * WORDS + lane;
             const float mine = top[0], theirs = from[0], next = fmaxf(mine, theirs);
@@ -234,17 +235,18 @@ __global__ __launch_bounds__(512) void window_forward_kernel(const WindowParams 
 }
 
 template <typename T, int DP>
-size_t lds_of(int len, int waves)
+size_t lds_of(const WindowParams &p)
 {
     using G = WinGeom<T, DP>;
-    const size_t staged = 2 * Stager<T, DP, true, false, false, true>::BYTES + (size_t)len * 4, joined = (size_t)waves * 256 * (2 + G::DT * 16);
+    const size_t staged = p.buffers * (size_t)Stager<T, DP, true, false, false, true>::BYTES + (size_t)p.len * 4;
+    const size_t joined = p.ksplit > 1 ? (size_t)p.owners * 256 * (2 + G::DT * 16) : 0;
     return staged > joined ? staged : joined;
 }
 
 template <typename T, int DP, int U, bool SAVE>
 hipError_t launch_one(const WindowParams &p, hipStream_t s)
 {
-    const size_t lds = lds_of<T, DP>(p.len, p.ksplit > 1 ? p.waves : 0);
+    const size_t lds = lds_of<T, DP>(p);
     if (lds > 64 * 1024) {
         const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&window_forward_kernel<T, DP, U, SAVE>), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
         if (e != hipSuccess) return e;
@@ -263,10 +265,10 @@ hipError_t launch(const WindowParams &p, hipStream_t s)
 
 }  // namespace
 
-size_t window_forward_lds(bool f32, int dp, int len, int joined)
+size_t window_forward_lds(const WindowParams &p, bool f32, int dp)
 {
-    if (f32) return dp == 16 ? lds_of<float, 16>(len, joined) : dp == 32 ? lds_of<float, 32>(len, joined) : lds_of<float, 64>(len, joined);
-    return dp == 16 ? lds_of<uint16_t, 16>(len, joined) : dp == 32 ? lds_of<uint16_t, 32>(len, joined) : lds_of<uint16_t, 64>(len, joined);
+    if (f32) return dp == 16 ? lds_of<float, 16>(p) : dp == 32 ? lds_of<float, 32>(p) : lds_of<float, 64>(p);
+    return dp == 16 ? lds_of<uint16_t, 16>(p) : dp == 32 ? lds_of<uint16_t, 32>(p) : lds_of<uint16_t, 64>(p);
 }
 
 hipError_t launch_window_forward(const WindowParams &p, bool f32, int dp, hipStream_t s)

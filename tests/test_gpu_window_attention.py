@@ -96,6 +96,10 @@ CASES = [
     (2, 32, 40, 2, 16, (16, 16), {"mask": whole_images_and_holes, "edges": [2, 4, 8]}),
     (2, 17, 19, 2, 16, (8, 8), {"bias": None}),
     (2, 12, 16, 2, 20, (8, 8), {"apart": True}),
+    (3, 5, 7, 1, 3, (3, 3), {"kv": 1}),                                # planes, images and tensors at odd elements
+    (2, 1, 9, 37, 1, (1, 5), {"kv": 1}),                               # one channel a head, 37 heads share a key
+    (40, 1, 2, 2, 16, (1, 2), {}),                                     # two tokens: nothing averages what rounding does
+    (9, 6, 5, 4, 24, (2, 3), {"kv": 2, "edges": [1, 2], "mask": whole_images_and_holes}),
 ]
 
 

@@ -97,6 +97,40 @@ def test_backward_rejects_bad_arguments_before_launch(lib):
     assert bw(gq=GQ, gk=GQ + 64 * 256 * 4, gv=GQ + 96 * 256 * 4, gqs=step, gks=step, gvs=step, wsb=0) == E_WS
 
 
+def test_launches_and_sizes_have_limits(lib):
+    # a lane count of 2^32 and more, sizes in bytes beyond 64 bits: refused, not cut off
+    big = 1 << 30
+    def sizes(**kw):
+        a = attn(**kw)
+        return lib.esc_window_attention_saved_bytes(ctypes.byref(a), 0), lib.esc_window_attention_backward_workspace_bytes(ctypes.byref(a))
+    tiny = dict(H=1, W=1, heads=1, kv_heads=1, head_dim=1, win_h=1, win_w=1, q_stride=1, k_stride=1, v_stride=1)
+    assert sizes(N=(1 << 26) - 64, **tiny) > (0, 0)
+    assert sizes(N=1 << 26, **tiny)[1] == 0
+    a = attn(N=1 << 26, **tiny)
+    assert lib.esc_window_attention_forward(Q, Q + (big << 4), Q + (big << 5), 0, ctypes.byref(a), Q + (big << 6), None, 0, None) == E_UNSUP
+    assert sizes(N=(1 << 31) - 1, H=46340, W=46340, heads=1024, kv_heads=1, head_dim=64, win_h=1, win_w=1) == (0, 0)
+
+
+@pytest.mark.parametrize("dt", [0, 1])
+@pytest.mark.parametrize("head_dim", [16, 32, 64])
+def test_windows_up_to_the_limit_have_a_plan(lib, head_dim, dt):
+    # whatever a window's shape, up to 16384 offsets; one wavefront or many (a workspace that is too small is found after the plans)
+    for h in [*range(1, 65), 100, 333, 1000, 1365, 2000, 2730, 4096, 8192]:
+        w = (16384 // (2 * h - 1) + 1) // 2
+        for win in {(h, w), (w, h), (h, max(1, w - 1)), (h, max(1, w // 2))}:
+            if min(win) < 1 or max(win) > 8192:
+                continue
+            for N in (1, 64):
+                pixels = win[0] * win[1]
+                a = attn(N=N, H=win[0], W=win[1], heads=1, kv_heads=1, head_dim=head_dim, win_h=win[0], win_w=win[1],
+                         q_stride=pixels * head_dim, k_stride=pixels * head_dim, v_stride=pixels * head_dim)
+                far = [0x1000000000 * i for i in range(1, 10)]
+                g = binding._WindowGrads(*far[:3], *[pixels * head_dim] * 3, None)
+                assert lib.esc_window_attention_backward_workspace_bytes(ctypes.byref(a)) > 0, (win, N)
+                assert lib.esc_window_attention_backward(*far[3:6], dt, ctypes.byref(a), far[6], far[7], far[8], 1 << 34, ctypes.byref(g), 0,
+                                                         None, 0, None) == E_WS, (win, N)
+
+
 def test_binding_refuses(lib):
     x = torch.zeros(1, 4, 8, 8)
     with pytest.raises(TypeError, match="device tensor"):

@@ -97,19 +97,16 @@ def tolerance(r, name, dtype, d, tokens):
     """What fp32 arithmetic and the stated roundings can make of result `name`, element by element.
 
     fp32 part, in units of 2^-24: a score is off by at most d + 8 roundings of its terms' magnitudes S (products of three-term operands leave out
-    another unit of each product); the exponent's argument by two roundings more of at most 2 S; an error of a score is a relative one of its
+    up to eight units of each product, one on average); the exponent's argument by two roundings more of at most 2 S; an error of a score is a relative one of its
     exponential, counted twice (numerator and sum).  The sums over the keys and the queries, of 32 at a time, take at most tokens / 8 + 64
     roundings of the sum of magnitudes, and the gradients' delta as many again.
-    bf16: the operands p or ds of the products are rounded once (half a step: 2^-8 of each term), results too."""
+    bf16: results but the bias' gradient are rounded (half a step: 2^-8 of them); in the products the p of the result and of v's gradient are
+    rounded once (2^-8 of each term), the ds of the gradients of q and k twice (2^-16)."""
     u = 2.0 ** -24
     rel = u * (2 * (2 * d + 16) * (r["score_abs"] + 1) + 2 * (tokens / 8 + 64))
     tol = rel * r[name + "_abs"]
-    if dtype == torch.bfloat16:
-        if name == "grad_bias":
-            # delta comes from out and what rounding took from it, of probabilities of two terms: 2^-16 of its terms together
-            tol = tol + 2.0 ** -16 * r[name + "_abs"]
-        else:
-            tol = tol + 2.0 ** -8 * r[name + "_abs"] + 2.0 ** -8 * r[name].abs()
+    if dtype == torch.bfloat16 and name != "grad_bias":
+        tol = tol + 2.0 ** (-8 if name in ("out", "grad_v") else -16) * r[name + "_abs"] + 2.0 ** -8 * r[name].abs()
     elif name != "grad_bias":
         tol = tol + u * r[name].abs()
     return tol + 1e-30
