@@ -41,39 +41,33 @@ int table_words(const WindowParams &p, long tokens)
     return widest(p, [&](int width) { return (p.wh - 1) * (2 * width - 1) + in_pairs(width) + span(p, width, tokens); });
 }
 
-// The backward's wavefronts: as many as leave a block for each compute unit, up to eight; fewer, and one staging buffer instead of two, where LDS
-// does not hold them.  Two blocks on a compute unit are worth more than wavefronts in one, where their registers fit (not with fp32 storage, nor with
-// heads wider than 32).  Blocks of fewer than four wavefronts (small windows): what leaves most of them on a compute unit, up to what its registers
-// hold; and one buffer where a window is one chunk (6 heads of 33 channels, fp32, windows of 6 x 6, gradients: 935 us, with two buffers 1449; 3 x 5,
-// 32 channels, forward: 127 and 281).
+// The backward's wavefronts, up to eight a block and no more than leave a block for each compute unit, and its staging buffers.  What is weighed: how many
+// wavefronts a compute unit holds (by LDS, and by registers: two a SIMD with fp32 storage or heads wider than 32, else four), how many of the blocks'
+// wavefronts have tokens, what a block's beginning and staging cost (as much as a wavefront's work), and that with one buffer nothing is on its way
+// while a block multiplies (where there is more than one chunk).
 template <typename F>
 bool choose_waves(WindowParams &p, int heads, bool f32, int dp, F lds)
 {
     const long tokens = (long)p.wh * in_pairs(p.ww), windows = (long)p.N * p.gy * p.gx * heads;
     const long all = (tokens + 31) / 32;
     const int want = (int)std::max<long>(1, std::min({(long)kWinMaxWaves, all, all * windows / kCus}));
-    const int most = tokens <= win_chunk(f32, dp) ? 1 : 2;
-    const bool alone = f32 || dp == 64;
-    auto take = [&](int owners, int buffers, size_t limit) {
+    const int most = tokens <= win_chunk(f32, dp) ? 1 : 2, slots = f32 || dp == 64 ? 8 : 16;
+    auto take = [&](int owners, int buffers) {
         p.owners = owners, p.buffers = buffers, p.len = (table_words(p, owners * 32) + 3) & ~3;
         p.blocks = (int)((all + owners - 1) / owners);
-        return lds(p) <= limit;
     };
-    if (want < 4) {
-        int best = 0, best_owners = 0, best_buffers = 0;
-        for (int buffers = most; buffers >= 1; --buffers)
-            for (int owners = want; owners >= 1; --owners)
-                if (take(owners, buffers, kLdsPerCu)) {
-                    const int resident = (int)std::min<size_t>(alone ? 8 : 16, kLdsPerCu / lds(p) * owners);
-                    if (resident > best) best = resident, best_owners = owners, best_buffers = buffers;
-                }
-        return best > 0 && take(best_owners, best_buffers, kLdsPerCu);
-    }
-    for (size_t limit : {alone ? kLdsPerCu : kLdsPerCu / 2, kLdsPerCu})
-        for (int buffers = most; buffers >= 1; --buffers)
-            for (int owners = want; owners >= (limit == kLdsPerCu ? 1 : 4); --owners)
-                if (take(owners, buffers, limit)) return true;
-    return false;
+    float best = 0.f;
+    int best_owners = 0, best_buffers = 0;
+    for (int buffers = most; buffers >= 1; --buffers)
+        for (int owners = want; owners >= 1; --owners) {
+            take(owners, buffers);
+            const int resident = (int)std::min<size_t>(kLdsPerCu / lds(p), slots / owners) * owners;
+            const float score = (float)resident * all / ((float)p.blocks * (owners + 1)) * (buffers < most ? 0.85f : 1.f);
+            if (score > best) best = score, best_owners = owners, best_buffers = buffers;
+        }
+    if (best == 0.f) return false;
+    take(best_owners, best_buffers);
+    return true;
 }
 
 // All blocks.  Where there are few, of few wavefronts, up to four help staging (6 heads of 48 channels that share one key, 8 sequences of 969 in
@@ -135,6 +129,11 @@ bool plan_forward(WindowParams &p, bool f32)
         p.len = (table_words(p, (int)queries * p.tiles * 32) + 3) & ~3;
         if (window_forward_lds(p, f32, dp) <= kLdsPerCu) {
             p.blocks = (int)((waves + queries - 1) / queries);
+            const long even = (waves + p.blocks - 1) / p.blocks;  // (equal blocks)
+            if (even < queries) {
+                queries = even + 1;
+                continue;
+            }
             return set_units(p, p.heads);
         }
     }
@@ -152,7 +151,9 @@ bool plan_dq(WindowParams &p, bool f32)
     const bool fits = choose_waves(p, p.heads, f32, dp, [&](const WindowParams &x) { return window_dq_lds(x, f32, dp); });
     p.grad_bias = grad;
     if (!fits || !set_units(p, p.heads)) return false;
-    p.splits = (int)std::min<long>(64, (long)p.N * p.gy * p.gx);
+    // the sums over the windows: blocks for the whole card, sixteen windows each at least
+    const long cells = (long)p.heads * ((p.th * p.tw + 1023) / 1024), all = (long)p.N * p.gy * p.gx;
+    p.splits = (int)std::min(all, std::max<long>(64, std::min(4 * kCus / cells, all / 16)));
     return true;
 }
 bool plan_dkv(WindowParams &p, bool f32)
