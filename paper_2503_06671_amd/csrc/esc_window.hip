@@ -70,15 +70,21 @@ bool choose_waves(WindowParams &p, int heads, bool f32, int dp, F lds)
     return true;
 }
 
-// All blocks.  Where there are few, of few wavefronts, up to four help staging (6 heads of 48 channels that share one key, 8 sequences of 969 in
-// windows of 600, bf16, gradients: 386 us, without 742; with many blocks they only take room: 3 x 339 x 511, windows of 13: 351, without 307).
+// All blocks, and how they go to the eight dies: in runs, so that what lies together meets in one L2 (heads that share keys; windows beside each
+// other, whose rows share cache lines), and in many runs, so that no die gets all the windows that the map's edge cuts short (2 x 29 x 579, windows of
+// 21 x 13, gradients: 568 us, with one run a die 806).  Where there are few blocks, of few wavefronts, up to four help staging (6 heads of 48
+// channels that share one key, 8 sequences of 969 in windows of 600, bf16, gradients: 386 us, without 742; with many blocks they only take
+// room: 3 x 339 x 511, windows of 13: 351, without 307).
 bool set_units(WindowParams &p, int heads)
 {
-    const __int128 units = (__int128)p.N * p.gy * p.gx * heads * p.blocks;
-    if (units * p.owners * 64 > 0xffff0000u) return false;  // (a launch has fewer than 2^32 lanes)
-    p.units = (int)units;
-    for (p.waves = p.owners; p.waves < 4 && (long)p.units * p.waves < 2 * kSimds;) p.waves *= 2;
-    return true;
+    const __int128 all = (__int128)p.N * p.gy * p.gx * heads * p.blocks;
+    if (all > 1 << 26) return false;
+    const long units = (long)all, windows = (long)p.N * p.gy * p.gx, share = (long)(heads / p.kv_heads) * p.blocks;
+    const long run = windows >= 64 ? windows / 64 * heads * p.blocks : windows * p.kv_heads >= 64 ? share : (units + 7) / 8;
+    const long runs = (units + run - 1) / run;
+    p.units = (int)units, p.run = (int)run, p.grid = (int)((runs + 7) / 8 * 8 * run);
+    for (p.waves = p.owners; p.waves < 4 && units * p.waves < 2 * kSimds;) p.waves *= 2;
+    return (size_t)p.grid * p.waves * 64 <= 0xffff0000u;  // (a launch has fewer than 2^32 lanes)
 }
 
 esc_status shape(const esc_window_attn *a, WindowParams *p)

@@ -55,6 +55,7 @@ struct WindowParams {
     int nby, nbx, n_edges;
     int edges[kWinMaxEdges];
     int blocks, units, waves, len;       // blocks a window and head, all blocks, wavefronts a block, words of a block's table
+    int run, grid;                       // how blocks go to the dies
     int owners;                          // so many of a block's wavefronts have tokens of their own (the others help staging)
     int tiles, ksplit;                   // tiles of 32 tokens of a wavefront; forward: wavefronts that share a tile's keys
     int buffers, ring, part_len;         // staging buffers; backward: words of a wavefront's ring (a power of two) and of its part
@@ -131,12 +132,11 @@ __device__ __forceinline__ Win win_of(const WindowParams &p, int n, int wy, int 
     return w;
 }
 
-// The block's place in the work: dies take contiguous eighths, so that the blocks of one window meet in one L2.
-__device__ __forceinline__ int unit_of(int units)
+// The block's place in the work: the dies, which blocks go to one after the other, take runs of it in turn.
+__device__ __forceinline__ int unit_of(const WindowParams &p)
 {
-    const int per = (units + 7) / 8, i = blockIdx.x >> 3;
-    const int u = (blockIdx.x & 7) * per + i;
-    return i < per && u < units ? u : -1;
+    const int i = blockIdx.x >> 3, r = i / p.run, u = (r * 8 + (blockIdx.x & 7)) * p.run + i - r * p.run;
+    return u < p.units ? u : -1;
 }
 
 // Range of offsets that the tokens [t0, t1) of a window see of all its tokens: first number (theirs subtracted), words.

@@ -45,7 +45,7 @@ __global__ __launch_bounds__(512, (WinGeom<T, DP>::F32 || DP == 64) ? 2 : 4) voi
     double *rings = reinterpret_cast<double *>(lds + (size_t)p.len * 4);  // one a wavefront
     char *const staged = reinterpret_cast<char *>(rings + (p.grad_bias != nullptr ? p.owners * (p.ring + kRingMore) : 0));
 
-    const int unit = unit_of(p.units);
+    const int unit = unit_of(p);
     if (unit < 0) return;
     const int block = unit % p.blocks, head = unit / p.blocks % p.heads, wi = unit / p.blocks / p.heads;
     const Win w = win_of(p, wi / (p.gy * p.gx), wi / p.gx % p.gy, wi % p.gx);
@@ -235,7 +235,7 @@ __global__ __launch_bounds__(512, (WinGeom<T, DP>::F32 || DP == 64) ? 2 : 3) voi
     float *table = reinterpret_cast<float *>(lds);
     char *const staged = lds + (size_t)p.len * 4;
 
-    const int unit = unit_of(p.units);
+    const int unit = unit_of(p);
     if (unit < 0) return;
     const int block = unit % p.blocks, kvh = unit / p.blocks % p.kv_heads, wi = unit / p.blocks / p.kv_heads;
     const Win w = win_of(p, wi / (p.gy * p.gx), wi / p.gx % p.gy, wi % p.gx);
@@ -516,7 +516,7 @@ hipError_t launch_dq(const WindowParams &p, hipStream_t s)
     const size_t lds = dq_lds<T, DP>(p);
     const hipError_t e = allow(reinterpret_cast<const void *>(&window_dq_kernel<T, DP>), lds);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((window_dq_kernel<T, DP>), dim3((unsigned)((p.units + 7) / 8 * 8)), dim3(64 * p.waves), lds, s, p);
+    hipLaunchKernelGGL((window_dq_kernel<T, DP>), dim3((unsigned)p.grid), dim3(64 * p.waves), lds, s, p);
     return hipGetLastError();
 }
 template <typename T, int DP>
@@ -525,7 +525,7 @@ hipError_t launch_dkv(const WindowParams &p, hipStream_t s)
     const size_t lds = dkv_lds<T, DP>(p);
     const hipError_t e = allow(reinterpret_cast<const void *>(&window_dkv_kernel<T, DP>), lds);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((window_dkv_kernel<T, DP>), dim3((unsigned)((p.units + 7) / 8 * 8)), dim3(64 * p.waves), lds, s, p);
+    hipLaunchKernelGGL((window_dkv_kernel<T, DP>), dim3((unsigned)p.grid), dim3(64 * p.waves), lds, s, p);
     return hipGetLastError();
 }
 

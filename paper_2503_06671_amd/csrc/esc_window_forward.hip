@@ -31,7 +31,7 @@ __global__ __launch_bounds__(512) void window_forward_kernel(const WindowParams 
     float *table = reinterpret_cast<float *>(lds);  // (first: its reads' addresses are then sums of two terms and a constant)
     char *const staged = lds + (size_t)p.len * 4;
 
-    const int unit = unit_of(p.units);
+    const int unit = unit_of(p);
     if (unit < 0) return;
     const int block = unit % p.blocks, head = unit / p.blocks % p.heads, wi = unit / p.blocks / p.heads;
     const Win w = win_of(p, wi / (p.gy * p.gx), wi / p.gx % p.gy, wi % p.gx);
@@ -251,7 +251,7 @@ hipError_t launch_one(const WindowParams &p, hipStream_t s)
         const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&window_forward_kernel<T, DP, U, SAVE>), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
         if (e != hipSuccess) return e;
     }
-    hipLaunchKernelGGL((window_forward_kernel<T, DP, U, SAVE>), dim3((unsigned)((p.units + 7) / 8 * 8)), dim3(64 * p.waves), lds, s, p);
+    hipLaunchKernelGGL((window_forward_kernel<T, DP, U, SAVE>), dim3((unsigned)p.grid), dim3(64 * p.waves), lds, s, p);
     return hipGetLastError();
 }
 
