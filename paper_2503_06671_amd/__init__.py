@@ -1,4 +1,4 @@
-"""MI355X-native ConvAttn forward pass (ESC paper, Sec. 3, Eq. 4).
+"""MI355X-native ConvAttn module (ESC paper, Sec. 3, Eq. 3 and 4), the window attention beside it, and the AdamW step.
 
 The compute lives in hand-written HIP kernels behind a C ABI
 (include/esc_convattn.h, built into csrc/libesc_convattn.so); `binding` is the

@@ -113,11 +113,11 @@ esc_status shape(const esc_window_attn *a, WindowParams *p)
 size_t table_bytes(const WindowParams &p) { return (size_t)p.heads * p.nby * p.nbx * 4; }
 
 // The forward's wavefronts.  A wavefront with two tiles of queries reads keys and values half as often, with one it takes so few registers that
-// four of a SIMD hide each other's waits.  Two: fp32 storage, whose three terms make the reads dear (180x320, windows of 32: 155 us, with one
-// 183), and bf16 storage in windows of fewer than 16 tiles, where a block's beginning weighs (3 x 339 x 511, windows of 13: 440 us, with one 573; windows of
-// 48: 361, with one 276) - where that leaves two wavefronts a SIMD.  Where even those are fewer than one a SIMD, up to four
-// wavefronts share a tile's keys.  Blocks are as large as leaves one for each compute unit: they stage a window's keys and values once for all their
-// queries.
+// four of a SIMD hide each other's waits.  Two: fp32 storage, whose three terms make the reads dear (180 x 320, windows of 32: 151 us, with one
+// 175), and bf16 storage in windows of fewer than 16 tiles, where a block's beginning weighs (3 x 339 x 511, windows of 13: 314 us, with one 499; windows of
+// 48: 275, with one 246) - where that leaves two wavefronts a SIMD.  Where even those are fewer than one a SIMD, up to four
+// wavefronts share a tile's keys (64 x 64, fp32: 30 us, without 39).  Blocks are as large as leaves one for each compute unit: they stage a
+// window's keys and values once for all their queries.
 bool plan_forward(WindowParams &p, bool f32)
 {
     const int dp = dim_padded(p.d);

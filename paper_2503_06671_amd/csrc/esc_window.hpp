@@ -1,16 +1,18 @@
 // Window attention with a learned relative position bias: what its forward (esc_window_forward.hip), its backward
 // (esc_window_backward.hip) and the host side (esc_window.hip) share.
 //
-// Tokens.  A window's pixels are numbered row by row, rows padded to a multiple of four, so that four consecutive tokens always
+// Tokens.  A window's pixels are numbered row by row, rows padded to whole pairs, so that the two tokens of a pair always
 // lie side by side in one row; a window at the map's edge is cut to the map first, so that only the padding is lost.  Pixels
 // beyond the row, beyond the last token and those that the mask hides are zeros in every operand.
 //
-// Offsets.  With off(t) = y(t) * tw + x(t), tw = 2 ww - 1, the offset of a key from a query has the number
+// Offsets.  With off(t) = y(t) * tw + x(t), tw = 2 w - 1 (w the window's own width), the offset of a key from a query has the number
 // off(key) - off(query) + centre, a sum of two terms: the bias of a score is one read of a table of offsets in LDS, at a
 // place that is linear in both tokens.  A block's queries see only the offsets of a range; that range alone is kept.
 //
 // Matrix instructions: v_mfma_f32_32x32x16_bf16.  bf16 storage as it is; fp32 values as three bf16 terms by truncation (exact),
 // the six products of terms whose orders add up to two at most (what is left out: below 2^-21 of a product, 2^-24 on average).
+// Where a branch lies between such an instruction and the first use of its result, the compiler has been seen to leave out the wait that
+// the use needs: the kernels have none there.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>

@@ -9,9 +9,13 @@
 //
 // The sums of equal offsets, in a fixed order.  Each wavefront adds to a ring of its own in LDS, in 64 bits: ds_add_f64 takes 8.5 clocks for 64
 // lanes where ds_add_f32 takes 193 (measured).  No instruction holds two values of one offset: its lanes are 32 queries and one
-// key, one half of the wavefront after the other.  What the ring
-// spans are the offsets between the wavefront's queries and ONE tile of keys; offsets that the next tile no longer reaches are complete and
-// leave for memory.  Two small kernels add the wavefronts' parts and the offsets of each bucket.
+// key, one half of the wavefront after the other.  What the ring spans are the offsets between the wavefront's queries and ONE tile of
+// keys; offsets that the next tile no longer reaches are complete and leave for memory.  Two small kernels add the wavefronts' parts and
+// the offsets of each bucket.
+//
+// What bounds it: window_dq_kernel the vector instructions and the LDS (half of its time the 32 additions in 64 bits a tile), window_dkv_kernel the
+// vector instructions and what its few wavefronts (168 to 256 registers) cannot hide.  Measured, 64 maps of 64 x 64, 4 heads of 16,
+// windows of 32, bf16: dq 629 us, dk and dv 640 us, the offsets' sums 76 us, the buckets 9 us, beside the forward's 440 us.
 #include "esc_window.hpp"
 
 namespace esc {

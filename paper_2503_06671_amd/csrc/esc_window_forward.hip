@@ -9,6 +9,11 @@
 //
 // Calls with fewer tiles than the chip has room for take one tile a wavefront and let up to four wavefronts share a tile's keys; their sums are
 // joined in LDS at the end.
+//
+// What bounds it: the issue of vector instructions (16 exponentials and as many multiplications, maxima, sums and conversions for a lane of a tile of
+// 32 x 32 pairs, beside two to four products in bf16); a products' share of the matrix units' time is 10 to 20 % with bf16 storage, 40 %
+// with fp32.  Measured, one MI355X: 180 x 320, 4 heads of 16, windows of 32 x 32: bf16 71 us, fp32 150 us; 6 heads of 32, windows of 48, bf16: 245 us;
+// 3 x 339 x 511, 6 heads of 8 that share 2 keys, windows of 13, bf16: 314 us; a map of 64 x 64 alone, fp32: 30 us.
 #include "esc_window.hpp"
 
 namespace esc {
