@@ -260,7 +260,9 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(const StepArgs a)
         if (aligned && base + kUnit * kUnits <= r.n) part_of_chunk<EIGHT, BF16, true>(r, f, keep, base);
         else if (base < r.n) part_of_chunk<EIGHT, BF16, false>(r, f, keep, base);
     }
-    // The last block to leave counts the step.  Two levels, so that no word sees more than kMaxGrid / kLeaves or kLeaves atomics.
+    // The last block to leave counts the step, after all of its wavefronts have read the count.  Two levels, so that no word sees more than
+    // kMaxGrid / kLeaves or kLeaves atomics.
+    __syncthreads();
     if (threadIdx.x == 0) {
         const unsigned leaf = blockIdx.x % kLeaves, leaves = min((unsigned)kLeaves, gridDim.x);
         const unsigned here = (gridDim.x - leaf + kLeaves - 1) / kLeaves;

@@ -169,3 +169,20 @@ def test_on_a_side_stream():
     side.synchronize()
     net.reference_step(*h)
     net.check()
+
+
+def test_only_empty_tensors():
+    net = Net("f32", sizes=[0, 0], seed=8)
+    net.opt.step(1e-3)
+    assert net.opt.steps == 5
+
+
+def test_short_tensors_step_after_step():
+    # blocks whose first wavefront has little to do beside others that have nothing: each step's count is that of all of them
+    net = Net("8bit", sizes=[1] * 40, seed=9)
+    for k in range(20):
+        h = dict(lr=1e-2, beta1=0.9, beta2=0.95, eps=1e-8, grad_scale=1.0)
+        net.opt.step(**h)
+        net.reference_step(**h)
+    net.check()
+    assert net.opt.steps == 24
