@@ -14,7 +14,7 @@
 //
 // What bounds it: memory.  28 bytes an element with fp32 states and gradients (p, g, m, v in; p, m, v out), 16 and a sixteenth with
 // 8-bit states, 14 and a sixteenth with bf16 gradients.  Measured, one MI355X: 8-bit states, bf16 gradients, 170 million elements: 497 us, 4.8 TB/s (a copy of 1 GiB:
-// 5.1); a network of 0.8 million elements, fp32: 8.5 us.
+// 5.1); a network of 0.8 million elements, fp32: 9.1 us.
 // Layout: the plan (device memory) holds one record per tensor and the tensor's number for every chunk of kChunk elements, so
 // that a block finds its work in two dependent loads whatever the number of tensors, and small tensors cost a block each, not
 // a launch.  A wavefront takes 256 consecutive elements at a time, four a lane (16-byte accesses; one block of

@@ -115,7 +115,8 @@ size_t table_bytes(const WindowParams &p) { return (size_t)p.heads * p.nby * p.n
 // The forward's wavefronts.  A wavefront with two tiles of queries reads keys and values half as often, with one it takes so few registers that
 // four of a SIMD hide each other's waits.  Two: fp32 storage, whose three terms make the reads dear (180 x 320, windows of 32: 151 us, with one
 // 175), and bf16 storage in windows of fewer than 16 tiles, where a block's beginning weighs (3 x 339 x 511, windows of 13: 314 us, with one 499; windows of
-// 48: 275, with one 246) - where that leaves two wavefronts a SIMD.  Where even those are fewer than one a SIMD, up to four
+// 48: 275, with one 246) - where a window has more than four tiles (4 x 171 x 171, windows of 9 x 9, fp32: 84 us, with one 71; 9 x 123 x 110, windows of
+// 13 x 7, bf16: 218, with one 208) and the call leaves two wavefronts a SIMD.  Where even those are fewer than one a SIMD, up to four
 // wavefronts share a tile's keys (64 x 64, fp32: 30 us, without 39).  Blocks are as large as leaves one for each compute unit: they stage a
 // window's keys and values once for all their queries.
 bool plan_forward(WindowParams &p, bool f32)
@@ -123,7 +124,7 @@ bool plan_forward(WindowParams &p, bool f32)
     const int dp = dim_padded(p.d);
     const long tokens = (long)p.wh * in_pairs(p.ww), each = (tokens + 31) / 32, windows = (long)p.N * p.gy * p.gx * p.heads;
     const long all = each * windows;
-    p.tiles = (f32 ? dp < 64 : each < 16) && all >= 2 * 2 * kSimds && each > 1 ? 2 : 1;
+    p.tiles = (f32 ? dp < 64 : each < 16) && each > 4 && all >= 2 * 2 * kSimds ? 2 : 1;
     const long waves = (each + p.tiles - 1) / p.tiles;
     p.ksplit = 1;
     while (p.tiles == 1 && p.ksplit < 4 && waves * windows * p.ksplit < 2 * kSimds && tokens >= 128 * p.ksplit) p.ksplit *= 2;
