@@ -100,6 +100,8 @@ CASES = [
     (2, 1, 9, 37, 1, (1, 5), {"kv": 1}),                               # one channel a head, 37 heads share a key
     (40, 1, 2, 2, 16, (1, 2), {}),                                     # two tokens: nothing averages what rounding does
     (9, 6, 5, 4, 24, (2, 3), {"kv": 2, "edges": [1, 2], "mask": whole_images_and_holes}),
+    (5, 33, 37, 3, 8, (4, 4), {"kv": 1}),                              # hundreds of windows, not a whole number of runs
+    (2, 23, 163, 2, 33, (5, 9), {"kv": 1, "mask": whole_images_and_holes}),  # rows that end in a window of one column
 ]
 
 
