@@ -166,7 +166,7 @@ __global__ __launch_bounds__(512, (WinGeom<T, DP>::F32 || DP == 64) ? 2 : 4) voi
                     ds[u][i] = exp2_of(s[i]) * (dp[i] - delta[u]);
                 }
                 if (!whole) {
-                                        leave_out(bits, 0.f, ds[u]);
+                    leave_out(bits, 0.f, ds[u]);
 #pragma unroll
                     for (int i = 0; i < 16; ++i) ds[u][i] = ok[u] ? ds[u][i] : 0.f;
                 }
@@ -362,7 +362,7 @@ __global__ __launch_bounds__(512, (WinGeom<T, DP>::F32 || DP == 64) ? 2 : 3) voi
                     }
                 }
                 if (!whole) {
-                                        leave_out(bits, 0.f, s);
+                    leave_out(bits, 0.f, s);
                 }
                 ep[u] = pack<G::NT>(s);
 #pragma unroll
