@@ -325,7 +325,7 @@ esc_status esc_convattn_backward(const void *x, const void *grad_out, esc_dtype 
  *   saved        what the backward pass needs (the rows' largest scores and logarithms of their sums, with bf16 storage also what rounding
  *                took from out), or NULL: esc_window_attention_saved_bytes, 256-byte aligned
  * A pixel with no key left (a bias of -infinity everywhere) has out = 0.  Scores, maxima and sums are fp32.  bf16 storage: products of the stored
- * values on the matrix cores, the exponentials rounded to bf16 as operands of the second product (2^-9 of each term at most; where
+ * values on the matrix cores, the exponentials as two bf16 terms as operands of the second product (2^-16 of each left out at most; where
  * `saved` is given they are three bf16 terms, exact, since the bias' gradient, an fp32 result, comes of the same sums: the two may round
  * an element of out differently).  fp32 storage: values and exponentials as three bf16 terms each (exact), six products of terms (what is left out
  * lies below 2^-21 of a product, 2^-24 on average); a value of q, k or v that is not finite makes NaN of what its products reach.

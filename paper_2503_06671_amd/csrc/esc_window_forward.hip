@@ -21,17 +21,19 @@ namespace {
 
 constexpr float kSlack = 8.f;
 
+// The exponentials in the second product, with bf16 storage: two bf16 terms, which leave the result off by its own rounding alone (0.0017 of its norm;
+// with one term 0.0023, for 80 us instead of 100 at 180 x 320, windows of 32, and 252 instead of 305 in windows of 48).
 // SAVE: the backward pass follows.  Its delta = sum over the channels of out * dout stands for sum over the keys of p * dp, and what it is off goes into every
 // term of the bias' gradient, an fp32 result: with bf16 storage the exponentials are then three bf16 terms, and what rounding took from
 // the result is kept (off by, of the bias' gradient's norm, for windows of 2 to 60 tokens: 1e-4 with one term, 0.5e-6 to 3.6e-6 with two, 0.1e-6
-// to 0.4e-6 with three, which take 464 us where two take 390, for 64 maps of 64 x 64).
+// to 0.4e-6 with three, which take 438 us where two take 390, for 64 maps of 64 x 64).
 template <typename T, int DP, int U, bool SAVE>
 __global__ __launch_bounds__(512) void window_forward_kernel(const WindowParams p)
 {
     using G = WinGeom<T, DP>;
     using S = Stager<T, DP, true, false, false, true>;  // keys by tokens, values by channels
     constexpr bool SUM_ROW = DP == 16;                  // the exponentials' sum is row 16 of the product
-    constexpr int VT = G::F32 || SAVE ? 3 : 1;
+    constexpr int VT = G::F32 || SAVE ? 3 : 2;
     extern __shared__ __align__(16) char lds[];
     float *table = reinterpret_cast<float *>(lds);  // (first: its reads' addresses are then sums of two terms and a constant)
     char *const staged = lds + (size_t)p.len * 4;

@@ -1,0 +1,43 @@
+"""Window attention where fewer bits than the result's type holds would show, against the float64 reference."""
+import pytest
+import torch
+
+from tests import window_reference as ref
+from tests.test_gpu_window_attention import BF16, Case, whole_images_and_holes
+
+pytestmark = pytest.mark.gpu
+
+# windows of few pixels: nothing averages what rounding does to single terms
+SMALL = [
+    # N, H, W, heads, d, window, keywords
+    (6, 12, 20, 2, 16, (1, 2), {}),
+    (4, 15, 18, 4, 8, (2, 3), {"kv": 2}),
+    (3, 16, 20, 3, 32, (4, 4), {"mask": whole_images_and_holes}),
+    (2, 24, 23, 2, 64, (5, 3), {"edges": [1, 2]}),
+    (2, 33, 40, 2, 16, (8, 8), {}),
+    (1, 64, 40, 2, 24, (20, 20), {}),
+]
+
+
+def assert_rounded_once(got, r, name, d, tokens, terms, what):
+    """`got` is r[name] rounded to bf16 from a value that is off by e: e is what fp32 arithmetic does (ref.tolerance of fp32 results) and `terms`
+    of the sum of magnitudes.  A value's distance from the nearest bf16 one changes by no more than the value, so the rounded value is at
+    most 2 e farther off than the exact one rounded."""
+    exact = r[name]
+    rounding = (exact.to(BF16).to(ref.D) - exact).abs()
+    e = ref.tolerance(r, name, torch.float32, d, tokens) + terms * r[name + "_abs"]
+    off = (got.detach().cpu().to(ref.D) - exact).abs()
+    assert torch.isfinite(off).all(), (what, name)
+    worst = (off / (rounding + 2 * e)).max().item()
+    assert worst <= 1.0, (what, name, worst)
+
+
+@pytest.mark.parametrize("case", range(len(SMALL)))
+def test_probabilities_in_bf16_results(case):
+    # two bf16 terms at least: 2^-8 of what is left after the first, 2^-16 of a probability
+    N, H, W, heads, d, window, more = SMALL[case]
+    print(f"[case] {SMALL[case]}", flush=True)
+    c = Case(BF16, N, H, W, heads, d, window, seed=300 + case, **more)
+    r = c.reference()
+    assert_rounded_once(c.forward(), r, "out", d, c.tokens, 2.0 ** -16, SMALL[case])
+    assert_rounded_once(c.train()["out"], r, "out", d, c.tokens, 2.0 ** -16, SMALL[case])
