@@ -357,8 +357,8 @@ esc_status esc_window_attention_forward(const void *q, const void *k, const void
  *   g->bias           fp32, shaped like bias, summed over images, windows and all pairs of a bucket, or NULL;
  *                     accumulate != 0 adds it to what the buffer holds
  * The scores are formed again.  Sums are fp32 (those of a bucket begin in 64 bits), each in a fixed order: equal calls give equal bits.  With bf16
- * storage, as operands of the products that give q's, k's and v's gradients, the probabilities are rounded to bf16 and the scores'
- * gradients to two bf16 terms; the bias' gradient takes them unrounded.  The workspace (esc_window_attention_backward_workspace_bytes, 256-byte
+ * storage, as operands of the products that give q's, k's and v's gradients, the probabilities and the scores'
+ * gradients are two bf16 terms each (2^-16 left out at most); the bias' gradient takes the latter unrounded.  The workspace (esc_window_attention_backward_workspace_bytes, 256-byte
  * aligned, either storage type) is plain scratch: it needs no preparation and its contents are undefined after the call.  What is
  * written may not overlap anything else.  Two launches, with the bias' gradient four.
  */

@@ -24,11 +24,11 @@ namespace {
 // A ring's places behind its end: a pair of offsets that runs over it stays together (two: an even number keeps what follows aligned).
 constexpr int kRingMore = 2;
 
-// ds in the products with keys and queries, with bf16 storage: two terms.  Its sum over a query's keys is 0, so what one rounding of each term takes
-// weighs more in the sums than it does in those of p: dq and dk were 0.0025 off with one term and are 0.0017, which is the rounding of the
-// results alone, for 50 us more of 571 (dq) and 77 of 589 (dkv) for 64 maps of 64 x 64.  p in dv's sums has one: 0.0023, and 135 us more with two.
+// p and ds in the products that give q's, k's and v's gradients, with bf16 storage: two terms, which leave the gradients off by their own rounding alone
+// (0.0017 of their norm).  With one term of p dv was 0.0023 off, for 95 us less of 1740 (64 maps of 64 x 64); ds sums to 0 over a query's keys, so that
+// what one rounding of each term takes weighs more: dq and dk were 0.0025 off, for 50 us less of 571 (dq) and 77 of 589 (dkv).
 template <typename T>
-constexpr int kDsTerms = std::is_same<T, float>::value ? 3 : 2;
+constexpr int kTerms = std::is_same<T, float>::value ? 3 : 2;
 
 __device__ __forceinline__ void lds_add(double *p, float v) { __hip_atomic_fetch_add(p, (double)v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP); }
 
@@ -145,7 +145,7 @@ __global__ __launch_bounds__(512, (WinGeom<T, DP>::F32 || DP == 64) ? 2 : 4) voi
 #pragma unroll
             for (int a = 0; a < 4; ++a) key[a] = *reinterpret_cast<const wi32x2 *>(off + tile * 16 + 4 * a + 2 * half);
             wf32x16 ds[U];
-            Packed<kDsTerms<T>> e[U];
+            Packed<kTerms<T>> e[U];
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 wf32x16 s;
@@ -170,7 +170,7 @@ __global__ __launch_bounds__(512, (WinGeom<T, DP>::F32 || DP == 64) ? 2 : 4) voi
 #pragma unroll
                     for (int i = 0; i < 16; ++i) ds[u][i] = ok[u] ? ds[u][i] : 0.f;
                 }
-                e[u] = pack<kDsTerms<T>>(ds[u]);
+                e[u] = pack<kTerms<T>>(ds[u]);
             }
             accumulate<T, DP>(buf + S::CM0_AT, tile, e, acc);
             if (bias_grad) {
@@ -331,8 +331,8 @@ __global__ __launch_bounds__(512, (WinGeom<T, DP>::F32 || DP == 64) ? 2 : 3) voi
         auto tile_of = [&](int tile, auto large) {
             const wu32x4 bits = *reinterpret_cast<const wu32x4 *>(buf + S::BITS_AT + tile * 16);
             const bool whole = all_take_part(bits);
-            Packed<G::NT> ep[U];
-            Packed<kDsTerms<T>> es[U];
+            Packed<kTerms<T>> ep[U];
+            Packed<kTerms<T>> es[U];
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 wf32x16 s, dp;
@@ -364,10 +364,10 @@ __global__ __launch_bounds__(512, (WinGeom<T, DP>::F32 || DP == 64) ? 2 : 3) voi
                 if (!whole) {
                     leave_out(bits, 0.f, s);
                 }
-                ep[u] = pack<G::NT>(s);
+                ep[u] = pack<kTerms<T>>(s);
 #pragma unroll
                 for (int i = 0; i < 16; ++i) s[i] *= dp[i];
-                es[u] = pack<kDsTerms<T>>(s);
+                es[u] = pack<kTerms<T>>(s);
             }
             accumulate<T, DP>(buf + S::CM1_AT, tile, ep, dv);
             accumulate<T, DP>(buf + S::CM0_AT, tile, es, dk);

@@ -41,3 +41,15 @@ def test_probabilities_in_bf16_results(case):
     r = c.reference()
     assert_rounded_once(c.forward(), r, "out", d, c.tokens, 2.0 ** -16, SMALL[case])
     assert_rounded_once(c.train()["out"], r, "out", d, c.tokens, 2.0 ** -16, SMALL[case])
+
+
+@pytest.mark.parametrize("case", range(len(SMALL)))
+def test_terms_of_the_gradients(case):
+    # p and the scores' gradients in two bf16 terms at least
+    N, H, W, heads, d, window, more = SMALL[case]
+    print(f"[case] {SMALL[case]}", flush=True)
+    c = Case(BF16, N, H, W, heads, d, window, seed=330 + case, **more)
+    r, got = c.reference(), c.train()
+    group = c.heads // c.kv
+    for name, tokens in (("grad_q", c.tokens), ("grad_k", c.tokens * group), ("grad_v", c.tokens * group)):
+        assert_rounded_once(got[name], r, name, d, tokens, 2.0 ** -16, SMALL[case])
