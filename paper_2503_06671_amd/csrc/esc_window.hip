@@ -42,16 +42,18 @@ int table_words(const WindowParams &p, long tokens)
 }
 
 // The backward's wavefronts, up to eight a block and no more than leave a block for each compute unit, and its staging buffers.  What is weighed: how many
-// wavefronts a compute unit holds (by LDS, and by registers: two a SIMD with fp32 storage or heads wider than 32, else four), how many of the blocks'
-// wavefronts have tokens, what a block's beginning and staging cost (as much as a wavefront's work), and that with one buffer nothing is on its way
-// while a block multiplies (where there is more than one chunk).
+// wavefronts a compute unit holds (by LDS, and by registers: `simd` a SIMD, over whose four a block's wavefronts go in turn, so that blocks of five to
+// eight take two places of each), how many of the blocks' wavefronts have tokens, what a block's beginning and staging cost (as much as a wavefront's work),
+// and that with one buffer nothing is on its way while a block multiplies (where there is more than one chunk).  Forward and gradients, bf16, dk and dv's
+// kernel with three wavefronts a SIMD in blocks of four, and, counted as four a SIMD, of eight or five: 64 x 64 x 64, windows of 32: 1667 and 1744 us;
+// 8 x 96 x 96, 6 heads of 32, windows of 24: 742 and 1007 us.
 template <typename F>
-bool choose_waves(WindowParams &p, int heads, bool f32, int dp, F lds)
+bool choose_waves(WindowParams &p, int heads, bool f32, int dp, int simd, F lds)
 {
     const long tokens = (long)p.wh * in_pairs(p.ww), windows = (long)p.N * p.gy * p.gx * heads;
     const long all = (tokens + 31) / 32;
     const int want = (int)std::max<long>(1, std::min({(long)kWinMaxWaves, all, all * windows / kCus}));
-    const int most = tokens <= win_chunk(f32, dp) ? 1 : 2, slots = f32 || dp == 64 ? 8 : 16;
+    const int most = tokens <= win_chunk(f32, dp) ? 1 : 2;
     auto take = [&](int owners, int buffers) {
         p.owners = owners, p.buffers = buffers, p.len = (table_words(p, owners * 32) + 3) & ~3;
         p.blocks = (int)((all + owners - 1) / owners);
@@ -61,7 +63,7 @@ bool choose_waves(WindowParams &p, int heads, bool f32, int dp, F lds)
     for (int buffers = most; buffers >= 1; --buffers)
         for (int owners = want; owners >= 1; --owners) {
             take(owners, buffers);
-            const int resident = (int)std::min<size_t>(kLdsPerCu / lds(p), slots / owners) * owners;
+            const int places = owners < 4 ? 4 * simd / owners : simd / ((owners + 3) / 4), resident = (int)std::min<size_t>(kLdsPerCu / lds(p), places) * owners;
             const float score = (float)resident * all / ((float)p.blocks * (owners + 1)) * (buffers < most ? 0.85f : 1.f);
             if (score > best) best = score, best_owners = owners, best_buffers = buffers;
         }
@@ -155,7 +157,7 @@ bool plan_dq(WindowParams &p, bool f32)
     // (the same plan with and without the table's gradient)
     float *const grad = p.grad_bias;
     p.grad_bias = reinterpret_cast<float *>(16);
-    const bool fits = choose_waves(p, p.heads, f32, dp, [&](const WindowParams &x) { return window_dq_lds(x, f32, dp); });
+    const bool fits = choose_waves(p, p.heads, f32, dp, window_dq_resident(f32, dp), [&](const WindowParams &x) { return window_dq_lds(x, f32, dp); });
     p.grad_bias = grad;
     if (!fits || !set_units(p, p.heads)) return false;
     // the sums over the windows: blocks for the whole card, sixteen windows each at least
@@ -166,7 +168,8 @@ bool plan_dq(WindowParams &p, bool f32)
 bool plan_dkv(WindowParams &p, bool f32)
 {
     const int dp = dim_padded(p.d);
-    return choose_waves(p, p.kv_heads, f32, dp, [&](const WindowParams &x) { return window_dkv_lds(x, f32, dp); }) && set_units(p, p.kv_heads);
+    return choose_waves(p, p.kv_heads, f32, dp, window_dkv_resident(f32, dp), [&](const WindowParams &x) { return window_dkv_lds(x, f32, dp); }) &&
+           set_units(p, p.kv_heads);
 }
 
 struct Scratch {

@@ -66,6 +66,10 @@ struct WindowParams {
     float scale, inv_scale, log2_scale;  // scale * log2(e) last
 };
 
+// Wavefronts of the backward's kernels that a SIMD holds, by the registers their launch bounds leave them.
+constexpr int window_dq_resident(bool f32, int dp) { return f32 || dp == 64 ? 2 : 4; }
+constexpr int window_dkv_resident(bool f32, int dp) { return f32 || dp == 64 ? 2 : 3; }
+
 size_t window_forward_lds(const WindowParams &p, bool f32, int dp);  // (buffers, waves, ksplit and len set)
 size_t window_dq_lds(const WindowParams &p, bool f32, int dp);  // (buffers, owners, ring, len and grad_bias set)
 size_t window_dkv_lds(const WindowParams &p, bool f32, int dp);

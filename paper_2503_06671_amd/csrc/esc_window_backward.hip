@@ -39,7 +39,7 @@ __device__ __forceinline__ TableRange wave_range(const Win &w, int t0)
 }
 
 template <typename T, int DP>
-__global__ __launch_bounds__(512, (WinGeom<T, DP>::F32 || DP == 64) ? 2 : 4) void window_dq_kernel(const WindowParams p)
+__global__ __launch_bounds__(512, window_dq_resident(WinGeom<T, DP>::F32, DP)) void window_dq_kernel(const WindowParams p)
 {
     using G = WinGeom<T, DP>;
     using S = Stager<T, DP, true, true, true, false>;  // keys by tokens and by channels, values by tokens
@@ -227,7 +227,7 @@ __global__ __launch_bounds__(512, (WinGeom<T, DP>::F32 || DP == 64) ? 2 : 4) voi
 }
 
 template <typename T, int DP>
-__global__ __launch_bounds__(512, (WinGeom<T, DP>::F32 || DP == 64) ? 2 : 3) void window_dkv_kernel(const WindowParams p)
+__global__ __launch_bounds__(512, window_dkv_resident(WinGeom<T, DP>::F32, DP)) void window_dkv_kernel(const WindowParams p)
 {
     using G = WinGeom<T, DP>;
     using S = Stager<T, DP, true, true, true, true>;  // queries and the result's gradient, by tokens and by channels
