@@ -41,9 +41,13 @@ int table_words(const WindowParams &p, long tokens)
     return widest(p, [&](int width) { return (p.wh - 1) * (2 * width - 1) + in_pairs(width) + span(p, width, tokens); });
 }
 
+// Blocks of so many wavefronts that fit a compute unit whose SIMDs hold `simd` each.  A block's wavefronts go to the four in turn: five to eight take two
+// places of each.
+int places(int waves, int simd) { return waves < 4 ? 4 * simd / waves : simd / ((waves + 3) / 4); }
+
 // The backward's wavefronts, up to eight a block and no more than leave a block for each compute unit, and its staging buffers.  What is weighed: how many
-// wavefronts a compute unit holds (by LDS, and by registers: `simd` a SIMD, over whose four a block's wavefronts go in turn, so that blocks of five to
-// eight take two places of each), how many of the blocks' wavefronts have tokens, what a block's beginning and staging cost (as much as a wavefront's work),
+// wavefronts a compute unit holds (by LDS, and by registers), how many of the blocks' wavefronts have tokens, what a block's beginning and staging cost (as
+// much as a wavefront's work),
 // and that with one buffer nothing is on its way while a block multiplies (where there is more than one chunk).  Forward and gradients, bf16, dk and dv's
 // kernel with three wavefronts a SIMD in blocks of four, and, counted as four a SIMD, of eight or five: 64 x 64 x 64, windows of 32: 1667 and 1744 us;
 // 8 x 96 x 96, 6 heads of 32, windows of 24: 742 and 1007 us.
@@ -63,7 +67,7 @@ bool choose_waves(WindowParams &p, int heads, bool f32, int dp, int simd, F lds)
     for (int buffers = most; buffers >= 1; --buffers)
         for (int owners = want; owners >= 1; --owners) {
             take(owners, buffers);
-            const int places = owners < 4 ? 4 * simd / owners : simd / ((owners + 3) / 4), resident = (int)std::min<size_t>(kLdsPerCu / lds(p), places) * owners;
+            const int resident = (int)std::min<size_t>(kLdsPerCu / lds(p), places(owners, simd)) * owners;
             const float score = (float)resident * all / ((float)p.blocks * (owners + 1)) * (buffers < most ? 0.85f : 1.f);
             if (score > best) best = score, best_owners = owners, best_buffers = buffers;
         }
@@ -118,9 +122,10 @@ size_t table_bytes(const WindowParams &p) { return (size_t)p.heads * p.nby * p.n
 // four of a SIMD hide each other's waits.  Two: fp32 storage, whose three terms make the reads dear (180 x 320, windows of 32: 151 us, with one
 // 175), and bf16 storage in windows of fewer than 16 tiles, where a block's beginning weighs (3 x 339 x 511, windows of 13: 314 us, with one 499; windows of
 // 48: 275, with one 246) - where a window has more than four tiles (4 x 171 x 171, windows of 9 x 9, fp32: 84 us, with one 71; 9 x 123 x 110, windows of
-// 13 x 7, bf16: 218, with one 208) and the call leaves two wavefronts a SIMD.  Where even those are fewer than one a SIMD, up to four
-// wavefronts share a tile's keys (64 x 64, fp32: 30 us, without 39).  Blocks are as large as leaves one for each compute unit: they stage a
-// window's keys and values once for all their queries.
+// 13 x 7, bf16: 218, with one 208) and the call leaves two wavefronts a SIMD.  Where even those are fewer than one a SIMD, up to four wavefronts, and
+// no more than a chunk has tiles, share a tile's keys (64 x 64, 4 heads, windows of 32: heads of 16 in bf16 18.3 us with four, 23.8 with two, 30 without;
+// in fp32 30 us with two, 40 without), and others help staging as long as there are pieces for them and all blocks are on the chip at once (heads of 64,
+// bf16: 33 us, without 47).  Blocks are as large as leaves one for each compute unit: they stage a window's keys and values once for all their queries.
 bool plan_forward(WindowParams &p, bool f32)
 {
     const int dp = dim_padded(p.d);
@@ -129,10 +134,13 @@ bool plan_forward(WindowParams &p, bool f32)
     p.tiles = (f32 ? dp < 64 : each < 16) && each > 4 && all >= 2 * 2 * kSimds ? 2 : 1;
     const long waves = (each + p.tiles - 1) / p.tiles;
     p.ksplit = 1;
-    while (p.tiles == 1 && p.ksplit < 4 && waves * windows * p.ksplit < 2 * kSimds && tokens >= 128 * p.ksplit) p.ksplit *= 2;
+    const int sharers = std::min(4, win_chunk(f32, dp) / 32);
+    while (p.tiles == 1 && p.ksplit < sharers && waves * windows * p.ksplit < 2 * kSimds && tokens >= 128 * p.ksplit) p.ksplit *= 2;
     long queries = std::min<long>(kWinMaxWaves / p.ksplit, waves);
     queries = std::max<long>(1, std::min(queries, waves * windows / kCus));
     p.buffers = tokens <= win_chunk(f32, dp) ? 1 : 2;
+    const int pieces = (p.d + 3) / 4 * win_chunk(f32, dp);  // (of keys and values, two tokens and four channels each)
+    const auto on_a_cu = [&](int waves) { return (long)std::min<size_t>(kLdsPerCu / window_forward_lds(p, f32, dp), places(waves, window_forward_resident(f32, dp))); };
     for (; queries >= 1; --queries) {
         p.owners = (int)queries * p.ksplit;
         p.len = (table_words(p, (int)queries * p.tiles * 32) + 3) & ~3;
@@ -143,7 +151,9 @@ bool plan_forward(WindowParams &p, bool f32)
                 queries = even + 1;
                 continue;
             }
-            return set_units(p, p.heads);
+            if (!set_units(p, p.heads)) return false;
+            while (p.ksplit > 1 && 2 * p.waves <= kWinMaxWaves && p.waves * 64 < pieces && p.units <= kCus * on_a_cu(2 * p.waves)) p.waves *= 2;
+            return true;
         }
     }
     return false;

@@ -66,7 +66,9 @@ struct WindowParams {
     float scale, inv_scale, log2_scale;  // scale * log2(e) last
 };
 
-// Wavefronts of the backward's kernels that a SIMD holds, by the registers their launch bounds leave them.
+// Wavefronts that a SIMD holds: of the forward's kernel with one tile a wavefront, by the registers it takes, and of the backward's, by those that their
+// launch bounds leave them.
+constexpr int window_forward_resident(bool f32, int dp) { return f32 ? (dp == 64 ? 2 : 3) : dp == 64 ? 3 : 4; }
 constexpr int window_dq_resident(bool f32, int dp) { return f32 || dp == 64 ? 2 : 4; }
 constexpr int window_dkv_resident(bool f32, int dp) { return f32 || dp == 64 ? 2 : 3; }
 

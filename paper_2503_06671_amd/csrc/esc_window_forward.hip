@@ -7,8 +7,8 @@
 // the right operand of the next product O^T = V^T P^T.  The bias is the product's starting value.  The running maximum is followed only
 // where a score exceeds it by more than kSlack: the exponentials then reach 2^kSlack, and most tiles rescale nothing.
 //
-// Calls with fewer tiles than the chip has room for take one tile a wavefront and let up to four wavefronts share a tile's keys; their sums are
-// joined in LDS at the end.
+// Calls with fewer tiles than the chip has room for take one tile a wavefront and let up to four wavefronts (no more than a chunk has tiles) share a
+// tile's keys; their sums are joined in LDS at the end.
 //
 // What bounds it: the issue of vector instructions (16 exponentials and as many multiplications, maxima, sums and conversions for a lane of a tile of
 // 32 x 32 pairs, beside two to four products in bf16); a products' share of the matrix units' time is 10 to 20 % with bf16 storage, 40 %

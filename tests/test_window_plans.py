@@ -29,7 +29,7 @@ int main()
         if (shape(&a, &p) != ESC_OK) return 1;
         const int dp = dim_padded(p.d);
         WindowParams f = p, q = p, k = p;
-        show("forward", plan_forward(f, f32), f, f32, 0);
+        show("forward", plan_forward(f, f32), f, f32, window_forward_resident(f32, dp));
         show("dq", plan_dq(q, f32), q, f32, window_dq_resident(f32, dp));
         show("dkv", plan_dkv(k, f32), k, f32, window_dkv_resident(f32, dp));
     }
@@ -60,13 +60,27 @@ def test_residency_is_that_of_the_built_kernels(plans):
     # a SIMD has 512 registers a lane, given out in eights
     built = {}
     for name, _, vgprs, _ in kernel_notes():
-        m = re.search(r"window_(dq|dkv)_kernelI([ft])Li(\d+)E", name)
+        m = re.search(r"window_(dq|dkv)_kernelI([ft])Li(\d+)E", name) or re.search(r"window_(forward)_kernelI([ft])Li(\d+)ELi1E", name)
         if m:
-            built[m.group(1), m.group(2) == "f", int(m.group(3))] = min(8, 512 // ((vgprs + 7) // 8 * 8))
-    assert len(built) == 2 * 2 * 3
+            key = m.group(1), m.group(2) == "f", int(m.group(3))
+            built[key] = min(built.get(key, 8), 512 // ((vgprs + 7) // 8 * 8))
+    assert len(built) == 3 * 2 * 3
     for (kernel, f32, dp), fits in built.items():
         row = next(r for r in plans([(1, 64, 64, 4, 4, dp, 32, 32, 0, f32)])[0] if r["pass"] == kernel)
         assert row["resident"] == fits, (kernel, f32, dp, fits)
+
+
+def test_every_sharer_of_a_tiles_keys_has_keys(plans):
+    # a chunk's tiles of 32 tokens are dealt to the wavefronts that share them: no more of those than tiles
+    cases = [(N, H, W, heads, kv, d, *win, 0, f32)
+             for N, H, W in ((1, 16, 16), (1, 64, 64), (3, 96, 96), (1, 180, 320), (5, 50, 61)) for heads, kv in ((1, 1), (4, 4), (6, 2))
+             for d in (8, 16, 24, 32, 48, 64) for win in ((1, 1), (8, 8), (13, 13), (16, 16), (32, 32), (48, 48), (5, 60), (1, 300)) for f32 in (0, 1)]
+    shared = 0
+    for c, (r, *_) in zip(cases, plans(cases)):
+        assert r["fits"] and 1 <= r["ksplit"] <= max(1, r["chunk"] // 32), (c, r)
+        assert r["owners"] % r["ksplit"] == 0 and r["owners"] <= r["waves"] <= 8, (c, r)
+        shared += r["ksplit"] > 1
+    assert shared > 50
 
 
 def test_backward_blocks_fill_the_places(plans):
