@@ -26,6 +26,9 @@ namespace esc {
 // Exponentials are exp2(fma(score, log2(e) scale, -shift)), shift the rounded product for the row's largest score.  What that rounding takes or
 // adds is the same for the row and falls out of the quotient - up to this size; larger ones subtract first (one operation more a score).
 constexpr float kLargeShift = 0x1p20f;
+// The running maximum that scores are taken relative to is followed only where one exceeds it by more than kSlack / (log2(e) scale), so that much, or its
+// rounding to the scores' last place (twice the slack at most), a score may lie above the largest that the backward pass gets.
+constexpr float kSlack = 8.f;
 constexpr int kWinMaxEdges = 32;
 constexpr int kWinMaxDim = 64;
 constexpr int kWinMaxOffsets = 16384;

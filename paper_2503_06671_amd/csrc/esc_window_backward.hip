@@ -56,6 +56,7 @@ __global__ __launch_bounds__(512, window_dq_resident(WinGeom<T, DP>::F32, DP)) v
     const int queries = p.owners * 32 * U, q0 = block * queries;
     if (q0 >= w.L) return;
     const TableRange range = table_range(w, q0, min(q0 + queries, w.L), -1);
+    const float above = 2 * kSlack / p.log2_scale;
     const bool bias_grad = p.grad_bias != nullptr;
 
     const long hw = (long)p.H * p.W;
@@ -161,7 +162,7 @@ __global__ __launch_bounds__(512, window_dq_resident(WinGeom<T, DP>::F32, DP)) v
                 const wf32x16 dp = score<T, DP>(buf + S::RM1_AT, tile, own_go[u], wf32x16{});
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    if constexpr (decltype(large)::value) s[i] = __builtin_fmaf(fminf(s[i] - top[u], 0.f), p.log2_scale, -log_sum[u]);
+                    if constexpr (decltype(large)::value) s[i] = __builtin_fmaf(fminf(s[i] - top[u], above), p.log2_scale, -log_sum[u]);
                     else s[i] = __builtin_fmaf(s[i], p.log2_scale, -shift[u]);
                     ds[u][i] = exp2_of(s[i]) * (dp[i] - delta[u]);
                 }
@@ -246,6 +247,7 @@ __global__ __launch_bounds__(512, window_dkv_resident(WinGeom<T, DP>::F32, DP)) 
     const int keys = p.owners * 32 * U, k0 = block * keys;
     if (k0 >= w.L) return;
     const TableRange range = table_range(w, k0, min(k0 + keys, w.L), 1);
+    const float above = 2 * kSlack / p.log2_scale;
 
     const long hw = (long)p.H * p.W;
     const int lane = threadIdx.x & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -357,7 +359,7 @@ __global__ __launch_bounds__(512, window_dkv_resident(WinGeom<T, DP>::F32, DP)) 
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         float x = s[4 * a + j];
-                        if constexpr (decltype(large)::value) x = fminf(x - m[j], 0.f);
+                        if constexpr (decltype(large)::value) x = fminf(x - m[j], above);
                         s[4 * a + j] = exp2_of(__builtin_fmaf(x, p.log2_scale, -l[j]));
                     }
                 }

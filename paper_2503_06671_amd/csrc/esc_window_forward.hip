@@ -19,8 +19,6 @@
 namespace esc {
 namespace {
 
-constexpr float kSlack = 8.f;
-
 // The exponentials in the second product, with bf16 storage: two bf16 terms, which leave the result off by its own rounding alone (0.0017 of its norm;
 // with one term 0.0023, for 80 us instead of 100 at 180 x 320, windows of 32, and 252 instead of 305 in windows of 48).
 // SAVE: the backward pass follows.  Its delta = sum over the channels of out * dout stands for sum over the keys of p * dp, and what it is off goes into every

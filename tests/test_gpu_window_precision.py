@@ -53,3 +53,36 @@ def test_terms_of_the_gradients(case):
     group = c.heads // c.kv
     for name, tokens in (("grad_q", c.tokens), ("grad_k", c.tokens * group), ("grad_v", c.tokens * group)):
         assert_rounded_once(got[name], r, name, d, tokens, 2.0 ** -16, SMALL[case])
+
+
+def exact_scores(dtype, base, N, heads, seed):
+    """A case whose scores are whole numbers, `base` and some tens around it, which fp32 holds as they are: whatever the results are off is the
+    softmax's own doing.  Biases that rise for half of a tile's queries only make its running maxima move together by anything between nothing and
+    tens."""
+    c = Case(dtype, N, 16, 16, heads, 16, (16, 16), seed=seed)
+    g = torch.Generator().manual_seed(seed + 1)
+    for t in (c.q, c.k):
+        t.copy_(torch.randint(-1, 2, t.shape, generator=g).to(dtype))
+    c.bias.copy_(base + torch.randint(0, 4, c.bias.shape, generator=g))
+    for i, oy in enumerate(range(-12, 13, 4)):
+        c.bias[:, 15 + oy, 15 + 8] += 8 * i
+    c.kw["scale"] = 1.0
+    cpu = [t.cpu() for t in (c.q, c.k, c.v, c.bias)]
+    r = ref.attention(*cpu[:3], heads, c.window, bias=cpu[3], scale=1.0, grad_out=c.go.cpu())
+    assert r["score_abs"] < 2 ** 24
+    # what may round are differences of scores from the largest, the largest being exact
+    r["score_abs"] = 3.0 + 48.0 + 2 * 16.0
+    return c, r
+
+
+# beyond 2^20 the backward pass subtracts the largest score first
+BASES = [0, 2 ** 10, 2 ** 21, -2 ** 21]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("base", BASES)
+def test_gradients_of_large_scores(base, dtype):
+    c, r = exact_scores(dtype, base, 2, 2, seed=400)
+    got = c.train()
+    for name in ("grad_q", "grad_k", "grad_v", "grad_bias"):
+        ref.assert_close(got[name], r, name, dtype, c.d, c.tokens * (c.N if name == "grad_bias" else 1), base)
