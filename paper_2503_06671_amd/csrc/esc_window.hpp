@@ -24,7 +24,8 @@
 namespace esc {
 
 // Exponentials are exp2(fma(score, log2(e) scale, -shift)), shift the rounded product for the row's largest score.  What that rounding takes or
-// adds is the same for the row and falls out of the quotient - up to this size; larger ones subtract first (one operation more a score).
+// adds is the same for the row and falls out of the quotient, where what has been summed is rescaled by the rounded shifts' difference (shift_rest) - up to
+// this size; larger ones subtract first (one operation more a score).
 constexpr float kLargeShift = 0x1p20f;
 // The running maximum that scores are taken relative to is followed only where one exceeds it by more than kSlack / (log2(e) scale), so that much, or its
 // rounding to the scores' last place (twice the slack at most), a score may lie above the largest that the backward pass gets.
@@ -549,6 +550,13 @@ __device__ __forceinline__ float sum_of_halves(float v)
 {
     const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
     return __uint_as_float(s[0]) + __uint_as_float(s[1]);
+}
+
+// What rounding took from the shift of a row whose largest score is `top` (0 where scores subtract it first).
+__device__ __forceinline__ float shift_rest(float top, float log2_scale)
+{
+    const float shift = top * log2_scale;
+    return __builtin_fabsf(shift) > kLargeShift ? 0.f : __builtin_fmaf(top, log2_scale, -shift);
 }
 
 __device__ __forceinline__ float exp2_of(float v) { return __builtin_amdgcn_exp2f(v); }

@@ -19,6 +19,12 @@
 namespace esc {
 namespace {
 
+// What exponentials relative to the score `old` are times, relative to `next`.
+__device__ __forceinline__ float rescale(const WindowParams &p, float old, float next)
+{
+    return exp2_of(__builtin_fmaf(old - next, p.log2_scale, shift_rest(next, p.log2_scale) - shift_rest(old, p.log2_scale)));
+}
+
 // The exponentials in the second product, with bf16 storage: two bf16 terms, which leave the result off by its own rounding alone (0.0017 of its norm;
 // with one term 0.0023, for 80 us instead of 100 at 180 x 320, windows of 32, and 252 instead of 305 in windows of 48).
 // SAVE: the backward pass follows.  Its delta = sum over the channels of out * dout stands for sum over the keys of p * dp, and what it is off goes into every
@@ -136,7 +142,7 @@ __global__ __launch_bounds__(512) void window_forward_kernel(const WindowParams 
                     for (int u = 0; u < U; ++u) {
                         const float old = top[u], next = fmaxf(old, m[u]);
                         // (a row that has seen no key yet has nothing to shrink)
-                        const float shrink = old == -__builtin_inff() ? 0.f : exp2_of((old - next) * p.log2_scale);
+                        const float shrink = old == -__builtin_inff() ? 0.f : rescale(p, old, next);
                         top[u] = next, limit[u] = next + slack;
                         shift[u] = next == -__builtin_inff() ? 0.f : next * p.log2_scale;
                         far = far || __any(__builtin_fabsf(shift[u]) > kLargeShift);
@@ -156,9 +162,9 @@ __global__ __launch_bounds__(512) void window_forward_kernel(const WindowParams 
                     asm volatile("; large scores");
 #pragma unroll
                     for (int u = 0; u < U; ++u) {
-                        const float from = top[u] == -__builtin_inff() ? 0.f : top[u];
+                        const float from = top[u] == -__builtin_inff() ? 0.f : top[u], rest = shift_rest(from, p.log2_scale);
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) s[u][i] = (s[u][i] - from) * p.log2_scale;
+                        for (int i = 0; i < 16; ++i) s[u][i] = __builtin_fmaf(s[u][i] - from, p.log2_scale, rest);
                     }
                 }
                 Packed<VT> e[U];
@@ -196,8 +202,8 @@ __global__ __launch_bounds__(512) void window_forward_kernel(const WindowParams 
         for (int other = 1; other < p.ksplit; ++other) {
             const float *from = room + (wave + other) * WORDS + lane;
             const float mine = top[0], theirs = from[0], next = fmaxf(mine, theirs);
-            const float fm = mine == -__builtin_inff() ? 0.f : exp2_of((mine - next) * p.log2_scale);
-            const float ft = theirs == -__builtin_inff() ? 0.f : exp2_of((theirs - next) * p.log2_scale);
+            const float fm = mine == -__builtin_inff() ? 0.f : rescale(p, mine, next);
+            const float ft = theirs == -__builtin_inff() ? 0.f : rescale(p, theirs, next);
             top[0] = next;
             sum[0] = sum[0] * fm + from[64] * ft;
 #pragma unroll

@@ -55,7 +55,7 @@ def test_terms_of_the_gradients(case):
         assert_rounded_once(got[name], r, name, d, tokens, 2.0 ** -16, SMALL[case])
 
 
-def exact_scores(dtype, base, N, heads, seed):
+def exact_scores(dtype, base, N, heads, seed, grads=True):
     """A case whose scores are whole numbers, `base` and some tens around it, which fp32 holds as they are: whatever the results are off is the
     softmax's own doing.  Biases that rise for half of a tile's queries only make its running maxima move together by anything between nothing and
     tens."""
@@ -68,7 +68,7 @@ def exact_scores(dtype, base, N, heads, seed):
         c.bias[:, 15 + oy, 15 + 8] += 8 * i
     c.kw["scale"] = 1.0
     cpu = [t.cpu() for t in (c.q, c.k, c.v, c.bias)]
-    r = ref.attention(*cpu[:3], heads, c.window, bias=cpu[3], scale=1.0, grad_out=c.go.cpu())
+    r = ref.attention(*cpu[:3], heads, c.window, bias=cpu[3], scale=1.0, grad_out=c.go.cpu() if grads else None)
     assert r["score_abs"] < 2 ** 24
     # what may round are differences of scores from the largest, the largest being exact
     r["score_abs"] = 3.0 + 48.0 + 2 * 16.0
@@ -86,3 +86,16 @@ def test_gradients_of_large_scores(base, dtype):
     got = c.train()
     for name in ("grad_q", "grad_k", "grad_v", "grad_bias"):
         ref.assert_close(got[name], r, name, dtype, c.d, c.tokens * (c.N if name == "grad_bias" else 1), base)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("N,heads", [(2, 2), (70, 4), (140, 4)])   # keys shared by wavefronts, one tile a wavefront, two
+@pytest.mark.parametrize("base", BASES + [2 ** 16, 2 ** 19, -2 ** 19])
+def test_sums_keep_step_with_a_rising_maximum(base, N, heads, dtype):
+    c, r = exact_scores(dtype, base, N, heads, seed=430, grads=False)
+    for saved in (None, c.buffers()[0]):
+        out = c.forward(saved=saved)
+        if dtype == BF16:
+            assert_rounded_once(out, r, "out", c.d, c.tokens, 2.0 ** -16, base)
+        else:
+            ref.assert_close(out, r, "out", dtype, c.d, c.tokens, base)
