@@ -27,6 +27,10 @@ namespace esc {
 // adds is the same for the row and falls out of the quotient, where what has been summed is rescaled by the rounded shifts' difference (shift_rest) - up to
 // this size; larger ones subtract first (one operation more a score).
 constexpr float kLargeShift = 0x1p20f;
+// The backward pass rounds shift and logarithm of the sum to one number, which scales a row's probabilities by up to 2^-24 of that number: it subtracts
+// first where shifts are beyond this.  1e-5 of a probability, as much as the rounding of scores of that size; at 2^16 it would be 2.7e-3.  Subtracting first
+// costs 64 x 64 x 64 in bf16 40 % (1667 us, 2373 where a row of each block is beyond), so not from smaller shifts on.
+constexpr float kLargeRow = 256.f;
 // The running maximum that scores are taken relative to is followed only where one exceeds it by more than kSlack / (log2(e) scale), so that much, or its
 // rounding to the scores' last place (twice the slack at most), a score may lie above the largest that the backward pass gets.
 constexpr float kSlack = 8.f;

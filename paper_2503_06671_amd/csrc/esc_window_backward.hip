@@ -114,7 +114,8 @@ __global__ __launch_bounds__(512, window_dq_resident(WinGeom<T, DP>::F32, DP)) v
             if (there[u] && half == 0) p.delta[row + pixel[u]] = delta[u];
             if (!ok[u]) top[u] = 0.f, log_sum[u] = __builtin_inff();
             shift[u] = top[u] * p.log2_scale + log_sum[u];
-            far = far || __any(__builtin_fabsf(top[u] * p.log2_scale) > kLargeShift);
+            log_sum[u] -= shift_rest(top[u], p.log2_scale);  // (for scores that have top subtracted)
+            far = far || __any(__builtin_fabsf(top[u] * p.log2_scale) > kLargeRow);
             all = all && __all(ok[u]);
 #pragma unroll
             for (int b = 0; b < G::DT; ++b) acc[u][b] = wf32x16{};
@@ -280,8 +281,9 @@ __global__ __launch_bounds__(512, window_dkv_resident(WinGeom<T, DP>::F32, DP)) 
             // (masked pixels have a sum of +infinity and a delta of 0; those beyond the window get them here)
             float *rows = reinterpret_cast<float *>(buf + ROWS_AT) + r;
             const float shift = in ? from * p.log2_scale : 0.f, l = in ? log_sum : __builtin_inff();
-            large = large || __builtin_fabsf(shift) > kLargeShift;
-            rows[0] = shift + l, rows[G::TK] = in ? -delta : 0.f, rows[2 * G::TK] = from, rows[3 * G::TK] = l;
+            large = large || __builtin_fabsf(shift) > kLargeRow;
+            rows[0] = shift + l, rows[G::TK] = in ? -delta : 0.f, rows[2 * G::TK] = from;
+            rows[3 * G::TK] = in ? l - shift_rest(from, p.log2_scale) : l;
         }
         int *flags = reinterpret_cast<int *>(buf + FAR_AT);
         const bool any = __any(large);
