@@ -470,35 +470,38 @@ __device__ __forceinline__ void bucket_range(const WindowParams &p, int b, int f
     *hi = min(*hi, n - 1);
 }
 
-// The sums of each bucket's offsets: a wavefront for each where every offset has its own, a block where buckets hold many.
+// The sums of each bucket's offsets: a wavefront for each where every offset has its own, a block where buckets hold many.  (A table may have far more
+// buckets than the map has offsets: up to kBucketBlocks blocks a head go through them.)
+constexpr int kBucketBlocks = 1 << 16;
 __global__ __launch_bounds__(256) void window_buckets_kernel(const WindowParams p)
 {
     __shared__ float part[4];
-    const int wave = threadIdx.x >> 6, head = blockIdx.y, lane = threadIdx.x & 63;
+    const int wave = threadIdx.x >> 6, head = blockIdx.y, lane = threadIdx.x & 63, buckets = p.nby * p.nbx;
     const bool whole = p.n_edges > 0;
-    const int b = whole ? blockIdx.x : blockIdx.x * 4 + wave, threads = whole ? 256 : 64;
-    float sum = 0.f;
-    if (b < p.nby * p.nbx) {
+    const int threads = whole ? 256 : 64, step = whole ? gridDim.x : gridDim.x * 4;
+    for (int b = whole ? blockIdx.x : blockIdx.x * 4 + wave; b < buckets; b += step) {
         int y0, y1, x0, x1;
         bucket_range(p, b / p.nbx, p.win_h, p.wh, &y0, &y1);
         bucket_range(p, b % p.nbx, p.win_w, p.ww, &x0, &x1);
         const int cols = x1 - x0 + 1, count = y1 >= y0 && cols > 0 ? (y1 - y0 + 1) * cols * p.splits : 0;
+        float sum = 0.f;
 #pragma unroll 4
         for (int i = whole ? threadIdx.x : lane; i < count; i += threads) {
             const int split = i % p.splits, o = i / p.splits, y = y0 + o / cols, x = x0 + o % cols;
             sum += p.part2[((long)split * p.heads + head) * p.th * p.tw + (y + p.wh - 1) * p.tw + x + p.ww - 1];
         }
-    }
 #pragma unroll
-    for (int m = 32; m >= 1; m >>= 1) sum += __shfl_xor(sum, m);
-    if (whole) {
-        if (lane == 0) part[wave] = sum;
-        __syncthreads();
-        sum = part[0] + part[1] + part[2] + part[3];
-    }
-    if ((whole ? threadIdx.x == 0 : lane == 0) && b < p.nby * p.nbx) {
-        float *to = p.grad_bias + (long)head * p.nby * p.nbx + b;
-        *to = p.accumulate != 0 ? *to + sum : sum;
+        for (int m = 32; m >= 1; m >>= 1) sum += __shfl_xor(sum, m);
+        if (whole) {  // (b is the block's then: all of it comes here)
+            if (lane == 0) part[wave] = sum;
+            __syncthreads();
+            sum = part[0] + part[1] + part[2] + part[3];
+            __syncthreads();
+        }
+        if (whole ? threadIdx.x == 0 : lane == 0) {
+            float *to = p.grad_bias + (long)head * buckets + b;
+            *to = p.accumulate != 0 ? *to + sum : sum;
+        }
     }
 }
 
@@ -568,7 +571,8 @@ hipError_t launch_window_bias_grad(const WindowParams &p, hipStream_t s)
     hipLaunchKernelGGL(window_offsets_kernel, dim3((unsigned)((p.th * p.tw + 1023) / 1024), (unsigned)p.heads, (unsigned)p.splits), dim3(256), 0, s, p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(window_buckets_kernel, dim3((unsigned)(p.n_edges > 0 ? p.nby * p.nbx : (p.nby * p.nbx + 3) / 4), (unsigned)p.heads), dim3(256), 0, s, p);
+    const int buckets = p.nby * p.nbx, blocks = p.n_edges > 0 ? buckets : (buckets + 3) / 4;
+    hipLaunchKernelGGL(window_buckets_kernel, dim3((unsigned)(blocks < kBucketBlocks ? blocks : kBucketBlocks), (unsigned)p.heads), dim3(256), 0, s, p);
     return hipGetLastError();
 }
 
