@@ -489,5 +489,6 @@ class AdamW:
 
     @property
     def steps(self) -> int:
-        """Steps the states have seen (waits for the device)."""
+        """Steps the states have seen (waits for the device: for steps on any of its streams)."""
+        torch.cuda.synchronize(self.device)
         return int(self.memory[:8].view(torch.int64).item())

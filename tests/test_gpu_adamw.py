@@ -186,3 +186,21 @@ def test_short_tensors_step_after_step():
         net.reference_step(**h)
     net.check()
     assert net.opt.steps == 24
+
+
+@pytest.mark.parametrize("replayed", [False, True])
+def test_steps_waits_for_every_stream(replayed):
+    net = Net("f32", seed=10)
+    net.opt.step(1e-3)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        net.opt.step(1e-3)
+    x = torch.randn(4096, 4096, device="cuda")
+    x @ x
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        for _ in range(20):  # (some milliseconds of work in front of the step)
+            x @ x
+        graph.replay() if replayed else net.opt.step(1e-3)
+    assert net.opt.steps == 6
