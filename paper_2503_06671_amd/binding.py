@@ -414,8 +414,8 @@ class AdamW:
     params: contiguous float32 device tensors; grads: their gradients, all float32 or all bfloat16, contiguous, filled anew by the
     caller before each step.  states "f32": m and v are float32; "8bit": torch.float8_e4m3fn codes with a float32 scale for each
     ADAMW_BLOCK elements (m_scale, v_scale; v's codes hold sqrt(v)).  States that are not given start as zeros.  weight_decay is one
-    number or one a tensor, `step` how many steps the states have seen.  The object keeps all tensors alive and works on
-    their memory: they have to stay where they are."""
+    number or one a tensor, `step` how many steps the states have seen.  New states and the plan are laid out on `stream` (None: the current
+    one), and steps are to be ordered behind that.  The object keeps all tensors alive and works on their memory: they have to stay where they are."""
 
     def __init__(self, params, grads, states: str = "f32", weight_decay=0.0, step: int = 0, m=None, v=None, m_scale=None,
                  v_scale=None, stream=None):
@@ -442,10 +442,15 @@ class AdamW:
                     raise ValueError(f"a tensor of {name} has {t.numel()} elements, {n} are needed")
             return tensors
 
+        # (zeros and the plan on one stream: the first step, ordered behind the plan, is behind the zeros too)
+        if stream is not None and not isinstance(stream, torch.cuda.Stream):
+            stream = torch.cuda.ExternalStream(stream.cuda_stream, device=device)
+
         def state(name, given, dtype, sizes):
             if given is None:
-                return [torch.zeros(n, dtype=torch.uint8, device=device).view(dtype) if eight and dtype is state_type
-                        else torch.zeros(n, dtype=dtype, device=device) for n in sizes]
+                with torch.cuda.stream(stream):
+                    return [torch.zeros(n, dtype=torch.uint8, device=device).view(dtype) if eight and dtype is state_type
+                            else torch.zeros(n, dtype=dtype, device=device) for n in sizes]
             return checked(name, given, dtype, sizes)
 
         counts = [p.numel() for p in params]
@@ -470,7 +475,8 @@ class AdamW:
         if nbytes == 0:
             raise ValueError("bad sizes for the optimiser")
         self.device = device
-        self.memory = torch.empty(nbytes, dtype=torch.uint8, device=device)
+        with torch.cuda.stream(stream):
+            self.memory = torch.empty(nbytes, dtype=torch.uint8, device=device)
         self.plan = _AdamwPlan()
         with torch.cuda.device(device):
             _check(lib.esc_adamw_plan_init(tensors, len(params), ADAMW_STATES[states],

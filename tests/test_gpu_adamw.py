@@ -204,3 +204,24 @@ def test_steps_waits_for_every_stream(replayed):
             x @ x
         graph.replay() if replayed else net.opt.step(1e-3)
     assert net.opt.steps == 6
+
+
+@pytest.mark.parametrize("states", ["f32", "8bit"])
+def test_laid_out_on_a_side_stream(states):
+    # the states' zeros and the plan come in front of a step on the same stream, whatever the current one is busy with
+    p, g = torch.randn(70001, device="cuda"), torch.randn(70001, device="cuda")
+    same = p.clone()
+    want = binding.AdamW([same], [g], states=states)
+    want.step(1e-2)
+    x = torch.randn(4096, 4096, device="cuda")
+    x @ x
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(20):
+        x @ x
+    opt = binding.AdamW([p], [g], states=states, stream=side)
+    opt.step(1e-2, stream=side)
+    assert opt.steps == 1
+    assert torch.equal(p, same)
+    for a, b in ((opt.m[0], want.m[0]), (opt.v[0], want.v[0])):
+        assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
