@@ -700,7 +700,7 @@ PyObject *window_attention_backward(PyObject *const *a, Py_ssize_t n)
     const Ws saved = workspace(a[5]), ws = workspace(a[8]);
     same_device(tensor(a[5], "saved"), q, "saved");
     same_device(tensor(a[8], "workspace"), q, "workspace");
-    const int acc = PyObject_IsTrue(a[14]);
+    int acc = PyObject_IsTrue(a[14]);
     if (acc < 0) throw PyError{};
     const c10::DeviceGuard guard(q.device());
     struct Dict {
@@ -742,7 +742,9 @@ PyObject *window_attention_backward(PyObject *const *a, Py_ssize_t n)
             same_device(t, q, "grad_bias");
             g.bias = static_cast<float *>(t.data_ptr());
         } else {
-            const at::Tensor t = acc != 0 ? at::zeros(at.bias->sizes(), at.bias->options()) : at::empty(at.bias->sizes(), at.bias->options());
+            // (nothing to add to: the call's own stream writes it, rather than add to another stream's zeros)
+            const at::Tensor t = at::empty(at.bias->sizes(), at.bias->options());
+            acc = 0;
             put("grad_bias", t);
             g.bias = static_cast<float *>(t.data_ptr());
         }

@@ -267,3 +267,21 @@ def test_stream_and_replayed_graph():
         torch.cuda.synchronize()
         for n in NAMES:
             assert torch.equal(room[n], eager[n]), (seed, n)
+
+
+def test_accumulate_without_a_buffer_on_a_side_stream():
+    c = Case(F32, 2, 24, 20, 2, 16, (8, 8), seed=17)
+    want = c.train()
+    saved, ws = c.buffers()
+    out = c.forward(saved=saved)
+    x = torch.randn(4096, 4096, device="cuda")
+    x @ x
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(20):  # (the current stream is busy meanwhile)
+        x @ x
+    got = binding.window_attention_backward(c.q, c.k, c.v, out, c.go, saved, c.heads, c.window, ws, **c.kw, accumulate=True, stream=side)
+    side.synchronize()
+    torch.cuda.synchronize()
+    for n in NAMES[1:]:
+        assert torch.equal(got[n], want[n]), n
