@@ -30,3 +30,17 @@ def test_windows_far_larger_than_the_map(window):
     assert (rest == 0).all()
     again = c.train(accumulate=True, grads={"grad_bias": got["grad_bias"]})["grad_bias"]
     assert torch.equal(again[middle], 2 * want["grad_bias"])
+
+
+def test_gradients_of_images_more_than_32_bits_apart():
+    c = Case(BF16, 2, 16, 16, 1, 16, (16, 16), seed=510)
+    want = c.train()
+    step, image = 2 ** 31 + 24, 16 * 256
+    room = torch.full((step + 3 * image,), 3.0, device="cuda", dtype=BF16)
+    grads = {n: room.as_strided((2, 16, 16, 16), (step, 256, 16, 1), i * image) for i, n in enumerate(NAMES[1:4])}
+    got = c.train(grads=grads)
+    for n in NAMES[1:]:
+        assert torch.equal(got[n], want[n]), n
+        assert n == "grad_bias" or got[n] is grads[n]
+    between = room[3 * image:step]
+    assert between.amin() == 3 and between.amax() == 3
