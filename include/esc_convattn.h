@@ -417,7 +417,7 @@ typedef struct esc_adamw_plan {
 typedef struct esc_adamw_hyper {
     double lr, beta1, beta2, eps; /* 0 <= lr, eps < 1e30; 0 <= beta < 1          */
     double grad_scale;            /* finite; 1 for gradients as they are         */
-    const float *lr_device;       /* device pointer; where not NULL its value is lr: a captured graph's steps can follow a schedule */
+    const float *lr_device;       /* device pointer; where not NULL its value is lr: a captured graph's steps can follow a schedule; not part of what a step writes */
 } esc_adamw_hyper;
 
 /* Device memory a plan takes (256-byte aligned).  0 on bad arguments.  `tensors` is HOST memory. */
@@ -427,7 +427,8 @@ size_t esc_adamw_plan_bytes(const esc_adamw_tensor *tensors, int n, esc_adamw_st
  * Lays the plan out: writes the tensors' addresses and sizes into `memory` (a launch for each 32 tensors, on `stream`) and fills *plan
  * (host).  `step` is how many steps the states have seen (0 for new ones, which are zeros); the count is kept in `memory` and
  * grows by one with each esc_adamw_step, replayed ones included.  What a step writes may not overlap anything else that the plan names
- * (ESC_ERR_ALIAS): a tensor appears once.  The tensors' memory has to stay where it is as long as the plan is used.
+ * (ESC_ERR_ALIAS): a tensor appears once.  The tensors' memory has to stay where it is as long as the plan is used, that
+ * of the gradients too: a step reads the addresses laid out here.  Gradients that are new tensors in each step need a new plan, or are copied to the plan's.
  */
 esc_status esc_adamw_plan_init(const esc_adamw_tensor *tensors, int n, esc_adamw_state state, esc_dtype grad_dt, long step, void *memory,
                                size_t bytes, esc_adamw_plan *plan, void *stream);

@@ -415,7 +415,10 @@ class AdamW:
     caller before each step.  states "f32": m and v are float32; "8bit": torch.float8_e4m3fn codes with a float32 scale for each
     ADAMW_BLOCK elements (m_scale, v_scale; v's codes hold sqrt(v)).  States that are not given start as zeros.  weight_decay is one
     number or one a tensor, `step` how many steps the states have seen.  New states and the plan are laid out on `stream` (None: the current
-    one), and steps are to be ordered behind that.  The object keeps all tensors alive and works on their memory: they have to stay where they are."""
+    one), and steps are to be ordered behind that.  The object keeps all tensors alive and works on their memory: they have to stay where they are.
+    A step reads these gradient tensors and no others: clear them with zero_(), since a loop that sets a parameter's .grad to None
+    (torch's zero_grad does) gets new tensors that the object knows nothing of.  Making one costs tens of steps (a launch for each 32 tensors, checks of
+    every tensor), so it is made once."""
 
     def __init__(self, params, grads, states: str = "f32", weight_decay=0.0, step: int = 0, m=None, v=None, m_scale=None,
                  v_scale=None, stream=None):

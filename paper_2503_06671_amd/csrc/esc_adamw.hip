@@ -13,8 +13,9 @@
 // step would divide what is left of m by eps.
 //
 // What bounds it: memory.  28 bytes an element with fp32 states and gradients (p, g, m, v in; p, m, v out), 16 and a sixteenth with
-// 8-bit states, 14 and a sixteenth with bf16 gradients.  Measured, one MI355X: 8-bit states, bf16 gradients, 170 million elements: 497 us, 4.8 TB/s (a copy of 1 GiB:
-// 5.1); a network of 0.8 million elements, fp32: 9.1 us.
+// 8-bit states, 14 and a sixteenth with bf16 gradients.  Measured, one MI355X, 169 million elements: 8-bit states, bf16 gradients 498 us, 4.8 TB/s (a copy of 1 GiB:
+// 5.1); fp32 states, fp32 gradients 1004 us, bf16 gradients 939, 4.7 TB/s both.  A network of 0.8 million elements, fp32 states: 9.0 us with fp32 gradients,
+// 10.3 with bf16.
 // Layout: the plan (device memory) holds one record per tensor and the tensor's number for every chunk of kChunk elements, so
 // that a block finds its work in two dependent loads whatever the number of tensors, and small tensors cost a block each, not
 // a launch.  A wavefront takes 256 consecutive elements at a time, four a lane (16-byte accesses; one block of

@@ -77,10 +77,10 @@ bool choose_waves(WindowParams &p, int heads, bool f32, int dp, int simd, F lds)
 }
 
 // All blocks, and how they go to the eight dies: in runs, so that what lies together meets in one L2 (heads that share keys; windows beside each
-// other, whose rows share cache lines), and in many runs, so that no die gets all the windows that the map's edge cuts short (2 x 29 x 579, windows of
-// 21 x 13, gradients: 568 us, with one run a die 806).  Where there are few blocks, of few wavefronts, up to four help staging (6 heads of 48
-// channels that share one key, 8 sequences of 969 in windows of 600, bf16, gradients: 386 us, without 742; with many blocks they only take
-// room: 3 x 339 x 511, windows of 13: 351, without 307).
+// other, whose rows share cache lines), and in many runs, so that no die gets all the windows that the map's edge cuts short (2 x 29 x 579, 3 heads of 33,
+// windows of 21 x 13, gradients: 320 us, with one run a die 454).  Where there are few blocks, of few wavefronts, up to four help staging (6 heads of 48
+// channels that share one key, 8 sequences of 969 in windows of 600, bf16, gradients: 390 us, without 720; with many blocks they only take
+// room: 3 x 339 x 511, windows of 13: 833, without 349).
 bool set_units(WindowParams &p, int heads)
 {
     const __int128 all = (__int128)p.N * p.gy * p.gx * heads * p.blocks;
@@ -119,13 +119,14 @@ esc_status shape(const esc_window_attn *a, WindowParams *p)
 size_t table_bytes(const WindowParams &p) { return (size_t)p.heads * p.nby * p.nbx * 4; }
 
 // The forward's wavefronts.  A wavefront with two tiles of queries reads keys and values half as often, with one it takes so few registers that
-// four of a SIMD hide each other's waits.  Two: fp32 storage, whose three terms make the reads dear (180 x 320, windows of 32: 151 us, with one
-// 175), and bf16 storage in windows of fewer than 16 tiles, where a block's beginning weighs (3 x 339 x 511, windows of 13: 314 us, with one 499; windows of
-// 48: 275, with one 246) - where a window has more than four tiles (4 x 171 x 171, windows of 9 x 9, fp32: 84 us, with one 71; 9 x 123 x 110, windows of
-// 13 x 7, bf16: 218, with one 208) and the call leaves two wavefronts a SIMD.  Where even those are fewer than one a SIMD, up to four wavefronts, and
-// no more than a chunk has tiles, share a tile's keys (64 x 64, 4 heads, windows of 32: heads of 16 in bf16 18.3 us with four, 23.8 with two, 30 without;
-// in fp32 30 us with two, 40 without), and others help staging as long as there are pieces for them and all blocks are on the chip at once (heads of 64,
-// bf16: 33 us, without 47).  Blocks are as large as leaves one for each compute unit: they stage a window's keys and values once for all their queries.
+// four of a SIMD hide each other's waits.  Two: fp32 storage, whose three terms make the reads dear (180 x 320, windows of 32: 174 us, with one
+// 195), and bf16 storage in windows of fewer than 16 tiles, where a block's beginning weighs (3 x 339 x 511, windows of 13: 349 us, with one 550; windows of
+// 48: 345, with one 308) - where a window has more than four tiles (4 x 171 x 171, windows of 9 x 9, fp32: 96 us, with one 81; 9 x 123 x 110, 8 heads, windows
+// of 13 x 7, bf16: heads of 32 217, with one 185, heads of 16 128, with one 138) and the call leaves two wavefronts a SIMD.  Where even those are fewer than
+// one a SIMD, up to four wavefronts, and no more than a chunk has tiles, share a tile's keys (64 x 64, 4 heads, windows of 32: heads of 16 in bf16 18.3 us
+// with four, 23.8 with two, 30 without; in fp32 30 us with two, 40 without), and others help staging as long as there are pieces for them and all blocks
+// are on the chip at once (heads of 64, bf16: 33 us, without 47).  Blocks are as large as leaves one for each compute unit: they stage a window's keys
+// and values once for all their queries.
 bool plan_forward(WindowParams &p, bool f32)
 {
     const int dp = dim_padded(p.d);

@@ -12,7 +12,7 @@
 // Matrix instructions: v_mfma_f32_32x32x16_bf16.  bf16 storage as it is; fp32 values as three bf16 terms by truncation (exact),
 // the six products of terms whose orders add up to two at most (what is left out: below 2^-21 of a product, 2^-24 on average).
 // Where a branch lies between such an instruction and the first use of its result, the compiler has been seen to leave out the wait that
-// the use needs: the kernels have none there.
+// the use needs.  The kernels keep branches away from there but for tiles that are not whole; tests/test_window_waits.py looks for such a use in the built code.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -124,8 +124,8 @@ struct WinGeom {
     static constexpr int CM_BYTES = NT * CM_TERM;
 };
 
-// A window's row in tokens: whole pairs, which share the address of a bias (pairs, not fours: windows of 13 x 13 are 6 tiles and not 7, 307 us and not 391 for
-// 3 x 339 x 511 bf16; the additions cost windows of 32 and 48 2 %).
+// A window's row in tokens: whole pairs, which share the address of a bias (pairs, not fours: windows of 13 x 13 are 6 tiles and not 7; when
+// it was tried, 307 us and not 391 for 3 x 339 x 511 bf16, and the additions cost windows of 32 and 48 2 %).
 __host__ __device__ __forceinline__ int in_pairs(int width) { return (width + 1) & ~1; }
 
 struct Win {

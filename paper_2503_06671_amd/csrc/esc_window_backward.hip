@@ -14,8 +14,10 @@
 // the offsets of each bucket.
 //
 // What bounds it: window_dq_kernel the vector instructions and the LDS (half of its time the 32 additions in 64 bits a tile), window_dkv_kernel the
-// vector instructions and what its few wavefronts (168 to 256 registers) cannot hide.  Measured, 64 maps of 64 x 64, 4 heads of 16,
-// windows of 32, bf16: dq 629 us, dk and dv 640 us, the offsets' sums 76 us, the buckets 9 us, beside the forward's 440 us.
+// vector instructions (80 % of the slots with 2.8 wavefronts a SIMD), and with fp32 storage what its few wavefronts (one block a compute unit)
+// cannot hide.  Kernels by themselves under the profiler, 64 maps of 64 x 64, 4 heads of 16, windows of 32, bf16: dq 639 us, dk and dv 666 us, the offsets' sums
+// 77 us, the buckets 9 us, beside the forward's 443 us; calls of both passes in a row take 1669 us.  Registers are short: all kernels with bf16
+// storage spill, with fp32 storage those for heads wider than 32, dk and dv's wider than 16 (8 to 232 bytes a lane).
 #include "esc_window.hpp"
 
 namespace esc {

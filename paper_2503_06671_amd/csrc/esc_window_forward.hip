@@ -11,9 +11,10 @@
 // tile's keys; their sums are joined in LDS at the end.
 //
 // What bounds it: the issue of vector instructions (16 exponentials and as many multiplications, maxima, sums and conversions for a lane of a tile of
-// 32 x 32 pairs, beside two to four products in bf16); a products' share of the matrix units' time is 10 to 20 % with bf16 storage, 40 %
-// with fp32.  Measured, one MI355X: 180 x 320, 4 heads of 16, windows of 32 x 32: bf16 71 us, fp32 150 us; 6 heads of 32, windows of 48, bf16: 245 us;
-// 3 x 339 x 511, 6 heads of 8 that share 2 keys, windows of 13, bf16: 314 us; a map of 64 x 64 alone, fp32: 30 us.
+// 32 x 32 pairs, beside three to six products in bf16) where there are wavefronts enough: 87 % of the slots for 64 maps of 64 x 64, 78 % in windows of 13; the
+// products' share of the matrix units' time is 12 to 24 % with bf16 storage, 32 % with fp32.  At 180 x 320 the two rounds of blocks, the second of them
+// short, leave 60 % (bf16) and 49 % (fp32) of the slots used.  Measured, one MI355X: 180 x 320, 4 heads of 16, windows of 32 x 32: bf16 88 us, fp32 151 us;
+// 6 heads of 32, windows of 48, bf16: 298 us; 3 x 339 x 511, 6 heads of 8 that share 2 keys, windows of 13, bf16: 350 us; a map of 64 x 64 alone, fp32: 29 us.
 #include "esc_window.hpp"
 
 namespace esc {
@@ -26,7 +27,7 @@ __device__ __forceinline__ float rescale(const WindowParams &p, float old, float
 }
 
 // The exponentials in the second product, with bf16 storage: two bf16 terms, which leave the result off by its own rounding alone (0.0017 of its norm;
-// with one term 0.0023, for 80 us instead of 100 at 180 x 320, windows of 32, and 252 instead of 305 in windows of 48).
+// with one term 0.0023, for 71 us instead of 88 at 180 x 320, windows of 32, and 245 instead of 298 in windows of 48).
 // SAVE: the backward pass follows.  Its delta = sum over the channels of out * dout stands for sum over the keys of p * dp, and what it is off goes into every
 // term of the bias' gradient, an fp32 result: with bf16 storage the exponentials are then three bf16 terms, and what rounding took from
 // the result is kept (off by, of the bias' gradient's norm, for windows of 2 to 60 tokens: 1e-4 with one term, 0.5e-6 to 3.6e-6 with two, 0.1e-6
