@@ -99,3 +99,23 @@ def test_sums_keep_step_with_a_rising_maximum(base, N, heads, dtype):
             assert_rounded_once(out, r, "out", c.d, c.tokens, 2.0 ** -16, base)
         else:
             ref.assert_close(out, r, "out", dtype, c.d, c.tokens, base)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("N,heads", [(2, 2), (70, 4)])
+def test_rows_of_very_different_scores_beside_each_other(N, heads, dtype):
+    # rows whose scores reach 2^4 to 2^21, in turn within each tile: each way of working out exponentials in each tile
+    c, _ = exact_scores(dtype, 0, N, heads, seed=460, grads=False)
+    factor = 2.0 ** torch.tensor([0, 5, 12, 17, 0, 3, 9])[torch.arange(256) % 7].reshape(16, 16)
+    c.q.mul_(factor.to("cuda", dtype))
+    cpu = [t.cpu() for t in (c.q, c.k, c.v, c.bias)]
+    r = ref.attention(*cpu[:3], heads, c.window, bias=cpu[3], scale=1.0, grad_out=c.go.cpu())
+    assert 2 ** 20 < r["score_abs"] < 2 ** 24
+    r["score_abs"] = 3.0 + 48.0 + 2 * 16.0  # (scores farther than that below the largest weigh nothing)
+    got = c.train()
+    for name in ("grad_q", "grad_k", "grad_v", "grad_bias"):
+        ref.assert_close(got[name], r, name, dtype, c.d, c.tokens * (N if name == "grad_bias" else 1), N)
+    if dtype == BF16:
+        assert_rounded_once(got["out"], r, "out", c.d, c.tokens, 2.0 ** -16, N)
+    else:
+        ref.assert_close(got["out"], r, "out", dtype, c.d, c.tokens, N)
