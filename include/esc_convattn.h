@@ -52,9 +52,9 @@
  *     expire, the values that never came are taken as NaN - the affected outputs
  *     are NaN, never silently wrong numbers - and the workspace's error word is
  *     raised; esc_workspace_errors reads it.
- *   - Window attention and the AdamW step wait for no other block and take no prepared
- *     workspace: on different streams, each with its own outputs and scratch, they may run
- *     at once.
+ *   - Window attention, the AdamW step, layer norm, the point-wise product and dropout
+ *     wait for no other block and take no prepared workspace: on different streams, each
+ *     with its own outputs and scratch, they may run at once.
  *   - Limits: 0 <= C_a <= min(C, 256); estimator hidden width <= 256; Ks odd,
  *     1 <= Ks <= 31; H*W < 2^31; N, C, H, W >= 1.  No lower bound on H or W
  *     relative to Ks.
@@ -371,6 +371,128 @@ size_t esc_window_attention_backward_workspace_bytes(const esc_window_attn *a); 
 esc_status esc_window_attention_backward(const void *q, const void *k, const void *v, esc_dtype dt, const esc_window_attn *a, const void *out,
                                          const void *grad_out, const void *saved, size_t saved_bytes, const esc_window_grads *g,
                                          int accumulate, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Layer norm over the channels of each pixel (in front of the attention and the feed-forward networks of a block, Eq. 3), over the
+ * pixels of [N, C, H, W]:
+ *
+ *   mean = sum_c x[c] / C     r = 1 / sqrt( sum_c (x[c] - mean)^2 / C + eps )     out[c] = weight[c] (x[c] - mean) r + bias[c]
+ *
+ *   x, out       storage type, contiguous images, *_stride ELEMENTS from image to image (ignored where N is 1)
+ *   weight, bias device, fp32 [C], or NULL (ones, zeros)
+ *   saved        mean and r of each pixel for the backward pass (fp32; esc_layernorm_saved_bytes, 256-byte aligned), or NULL
+ * Means and sums are fp32, of differences from the mean (not of squares of x); out is rounded once.  A value that is not finite makes NaN of
+ * its own pixel's outputs and of no other's.  Limits: C <= 65536, H W < 2^31, N H W < 2^40, 0 < eps < infinity.  One launch; no workspace.
+ */
+typedef struct esc_layernorm {
+    int N, C, H, W;
+    float eps;
+    const float *weight, *bias;
+    long x_stride, out_stride; /* in the backward pass out_stride is grad_out's      */
+    long skip_stride;          /* the backward pass: grad_skip's                     */
+} esc_layernorm;
+
+size_t esc_layernorm_saved_bytes(const esc_layernorm *a); /* pointers, strides and eps in *a are ignored; 0 on bad sizes */
+esc_status esc_layernorm_forward(const void *x, esc_dtype dt, const esc_layernorm *a, void *out, void *saved, size_t saved_bytes, void *stream);
+
+/*
+ * Backward of esc_layernorm_forward, of its x and its saved, given grad_out (shaped like out): with u = (x - mean) r and
+ * a[c] = weight[c] grad_out[c], for each pixel
+ *
+ *   g->x[c]      = r (a[c] - sum a / C - u[c] sum(a u) / C) + grad_skip[c]     storage type, shaped like x, a stride of its own
+ *   g->weight[c] = sum over pixels of grad_out[c] u[c]     g->bias[c] = sum over pixels of grad_out[c]     fp32; accumulate != 0 adds to the buffers
+ *
+ * grad_skip (storage type, or NULL) is the gradient that reaches x around the norm, as in x + f(norm(x)).  Any of the three results may be NULL, not
+ * all.  Sums over pixels are fp32 in a fixed order: equal calls give equal bits.  The workspace
+ * (esc_layernorm_backward_workspace_bytes, 256-byte aligned) is plain scratch; what is written may not overlap anything else.
+ */
+typedef struct esc_layernorm_grads {
+    void *x;
+    long x_stride;
+    float *weight, *bias;
+} esc_layernorm_grads;
+size_t esc_layernorm_backward_workspace_bytes(const esc_layernorm *a); /* as above */
+esc_status esc_layernorm_backward(const void *x, const void *grad_out, const void *grad_skip, esc_dtype dt, const esc_layernorm *a, const void *saved,
+                                  size_t saved_bytes, const esc_layernorm_grads *g, int accumulate, void *workspace, size_t workspace_bytes,
+                                  void *stream);
+
+/*
+ * Point-wise product (1x1 convolution) of any width with bias, activation and residual in its epilogue, as the projections in front of
+ * window attention and behind it and the layers of a feed-forward network are.  For each pixel
+ *
+ *   out[m] = act( b[m] + sum_k w[m, k] x[k] ) + residual[m]        m < M, k < K
+ *
+ *   x            [N, K, H, W], residual and out [N, M, H, W]: storage type, contiguous images, *_stride ELEMENTS from image to image
+ *                (ignored where N is 1); residual may be NULL
+ *   w, b         device, fp32 [M, K] row by row, and [M] or NULL (zeros)
+ *   act          none; gelu: v Phi(v), the exact (erf) form; silu: v / (1 + exp(-v))
+ * Accumulation is fp32, out is rounded once.  fp32 storage: values and weights as three bf16 terms each (exact down to 2^-110), six products of
+ * terms on the matrix cores (what is left out lies below 2^-21 of a product).  bf16 storage: the stored values, weights as two bf16 terms (2^-16 left out at
+ * most).  A value or weight that is not finite makes what its products reach not finite (NaN also where the definition has an infinity), and
+ * nothing else.  Limits: K, M <= 65536, H W < 2^31, N H W < 2^40; ESC_ERR_UNSUPPORTED beyond.  One launch; no workspace.
+ */
+typedef enum { ESC_ACT_NONE = 0, ESC_ACT_GELU = 1, ESC_ACT_SILU = 2, ESC_ACT_INT_RANGE = 0x7fffffff } esc_activation;
+
+typedef struct esc_pointwise {
+    int N, K, M, H, W;
+    esc_activation act;
+    const float *w, *b;
+    long x_stride, out_stride, residual_stride; /* in the backward pass out_stride is grad_out's, residual_stride is ignored */
+} esc_pointwise;
+
+esc_status esc_pointwise_forward(const void *x, const void *residual, esc_dtype dt, const esc_pointwise *a, void *out, void *stream);
+
+/*
+ * Backward of esc_pointwise_forward, given grad_out (shaped like out): with pre = b + w x and gp = grad_out act'(pre)
+ *
+ *   g->x[k]    = sum_m w[m, k] gp[m]               storage type, shaped like x, a stride of its own
+ *   g->w[m, k] = sum over pixels of gp[m] x[k]     g->b[m] = sum over pixels of gp[m]      fp32; accumulate != 0 adds to the buffers
+ *
+ * (the residual's gradient is grad_out itself).  pre is formed again, nothing is kept from the forward pass.  Any of the three results may be NULL,
+ * not all; g->b does not need b.  With bf16 storage gp is held unrounded (fp32), as operands two bf16 terms for g->x and three (exact) for g->w, an
+ * fp32 result.  Sums are fp32 in a fixed order: equal calls give equal bits.  The workspace (esc_pointwise_backward_workspace_bytes, 256-byte
+ * aligned) is plain scratch; what is written may not overlap anything else.
+ */
+typedef struct esc_pointwise_grads {
+    void *x;
+    long x_stride;
+    float *w, *b;
+} esc_pointwise_grads;
+size_t esc_pointwise_backward_workspace_bytes(const esc_pointwise *a, esc_dtype dt); /* pointers and strides in *a are ignored; 0 on bad sizes */
+esc_status esc_pointwise_backward(const void *x, const void *grad_out, esc_dtype dt, const esc_pointwise *a, const esc_pointwise_grads *g, int accumulate,
+                                  void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Dropout from a counter-based generator, with the residual added in the same pass; the mask is a function of (seed, offset) and stored nowhere:
+ *
+ *   out[i] = residual[i] + ( draw(unit(i)) >= q ? x[i] * 65536 / (65536 - q) : 0 )          q = floor(65536 p + 1/2)
+ *
+ * unit(i) is the element's place in a contiguous [N, C, H, W] (ESC_DROPOUT_ELEMENT), its plane n C + c (ESC_DROPOUT_PLANE: whole channels) or its image n
+ * (ESC_DROPOUT_IMAGE: stochastic depth); it does not depend on strides.  draw(u) is 16 bits of Philox4x32 with ten rounds (Salmon, Moraes,
+ * Dror, Shaw: Parallel random numbers: as easy as 1, 2, 3): key (seed's low word, high word), counter (low and high word of u / 8, low and high
+ * word of the offset); of the four words, word (u % 8) / 2, its low half where u is even.  The probability is thus p rounded to a multiple of 2^-16, and
+ * the scale goes by the rounded one.  A dropped value counts as 0 whatever it is (NaN too).  The offset is a->offset plus, where it is not NULL, the
+ * number at a->offset_device, read on the device: a captured step draws anew in each replay when the graph also counts that up.  Calls that shall
+ * draw independently need different offsets (or seeds).
+ *   x, residual, out   [N, C, H, W], storage type, contiguous images, *_stride ELEMENTS from image to image (ignored where N is 1); residual
+ *                      may be NULL; out overlaps neither
+ * One fp32 multiplication, one addition, one rounding.  0 <= p < 1 - 2^-17; H W < 2^31, N C H W < 2^48.  One launch; no workspace.
+ */
+typedef enum { ESC_DROPOUT_ELEMENT = 0, ESC_DROPOUT_PLANE = 1, ESC_DROPOUT_IMAGE = 2, ESC_DROPOUT_INT_RANGE = 0x7fffffff } esc_dropout_over;
+
+typedef struct esc_dropout {
+    int N, C, H, W;
+    double p;
+    esc_dropout_over over;
+    unsigned long long seed, offset;
+    const long long *offset_device; /* device, 8-byte aligned, or NULL                                        */
+    long x_stride, out_stride, residual_stride;
+} esc_dropout;
+
+esc_status esc_dropout_forward(const void *x, const void *residual, esc_dtype dt, const esc_dropout *a, void *out, void *stream);
+
+/* grad_x = draw(unit(i)) >= q ? grad_out[i] * 65536 / (65536 - q) : 0, of the same mask; grad_out has a->out_stride, grad_x a->x_stride. */
+esc_status esc_dropout_backward(const void *grad_out, esc_dtype dt, const esc_dropout *a, void *grad_x, void *stream);
 
 /*
  * The AdamW step over all of a network's parameter tensors, in one launch.  For every element, in fp32, each

@@ -28,10 +28,14 @@ EXPORTS = ("esc_workspace_bytes", "esc_workspace_init", "esc_workspace_errors", 
            "esc_backward_workspace_bytes", "esc_convattn_backward", "esc_convffn_workspace_bytes",
            "esc_convffn_forward", "esc_residual_step_workspace_bytes", "esc_residual_step_forward", "esc_window_attention_saved_bytes",
            "esc_window_attention_forward", "esc_window_attention_backward_workspace_bytes", "esc_window_attention_backward",
-           "esc_adamw_plan_bytes", "esc_adamw_plan_init", "esc_adamw_step", "esc_status_string")
+           "esc_adamw_plan_bytes", "esc_adamw_plan_init", "esc_adamw_step", "esc_layernorm_saved_bytes", "esc_layernorm_forward",
+           "esc_layernorm_backward_workspace_bytes", "esc_layernorm_backward", "esc_pointwise_forward", "esc_pointwise_backward_workspace_bytes",
+           "esc_pointwise_backward", "esc_dropout_forward", "esc_dropout_backward", "esc_status_string")
 NOALLOC_SCRATCH_BYTES = 1 << 20
 ADAMW_BLOCK = 256  # elements that share a scale in the optimiser's 8-bit states
 ADAMW_STATES = {"f32": 0, "8bit": 1}
+ACTIVATIONS = {"none": 0, "gelu": 1, "silu": 2}
+DROPOUT_UNITS = {"element": 0, "plane": 1, "image": 2}
 
 
 class EscError(RuntimeError):
@@ -74,6 +78,30 @@ class _AdamwPlan(ctypes.Structure):
 
 class _AdamwHyper(ctypes.Structure):
     _fields_ = [(n, ctypes.c_double) for n in ("lr", "beta1", "beta2", "eps", "grad_scale")] + [("lr_device", ctypes.c_void_p)]
+
+
+class _LayerNorm(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int) for n in ("N", "C", "H", "W")] + [("eps", ctypes.c_float), ("weight", ctypes.c_void_p), ("bias", ctypes.c_void_p)] + \
+               [(n, ctypes.c_long) for n in ("x_stride", "out_stride", "skip_stride")]
+
+
+class _LayerNormGrads(ctypes.Structure):
+    _fields_ = [("x", ctypes.c_void_p), ("x_stride", ctypes.c_long), ("weight", ctypes.c_void_p), ("bias", ctypes.c_void_p)]
+
+
+class _Pointwise(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int) for n in ("N", "K", "M", "H", "W", "act")] + [("w", ctypes.c_void_p), ("b", ctypes.c_void_p)] + \
+               [(n, ctypes.c_long) for n in ("x_stride", "out_stride", "residual_stride")]
+
+
+class _PointwiseGrads(ctypes.Structure):
+    _fields_ = [("x", ctypes.c_void_p), ("x_stride", ctypes.c_long), ("w", ctypes.c_void_p), ("b", ctypes.c_void_p)]
+
+
+class _Dropout(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int) for n in ("N", "C", "H", "W")] + [("p", ctypes.c_double), ("over", ctypes.c_int), ("seed", ctypes.c_ulonglong),
+                                                                    ("offset", ctypes.c_ulonglong), ("offset_device", ctypes.c_void_p)] + \
+               [(n, ctypes.c_long) for n in ("x_stride", "out_stride", "residual_stride")]
 
 
 class _NativeModule:
@@ -157,6 +185,25 @@ def load_library():
         lib.esc_adamw_plan_init.restype = ci
         lib.esc_adamw_step.argtypes = [ctypes.POINTER(_AdamwPlan), ctypes.POINTER(_AdamwHyper), vp]
         lib.esc_adamw_step.restype = ci
+        ln, pw, dr = ctypes.POINTER(_LayerNorm), ctypes.POINTER(_Pointwise), ctypes.POINTER(_Dropout)
+        lib.esc_layernorm_saved_bytes.argtypes = [ln]
+        lib.esc_layernorm_saved_bytes.restype = sz
+        lib.esc_layernorm_forward.argtypes = [vp, ci, ln, vp, vp, sz, vp]
+        lib.esc_layernorm_forward.restype = ci
+        lib.esc_layernorm_backward_workspace_bytes.argtypes = [ln]
+        lib.esc_layernorm_backward_workspace_bytes.restype = sz
+        lib.esc_layernorm_backward.argtypes = [vp, vp, vp, ci, ln, vp, sz, ctypes.POINTER(_LayerNormGrads), ci, vp, sz, vp]
+        lib.esc_layernorm_backward.restype = ci
+        lib.esc_pointwise_forward.argtypes = [vp, vp, ci, pw, vp, vp]
+        lib.esc_pointwise_forward.restype = ci
+        lib.esc_pointwise_backward_workspace_bytes.argtypes = [pw, ci]
+        lib.esc_pointwise_backward_workspace_bytes.restype = sz
+        lib.esc_pointwise_backward.argtypes = [vp, vp, ci, pw, ctypes.POINTER(_PointwiseGrads), ci, vp, sz, vp]
+        lib.esc_pointwise_backward.restype = ci
+        lib.esc_dropout_forward.argtypes = [vp, vp, ci, dr, vp, vp]
+        lib.esc_dropout_forward.restype = ci
+        lib.esc_dropout_backward.argtypes = [vp, ci, dr, vp, vp]
+        lib.esc_dropout_backward.restype = ci
         lib.esc_status_string.argtypes = [ci]
         lib.esc_status_string.restype = ctypes.c_char_p
         _lib = lib
@@ -406,6 +453,91 @@ def window_attention_backward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
     carry buffers to write into (slices of one tensor too); accumulate=True adds the bias' gradient to its buffer."""
     return _native.window_attention_backward(q, k, v, out, grad_out, saved, heads, window, workspace, bias, edges, mask, scale,
                                              kv_heads, accumulate, grads, stream)
+
+
+def new_layernorm_saved(N: int, H: int, W: int, device="cuda") -> torch.Tensor:
+    """Allocate (with torch) what layernorm_forward keeps for the backward pass."""
+    nbytes = int(load_library().esc_layernorm_saved_bytes(_LayerNorm(N=N, C=1, H=H, W=W)))
+    if nbytes == 0:
+        raise ValueError("bad shape for layer norm")
+    return torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+
+def new_layernorm_backward_workspace(N: int, C: int, H: int, W: int, device="cuda") -> torch.Tensor:
+    """Allocate (with torch) the scratch workspace of layernorm_backward (needs no preparation)."""
+    nbytes = int(load_library().esc_layernorm_backward_workspace_bytes(_LayerNorm(N=N, C=C, H=H, W=W)))
+    if nbytes == 0:
+        raise ValueError("bad shape for layer norm")
+    return torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+
+def layernorm_forward(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, eps: float = 1e-5,
+                      out: Optional[torch.Tensor] = None, saved: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """esc_layernorm_forward: each pixel of x [N, C, H, W] normalised over its channels; weight and bias [C] float32.  x and out may be slices of
+    larger tensors along the channels.  With `saved` (new_layernorm_saved) the backward pass can follow.  Runs on the tensors' device and that
+    device's current stream."""
+    return _native.layernorm_forward(x, weight, bias, eps, out, saved, stream)
+
+
+def layernorm_backward(x: torch.Tensor, grad_out: torch.Tensor, saved: torch.Tensor, workspace: torch.Tensor,
+                       weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, grad_skip: Optional[torch.Tensor] = None,
+                       accumulate: bool = False, grads: Optional[dict] = None, need=None, stream=None) -> dict:
+    """esc_layernorm_backward.  Returns a dict of device tensors: grad_x (with grad_skip, the gradient that reaches x around the norm, added) and, with
+    a weight and a bias, grad_weight and grad_bias; `need` names those that are wanted (None: all).  `grads` may carry buffers to write into;
+    accumulate=True adds the parameters' gradients to theirs."""
+    return _native.layernorm_backward(x, grad_out, saved, workspace, weight, bias, grad_skip, accumulate, grads, need, stream)
+
+
+def _activation(act: str) -> int:
+    if act not in ACTIVATIONS:
+        raise ValueError(f"act must be one of {sorted(ACTIVATIONS)}, got {act!r}")
+    return ACTIVATIONS[act]
+
+
+def pointwise_forward(x: torch.Tensor, w: torch.Tensor, b: Optional[torch.Tensor] = None, act: str = "none",
+                      residual: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """esc_pointwise_forward: act(w x + b) + residual for each pixel of x [N, K, H, W]; w [M, K] and b [M] float32, act "none", "gelu" (erf
+    form) or "silu".  x, residual and out may be slices of larger tensors along the channels.  Runs on the tensors' device and that device's
+    current stream."""
+    return _native.pointwise_forward(x, w, b, _activation(act), residual, out, stream)
+
+
+def new_pointwise_backward_workspace(N: int, K: int, M: int, H: int, W: int, dtype: torch.dtype, act: str = "none", device="cuda") -> torch.Tensor:
+    """Allocate (with torch) the scratch workspace of pointwise_backward (needs no preparation)."""
+    dt = ESC_F32 if dtype == torch.float32 else ESC_BF16
+    nbytes = int(load_library().esc_pointwise_backward_workspace_bytes(_Pointwise(N=N, K=K, M=M, H=H, W=W, act=_activation(act)), dt))
+    if nbytes == 0:
+        raise ValueError("bad shape for a point-wise product")
+    return torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+
+def pointwise_backward(x: torch.Tensor, grad_out: torch.Tensor, w: torch.Tensor, workspace: torch.Tensor, b: Optional[torch.Tensor] = None,
+                       act: str = "none", accumulate: bool = False, grads: Optional[dict] = None, need=None, stream=None) -> dict:
+    """esc_pointwise_backward.  Returns a dict of device tensors: grad_x, grad_w and, with a bias, grad_b; `need` names those that are wanted (None:
+    all).  (The residual's gradient is grad_out.)  `grads` may carry buffers to write into; accumulate=True adds the parameters' gradients to theirs."""
+    return _native.pointwise_backward(x, grad_out, w, workspace, b, _activation(act), accumulate, grads, need, stream)
+
+
+def _dropout_unit(over: str) -> int:
+    if over not in DROPOUT_UNITS:
+        raise ValueError(f"over must be one of {sorted(DROPOUT_UNITS)}, got {over!r}")
+    return DROPOUT_UNITS[over]
+
+
+def dropout_forward(x: torch.Tensor, p: float, seed: int, offset: int = 0, offset_device: Optional[torch.Tensor] = None, over: str = "element",
+                    residual: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """esc_dropout_forward: residual + x with elements, channel planes or images dropped with probability p (rounded to a multiple of 2^-16), the
+    rest scaled by 1 / (1 - p).  The mask is a function of seed and offset; calls that shall draw independently take different ones.
+    offset_device (int64, one element) is added to the offset on the device: a captured step that counts it up draws anew in each replay.
+    Runs on the tensors' device and that device's current stream."""
+    return _native.dropout_forward(x, p, seed, offset, offset_device, _dropout_unit(over), residual, out, stream)
+
+
+def dropout_backward(grad_out: torch.Tensor, p: float, seed: int, offset: int = 0, offset_device: Optional[torch.Tensor] = None, over: str = "element",
+                     grad_x: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """esc_dropout_backward: the gradient of x, of the mask that the forward call with the same p, seed, offsets and `over` drew.  (The residual's gradient
+    is grad_out.)"""
+    return _native.dropout_backward(grad_out, p, seed, offset, offset_device, _dropout_unit(over), grad_x, stream)
 
 
 class AdamW:

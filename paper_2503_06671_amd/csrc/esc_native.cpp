@@ -759,16 +759,321 @@ PyObject *window_attention_backward(PyObject *const *a, Py_ssize_t n)
     return r;
 }
 
+// ---- layer norm, the point-wise product, dropout ----
+
+double number(PyObject *o)
+{
+    const double d = PyFloat_AsDouble(o);
+    if (d == -1.0 && PyErr_Occurred()) throw PyError{};
+    return d;
+}
+
+// A [N,C,H,W] device tensor of the storage types with contiguous images, its sizes and step.
+struct Map {
+    const at::Tensor *t;
+    esc_dtype dt;
+    int N, C, H, W;
+    long stride;
+};
+
+Map map_checked(PyObject *o, const char *name)
+{
+    Map m;
+    m.t = &tensor(o, name);
+    m.stride = images(*m.t, name);
+    m.dt = storage_type(*m.t, name);
+    m.N = fits_int(m.t->size(0), name), m.C = fits_int(m.t->size(1), name), m.H = fits_int(m.t->size(2), name), m.W = fits_int(m.t->size(3), name);
+    return m;
+}
+
+// Another tensor of x's type and device with `channels` planes of x's size; gives its step.
+long map_beside(const at::Tensor &t, const Map &x, int64_t channels, const char *name)
+{
+    const long stride = images(t, name);
+    if (t.scalar_type() != x.t->scalar_type()) fail(PyExc_TypeError, std::string(name) + " must have the dtype of the other tensors");
+    if (t.size(0) != x.N || t.size(1) != channels || t.size(2) != x.H || t.size(3) != x.W)
+        fail(PyExc_ValueError, std::string(name) + " must be [" + std::to_string(x.N) + ", " + std::to_string(channels) + ", " + std::to_string(x.H) + ", " +
+                                   std::to_string(x.W) + "]");
+    same_device(t, *x.t, name);
+    return stride;
+}
+
+at::Tensor map_or_new(PyObject *o, const Map &x, int64_t channels, const char *name, long *stride)
+{
+    if (given(o)) {
+        const at::Tensor &t = tensor(o, name);
+        *stride = map_beside(t, x, channels, name);
+        return t;
+    }
+    *stride = (long)(channels * x.H * x.W);
+    return at::empty({x.N, channels, x.H, x.W}, x.t->options());
+}
+
+// An optional fp32 tensor of given sizes beside x.
+const float *weights_beside(PyObject *o, const Map &x, at::IntArrayRef sizes, const char *name)
+{
+    const at::Tensor *t = dev_f32(o, name);
+    if (t == nullptr) return nullptr;
+    if (t->sizes() != sizes) fail(PyExc_ValueError, std::string(name) + " has the wrong shape");
+    same_device(*t, *x.t, name);
+    return static_cast<const float *>(t->data_ptr());
+}
+
+// The dict of gradients that a call gives back, begun with the buffers that the caller brought.
+struct Grads {
+    PyObject *d = nullptr;
+    explicit Grads(PyObject *brought)
+    {
+        const int any = given(brought) ? PyObject_IsTrue(brought) : 0;
+        if (any < 0) throw PyError{};
+        d = any != 0 ? PyObject_CallFunctionObjArgs((PyObject *)&PyDict_Type, brought, nullptr) : PyDict_New();
+        if (d == nullptr) throw PyError{};
+    }
+    Grads(const Grads &) = delete;
+    ~Grads() { Py_XDECREF(d); }
+    void put(const char *name, const at::Tensor &t)
+    {
+        PyObject *o = wrap(t);
+        const int rc = o != nullptr ? PyDict_SetItemString(d, name, o) : -1;
+        Py_XDECREF(o);
+        if (rc != 0) throw PyError{};
+    }
+    void *map(const char *name, const Map &x, long *stride)
+    {
+        PyObject *v = item(d, name);
+        const at::Tensor t = map_or_new(v, x, x.C, name, stride);
+        if (v == nullptr) put(name, t);
+        return t.data_ptr();
+    }
+    // (a buffer that the call allocates is written, not added to: whether it was there says *brought)
+    float *weights(const char *name, const Map &x, at::IntArrayRef sizes, bool *brought)
+    {
+        PyObject *v = item(d, name);
+        *brought = v != nullptr;
+        if (v != nullptr) return const_cast<float *>(weights_beside(v, x, sizes, name));
+        const at::Tensor t = at::empty(sizes, x.t->options().dtype(at::kFloat));
+        put(name, t);
+        return static_cast<float *>(t.data_ptr());
+    }
+    PyObject *release()
+    {
+        PyObject *r = d;
+        d = nullptr;
+        return r;
+    }
+};
+
+Ws scratch_beside(PyObject *o, const Map &x, const char *name)
+{
+    const at::Tensor &t = tensor(o, name);
+    if (!t.is_cuda() || !t.is_contiguous()) fail(PyExc_TypeError, std::string(name) + " must be a contiguous device tensor");
+    same_device(t, *x.t, name);
+    return Ws{t.data_ptr(), (size_t)t.numel() * (size_t)t.element_size()};
+}
+
+// Which gradients are wanted: all that there are where `need` is None, else those that it names.
+bool wanted(PyObject *need, const char *name)
+{
+    if (!given(need)) return true;
+    PyObject *key = PyUnicode_FromString(name);
+    if (key == nullptr) throw PyError{};
+    const int in = PySequence_Contains(need, key);
+    Py_DECREF(key);
+    if (in < 0) throw PyError{};
+    return in != 0;
+}
+
+int truth(PyObject *o)
+{
+    const int t = PyObject_IsTrue(o);
+    if (t < 0) throw PyError{};
+    return t;
+}
+
+// Whether a call adds to its two parameter gradients: to buffers that the caller brought, both or none.
+int adds(int accumulate, bool brought_a, bool brought_b, const float *a, const float *b, const char *name_a, const char *name_b)
+{
+    if (accumulate == 0 || (!brought_a && !brought_b)) return 0;
+    if (a != nullptr && !brought_a) fail(PyExc_ValueError, std::string("accumulate needs ") + name_a + " in grads where it has " + name_b);
+    if (b != nullptr && !brought_b) fail(PyExc_ValueError, std::string("accumulate needs ") + name_b + " in grads where it has " + name_a);
+    return 1;
+}
+
+PyObject *layernorm_forward(PyObject *const *a, Py_ssize_t n)
+{
+    want_args(n, 7);  // x, weight, bias, eps, out, saved, stream
+    const Map x = map_checked(a[0], "x");
+    esc_layernorm l{};
+    l.N = x.N, l.C = x.C, l.H = x.H, l.W = x.W, l.eps = (float)number(a[3]), l.x_stride = x.stride;
+    l.weight = weights_beside(a[1], x, {x.C}, "weight"), l.bias = weights_beside(a[2], x, {x.C}, "bias");
+    const c10::DeviceGuard guard(x.t->device());
+    const at::Tensor out = map_or_new(a[4], x, x.C, "out", &l.out_stride);
+    Ws saved{nullptr, 0};
+    if (given(a[5])) saved = scratch_beside(a[5], x, "saved");
+    void *st = stream_of(a[6]);
+    const void *xp = x.t->data_ptr();
+    void *op = out.data_ptr();
+    check(unlocked([&] { return esc_layernorm_forward(xp, x.dt, &l, op, saved.ptr, saved.bytes, st); }));
+    return result(a[4], out);
+}
+
+PyObject *layernorm_backward(PyObject *const *a, Py_ssize_t n)
+{
+    want_args(n, 11);  // x, grad_out, saved, workspace, weight, bias, grad_skip, accumulate, grads, need, stream
+    const Map x = map_checked(a[0], "x");
+    esc_layernorm l{};
+    l.N = x.N, l.C = x.C, l.H = x.H, l.W = x.W, l.x_stride = x.stride;
+    const at::Tensor &go = tensor(a[1], "grad_out");
+    l.out_stride = map_beside(go, x, x.C, "grad_out");
+    const Ws saved = scratch_beside(a[2], x, "saved"), ws = scratch_beside(a[3], x, "workspace");
+    l.weight = weights_beside(a[4], x, {x.C}, "weight"), l.bias = weights_beside(a[5], x, {x.C}, "bias");
+    const void *skip = nullptr;
+    if (given(a[6])) {
+        const at::Tensor &t = tensor(a[6], "grad_skip");
+        l.skip_stride = map_beside(t, x, x.C, "grad_skip");
+        skip = t.data_ptr();
+    }
+    int acc = truth(a[7]);
+    const c10::DeviceGuard guard(x.t->device());
+    Grads grads(a[8]);
+    esc_layernorm_grads g{};
+    bool brought_w = false, brought_b = false;
+    if (wanted(a[9], "grad_x")) g.x = grads.map("grad_x", x, &g.x_stride);
+    if (l.weight != nullptr && wanted(a[9], "grad_weight")) g.weight = grads.weights("grad_weight", x, {x.C}, &brought_w);
+    if (l.bias != nullptr && wanted(a[9], "grad_bias")) g.bias = grads.weights("grad_bias", x, {x.C}, &brought_b);
+    acc = adds(acc, brought_w, brought_b, g.weight, g.bias, "grad_weight", "grad_bias");
+    void *st = stream_of(a[10]);
+    const void *xp = x.t->data_ptr(), *gop = go.data_ptr();
+    check(unlocked([&] { return esc_layernorm_backward(xp, gop, skip, x.dt, &l, saved.ptr, saved.bytes, &g, acc, ws.ptr, ws.bytes, st); }));
+    return grads.release();
+}
+
+// x, w, b, act
+esc_pointwise pointwise_checked(const Map &x, PyObject *w, PyObject *b, PyObject *act)
+{
+    esc_pointwise p{};
+    const at::Tensor &wt = dev_f32_required(w, "w");
+    if (wt.dim() != 2 || wt.size(1) != x.C) fail(PyExc_ValueError, "w must be [M, K] with K = " + std::to_string(x.C) + " channels of x");
+    same_device(wt, *x.t, "w");
+    p.N = x.N, p.K = x.C, p.M = fits_int(wt.size(0), "w"), p.H = x.H, p.W = x.W, p.x_stride = x.stride;
+    p.act = (esc_activation)integer(act);
+    p.w = static_cast<const float *>(wt.data_ptr()), p.b = weights_beside(b, x, {p.M}, "b");
+    return p;
+}
+
+PyObject *pointwise_forward(PyObject *const *a, Py_ssize_t n)
+{
+    want_args(n, 7);  // x, w, b, act, residual, out, stream
+    const Map x = map_checked(a[0], "x");
+    esc_pointwise p = pointwise_checked(x, a[1], a[2], a[3]);
+    const void *res = nullptr;
+    if (given(a[4])) {
+        const at::Tensor &t = tensor(a[4], "residual");
+        p.residual_stride = map_beside(t, x, p.M, "residual");
+        res = t.data_ptr();
+    }
+    const c10::DeviceGuard guard(x.t->device());
+    const at::Tensor out = map_or_new(a[5], x, p.M, "out", &p.out_stride);
+    void *st = stream_of(a[6]);
+    const void *xp = x.t->data_ptr();
+    void *op = out.data_ptr();
+    check(unlocked([&] { return esc_pointwise_forward(xp, res, x.dt, &p, op, st); }));
+    return result(a[5], out);
+}
+
+PyObject *pointwise_backward(PyObject *const *a, Py_ssize_t n)
+{
+    want_args(n, 10);  // x, grad_out, w, workspace, b, act, accumulate, grads, need, stream
+    const Map x = map_checked(a[0], "x");
+    esc_pointwise p = pointwise_checked(x, a[2], a[4], a[5]);
+    const at::Tensor &go = tensor(a[1], "grad_out");
+    p.out_stride = map_beside(go, x, p.M, "grad_out");
+    const Ws ws = scratch_beside(a[3], x, "workspace");
+    int acc = truth(a[6]);
+    const c10::DeviceGuard guard(x.t->device());
+    Grads grads(a[7]);
+    esc_pointwise_grads g{};
+    bool brought_w = false, brought_b = false;
+    if (wanted(a[8], "grad_x")) g.x = grads.map("grad_x", x, &g.x_stride);
+    if (wanted(a[8], "grad_w")) g.w = grads.weights("grad_w", x, {p.M, p.K}, &brought_w);
+    if (p.b != nullptr && wanted(a[8], "grad_b")) g.b = grads.weights("grad_b", x, {p.M}, &brought_b);
+    acc = adds(acc, brought_w, brought_b, g.w, g.b, "grad_w", "grad_b");
+    void *st = stream_of(a[9]);
+    const void *xp = x.t->data_ptr(), *gop = go.data_ptr();
+    check(unlocked([&] { return esc_pointwise_backward(xp, gop, x.dt, &p, &g, acc, ws.ptr, ws.bytes, st); }));
+    return grads.release();
+}
+
+unsigned long long word(PyObject *o, const char *name)
+{
+    PyObject *i = PyNumber_Index(o);
+    if (i == nullptr) throw PyError{};
+    const unsigned long long v = PyLong_AsUnsignedLongLong(i);
+    Py_DECREF(i);
+    if (v == (unsigned long long)-1 && PyErr_Occurred()) {
+        PyErr_Clear();
+        fail(PyExc_ValueError, std::string(name) + " must be a whole number of 64 bits, not negative");
+    }
+    return v;
+}
+
+// in, p, seed, offset, offset_device, over
+esc_dropout dropout_checked(const Map &x, PyObject *p, PyObject *seed, PyObject *offset, PyObject *offset_device, PyObject *over)
+{
+    esc_dropout d{};
+    d.N = x.N, d.C = x.C, d.H = x.H, d.W = x.W, d.p = number(p);
+    d.over = (esc_dropout_over)integer(over);
+    d.seed = word(seed, "seed"), d.offset = word(offset, "offset");
+    if (given(offset_device)) {
+        const at::Tensor &t = tensor(offset_device, "offset_device");
+        if (!t.is_cuda() || t.scalar_type() != at::kLong || t.numel() != 1) fail(PyExc_TypeError, "offset_device must be an int64 device tensor of one element");
+        same_device(t, *x.t, "offset_device");
+        d.offset_device = static_cast<const long long *>(t.data_ptr());
+    }
+    return d;
+}
+
+PyObject *dropout_forward(PyObject *const *a, Py_ssize_t n)
+{
+    want_args(n, 9);  // x, p, seed, offset, offset_device, over, residual, out, stream
+    const Map x = map_checked(a[0], "x");
+    esc_dropout d = dropout_checked(x, a[1], a[2], a[3], a[4], a[5]);
+    d.x_stride = x.stride;
+    const void *res = nullptr;
+    if (given(a[6])) {
+        const at::Tensor &t = tensor(a[6], "residual");
+        d.residual_stride = map_beside(t, x, x.C, "residual");
+        res = t.data_ptr();
+    }
+    const c10::DeviceGuard guard(x.t->device());
+    const at::Tensor out = map_or_new(a[7], x, x.C, "out", &d.out_stride);
+    void *st = stream_of(a[8]);
+    const void *xp = x.t->data_ptr();
+    void *op = out.data_ptr();
+    check(unlocked([&] { return esc_dropout_forward(xp, res, x.dt, &d, op, st); }));
+    return result(a[7], out);
+}
+
+PyObject *dropout_backward(PyObject *const *a, Py_ssize_t n)
+{
+    want_args(n, 8);  // grad_out, p, seed, offset, offset_device, over, grad_x, stream
+    const Map g = map_checked(a[0], "grad_out");
+    esc_dropout d = dropout_checked(g, a[1], a[2], a[3], a[4], a[5]);
+    d.out_stride = g.stride;
+    const c10::DeviceGuard guard(g.t->device());
+    const at::Tensor gx = map_or_new(a[6], g, g.C, "grad_x", &d.x_stride);
+    void *st = stream_of(a[7]);
+    const void *gop = g.t->data_ptr();
+    void *gxp = gx.data_ptr();
+    check(unlocked([&] { return esc_dropout_backward(gop, g.dt, &d, gxp, st); }));
+    return result(a[6], gx);
+}
+
 // ---- AdamW: one step of a plan (laid out once by binding.AdamW) ----
 
 PyObject *adamw_step(PyObject *const *a, Py_ssize_t n)
 {
     want_args(n, 9);  // address of the plan, device index, lr, beta1, beta2, eps, grad_scale, address of lr_device, stream
-    auto number = [](PyObject *o) {
-        const double d = PyFloat_AsDouble(o);
-        if (d == -1.0 && PyErr_Occurred()) throw PyError{};
-        return d;
-    };
     const esc_adamw_plan *plan = static_cast<const esc_adamw_plan *>(PyLong_AsVoidPtr(a[0]));
     if (plan == nullptr) fail(PyExc_ValueError, "no plan");
     const c10::DeviceGuard guard(c10::Device(c10::DeviceType::CUDA, (c10::DeviceIndex)integer(a[1])));
@@ -809,7 +1114,9 @@ PyObject *entry(PyObject *, PyObject *const *args, Py_ssize_t n)
 PyMethodDef kMethods[] = {ESC_ENTRY(gen_handle),         ESC_ENTRY(dynkernel_gen),    ESC_ENTRY(convattn_forward),
                           ESC_ENTRY(convattn_fused_forward), ESC_ENTRY(convffn_forward), ESC_ENTRY(residual_step_forward),
                           ESC_ENTRY(convattn_dense_forward), ESC_ENTRY(convattn_backward),
-                          ESC_ENTRY(window_attention_forward), ESC_ENTRY(window_attention_backward), ESC_ENTRY(adamw_step), {nullptr, nullptr, 0, nullptr}};
+                          ESC_ENTRY(window_attention_forward), ESC_ENTRY(window_attention_backward), ESC_ENTRY(adamw_step),
+                          ESC_ENTRY(layernorm_forward), ESC_ENTRY(layernorm_backward), ESC_ENTRY(pointwise_forward), ESC_ENTRY(pointwise_backward),
+                          ESC_ENTRY(dropout_forward), ESC_ENTRY(dropout_backward), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_native", "Argument handling of the binding over the C ABI.", -1, kMethods,
                        nullptr, nullptr, nullptr, nullptr};
 

@@ -203,25 +203,6 @@ size_t saved_size(const WindowParams &p, esc_dtype dt)
     return rows_bytes(p) + (dt == ESC_BF16 ? round_up((size_t)p.N * p.heads * p.d * p.H * p.W * 2, kAlign) : 0);
 }
 
-// Planes of N images, `stride` bytes from image to image.
-struct Images {
-    const void *at;
-    size_t stride, bytes;  // bytes: one image's
-    int N;
-    size_t extent() const { return (size_t)(N - 1) * stride + bytes; }
-};
-
-bool meet(const Images &a, const Images &b)
-{
-    if (!overlaps(a.at, a.extent(), b.at, b.extent())) return false;
-    if (a.stride != b.stride || a.N == 1 || b.N == 1) return true;
-    // the same step from image to image: parts of one tensor may lie between each other
-    const uintptr_t ua = (uintptr_t)a.at, ub = (uintptr_t)b.at;
-    const size_t s = a.stride, from = ub >= ua ? (ub - ua) % s : (s - (ua - ub) % s) % s;
-    return from < a.bytes || from + b.bytes > s;
-}
-bool meets(const Images &a, const void *b, size_t bytes) { return b != nullptr && overlaps(a.at, a.extent(), b, bytes); }
-
 // Checks what both directions take, and fills in the parameters.
 esc_status common(const void *q, const void *k, const void *v, esc_dtype dt, const esc_window_attn *a, WindowParams *p, Images (&in)[3])
 {
