@@ -17,6 +17,7 @@
 
 #include "esc_convattn.h"
 #include "esc_host.hpp"
+#include "esc_parts.hpp"
 #include "esc_terms.hpp"
 
 namespace {
@@ -501,16 +502,6 @@ __global__ __launch_bounds__(kThreads, 2) void product_weights_kernel(const Weig
     }
 }
 
-// Adds the parts of all splits up, in their order.
-__global__ __launch_bounds__(kThreads) void product_parts_kernel(const float *part, int splits, long n, float *to, int accumulate)
-{
-    const long i = (long)blockIdx.x * kThreads + threadIdx.x;
-    if (i >= n) return;
-    float t = 0.f;
-    for (int k = 0; k < splits; ++k) t += part[k * n + i];
-    to[i] = accumulate ? to[i] + t : t;
-}
-
 template <typename TG, typename TI, int QG, int QX>
 hipError_t launch_weights(const WeightParams &p, hipStream_t s)
 {
@@ -650,12 +641,8 @@ esc_status esc_pointwise_backward(const void *x, const void *grad_out, esc_dtype
         p.K = a->K, p.M = a->M, p.splits = splits_of(a, P), p.P = P, p.pixels = P * a->N;
         const hipError_t e = f32 ? launch_weights<float, float, 3, 3>(p, s) : act ? launch_weights<float, bf16s, 3, 1>(p, s) : launch_weights<bf16s, bf16s, 1, 1>(p, s);
         if (e != hipSuccess) return ESC_ERR_HIP;
-        const auto add = [&](const float *part, long count, float *to) {
-            hipLaunchKernelGGL(product_parts_kernel, dim3((unsigned)((count + kThreads - 1) / kThreads)), dim3(kThreads), 0, s, part, p.splits, count, to, accumulate);
-            return hipGetLastError();
-        };
-        if (g->w != nullptr && add(p.part, (long)a->M * a->K, g->w) != hipSuccess) return ESC_ERR_HIP;
-        if (g->b != nullptr && add(p.part_b, a->M, g->b) != hipSuccess) return ESC_ERR_HIP;
+        if (g->w != nullptr && add_parts(p.part, p.splits, (long)a->M * a->K, g->w, 0, nullptr, accumulate, s) != hipSuccess) return ESC_ERR_HIP;
+        if (g->b != nullptr && add_parts(p.part_b, p.splits, a->M, g->b, 0, nullptr, accumulate, s) != hipSuccess) return ESC_ERR_HIP;
     }
     return ESC_OK;
 }
