@@ -18,126 +18,14 @@
 #include "esc_convattn.h"
 #include "esc_host.hpp"
 #include "esc_parts.hpp"
-#include "esc_terms.hpp"
+#include "esc_product.hpp"
 
 namespace {
 
 using namespace esc;
 
-typedef float f32x16 __attribute__((ext_vector_type(16)));
-typedef float f32x2 __attribute__((ext_vector_type(2)));
-typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-
 constexpr size_t kAlign = 256;
-constexpr int kThreads = 256;
-constexpr long kCus = 256;
-
-struct bf16s {
-    uint16_t bits;
-};
-template <typename T>
-constexpr bool kWide = sizeof(T) == 4;
-
-__device__ __forceinline__ uint32_t pack2(float a, float b) { return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, bf16x2)); }
-
-// N terms of two values, a word of two for each: three are exact, by truncation; two, and one, are the nearest.
-template <int N>
-__device__ __forceinline__ void terms_of(float a, float b, uint32_t (&t)[N])
-{
-    if constexpr (N == 3) {
-        split_bf16(a, b, t);
-    } else {
-#pragma unroll
-        for (int q = 0; q < N; ++q) {
-            t[q] = pack2(a, b);
-            if (q + 1 < N) a -= __uint_as_float(t[q] << 16), b -= __uint_as_float(t[q] & 0xffff0000u);
-        }
-    }
-}
-
-// Behind the last product: an ordinary instruction may read a product's result twelve issue slots later.
-__device__ __forceinline__ void settle()
-{
-    __builtin_amdgcn_sched_barrier(0);
-    asm volatile("s_nop 15");
-    __builtin_amdgcn_sched_barrier(0);
-}
-
-template <typename T>
-__device__ __forceinline__ float widen(T v)
-{
-    if constexpr (kWide<T>) return v;
-    else return __uint_as_float((uint32_t)v.bits << 16);
-}
-// Two neighbours at any address their type allows.
-template <typename T>
-struct __attribute__((packed, aligned(sizeof(T)))) Two {
-    T a, b;
-};
-
-enum : int { kNone = 0, kGelu = 1, kSilu = 2 };
-
-// e = erfc(|v| / sqrt 2) as 2^-(t P(t)), t = |v| (esc_gelu.hpp has the polynomial's derivation)
-__device__ __forceinline__ float erfc_of(float t)
-{
-    float q = fmaf(2.834909764715121e-06f, t, -3.937766086892225e-05f);
-    q = fmaf(q, t, 0.0001861801283666864f);
-    q = fmaf(q, t, 0.0001369366073049605f);
-    q = fmaf(q, t, -0.0070634204894304276f);
-    q = fmaf(q, t, 0.052496179938316345f);
-    q = fmaf(q, t, 0.4592081904411316f);
-    q = fmaf(q, t, 1.1511051654815674f);
-    return __builtin_amdgcn_exp2f(-q * t);
-}
-__device__ __forceinline__ float sigmoid(float v) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(v * -1.44269504f)); }
-
-__device__ __forceinline__ float activation(int act, float v)
-{
-    if (act == kGelu) {
-        const float h = 0.5f * v;
-        return fmaf(fabsf(h), 1.f - erfc_of(fabsf(v)), h);
-    }
-    return act == kSilu ? v * sigmoid(v) : v;
-}
-__device__ __forceinline__ float slope(int act, float v)
-{
-    if (act == kGelu) {
-        // Phi(v) + v phi(v)
-        const float e = 0.5f * erfc_of(fabsf(v));
-        return fmaf(v * 0.3989422804f, __builtin_amdgcn_exp2f(v * v * -0.7213475204f), v >= 0.f ? 1.f - e : e);
-    }
-    if (act == kSilu) {
-        const float s = sigmoid(v);
-        return s * fmaf(v, 1.f - s, 1.f);
-    }
-    return 1.f;
-}
-
 // ---- out = act(w x + b) + residual, and the products of the same form in the backward pass ----
-
-struct ProductParams {
-    const void *x;         // K planes an image
-    const void *extra;     // M planes an image: the residual, or grad_out, or nullptr
-    void *out;             // M planes an image
-    long x_stride, extra_stride, out_stride;  // elements
-    const float *w, *b;
-    int K, M, w_ld, act;
-    long P, pixels;        // of an image, of all
-    long tiles;            // of an image (or of all, where tiles pass images' borders)
-    bool across;           // tiles pass images' borders
-};
-
-// kForward: out = act(pre) + extra.  kSlope: out = extra act'(pre), fp32.
-enum : int { kForward = 0, kSlope = 1 };
-
-// Which eighths of the grid the dies get: consecutive pieces on one die.
-__device__ __forceinline__ unsigned piece_of(unsigned block, unsigned blocks)
-{
-    const unsigned each = blocks / 8u, rest = blocks % 8u, die = block % 8u;
-    return die * each + (die < rest ? die : rest) + block / 8u;
-}
 
 // A block's tile is 32 MT WM outputs x 64 WP pixels; a wavefront has 32 MT outputs of 64 pixels.  Two neighbouring pixels are a
 // lane's in two column blocks: columns of even pixels, then those of odd ones.  Operands lie in LDS as units of eight
@@ -387,6 +275,22 @@ hipError_t launch_product(const ProductParams &p, long N, hipStream_t s)
     return launch_product_as<TI, TO, TE, TX, TW, 2, 1, 4, TRANS, MODE>(p, N, s);
 }
 
+hipError_t launch_any(int kind, const ProductParams &p, long N, hipStream_t s)
+{
+    if (strip_fits(kind, p, N)) return launch_strip(kind, p, N, s);
+    switch (kind) {
+    case kForwardF32: return launch_product<float, float, float, 3, 3, false, kForward>(p, N, s);
+    case kForwardBf16: return launch_product<bf16s, bf16s, bf16s, 1, 2, false, kForward>(p, N, s);
+    case kSlopeF32: return launch_product<float, float, float, 3, 3, false, kSlope>(p, N, s);
+    // (weights in three terms with bf16 storage too: what is left of them goes into every pixel's gradient)
+    case kSlopeBf16: return launch_product<bf16s, float, bf16s, 1, 3, false, kSlope>(p, N, s);
+    case kBackF32: return launch_product<float, float, float, 3, 3, true, kForward>(p, N, s);
+    case kBackBf16: return launch_product<bf16s, bf16s, bf16s, 1, 2, true, kForward>(p, N, s);
+    case kBackGp: return launch_product<float, bf16s, bf16s, 2, 2, true, kForward>(p, N, s);
+    default: return hipErrorInvalidValue;
+    }
+}
+
 // ---- grad_w[m, k] = sum over pixels of g[m, q] x[k, q], grad_b[m] = sum over pixels of g[m, q] ----
 
 constexpr int kSide = 64;     // of a block's tile of grad_w; a wavefront has 32 x 32
@@ -571,8 +475,7 @@ esc_status esc_pointwise_forward(const void *x, const void *residual, esc_dtype 
     p.x_stride = (long)(xi.stride / es), p.out_stride = (long)(oi.stride / es), p.extra_stride = (long)(ri.stride / es);
     p.w = a->w, p.b = a->b, p.K = a->K, p.M = a->M, p.w_ld = a->K, p.act = (int)a->act, p.P = P, p.pixels = P * a->N;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    const hipError_t e = dt == ESC_F32 ? launch_product<float, float, float, 3, 3, false, kForward>(p, a->N, s)
-                                       : launch_product<bf16s, bf16s, bf16s, 1, 2, false, kForward>(p, a->N, s);
+    const hipError_t e = launch_any(dt == ESC_F32 ? kForwardF32 : kForwardBf16, p, a->N, s);
     return e == hipSuccess ? ESC_OK : ESC_ERR_HIP;
 }
 
@@ -618,9 +521,7 @@ esc_status esc_pointwise_backward(const void *x, const void *grad_out, esc_dtype
         p.x = x, p.extra = grad_out, p.out = mem;
         p.x_stride = x_stride, p.extra_stride = g_stride, p.out_stride = (long)a->M * P;
         p.w = a->w, p.b = a->b, p.K = a->K, p.M = a->M, p.w_ld = a->K, p.act = (int)a->act, p.P = P, p.pixels = P * a->N;
-        // (weights in three terms in either storage: what is left of them goes into every pixel's gradient)
-        const hipError_t e = f32 ? launch_product<float, float, float, 3, 3, false, kSlope>(p, a->N, s)
-                                 : launch_product<bf16s, float, bf16s, 1, 3, false, kSlope>(p, a->N, s);
+        const hipError_t e = launch_any(f32 ? kSlopeF32 : kSlopeBf16, p, a->N, s);
         if (e != hipSuccess) return ESC_ERR_HIP;
     }
     if (g->x != nullptr) {
@@ -628,9 +529,7 @@ esc_status esc_pointwise_backward(const void *x, const void *grad_out, esc_dtype
         p.x = act ? mem : grad_out, p.out = g->x;
         p.x_stride = act ? (long)a->M * P : g_stride, p.out_stride = (long)(gxi.stride / es);
         p.w = a->w, p.K = a->M, p.M = a->K, p.w_ld = a->K, p.act = kNone, p.P = P, p.pixels = P * a->N;
-        const hipError_t e = f32 ? launch_product<float, float, float, 3, 3, true, kForward>(p, a->N, s)
-                           : act ? launch_product<float, bf16s, bf16s, 2, 2, true, kForward>(p, a->N, s)
-                                 : launch_product<bf16s, bf16s, bf16s, 1, 2, true, kForward>(p, a->N, s);
+        const hipError_t e = launch_any(f32 ? kBackF32 : act ? kBackGp : kBackBf16, p, a->N, s);
         if (e != hipSuccess) return ESC_ERR_HIP;
     }
     if (g->w != nullptr || g->b != nullptr) {
