@@ -47,10 +47,24 @@ __global__ __launch_bounds__(kPartsThreads) void parts_kernel(const PartsParams 
     *to = p.accumulate ? *to + v : v;
 }
 
+// Few parts: a thread a result.
+__global__ __launch_bounds__(256) void few_parts_kernel(const PartsParams p)
+{
+    const long i = (long)blockIdx.x * 256 + threadIdx.x;
+    if (i >= p.n) return;
+    float t = 0.f;
+    for (int k = 0; k < p.splits; ++k) t += p.part[(long)k * p.n + i];
+    float *to = i < p.n0 ? p.to[0] : p.to[1];
+    if (to == nullptr) return;
+    to += i < p.n0 ? i : i - p.n0;
+    *to = p.accumulate ? *to + t : t;
+}
+
 inline hipError_t add_parts(const float *part, int splits, long n0, float *to0, long n1, float *to1, int accumulate, hipStream_t s)
 {
     const PartsParams p{part, {to0, to1}, n0 + n1, n0, splits, accumulate};
-    if (p.n <= 2048) hipLaunchKernelGGL(parts_kernel<8>, dim3((unsigned)((p.n + 7) / 8)), dim3(kPartsThreads), 0, s, p);
+    if (splits <= 16) hipLaunchKernelGGL(few_parts_kernel, dim3((unsigned)((p.n + 255) / 256)), dim3(256), 0, s, p);
+    else if (p.n <= 2048) hipLaunchKernelGGL(parts_kernel<8>, dim3((unsigned)((p.n + 7) / 8)), dim3(kPartsThreads), 0, s, p);
     else hipLaunchKernelGGL(parts_kernel<32>, dim3((unsigned)((p.n + 31) / 32)), dim3(kPartsThreads), 0, s, p);
     return hipGetLastError();
 }

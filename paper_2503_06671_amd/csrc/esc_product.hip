@@ -27,243 +27,254 @@ using namespace esc;
 constexpr size_t kAlign = 256;
 // ---- out = act(w x + b) + residual, and the products of the same form in the backward pass ----
 
-// A block's tile is 32 MT WM outputs x 64 WP pixels; a wavefront has 32 MT outputs of 64 pixels.  Two neighbouring pixels are a
-// lane's in two column blocks: columns of even pixels, then those of odd ones.  Operands lie in LDS as units of eight
-// consecutive channels (k) of one pixel or output, a unit 16 bytes, [term][k / 8][place].
-template <typename TI, typename TO, typename TE, int TX, int TW, int MT, int WM, int WP, bool TRANS, int MODE>
-struct Product {
-    static constexpr int kTop = TX > TW ? TX : TW;               // products of terms whose orders add up to less
-    static constexpr int kStage = TX == 3 ? 16 : 32;             // channels of a stage
-    static constexpr int kEights = kStage / 8;
-    static constexpr int BM = 32 * MT * WM, BP = 64 * WP;
-    static constexpr int kHalf = BP / 2 + 4;                     // places from even to odd pixels (four: other banks)
-    static constexpr int kXPitch = BP / 2 + kHalf;
-    static constexpr int kWPitch = BM + (TRANS ? 0 : 8 / kEights);
-    static constexpr int kXUnits = TX * kEights * kXPitch, kWUnits = TW * kEights * kWPitch;
-    static constexpr int kBuffer = kXUnits + kWUnits;
-    static constexpr int kAt = kWide<TI> ? 1 : 2;                // pixels of a load
-    static constexpr int kXLoads = kEights * BP / kAt, kXEach = (kXLoads + kThreads - 1) / kThreads;
-    static constexpr int kWLoads = kEights * BM, kWEach = (kWLoads + kThreads - 1) / kThreads;
-    static constexpr size_t kLds = (size_t)2 * kBuffer * 16 + BM * 4;
+// A wavefront owns 32 MT outputs of 32 NT pixels, a block four such runs of pixels.  Its input channels come in stages of 32, two stages ahead, straight into
+// the registers of the right operand (esc_product_strip.hip); the weights pass LDS, split into terms there by the block a stage ahead, two buffers, one barrier a
+// stage: units of eight consecutive channels of one output, [term][eighth of the stage][output].
+//
+// ACROSS: tiles pass images' borders (small images), or offsets take more than 32 bits: pixels by pointers of their own, one by one.
+template <int MT, int TW>
+struct Streamed {
+    static constexpr int kPitch = 32 * MT + 2;   // (two: other banks for the eighths of a row, which neighbouring threads write)
+    static constexpr int kBuffer = TW * 4 * kPitch;
+    static constexpr size_t kLds = (size_t)2 * kBuffer * 16 + 32 * MT * 4;
 };
-
 extern __shared__ __align__(16) u32x4 product_lds[];
 
-template <typename TI, typename TO, typename TE, int TX, int TW, int MT, int WM, int WP, bool TRANS, int MODE>
+template <typename TI, typename TO, typename TE, int TX, int TW, int MT, int NT, bool TRANS, int MODE, bool ACROSS>
 __global__ __launch_bounds__(kThreads, 2) void product_kernel(const ProductParams p)
 {
-    using C = Product<TI, TO, TE, TX, TW, MT, WM, WP, TRANS, MODE>;
+    using C = Streamed<MT, TW>;
+    constexpr int kTop = TX > TW ? TX : TW;      // products of terms whose orders add up to less
+    constexpr int kRuns = 256 * MT, kEach = kRuns / kThreads;  // runs of four weights of a stage, of a thread
     const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int l32 = lane & 31, half = lane >> 5, wm = wave % WM, wp = wave / WM;
-    const int K = p.K, M = p.M, stages = (K + C::kStage - 1) / C::kStage;
-    const long P = p.P;
-    const unsigned groups = (unsigned)(M + C::BM - 1) / C::BM;
+    const int l32 = lane & 31, half = lane >> 5;
+    const int K = p.K, M = p.M, stages = (K + 31) / 32;
+    const unsigned groups = (unsigned)(M + 32 * MT - 1) / (32u * MT);
     const unsigned piece = piece_of(blockIdx.x, gridDim.x), tile = piece / groups;
-    const int m0 = (int)(piece - tile * groups) * C::BM;
-    const long image = p.across ? 0 : tile / p.tiles;
-    const long q0 = ((long)tile - image * p.tiles) * C::BP;   // the tile's first pixel, of its image or of all
+    const int m0 = (int)(piece - tile * groups) * 32 * MT;
+    const unsigned mine = 32u * NT * (unsigned)wave + NT * (unsigned)l32;   // this lane's first pixel, of the tile
 
-    // where pixel q0 + i is: its image and its place there.  What lies beyond the last pixel is the last pair again, computed and stored
-    // with the same bits, or, in tiles that pass images' borders, the last pixel, not stored.
-    auto place = [&](int i, long &n, long &at) {
-        if (p.across) {
-            const long q = min(q0 + i, p.pixels - 1);
-            n = q / P, at = q - n * P;
-        } else {
-            n = image, at = min(q0 + (i & ~1), P - 2) + (i & 1);
-        }
-    };
-
-    // ---- this thread's share of a stage's loads: eight channels of kAt pixels, eight weights of a row ----
-    const TI *xp[C::kXEach][C::kAt];
-    int xk[C::kXEach], xto[C::kXEach];
+    // ---- where the pixels are ----
+    const long image = ACROSS ? 0 : tile / p.tiles;
+    long pn[NT], pat[NT];   // ACROSS: each pixel's image, and its place there
+    bool there[NT];
+    unsigned pxc = 0;       // else the first one's place (a lane whose pixels reach beyond the plane takes its last ones again: the same bits are stored)
+    if constexpr (ACROSS) {
 #pragma unroll
-    for (int i = 0; i < C::kXEach; ++i) {
-        const int u = tid + i * kThreads, unit = u % (C::BP / C::kAt);
-        xk[i] = __builtin_amdgcn_readfirstlane(u / (C::BP / C::kAt));
-        const int px = unit * C::kAt;
-#pragma unroll
-        for (int j = 0; j < C::kAt; ++j) {
-            long n, at;
-            place(px + j, n, at);
-            xp[i][j] = static_cast<const TI *>(p.x) + n * p.x_stride + at;
+        for (int t = 0; t < NT; ++t) {
+            const long q = (long)tile * (128 * NT) + mine + t, in = min(q, p.pixels - 1);
+            there[t] = q < p.pixels, pn[t] = in / p.P, pat[t] = in - pn[t] * p.P;
         }
-        xto[i] = xk[i] * C::kXPitch + (px >> 1) + (px & 1) * C::kHalf;
+    } else {
+        const unsigned px = (unsigned)(tile - image * p.tiles) * (128u * NT) + mine, P = (unsigned)p.P;
+        pxc = px + NT <= P ? px : P - NT;
     }
-    TI xr[C::kXEach][C::kAt][8];
-    float wr[C::kWEach][8];
-    auto fetch = [&](int st) {
+
+    // ---- channels of a stage: 32 st + 16 c + 8 half + j of this lane's pixels ----
+    typedef Raw<TI, ACROSS ? 1 : NT> X;
+    constexpr int kLoads = ACROSS ? NT : 1;
+    const unsigned ib = (unsigned)p.P * (unsigned)sizeof(TI);
+    const Rsrc rx = resource(static_cast<const TI *>(p.x) + image * p.x_stride, ACROSS ? 0 : (long)K * ib);
+    const unsigned in_off = 8u * (unsigned)half * ib + pxc * (unsigned)sizeof(TI);
+    auto xfetch = [&](int st, X (&r)[2][8][kLoads]) {
 #pragma unroll
-        for (int i = 0; i < C::kXEach; ++i) {
-            if (C::kXLoads % kThreads != 0 && xk[i] >= C::kEights) continue;
-            const int k0 = st * C::kStage + 8 * xk[i];
+        for (int c = 0; c < 2; ++c)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const long row = (long)min(k0 + e, K - 1) * P;
-                if constexpr (C::kAt == 2) {
-                    if (p.across) {
-                        xr[i][0][e] = xp[i][0][row], xr[i][1][e] = xp[i][1][row];
-                    } else {
-                        const Two<TI> t = *reinterpret_cast<const Two<TI> *>(xp[i][0] + row);
-                        xr[i][0][e] = t.a, xr[i][1][e] = t.b;
+            for (int j = 0; j < 8; ++j) {
+                const int k = 32 * st + 16 * c + j, mine = k + 8 * half;
+                if constexpr (ACROSS) {
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) {
+                        const TI v = static_cast<const TI *>(p.x)[pn[t] * p.x_stride + (long)min(mine, K - 1) * p.P + pat[t]];
+                        if constexpr (kWide<TI>) r[c][j][t].w[0] = mine < K ? __float_as_uint(v) : 0u;
+                        else r[c][j][t].w[0] = mine < K ? v.bits : 0u;
                     }
                 } else {
-                    xr[i][0][e] = xp[i][0][row];
+                    r[c][j][0] = load<TI, NT>(rx, mine < K ? in_off : kBeyond, k < K ? (unsigned)k * ib : 0u);
                 }
             }
-        }
+    };
+
+    // ---- weights of a stage ----
+    const Rsrc rw = weights_of(p);
+    const bool four = (K & 3) == 0;
+    float wr[kEach][4];
+    // (a row's runs, neighbours in memory, by neighbouring threads; TRANS: a channel's outputs)
+    auto run_of = [&](int i, int &row, int &k4) {
+        const int u = tid + i * kThreads;
+        row = TRANS ? u % (32 * MT) : u >> 3, k4 = TRANS ? u / (32 * MT) : u & 7;
+    };
+    auto wfetch = [&](int st) {
 #pragma unroll
-        for (int i = 0; i < C::kWEach; ++i) {
-            const int u = tid + i * kThreads;
-            const int k8 = TRANS ? u / C::BM : u % C::kEights, row = TRANS ? u % C::BM : u / C::kEights;
-            const int m = m0 + row, k = st * C::kStage + 8 * k8;
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                wr[i][e] = (m < M && k + e < K && k8 < C::kEights && row < C::BM) ? (TRANS ? p.w[(size_t)(k + e) * p.w_ld + m] : p.w[(size_t)m * p.w_ld + k + e]) : 0.f;
+        for (int i = 0; i < kEach; ++i) {
+            int row, k4;
+            run_of(i, row, k4);
+            load_weights<TRANS>(rw, p, four, m0 + row, 32 * st + 4 * k4, wr[i]);
         }
     };
-    auto put = [&](int st) {
-        u32x4 *xs = product_lds + (st & 1) * C::kBuffer, *ws = xs + C::kXUnits;
+    auto wput = [&](int st) {
+        u32x2 *ws = reinterpret_cast<u32x2 *>(product_lds + (st & 1) * C::kBuffer);
 #pragma unroll
-        for (int i = 0; i < C::kXEach; ++i) {
-            if (C::kXLoads % kThreads != 0 && xk[i] >= C::kEights) continue;
-            const int in = K - (st * C::kStage + 8 * xk[i]);   // how many of the eight there are
+        for (int i = 0; i < kEach; ++i) {
+            int row, k4;
+            run_of(i, row, k4);
+            uint32_t t[2][TW];
+            terms_of<TW>(wr[i][0], wr[i][1], t[0]);
+            terms_of<TW>(wr[i][2], wr[i][3], t[1]);
 #pragma unroll
-            for (int j = 0; j < C::kAt; ++j) {
-                uint32_t t[4][TX];
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    terms_of<TX>(2 * e < in ? widen(xr[i][j][2 * e]) : 0.f, 2 * e + 1 < in ? widen(xr[i][j][2 * e + 1]) : 0.f, t[e]);
-#pragma unroll
-                for (int q = 0; q < TX; ++q) xs[q * C::kEights * C::kXPitch + xto[i] + j * C::kHalf] = u32x4{t[0][q], t[1][q], t[2][q], t[3][q]};
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < C::kWEach; ++i) {
-            const int u = tid + i * kThreads;
-            const int k8 = TRANS ? u / C::BM : u % C::kEights, row = TRANS ? u % C::BM : u / C::kEights;
-            if (C::kWLoads % kThreads != 0 && u >= C::kWLoads) continue;
-            uint32_t t[4][TW];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) terms_of<TW>(wr[i][2 * e], wr[i][2 * e + 1], t[e]);
-#pragma unroll
-            for (int q = 0; q < TW; ++q) ws[(q * C::kEights + k8) * C::kWPitch + row] = u32x4{t[0][q], t[1][q], t[2][q], t[3][q]};
+            for (int q = 0; q < TW; ++q) ws[2 * ((q * 4 + (k4 >> 1)) * C::kPitch + row) + (k4 & 1)] = u32x2{t[0][q], t[1][q]};
         }
     };
 
+    // what is asked for stays in the order it is written in: at a wait for some of it the rest stays under way
+    auto order = [] { __builtin_amdgcn_sched_barrier(0x38f); };
+    X ra[2][8][kLoads], rb[2][8][kLoads];
+    wfetch(0);
+    order();
+    xfetch(0, ra);
+    order();
+    xfetch(1, rb);
+    order();
     float *bias = reinterpret_cast<float *>(product_lds + 2 * C::kBuffer);
-    if (tid < C::BM) bias[tid] = p.b != nullptr && m0 + tid < M ? p.b[m0 + tid] : 0.f;
-    static_assert(C::BM <= kThreads, "a thread for each output's bias");
-
-    f32x16 acc[MT][2];
+    if (tid < 32 * MT) bias[tid] = p.b != nullptr && m0 + tid < M ? p.b[m0 + tid] : 0.f;
+    wput(0);
+    f32x16 acc[MT][NT];
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
+        for (int t = 0; t < NT; ++t)
 #pragma unroll
             for (int i = 0; i < 16; ++i) acc[mt][t][i] = 0.f;
-
-    fetch(0);
-    put(0);
     __syncthreads();
-    for (int st = 0; st < stages; ++st) {
-        if (st + 1 < stages) fetch(st + 1);
-        const u32x4 *xs = product_lds + (st & 1) * C::kBuffer, *ws = xs + C::kXUnits;
-#pragma unroll
-        for (int c = 0; c < C::kEights / 2; ++c) {
-            u32x4 a[MT][TW], b[2][TX];
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int q = 0; q < TX; ++q) b[t][q] = xs[(q * C::kEights + 2 * c + half) * C::kXPitch + t * C::kHalf + 32 * wp + l32];
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-                for (int q = 0; q < TW; ++q) a[mt][q] = ws[(q * C::kEights + 2 * c + half) * C::kWPitch + 32 * (MT * wm + mt) + l32];
-            // small terms first; neighbouring instructions on different sums
-#pragma unroll
-            for (int qw = TW - 1; qw >= 0; --qw)
-#pragma unroll
-                for (int qx = TX - 1; qx >= 0; --qx) {
-                    if (qw + qx >= C::kTop) continue;
-#pragma unroll
-                    for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-                        for (int t = 0; t < 2; ++t)
-                            acc[mt][t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a[mt][qw]), __builtin_bit_cast(bf16x8, b[t][qx]),
-                                                                                 acc[mt][t], 0, 0, 0);
-                }
-        }
-        if (st + 1 < stages) put(st + 1);
-        __syncthreads();
-    }
-    settle();
 
-    // ---- lane l has outputs m0 + 32 (MT wm + mt) + 8 (i / 4) + 4 half + i % 4 of the pixels of places l32 of its two column blocks ----
-    const int px = 64 * wp + 2 * l32;
-    long n0, n1, at0, at1;
-    place(px, n0, at0);
-    place(px + 1, n1, at1);
-    const bool in0 = !p.across || q0 + px < p.pixels, in1 = !p.across || q0 + px + 1 < p.pixels;
-    TO *o0 = static_cast<TO *>(p.out) + n0 * p.out_stride + at0, *o1 = static_cast<TO *>(p.out) + n1 * p.out_stride + at1;
-    const TE *e0 = static_cast<const TE *>(p.extra) + n0 * p.extra_stride + at0, *e1 = static_cast<const TE *>(p.extra) + n1 * p.extra_stride + at1;
-    auto finish = [&](float v, float e) {
-        if constexpr (MODE == kSlope) return e * slope(p.act, v);
-        else return p.extra != nullptr ? activation(p.act, v) + e : activation(p.act, v);
-    };
+    auto body = [&](int st, X (&raw)[2][8][kLoads]) {
+        wfetch(st + 1);
+        order();
+        const u32x4 *ws = product_lds + (st & 1) * C::kBuffer + half * C::kPitch + l32;
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
+        for (int c = 0; c < 2; ++c) {
+            u32x4 b[NT][TX];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const int row = 32 * (MT * wm + mt) + 8 * (i >> 2) + 4 * half + (i & 3), m = m0 + row;
-            const float v0 = acc[mt][0][i] + bias[row], v1 = acc[mt][1][i] + bias[row];
-            if (m >= M) continue;
-            const long off = (long)m * P;
-            if (p.across) {
-                if (in0) {
-                    const float r = finish(v0, p.extra != nullptr ? widen(e0[off]) : 0.f);
-                    if constexpr (kWide<TO>) o0[off] = r;
-                    else o0[off].bits = (uint16_t)pack2(r, r);
-                }
-                if (in1) {
-                    const float r = finish(v1, p.extra != nullptr ? widen(e1[off]) : 0.f);
-                    if constexpr (kWide<TO>) o1[off] = r;
-                    else o1[off].bits = (uint16_t)pack2(r, r);
-                }
-            } else {
-                float x0 = 0.f, x1 = 0.f;
-                if (p.extra != nullptr) {
-                    const Two<TE> e = *reinterpret_cast<const Two<TE> *>(e0 + off);
-                    x0 = widen(e.a), x1 = widen(e.b);
-                }
-                const float r0 = finish(v0, x0), r1 = finish(v1, x1);
-                Two<TO> r;
-                if constexpr (kWide<TO>) {
-                    r.a = r0, r.b = r1;
+            for (int e = 0; e < 4; ++e) {
+                if constexpr (!kWide<TI> && TX == 1 && !ACROSS) {
+                    b[0][0][e] = __builtin_amdgcn_perm(raw[c][2 * e + 1][0].w[0], raw[c][2 * e][0].w[0], 0x05040100u);
+                    if constexpr (NT == 2) b[NT - 1][0][e] = __builtin_amdgcn_perm(raw[c][2 * e + 1][0].w[0], raw[c][2 * e][0].w[0], 0x07060302u);
                 } else {
-                    const uint32_t two = pack2(r0, r1);
-                    r.a.bits = (uint16_t)two, r.b.bits = (uint16_t)(two >> 16);
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) {
+                        constexpr bool one = kLoads > 1;
+                        uint32_t q[TX];
+                        terms_of<TX>(raw[c][2 * e][one ? t : 0].value(one ? 0 : t), raw[c][2 * e + 1][one ? t : 0].value(one ? 0 : t), q);
+#pragma unroll
+                        for (int i = 0; i < TX; ++i) b[t][i][e] = q[i];
+                    }
                 }
-                *reinterpret_cast<Two<TO> *>(o0 + off) = r;
+            }
+            if (c == 1) {
+                order();
+                xfetch(st + 2, raw);
+                order();
+            }
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+                u32x4 a[TW];
+#pragma unroll
+                for (int q = 0; q < TW; ++q) a[q] = ws[(q * 4 + 2 * c) * C::kPitch + 32 * mt];
+                // small terms first; neighbouring instructions on different sums
+#pragma unroll
+                for (int qw = TW - 1; qw >= 0; --qw)
+#pragma unroll
+                    for (int qx = TX - 1; qx >= 0; --qx) {
+                        if (qw + qx >= kTop) continue;
+#pragma unroll
+                        for (int t = 0; t < NT; ++t)
+                            acc[mt][t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a[qw]), __builtin_bit_cast(bf16x8, b[t][qx]),
+                                                                                 acc[mt][t], 0, 0, 0);
+                    }
             }
         }
+        wput(st + 1);
+        __syncthreads();
+    };
+    // (beyond the last stage loads bring nothing, and zeros are put)
+    int st = 0;
+    for (; st + 1 < stages; st += 2) {
+        body(st, ra);
+        body(st + 1, rb);
+    }
+    if (st < stages) body(st, ra);
+    settle();
+
+    // ---- lane l has outputs m0 + 32 mt + 8 (i / 4) + 4 half + i % 4 in element i of its pixels' sums ----
+    auto row_of = [](int i) { return 8 * (i >> 2) + (i & 3); };
+    const unsigned ob = (unsigned)p.P * (unsigned)sizeof(TO), eb = (unsigned)p.P * (unsigned)sizeof(TE);
+    const bool has = p.extra != nullptr;
+    const Rsrc ro = resource(static_cast<TO *>(p.out) + image * p.out_stride, ACROSS ? 0 : (long)M * ob);
+    const Rsrc re = resource(has ? static_cast<const TE *>(p.extra) + image * p.extra_stride : nullptr, ACROSS || !has ? 0 : (long)M * eb);
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+        const int left = M - (m0 + 32 * mt) - 4 * half;
+        float v[NT * 16], e[NT * 16];
+#pragma unroll
+        for (int i = 0; i < NT * 16; ++i) e[i] = 0.f;
+        if (has) {
+            if constexpr (ACROSS) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+#pragma unroll
+                    for (int t = 0; t < NT; ++t)
+                        e[16 * t + i] = widen(static_cast<const TE *>(p.extra)[pn[t] * p.extra_stride + (long)min(m0 + 32 * mt + 4 * half + row_of(i), M - 1) * p.P + pat[t]]);
+            } else {
+                const unsigned off = (unsigned)(m0 + 32 * mt + 4 * half) * eb + pxc * (unsigned)sizeof(TE);
+                Raw<TE, NT> ex[16];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) ex[i] = load<TE, NT>(re, row_of(i) < left ? off : kBeyond, (unsigned)row_of(i) * eb);
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) e[16 * t + i] = ex[i].value(t);
+            }
+        }
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) v[16 * t + i] = acc[mt][t][i] + bias[32 * mt + 4 * half + row_of(i)];
+        if constexpr (MODE == kSlope) {
+            slopes(p.act, v);
+#pragma unroll
+            for (int i = 0; i < NT * 16; ++i) v[i] *= e[i];
+        } else {
+            activate(p.act, v);
+#pragma unroll
+            for (int i = 0; i < NT * 16; ++i) v[i] += e[i];
+        }
+        if constexpr (ACROSS) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+                    if (there[t] && row_of(i) < left) {
+                        TO *to = static_cast<TO *>(p.out) + pn[t] * p.out_stride + (long)(m0 + 32 * mt + 4 * half + row_of(i)) * p.P + pat[t];
+                        if constexpr (kWide<TO>) *to = v[16 * t + i];
+                        else to->bits = (uint16_t)pack2(v[16 * t + i], 0.f);
+                    }
+        } else {
+            const unsigned off = (unsigned)(m0 + 32 * mt + 4 * half) * ob + pxc * (unsigned)sizeof(TO);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) store<TO, NT>(ro, row_of(i) < left ? off : kBeyond, (unsigned)row_of(i) * ob, v[i], v[16 * (NT - 1) + i]);
+        }
+    }
 }
 
-template <typename TI, typename TO, typename TE, int TX, int TW, int MT, int WM, int WP, bool TRANS, int MODE>
-hipError_t launch_product_as(ProductParams p, long N, hipStream_t s)
+template <typename TI, typename TO, typename TE, int TX, int TW, int MT, int NT, bool TRANS, int MODE, bool ACROSS>
+hipError_t launch_as(ProductParams p, long N, hipStream_t s)
 {
-    using C = Product<TI, TO, TE, TX, TW, MT, WM, WP, TRANS, MODE>;
-    const long groups = (p.M + C::BM - 1) / C::BM, apart = N * ((p.P + C::BP - 1) / C::BP), together = (p.pixels + C::BP - 1) / C::BP;
-    // small images share tiles (single pixels have no pair to load at once)
-    p.across = N > 1 ? p.P < 2 || 4 * together < 3 * apart : p.P < 2;
-    p.tiles = p.across ? together : apart / N;
-    const long grid = (p.across ? together : apart) * groups;
+    using C = Streamed<MT, TW>;
+    p.tiles = ((ACROSS ? p.pixels : p.P) + 128 * NT - 1) / (128 * NT);
+    const long grid = p.tiles * (ACROSS ? 1 : N) * ((p.M + 32 * MT - 1) / (32 * MT));
     if (grid >= (1L << 31)) return hipErrorInvalidValue;
-    const auto kernel = product_kernel<TI, TO, TE, TX, TW, MT, WM, WP, TRANS, MODE>;
-    if (C::kLds > 64 * 1024) {
-        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
-        if (e != hipSuccess) return e;
-    }
+    const auto kernel = product_kernel<TI, TO, TE, TX, TW, MT, NT, TRANS, MODE, ACROSS>;
+    static_assert(C::kLds <= 64 * 1024, "");
     hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(kThreads), C::kLds, s, p);
     return hipGetLastError();
 }
@@ -271,8 +282,14 @@ hipError_t launch_product_as(ProductParams p, long N, hipStream_t s)
 template <typename TI, typename TO, typename TE, int TX, int TW, bool TRANS, int MODE>
 hipError_t launch_product(const ProductParams &p, long N, hipStream_t s)
 {
-    if (p.M > 64) return launch_product_as<TI, TO, TE, TX, TW, 2, 2, 2, TRANS, MODE>(p, N, s);
-    return launch_product_as<TI, TO, TE, TX, TW, 2, 1, 4, TRANS, MODE>(p, N, s);
+    // small images share tiles; their pixels, and those of images beyond 2 GiB, go one by one
+    const size_t widest = std::max(std::max(p.K * sizeof(TI), p.M * sizeof(TO)), p.M * sizeof(TE)) * (size_t)p.P;
+    if (widest >= kMostImage || p.P < 2 || (N > 1 && p.P < 96)) return launch_as<TI, TO, TE, TX, TW, 2, 1, TRANS, MODE, true>(p, N, s);
+    const auto blocks = [&](int mt, int nt) { return N * ((p.P + 128 * nt - 1) / (128 * nt)) * ((p.M + 32 * mt - 1) / (32 * mt)); };
+    // as much for a wavefront as leaves every compute unit two blocks
+    if (p.M > 64 && blocks(4, 2) >= 2 * kCus) return launch_as<TI, TO, TE, TX, TW, 4, 2, TRANS, MODE, false>(p, N, s);
+    if (blocks(2, 2) >= 2 * kCus) return launch_as<TI, TO, TE, TX, TW, 2, 2, TRANS, MODE, false>(p, N, s);
+    return launch_as<TI, TO, TE, TX, TW, 2, 1, TRANS, MODE, false>(p, N, s);
 }
 
 hipError_t launch_any(int kind, const ProductParams &p, long N, hipStream_t s)
@@ -293,77 +310,118 @@ hipError_t launch_any(int kind, const ProductParams &p, long N, hipStream_t s)
 
 // ---- grad_w[m, k] = sum over pixels of g[m, q] x[k, q], grad_b[m] = sum over pixels of g[m, q] ----
 
-constexpr int kSide = 64;     // of a block's tile of grad_w; a wavefront has 32 x 32
 constexpr int kPixels = 32;   // of a stage
 
 struct WeightParams {
     const void *g, *x;
     long g_stride, x_stride;
     float *part, *part_b;     // [splits][M][K], [splits][M], or nullptr
-    int K, M, splits;
+    int K, M, splits, tiles, across;   // (tiles of grad_w, and those side by side)
     long P, pixels;
 };
 
+// A run of pixels of one row, 16 bytes of it.
 template <typename T>
-struct __attribute__((packed, aligned(sizeof(T)))) Eight {
-    T e[8];
+struct __attribute__((packed, aligned(sizeof(T)))) Run {
+    static constexpr int kCount = 16 / (int)sizeof(T);
+    T e[kCount];
 };
 
-template <typename TG, typename TI, int QG, int QX>
+// One operand of a block's tile: ROWS rows, staged as units of eight consecutive pixels, [term][eighth of the stage][row].
+template <typename T, int Q, int ROWS>
+struct Staged {
+    typedef Run<T> R;
+    static constexpr int kEights = kPixels / 8, kPitch = ROWS + 2, kUnits = Q * kEights * kPitch;
+    static constexpr int kRunsOfRow = kPixels / R::kCount, kEach = ROWS * kRunsOfRow / kThreads;
+    R r[kEach];
+    __device__ __forceinline__ static int row_of(int i) { return ((int)threadIdx.x + i * kThreads) / kRunsOfRow; }
+    __device__ __forceinline__ static int run_of(int i) { return ((int)threadIdx.x + i * kThreads) % kRunsOfRow; }
+    // Rows first, first + 1, ... (the last one's again beyond it) of a stage that lies in one image, `at` its first pixel there.
+    __device__ __forceinline__ void whole(const T *image, long P, long at, int first, int rows)
+    {
+#pragma unroll
+        for (int i = 0; i < kEach; ++i)
+            r[i] = *reinterpret_cast<const R *>(image + (long)min(first + row_of(i), rows - 1) * P + at + R::kCount * run_of(i));
+    }
+    // The same of a stage that begins with pixel q of all images' and lies where it likes: pixel by pixel, zeros beyond the last.
+    __device__ __forceinline__ void scattered(const T *base, long stride, long P, long pixels, long q, int first, int rows)
+    {
+#pragma unroll
+        for (int i = 0; i < kEach; ++i)
+#pragma unroll
+            for (int j = 0; j < R::kCount; ++j) {
+                const long mine = q + R::kCount * run_of(i) + j, one = min(mine, pixels - 1), n = one / P;
+                r[i].e[j] = mine < pixels ? base[n * stride + (long)min(first + row_of(i), rows - 1) * P + one - n * P] : T{};
+            }
+    }
+    __device__ __forceinline__ void put(u32x4 *lds, float *sums) const
+    {
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            if constexpr (R::kCount == 4) {
+                uint32_t t[2][Q];
+                terms_of<Q>(widen(r[i].e[0]), widen(r[i].e[1]), t[0]);
+                terms_of<Q>(widen(r[i].e[2]), widen(r[i].e[3]), t[1]);
+#pragma unroll
+                for (int q = 0; q < Q; ++q)
+                    reinterpret_cast<uint2 *>(lds + (q * kEights + (run_of(i) >> 1)) * kPitch + row_of(i))[run_of(i) & 1] = uint2{t[0][q], t[1][q]};
+                if (sums != nullptr) sums[i] += (widen(r[i].e[0]) + widen(r[i].e[1])) + (widen(r[i].e[2]) + widen(r[i].e[3]));
+            } else {
+                static_assert(R::kCount == 4 || Q == 1, "two bytes an element are a term each");
+                lds[run_of(i) * kPitch + row_of(i)] = __builtin_bit_cast(u32x4, r[i]);
+                if (sums != nullptr) {
+#pragma unroll
+                    for (int j = 0; j < 8; j += 2) sums[i] += widen(r[i].e[j]) + widen(r[i].e[j + 1]);
+                }
+            }
+        }
+    }
+};
+
+// A block's tile of grad_w is 64 MT x 64 KT, a wavefront's 32 MT x 32 KT.
+template <typename TG, typename TI, int QG, int QX, int MT, int KT>
 __global__ __launch_bounds__(kThreads, 2) void product_weights_kernel(const WeightParams p)
 {
-    constexpr int kTop = QG > QX ? QG : QX, kPitch = kSide + 2, kEights = kPixels / 8;
-    __shared__ u32x4 s[2][(QG + QX) * kEights * kPitch];
-    __shared__ float s_b[kThreads];
+    constexpr int kTop = QG > QX ? QG : QX, BM = 64 * MT, BK = 64 * KT;
+    typedef Staged<TG, QG, BM> G;
+    typedef Staged<TI, QX, BK> X;
+    __shared__ u32x4 s[2][G::kUnits + X::kUnits];
     const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l32 = lane & 31, half = lane >> 5, wm = wave & 1, wk = wave >> 1;
-    const int across = (p.K + kSide - 1) / kSide;
-    const int m0 = (int)blockIdx.x / across * kSide, k0 = (int)blockIdx.x % across * kSide;
+    // the tiles of a split, which read the same pixels, follow one another on one die
+    const unsigned piece = piece_of(blockIdx.x, gridDim.x), split = piece / (unsigned)p.tiles;
+    const int tile = (int)(piece - split * (unsigned)p.tiles), m0 = tile / p.across * BM, k0 = tile % p.across * BK;
     const long stages = (p.pixels + kPixels - 1) / kPixels;
-    const long first = stages * blockIdx.y / p.splits, end = stages * (blockIdx.y + 1) / p.splits;
-    const int row = tid >> 2, e8 = tid & 3;  // this thread's unit of both operands: eight pixels of a row
-    const int gm = min(m0 + row, p.M - 1), xk = min(k0 + row, p.K - 1);
-    TG gr[8];
-    TI xr[8];
-    int in = 0;
+    const long first = stages * split / p.splits, end = stages * (split + 1) / p.splits;
+    const TG *const gp = static_cast<const TG *>(p.g);
+    const TI *const xp = static_cast<const TI *>(p.x);
+    G g;
+    X x;
     auto fetch = [&](long st) {
         const long q = st * kPixels, n = q / p.P, at = q - n * p.P;
         if (at + kPixels <= p.P) {  // (the same for the block)
-            const Eight<TG> a = *reinterpret_cast<const Eight<TG> *>(static_cast<const TG *>(p.g) + n * p.g_stride + gm * p.P + at + 8 * e8);
-            const Eight<TI> b = *reinterpret_cast<const Eight<TI> *>(static_cast<const TI *>(p.x) + n * p.x_stride + xk * p.P + at + 8 * e8);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) gr[j] = a.e[j], xr[j] = b.e[j];
-            in = 8;
+            g.whole(gp + n * p.g_stride, p.P, at, m0, p.M);
+            x.whole(xp + n * p.x_stride, p.P, at, k0, p.K);
         } else {
-            const long mine = q + 8 * e8;
-            in = (int)(p.pixels - mine < 0 ? 0 : p.pixels - mine < 8 ? p.pixels - mine : 8);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const long one = min(mine + j, p.pixels - 1), i = one / p.P, a = one - i * p.P;
-                gr[j] = static_cast<const TG *>(p.g)[i * p.g_stride + gm * p.P + a];
-                xr[j] = static_cast<const TI *>(p.x)[i * p.x_stride + xk * p.P + a];
-            }
+            g.scattered(gp, p.g_stride, p.P, p.pixels, q, m0, p.M);
+            x.scattered(xp, p.x_stride, p.P, p.pixels, q, k0, p.K);
         }
     };
-    float sum_b = 0.f;
+    const bool has_b = p.part_b != nullptr && k0 == 0;
+    float sums[G::kEach];
+#pragma unroll
+    for (int i = 0; i < G::kEach; ++i) sums[i] = 0.f;
     auto put = [&](int buffer) {
-        uint32_t t[4][QG], u[4][QX];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const float a0 = 2 * j < in ? widen(gr[2 * j]) : 0.f, a1 = 2 * j + 1 < in ? widen(gr[2 * j + 1]) : 0.f;
-            const float b0 = 2 * j < in ? widen(xr[2 * j]) : 0.f, b1 = 2 * j + 1 < in ? widen(xr[2 * j + 1]) : 0.f;
-            sum_b += a0 + a1;
-            terms_of<QG>(a0, a1, t[j]);
-            terms_of<QX>(b0, b1, u[j]);
-        }
-#pragma unroll
-        for (int q = 0; q < QG; ++q) s[buffer][(q * kEights + e8) * kPitch + row] = u32x4{t[0][q], t[1][q], t[2][q], t[3][q]};
-#pragma unroll
-        for (int q = 0; q < QX; ++q) s[buffer][((QG + q) * kEights + e8) * kPitch + row] = u32x4{u[0][q], u[1][q], u[2][q], u[3][q]};
+        g.put(s[buffer], has_b ? sums : nullptr);
+        x.put(s[buffer] + G::kUnits, nullptr);
     };
-    f32x16 acc;
+    f32x16 acc[MT][KT];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) acc[i] = 0.f;
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < KT; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
     if (first < end) {
         fetch(first);
         put(0);
@@ -372,45 +430,88 @@ __global__ __launch_bounds__(kThreads, 2) void product_weights_kernel(const Weig
     for (long st = first; st < end; ++st) {
         const int buffer = (int)(st - first) & 1;
         if (st + 1 < end) fetch(st + 1);
+        const u32x4 *gs = s[buffer] + 32 * MT * wm + l32, *xs = s[buffer] + G::kUnits + 32 * KT * wk + l32;
 #pragma unroll
-        for (int c = 0; c < kEights / 2; ++c) {
-            u32x4 a[QG], b[QX];
+        for (int c = 0; c < kPixels / 16; ++c) {
+            u32x4 a[MT][QG], b[KT][QX];
 #pragma unroll
-            for (int q = 0; q < QG; ++q) a[q] = s[buffer][(q * kEights + 2 * c + half) * kPitch + 32 * wm + l32];
+            for (int j = 0; j < KT; ++j)
 #pragma unroll
-            for (int q = 0; q < QX; ++q) b[q] = s[buffer][((QG + q) * kEights + 2 * c + half) * kPitch + 32 * wk + l32];
+                for (int q = 0; q < QX; ++q) b[j][q] = xs[(q * X::kEights + 2 * c + half) * X::kPitch + 32 * j];
 #pragma unroll
-            for (int i = QG - 1; i >= 0; --i)
+            for (int i = 0; i < MT; ++i)
 #pragma unroll
-                for (int j = QX - 1; j >= 0; --j)
-                    if (i + j < kTop)
-                        acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a[i]), __builtin_bit_cast(bf16x8, b[j]), acc, 0, 0, 0);
+                for (int q = 0; q < QG; ++q) a[i][q] = gs[(q * G::kEights + 2 * c + half) * G::kPitch + 32 * i];
+#pragma unroll
+            for (int qg = QG - 1; qg >= 0; --qg)
+#pragma unroll
+                for (int qx = QX - 1; qx >= 0; --qx) {
+                    if (qg + qx >= kTop) continue;
+#pragma unroll
+                    for (int i = 0; i < MT; ++i)
+#pragma unroll
+                        for (int j = 0; j < KT; ++j)
+                            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a[i][qg]), __builtin_bit_cast(bf16x8, b[j][qx]), acc[i][j], 0, 0, 0);
+                }
         }
         if (st + 1 < end) put(buffer ^ 1);
         __syncthreads();
     }
     settle();
     if (p.part != nullptr) {
-        const int k = k0 + 32 * wk + l32;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const int m = m0 + 32 * wm + 8 * (i >> 2) + 4 * half + (i & 3);
-            const float v = acc[i];
-            if (m < p.M && k < p.K) p.part[((size_t)blockIdx.y * p.M + m) * p.K + k] = v;
-        }
+        for (int t = 0; t < MT; ++t)
+#pragma unroll
+            for (int j = 0; j < KT; ++j) {
+                const int k = k0 + 32 * (KT * wk + j) + l32;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int m = m0 + 32 * (MT * wm + t) + 8 * (i >> 2) + 4 * half + (i & 3);
+                    const float v = acc[t][j][i];
+                    if (m < p.M && k < p.K) p.part[((size_t)split * p.M + m) * p.K + k] = v;
+                }
+            }
     }
-    if (p.part_b != nullptr && k0 == 0) {
-        s_b[tid] = sum_b;
+    if (has_b) {
+        // a row's runs are neighbouring threads'
+        float *const all = reinterpret_cast<float *>(s[0]);
+#pragma unroll
+        for (int i = 0; i < G::kEach; ++i) all[tid + i * kThreads] = sums[i];
         __syncthreads();
-        if (tid < kSide && m0 + tid < p.M) p.part_b[(size_t)blockIdx.y * p.M + m0 + tid] = (s_b[4 * tid] + s_b[4 * tid + 1]) + (s_b[4 * tid + 2] + s_b[4 * tid + 3]);
+        if (tid < BM && m0 + tid < p.M) {
+            float t = 0.f;
+#pragma unroll
+            for (int j = 0; j < G::kRunsOfRow; ++j) t += all[tid * G::kRunsOfRow + j];
+            p.part_b[(size_t)split * p.M + m0 + tid] = t;
+        }
     }
 }
 
-template <typename TG, typename TI, int QG, int QX>
-hipError_t launch_weights(const WeightParams &p, hipStream_t s)
+// A block's sides of grad_w in 64s: 128 where there are more than 64 channels, but one of them alone where six terms take all the LDS.
+struct Sides {
+    int mt, kt;
+};
+Sides sides_of(int M, int K, bool f32)
 {
-    const unsigned tiles = (unsigned)(((p.M + kSide - 1) / kSide) * ((p.K + kSide - 1) / kSide));
-    hipLaunchKernelGGL((product_weights_kernel<TG, TI, QG, QX>), dim3(tiles, p.splits), dim3(kThreads), 0, s, p);
+    const int mt = M > 64 ? 2 : 1;
+    return Sides{mt, K > 64 && !(f32 && mt == 2) ? 2 : 1};
+}
+
+template <typename TG, typename TI, int QG, int QX>
+hipError_t launch_weights(WeightParams p, hipStream_t s)
+{
+    const auto [mt, kt] = sides_of(p.M, p.K, kWide<TI>);
+    p.across = (p.K + 64 * kt - 1) / (64 * kt), p.tiles = p.across * ((p.M + 64 * mt - 1) / (64 * mt));
+    const dim3 grid((unsigned)p.tiles * (unsigned)p.splits), block(kThreads);
+    if constexpr (!kWide<TI>) {
+        if (mt == 2 && kt == 2) {
+            hipLaunchKernelGGL((product_weights_kernel<TG, TI, QG, QX, 2, 2>), grid, block, 0, s, p);
+            return hipGetLastError();
+        }
+    }
+    if (mt == 2) hipLaunchKernelGGL((product_weights_kernel<TG, TI, QG, QX, 2, 1>), grid, block, 0, s, p);
+    else if (kt == 2) hipLaunchKernelGGL((product_weights_kernel<TG, TI, QG, QX, 1, 2>), grid, block, 0, s, p);
+    else hipLaunchKernelGGL((product_weights_kernel<TG, TI, QG, QX, 1, 1>), grid, block, 0, s, p);
     return hipGetLastError();
 }
 
@@ -422,24 +523,26 @@ esc_status shape(const esc_pointwise *a, long *P)
     if (a->N < 1 || a->K < 1 || a->M < 1 || a->H < 1 || a->W < 1) return ESC_ERR_SHAPE;
     if (a->act != ESC_ACT_NONE && a->act != ESC_ACT_GELU && a->act != ESC_ACT_SILU) return ESC_ERR_SHAPE;
     *P = (long)a->H * a->W;
-    if (a->K > 65536 || a->M > 65536 || *P >= (1L << 31) || (double)*P * a->N >= 0x1p40) return ESC_ERR_UNSUPPORTED;
+    if (a->K > 65536 || a->M > 65536 || (long)a->K * a->M >= (1L << 29) || *P >= (1L << 31) || (double)*P * a->N >= 0x1p40) return ESC_ERR_UNSUPPORTED;
     return ESC_OK;
 }
 
-// blocks for the whole card a few times over, 16 stages each at least
-int splits_of(const esc_pointwise *a, long P)
+// Shares of the pixels: two blocks a compute unit, four stages each at least.
+int splits_of(const esc_pointwise *a, long P, bool f32)
 {
-    const long tiles = (long)((a->M + kSide - 1) / kSide) * ((a->K + kSide - 1) / kSide), stages = ((long)a->N * P + kPixels - 1) / kPixels;
-    return (int)std::max<long>(1, std::min((4 * kCus + tiles - 1) / tiles, stages / 16));
+    const Sides side = sides_of(a->M, a->K, f32);
+    const long mt = 64 * side.mt, kt = 64 * side.kt;
+    const long tiles = ((a->M + mt - 1) / mt) * ((a->K + kt - 1) / kt), stages = ((long)a->N * P + kPixels - 1) / kPixels;
+    return (int)std::max<long>(1, std::min((2 * kCus + tiles - 1) / tiles, stages / 4));
 }
 
 struct Scratch {
     size_t gp, part, part_b, total;
 };
-Scratch scratch(const esc_pointwise *a, long P)
+Scratch scratch(const esc_pointwise *a, long P, bool f32)
 {
     Scratch s;
-    const size_t splits = (size_t)splits_of(a, P);
+    const size_t splits = (size_t)splits_of(a, P, f32);
     s.gp = 0;
     s.part = a->act != ESC_ACT_NONE ? round_up((size_t)a->N * P * a->M * 4, kAlign) : 0;
     s.part_b = s.part + round_up(splits * a->M * a->K * 4, kAlign);
@@ -454,7 +557,7 @@ extern "C" {
 size_t esc_pointwise_backward_workspace_bytes(const esc_pointwise *a, esc_dtype dt)
 {
     long P;
-    return (dt == ESC_F32 || dt == ESC_BF16) && shape(a, &P) == ESC_OK ? scratch(a, P).total : 0;
+    return (dt == ESC_F32 || dt == ESC_BF16) && shape(a, &P) == ESC_OK ? scratch(a, P, dt == ESC_F32).total : 0;
 }
 
 esc_status esc_pointwise_forward(const void *x, const void *residual, esc_dtype dt, const esc_pointwise *a, void *out, void *stream)
@@ -494,7 +597,7 @@ esc_status esc_pointwise_backward(const void *x, const void *grad_out, esc_dtype
     if (!images_of(x, a->x_stride, a->N, (size_t)a->K * P, es, &xi) || !images_of(grad_out, a->out_stride, a->N, (size_t)a->M * P, es, &gi)) return ESC_ERR_SHAPE;
     if (g->x != nullptr && !images_of(g->x, g->x_stride, a->N, (size_t)a->K * P, es, &gxi)) return ESC_ERR_SHAPE;
     if (((uintptr_t)a->w | (uintptr_t)a->b | (uintptr_t)g->w | (uintptr_t)g->b) % 4 != 0) return ESC_ERR_SHAPE;
-    const Scratch sc = scratch(a, P);
+    const Scratch sc = scratch(a, P, f32);
     if (workspace == nullptr || (uintptr_t)workspace % kAlign != 0 || workspace_bytes < sc.total) return ESC_ERR_WORKSPACE;
     // what is written overlaps nothing else
     const struct {
@@ -537,7 +640,7 @@ esc_status esc_pointwise_backward(const void *x, const void *grad_out, esc_dtype
         p.g = act ? mem : grad_out, p.x = x, p.g_stride = act ? (long)a->M * P : g_stride, p.x_stride = x_stride;
         p.part = g->w != nullptr ? reinterpret_cast<float *>(mem + sc.part) : nullptr;
         p.part_b = g->b != nullptr ? reinterpret_cast<float *>(mem + sc.part_b) : nullptr;
-        p.K = a->K, p.M = a->M, p.splits = splits_of(a, P), p.P = P, p.pixels = P * a->N;
+        p.K = a->K, p.M = a->M, p.splits = splits_of(a, P, f32), p.P = P, p.pixels = P * a->N;
         const hipError_t e = f32 ? launch_weights<float, float, 3, 3>(p, s) : act ? launch_weights<float, bf16s, 3, 1>(p, s) : launch_weights<bf16s, bf16s, 1, 1>(p, s);
         if (e != hipSuccess) return ESC_ERR_HIP;
         if (g->w != nullptr && add_parts(p.part, p.splits, (long)a->M * a->K, g->w, 0, nullptr, accumulate, s) != hipSuccess) return ESC_ERR_HIP;

@@ -17,8 +17,7 @@ struct ProductParams {
     const float *w, *b;
     int K, M, w_ld, act;
     long P, pixels;        // of an image, of all
-    long tiles;            // of an image (or of all, where tiles pass images' borders)
-    bool across;           // tiles pass images' borders
+    long tiles;            // of pixels, of an image (or of all, where they pass images' borders)
 };
 
 namespace {
@@ -138,6 +137,81 @@ __device__ __forceinline__ void slopes(int act, float (&v)[N])
 }
 // kForward: out = act(pre) + extra.  kSlope: out = extra act'(pre), fp32.
 enum : int { kForward = 0, kSlope = 1 };
+
+// ---- accesses to an image's planes by 32-bit offsets ----
+
+typedef __amdgpu_buffer_rsrc_t Rsrc;
+typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kRawBuffer = 0x00020000;     // raw buffer (no stride, no swizzle), 32-bit data format
+constexpr unsigned kBeyond = 0x80000000u;  // an offset beyond every resource (an image of a tensor is < 2 GiB)
+constexpr size_t kMostImage = (size_t)1 << 31;
+
+__device__ __forceinline__ Rsrc resource(const void *at, long bytes)
+{
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(at), 0, (int)bytes, kRawBuffer);
+}
+
+// NT neighbouring elements of a lane, as words.
+template <typename T, int NT>
+struct Raw {
+    static constexpr int kWords = NT * (int)sizeof(T) == 8 ? 2 : 1;
+    uint32_t w[kWords];
+    __device__ __forceinline__ float value(int t) const
+    {
+        if constexpr (kWide<T>) return __uint_as_float(w[t]);
+        else return __uint_as_float(t == 0 ? w[0] << 16 : w[0] & 0xffff0000u);
+    }
+};
+template <typename T, int NT>
+__device__ __forceinline__ Raw<T, NT> load(Rsrc r, unsigned voff, unsigned soff)
+{
+    Raw<T, NT> v;
+    if constexpr (Raw<T, NT>::kWords == 2) {
+        const u32x2 two = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(r, (int)voff, (int)soff, 0));
+        v.w[0] = two.x, v.w[1] = two.y;
+    } else if constexpr (NT * sizeof(T) == 4) {
+        v.w[0] = (unsigned)__builtin_amdgcn_raw_buffer_load_b32(r, (int)voff, (int)soff, 0);
+    } else {
+        v.w[0] = (unsigned)__builtin_amdgcn_raw_buffer_load_b16(r, (int)voff, (int)soff, 0);
+    }
+    return v;
+}
+template <typename T, int NT>
+__device__ __forceinline__ void store(Rsrc r, unsigned voff, unsigned soff, float a, float b)
+{
+    if constexpr (NT * sizeof(T) == 8) {
+        typedef decltype(__builtin_amdgcn_raw_buffer_load_b64(r, 0, 0, 0)) B64;
+        __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(B64, u32x2{__float_as_uint(a), __float_as_uint(b)}), r, (int)voff, (int)soff, 0);
+    } else if constexpr (kWide<T>) {
+        __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(a), r, (int)voff, (int)soff, 0);
+    } else if constexpr (NT == 2) {
+        __builtin_amdgcn_raw_buffer_store_b32(pack2(a, b), r, (int)voff, (int)soff, 0);
+    } else {
+        __builtin_amdgcn_raw_buffer_store_b16((unsigned short)pack2(a, a), r, (int)voff, (int)soff, 0);
+    }
+}
+
+// ---- weights: runs of four channels of one output, zeros beyond K and M ----
+
+// Four weights of output m from channel k on (TRANS: w's rows are the channels).  FOUR: K is a multiple of four, a run is inside or outside as a whole.
+template <bool TRANS>
+__device__ __forceinline__ void load_weights(Rsrc rw, const ProductParams &p, bool four, int m, int k, float (&w)[4])
+{
+    if (!TRANS && four) {
+        const u32x4 v = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rw, (int)(m < p.M && k < p.K ? 4u * ((unsigned)m * (unsigned)p.w_ld + (unsigned)k) : kBeyond), 0, 0));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] = __uint_as_float(v[e]);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const unsigned at = TRANS ? (unsigned)(k + e) * (unsigned)p.w_ld + (unsigned)m : (unsigned)m * (unsigned)p.w_ld + (unsigned)(k + e);
+            w[e] = __uint_as_float((unsigned)__builtin_amdgcn_raw_buffer_load_b32(rw, (int)(m < p.M && k + e < p.K ? 4u * at : kBeyond), 0, 0));
+        }
+    }
+}
+__device__ __forceinline__ Rsrc weights_of(const ProductParams &p) { return resource(p.w, 4L * p.K * p.M); }
 
 // Which eighths of the grid the dies get: consecutive pieces on one die.
 __device__ __forceinline__ unsigned piece_of(unsigned block, unsigned blocks)

@@ -12,59 +12,6 @@
 namespace esc {
 namespace {
 
-typedef __amdgpu_buffer_rsrc_t Rsrc;
-typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-
-constexpr int kRawBuffer = 0x00020000;     // raw buffer (no stride, no swizzle), 32-bit data format
-constexpr unsigned kBeyond = 0x80000000u;  // an offset beyond every resource (an image of a tensor is < 2 GiB)
-constexpr size_t kMostImage = (size_t)1 << 31;
-
-__device__ __forceinline__ Rsrc resource(const void *at, long bytes)
-{
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(at), 0, (int)bytes, kRawBuffer);
-}
-
-// NT neighbouring elements of a lane, as words.
-template <typename T, int NT>
-struct Raw {
-    static constexpr int kWords = NT * (int)sizeof(T) == 8 ? 2 : 1;
-    uint32_t w[kWords];
-    __device__ __forceinline__ float value(int t) const
-    {
-        if constexpr (kWide<T>) return __uint_as_float(w[t]);
-        else return __uint_as_float(t == 0 ? w[0] << 16 : w[0] & 0xffff0000u);
-    }
-};
-template <typename T, int NT>
-__device__ __forceinline__ Raw<T, NT> load(Rsrc r, unsigned voff, unsigned soff)
-{
-    Raw<T, NT> v;
-    if constexpr (Raw<T, NT>::kWords == 2) {
-        const u32x2 two = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(r, (int)voff, (int)soff, 0));
-        v.w[0] = two.x, v.w[1] = two.y;
-    } else if constexpr (NT * sizeof(T) == 4) {
-        v.w[0] = (unsigned)__builtin_amdgcn_raw_buffer_load_b32(r, (int)voff, (int)soff, 0);
-    } else {
-        v.w[0] = (unsigned)__builtin_amdgcn_raw_buffer_load_b16(r, (int)voff, (int)soff, 0);
-    }
-    return v;
-}
-template <typename T, int NT>
-__device__ __forceinline__ void store(Rsrc r, unsigned voff, unsigned soff, float a, float b)
-{
-    if constexpr (NT * sizeof(T) == 8) {
-        typedef decltype(__builtin_amdgcn_raw_buffer_load_b64(r, 0, 0, 0)) B64;
-        __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(B64, u32x2{__float_as_uint(a), __float_as_uint(b)}), r, (int)voff, (int)soff, 0);
-    } else if constexpr (kWide<T>) {
-        __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(a), r, (int)voff, (int)soff, 0);
-    } else if constexpr (NT == 2) {
-        __builtin_amdgcn_raw_buffer_store_b32(pack2(a, b), r, (int)voff, (int)soff, 0);
-    } else {
-        __builtin_amdgcn_raw_buffer_store_b16((unsigned short)pack2(a, a), r, (int)voff, (int)soff, 0);
-    }
-}
-
 // Weights of a chunk in LDS: units of eight consecutive channels of one output, [channels / 16][term][half of the sixteen][output], halves a unit
 // further apart than outputs take (other banks for a thread's neighbours, who write other eighths of the same output).
 constexpr int kPitch = 33;
@@ -86,7 +33,7 @@ template <typename TI, typename TO, typename TE, int TX, int TW, int KC, int NT,
 __global__ __launch_bounds__(kThreads, 2) void strip_kernel(const StripParams p)
 {
     constexpr int kTop = TX > TW ? TX : TW;      // products of terms whose orders add up to less
-    constexpr int kUnits = 64 * KC, kEach = (kUnits + kThreads - 1) / kThreads;  // runs of eight weights of a chunk, of a thread
+    constexpr int kRuns = 128 * KC, kEach = kRuns / kThreads;  // runs of four weights of a chunk, of a thread
     const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l32 = lane & 31, half = lane >> 5;
     const int K = p.K, M = p.M;
@@ -98,48 +45,35 @@ __global__ __launch_bounds__(kThreads, 2) void strip_kernel(const StripParams p)
     const unsigned pxc = px + NT <= P ? px : P - NT;
 
     // ---- weights ----
-    struct __attribute__((packed, aligned(4))) W4 {
-        float v[4];
-    };
-    const bool k8 = (K & 7) == 0;   // a run of eight is inside or outside as a whole
-    float wr[kEach][8];
+    const Rsrc rw = weights_of(p);
+    const bool four = (K & 3) == 0;
+    float wr[kEach][4];
     float br = 0.f;
+    // (a row's runs, neighbours in memory, by neighbouring threads; TRANS: a channel's outputs)
+    auto run_of = [&](int i, int &row, int &k4) {
+        const int u = tid + i * kThreads;
+        row = TRANS ? u & 31 : u / (4 * KC), k4 = TRANS ? u >> 5 : u % (4 * KC);
+    };
     auto wfetch = [&](int chunk) {
         br = p.b != nullptr && tid < 32 ? p.b[min(32 * chunk + tid, M - 1)] : 0.f;
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
-            const int u = tid + i * kThreads;
-            const int row = TRANS ? u & 31 : u / (2 * KC), e8 = TRANS ? u >> 5 : u % (2 * KC);
-            const int m = 32 * chunk + row, k = 8 * e8;
-            if constexpr (TRANS) {
-                const float *s = p.w + min(m, M - 1);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) wr[i][e] = s[(size_t)min(k + e, K - 1) * p.w_ld];
-            } else if (k8) {
-                const float *s = p.w + (m < M && k < K ? (size_t)m * p.w_ld + k : 0);
-                const W4 a = *reinterpret_cast<const W4 *>(s), b = *reinterpret_cast<const W4 *>(s + 4);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) wr[i][e] = a.v[e], wr[i][4 + e] = b.v[e];
-            } else {
-                const float *s = p.w + (size_t)min(m, M - 1) * p.w_ld;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) wr[i][e] = s[min(k + e, K - 1)];
-            }
+            int row, k4;
+            run_of(i, row, k4);
+            load_weights<TRANS>(rw, p, four, 32 * chunk + row, 4 * k4, wr[i]);
         }
     };
-    auto wput = [&](int chunk, int buffer) {
-        u32x4 *ws = strip_lds + buffer * StripLds<KC, TW>::kUnits;
+    auto wput = [&](int buffer) {
+        u32x2 *ws = reinterpret_cast<u32x2 *>(strip_lds + buffer * StripLds<KC, TW>::kUnits);
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
-            const int u = tid + i * kThreads;
-            if (kUnits % kThreads != 0 && u >= kUnits) break;
-            const int row = TRANS ? u & 31 : u / (2 * KC), e8 = TRANS ? u >> 5 : u % (2 * KC);
-            const int in = 32 * chunk + row < M ? K - 8 * e8 : 0;   // how many of the eight there are
-            uint32_t t[4][TW];
+            int row, k4;
+            run_of(i, row, k4);
+            uint32_t t[2][TW];
+            terms_of<TW>(wr[i][0], wr[i][1], t[0]);
+            terms_of<TW>(wr[i][2], wr[i][3], t[1]);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) terms_of<TW>(2 * e < in ? wr[i][2 * e] : 0.f, 2 * e + 1 < in ? wr[i][2 * e + 1] : 0.f, t[e]);
-#pragma unroll
-            for (int q = 0; q < TW; ++q) ws[(((e8 >> 1) * TW + q) * 2 + (e8 & 1)) * kPitch + row] = u32x4{t[0][q], t[1][q], t[2][q], t[3][q]};
+            for (int q = 0; q < TW; ++q) ws[2 * ((((k4 >> 2) * TW + q) * 2 + (k4 >> 1 & 1)) * kPitch + row) + (k4 & 1)] = u32x2{t[0][q], t[1][q]};
         }
         float *bias = reinterpret_cast<float *>(strip_lds + 2 * StripLds<KC, TW>::kUnits) + 32 * buffer;
         if (tid < 32) bias[tid] = br;
@@ -160,7 +94,7 @@ __global__ __launch_bounds__(kThreads, 2) void strip_kernel(const StripParams p)
                 const bool in = 16 * c + 8 * half + j < K;
                 r[c][j] = load<TI, NT>(rx, in ? in_off : kBeyond, 16 * c + j < K ? (unsigned)(16 * c + j) * ib : 0u);
             }
-        wput(c0, 0);
+        wput(0);
 #pragma unroll
         for (int c = 0; c < KC; ++c)
 #pragma unroll
@@ -255,7 +189,7 @@ __global__ __launch_bounds__(kThreads, 2) void strip_kernel(const StripParams p)
         const unsigned off = (unsigned)(32 * chunk + 4 * half) * ob + pxc * (unsigned)sizeof(TO);
 #pragma unroll
         for (int i = 0; i < 16; ++i) store<TO, NT>(ro, row_of(i) < left ? off : kBeyond, (unsigned)row_of(i) * ob, v[i], v[16 * (NT - 1) + i]);
-        if (chunk + 1 < c1) wput(chunk + 1, buffer ^ 1);
+        if (chunk + 1 < c1) wput(buffer ^ 1);
         __syncthreads();
     }
 }
@@ -265,8 +199,13 @@ hipError_t launch_as(const ProductParams &q, long N, hipStream_t s)
 {
     const long tiles = (q.P + 128 * NT - 1) / (128 * NT), all = tiles * N;
     const int chunks = (q.M + 31) / 32;
-    // where pixels alone do not give each compute unit two blocks, the outputs are shared out too
-    const long parts = std::max<long>(1, std::min<long>(chunks, (2 * kCus + all - 1) / all));
+    // The outputs are shared out over blocks where pixels alone leave compute units without two blocks, or the last round of blocks short:
+    // the fewest chunks on the longest way, a block's beginning and its reading of x counted as two.
+    long parts = 1, best = 0;
+    for (int k = 1; k <= chunks; ++k) {
+        const long way = (all * k + 2 * kCus - 1) / (2 * kCus) * ((chunks + k - 1) / k + 2);
+        if (best == 0 || way < best) parts = k, best = way;
+    }
     StripParams p;
     static_cast<ProductParams &>(p) = q;
     p.each = (int)((chunks + parts - 1) / parts);
@@ -283,12 +222,12 @@ hipError_t launch_as(const ProductParams &q, long N, hipStream_t s)
     return hipGetLastError();
 }
 
-// Two pixels a lane where the registers hold their channels and every compute unit has two blocks.
+// Two pixels a lane where the registers hold their channels and every compute unit has two blocks, of a third of the outputs at least.
 template <typename TI, typename TO, typename TE, int TX, int TW, int KC, bool TRANS, int MODE>
 hipError_t launch_nt(const ProductParams &p, long N, hipStream_t s)
 {
     if constexpr (KC * TX <= 16)
-        if (p.P >= 2 && N * ((p.P + 255) / 256) >= 2 * kCus) return launch_as<TI, TO, TE, TX, TW, KC, 2, TRANS, MODE>(p, N, s);
+        if (p.P >= 2 && N * ((p.P + 255) / 256) * std::min(3, (p.M + 31) / 32) >= 2 * kCus) return launch_as<TI, TO, TE, TX, TW, KC, 2, TRANS, MODE>(p, N, s);
     return launch_as<TI, TO, TE, TX, TW, KC, 1, TRANS, MODE>(p, N, s);
 }
 template <typename TI, typename TO, typename TE, int TX, int TW, bool TRANS, int MODE>
