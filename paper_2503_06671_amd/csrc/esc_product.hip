@@ -27,7 +27,7 @@ using namespace esc;
 constexpr size_t kAlign = 256;
 // ---- out = act(w x + b) + residual, and the products of the same form in the backward pass ----
 
-// A wavefront owns 32 MT outputs of 32 NT pixels, a block four such runs of pixels.  Its input channels come in stages of 32, two stages ahead, straight into
+// A wavefront owns 32 MT outputs of 32 NT pixels, a block four such runs of pixels.  Its input channels come in stages of 32, one or two stages ahead, straight into
 // the registers of the right operand (esc_product_strip.hip); the weights pass LDS, split into terms there by the block a stage ahead, two buffers, one barrier a
 // stage: units of eight consecutive channels of one output, [term][eighth of the stage][output].
 //
@@ -73,30 +73,29 @@ __global__ __launch_bounds__(kThreads, 2) void product_kernel(const ProductParam
     // ---- channels of a stage: 32 st + 16 c + 8 half + j of this lane's pixels ----
     typedef Raw<TI, ACROSS ? 1 : NT> X;
     constexpr int kLoads = ACROSS ? NT : 1;
+    constexpr int kAhead = kWide<TI> ? 1 : 2;   // stages that are asked for ahead: four bytes an element take the registers, and products the time
     const unsigned ib = (unsigned)p.P * (unsigned)sizeof(TI);
     const Rsrc rx = resource(static_cast<const TI *>(p.x) + image * p.x_stride, ACROSS ? 0 : (long)K * ib);
     const unsigned in_off = 8u * (unsigned)half * ib + pxc * (unsigned)sizeof(TI);
-    auto xfetch = [&](int st, X (&r)[2][8][kLoads]) {
+    auto xfetch = [&](int st, int c, X (&r)[8][kLoads]) {
 #pragma unroll
-        for (int c = 0; c < 2; ++c)
+        for (int j = 0; j < 8; ++j) {
+            const int k = 32 * st + 16 * c + j, mine = k + 8 * half;
+            if constexpr (ACROSS) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int k = 32 * st + 16 * c + j, mine = k + 8 * half;
-                if constexpr (ACROSS) {
-#pragma unroll
-                    for (int t = 0; t < NT; ++t) {
-                        const TI v = static_cast<const TI *>(p.x)[pn[t] * p.x_stride + (long)min(mine, K - 1) * p.P + pat[t]];
-                        if constexpr (kWide<TI>) r[c][j][t].w[0] = mine < K ? __float_as_uint(v) : 0u;
-                        else r[c][j][t].w[0] = mine < K ? v.bits : 0u;
-                    }
-                } else {
-                    r[c][j][0] = load<TI, NT>(rx, mine < K ? in_off : kBeyond, k < K ? (unsigned)k * ib : 0u);
+                for (int t = 0; t < NT; ++t) {
+                    const TI v = static_cast<const TI *>(p.x)[pn[t] * p.x_stride + (long)min(mine, K - 1) * p.P + pat[t]];
+                    if constexpr (kWide<TI>) r[j][t].w[0] = mine < K ? __float_as_uint(v) : 0u;
+                    else r[j][t].w[0] = mine < K ? v.bits : 0u;
                 }
+            } else {
+                r[j][0] = load<TI, NT>(rx, mine < K ? in_off : kBeyond, k < K ? (unsigned)k * ib : 0u);
             }
+        }
     };
 
     // ---- weights of a stage ----
-    const Rsrc rw = weights_of(p);
+    const Rsrc rw = resource(p.w, 4L * K * M);
     const bool four = (K & 3) == 0;
     float wr[kEach][4];
     // (a row's runs, neighbours in memory, by neighbouring threads; TRANS: a channel's outputs)
@@ -109,7 +108,7 @@ __global__ __launch_bounds__(kThreads, 2) void product_kernel(const ProductParam
         for (int i = 0; i < kEach; ++i) {
             int row, k4;
             run_of(i, row, k4);
-            load_weights<TRANS>(rw, p, four, m0 + row, 32 * st + 4 * k4, wr[i]);
+            load_weights<TRANS>(rw, M, K, p.w_ld, four, m0 + row, 32 * st + 4 * k4, wr[i]);
         }
     };
     auto wput = [&](int st) {
@@ -126,15 +125,18 @@ __global__ __launch_bounds__(kThreads, 2) void product_kernel(const ProductParam
         }
     };
 
-    // what is asked for stays in the order it is written in: at a wait for some of it the rest stays under way
-    auto order = [] { __builtin_amdgcn_sched_barrier(0x38f); };
-    X ra[2][8][kLoads], rb[2][8][kLoads];
+    // what is asked for stays in the order it is written in, and in front of the products that follow: at a wait for some of it the rest stays under way
+    auto order = [] { __builtin_amdgcn_sched_barrier(kSchedNoVmemNoMfma); };
+    X raw[kAhead][2][8][kLoads];
     wfetch(0);
     order();
-    xfetch(0, ra);
-    order();
-    xfetch(1, rb);
-    order();
+#pragma unroll
+    for (int d = 0; d < kAhead; ++d)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            xfetch(d, c, raw[d][c]);
+            order();
+        }
     float *bias = reinterpret_cast<float *>(product_lds + 2 * C::kBuffer);
     if (tid < 32 * MT) bias[tid] = p.b != nullptr && m0 + tid < M ? p.b[m0 + tid] : 0.f;
     wput(0);
@@ -170,11 +172,9 @@ __global__ __launch_bounds__(kThreads, 2) void product_kernel(const ProductParam
                     }
                 }
             }
-            if (c == 1) {
-                order();
-                xfetch(st + 2, raw);
-                order();
-            }
+            order();
+            xfetch(st + kAhead, c, raw[c]);
+            order();
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) {
                 u32x4 a[TW];
@@ -199,10 +199,10 @@ __global__ __launch_bounds__(kThreads, 2) void product_kernel(const ProductParam
     // (beyond the last stage loads bring nothing, and zeros are put)
     int st = 0;
     for (; st + 1 < stages; st += 2) {
-        body(st, ra);
-        body(st + 1, rb);
+        body(st, raw[0]);
+        body(st + 1, raw[kAhead - 1]);
     }
-    if (st < stages) body(st, ra);
+    if (st < stages) body(st, raw[0]);
     settle();
 
     // ---- lane l has outputs m0 + 32 mt + 8 (i / 4) + 4 half + i % 4 in element i of its pixels' sums ----
@@ -315,7 +315,8 @@ constexpr int kPixels = 32;   // of a stage
 struct WeightParams {
     const void *g, *x;
     long g_stride, x_stride;
-    float *part, *part_b;     // [splits][M][K], [splits][M], or nullptr
+    float *part;              // [splits][M K of grad_w where that is wanted, then M of grad_b where that is]
+    bool has_w, has_b;
     int K, M, splits, tiles, across;   // (tiles of grad_w, and those side by side)
     long P, pixels;
 };
@@ -407,7 +408,9 @@ __global__ __launch_bounds__(kThreads, 2) void product_weights_kernel(const Weig
             x.scattered(xp, p.x_stride, p.P, p.pixels, q, k0, p.K);
         }
     };
-    const bool has_b = p.part_b != nullptr && k0 == 0;
+    const bool has_b = p.has_b && k0 == 0;
+    const size_t of_w = p.has_w ? (size_t)p.M * p.K : 0;
+    float *const part = p.part + split * (of_w + (p.has_b ? p.M : 0));
     float sums[G::kEach];
 #pragma unroll
     for (int i = 0; i < G::kEach; ++i) sums[i] = 0.f;
@@ -458,7 +461,7 @@ __global__ __launch_bounds__(kThreads, 2) void product_weights_kernel(const Weig
         __syncthreads();
     }
     settle();
-    if (p.part != nullptr) {
+    if (p.has_w) {
 #pragma unroll
         for (int t = 0; t < MT; ++t)
 #pragma unroll
@@ -468,7 +471,7 @@ __global__ __launch_bounds__(kThreads, 2) void product_weights_kernel(const Weig
                 for (int i = 0; i < 16; ++i) {
                     const int m = m0 + 32 * (MT * wm + t) + 8 * (i >> 2) + 4 * half + (i & 3);
                     const float v = acc[t][j][i];
-                    if (m < p.M && k < p.K) p.part[((size_t)split * p.M + m) * p.K + k] = v;
+                    if (m < p.M && k < p.K) part[(size_t)m * p.K + k] = v;
                 }
             }
     }
@@ -482,7 +485,7 @@ __global__ __launch_bounds__(kThreads, 2) void product_weights_kernel(const Weig
             float t = 0.f;
 #pragma unroll
             for (int j = 0; j < G::kRunsOfRow; ++j) t += all[tid * G::kRunsOfRow + j];
-            p.part_b[(size_t)split * p.M + m0 + tid] = t;
+            part[of_w + m0 + tid] = t;
         }
     }
 }
@@ -527,17 +530,18 @@ esc_status shape(const esc_pointwise *a, long *P)
     return ESC_OK;
 }
 
-// Shares of the pixels: two blocks a compute unit, four stages each at least.
+// Shares of the pixels: two blocks a compute unit and no more (11 shares of 50 tiles, a round of 38 blocks behind one of 512: 560 us, 10 shares 390), two stages
+// each at least.
 int splits_of(const esc_pointwise *a, long P, bool f32)
 {
     const Sides side = sides_of(a->M, a->K, f32);
     const long mt = 64 * side.mt, kt = 64 * side.kt;
     const long tiles = ((a->M + mt - 1) / mt) * ((a->K + kt - 1) / kt), stages = ((long)a->N * P + kPixels - 1) / kPixels;
-    return (int)std::max<long>(1, std::min((2 * kCus + tiles - 1) / tiles, stages / 4));
+    return (int)std::max<long>(1, std::min(2 * kCus / tiles, stages / 2));
 }
 
 struct Scratch {
-    size_t gp, part, part_b, total;
+    size_t gp, part, total;
 };
 Scratch scratch(const esc_pointwise *a, long P, bool f32)
 {
@@ -545,8 +549,7 @@ Scratch scratch(const esc_pointwise *a, long P, bool f32)
     const size_t splits = (size_t)splits_of(a, P, f32);
     s.gp = 0;
     s.part = a->act != ESC_ACT_NONE ? round_up((size_t)a->N * P * a->M * 4, kAlign) : 0;
-    s.part_b = s.part + round_up(splits * a->M * a->K * 4, kAlign);
-    s.total = s.part_b + round_up(splits * a->M * 4, kAlign);
+    s.total = s.part + round_up(splits * a->M * ((size_t)a->K + 1) * 4, kAlign);
     return s;
 }
 
@@ -619,7 +622,15 @@ esc_status esc_pointwise_backward(const void *x, const void *grad_out, esc_dtype
     const bool act = a->act != ESC_ACT_NONE;
     char *mem = static_cast<char *>(workspace);
     const long x_stride = (long)(xi.stride / es), g_stride = (long)(gi.stride / es);
-    if (act) {  // gp, fp32
+    const bool sums = g->w != nullptr || g->b != nullptr;
+    const bool joint = act && g->x != nullptr && back_fits(f32, a->K, a->M, P, a->N);
+    if (joint) {
+        BackParams p{};
+        p.x = x, p.grad_out = grad_out, p.gp = sums ? reinterpret_cast<float *>(mem) : nullptr, p.grad_x = g->x;
+        p.x_stride = x_stride, p.g_stride = g_stride, p.gp_stride = (long)a->M * P, p.gx_stride = (long)(gxi.stride / es);
+        p.w = a->w, p.b = a->b, p.K = a->K, p.M = a->M, p.act = (int)a->act, p.P = P;
+        if (launch_back(f32, p, a->N, s) != hipSuccess) return ESC_ERR_HIP;
+    } else if (act) {  // gp, fp32
         ProductParams p{};
         p.x = x, p.extra = grad_out, p.out = mem;
         p.x_stride = x_stride, p.extra_stride = g_stride, p.out_stride = (long)a->M * P;
@@ -627,7 +638,7 @@ esc_status esc_pointwise_backward(const void *x, const void *grad_out, esc_dtype
         const hipError_t e = launch_any(f32 ? kSlopeF32 : kSlopeBf16, p, a->N, s);
         if (e != hipSuccess) return ESC_ERR_HIP;
     }
-    if (g->x != nullptr) {
+    if (g->x != nullptr && !joint) {
         ProductParams p{};
         p.x = act ? mem : grad_out, p.out = g->x;
         p.x_stride = act ? (long)a->M * P : g_stride, p.out_stride = (long)(gxi.stride / es);
@@ -635,16 +646,14 @@ esc_status esc_pointwise_backward(const void *x, const void *grad_out, esc_dtype
         const hipError_t e = launch_any(f32 ? kBackF32 : act ? kBackGp : kBackBf16, p, a->N, s);
         if (e != hipSuccess) return ESC_ERR_HIP;
     }
-    if (g->w != nullptr || g->b != nullptr) {
+    if (sums) {
         WeightParams p{};
         p.g = act ? mem : grad_out, p.x = x, p.g_stride = act ? (long)a->M * P : g_stride, p.x_stride = x_stride;
-        p.part = g->w != nullptr ? reinterpret_cast<float *>(mem + sc.part) : nullptr;
-        p.part_b = g->b != nullptr ? reinterpret_cast<float *>(mem + sc.part_b) : nullptr;
+        p.part = reinterpret_cast<float *>(mem + sc.part), p.has_w = g->w != nullptr, p.has_b = g->b != nullptr;
         p.K = a->K, p.M = a->M, p.splits = splits_of(a, P, f32), p.P = P, p.pixels = P * a->N;
         const hipError_t e = f32 ? launch_weights<float, float, 3, 3>(p, s) : act ? launch_weights<float, bf16s, 3, 1>(p, s) : launch_weights<bf16s, bf16s, 1, 1>(p, s);
         if (e != hipSuccess) return ESC_ERR_HIP;
-        if (g->w != nullptr && add_parts(p.part, p.splits, (long)a->M * a->K, g->w, 0, nullptr, accumulate, s) != hipSuccess) return ESC_ERR_HIP;
-        if (g->b != nullptr && add_parts(p.part_b, p.splits, a->M, g->b, 0, nullptr, accumulate, s) != hipSuccess) return ESC_ERR_HIP;
+        if (add_parts(p.part, p.splits, p.has_w ? (long)a->M * a->K : 0, g->w, p.has_b ? a->M : 0, g->b, accumulate, s) != hipSuccess) return ESC_ERR_HIP;
     }
     return ESC_OK;
 }

@@ -146,6 +146,7 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kRawBuffer = 0x00020000;     // raw buffer (no stride, no swizzle), 32-bit data format
 constexpr unsigned kBeyond = 0x80000000u;  // an offset beyond every resource (an image of a tensor is < 2 GiB)
+constexpr int kSchedNoVmemNoMfma = 0x386;  // a scheduling barrier for accesses to memory and matrix instructions
 constexpr size_t kMostImage = (size_t)1 << 31;
 
 __device__ __forceinline__ Rsrc resource(const void *at, long bytes)
@@ -197,21 +198,21 @@ __device__ __forceinline__ void store(Rsrc r, unsigned voff, unsigned soff, floa
 
 // Four weights of output m from channel k on (TRANS: w's rows are the channels).  FOUR: K is a multiple of four, a run is inside or outside as a whole.
 template <bool TRANS>
-__device__ __forceinline__ void load_weights(Rsrc rw, const ProductParams &p, bool four, int m, int k, float (&w)[4])
+__device__ __forceinline__ void load_weights(Rsrc rw, int M, int K, int ld, bool four, int m, int k, float (&w)[4])
 {
     if (!TRANS && four) {
-        const u32x4 v = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rw, (int)(m < p.M && k < p.K ? 4u * ((unsigned)m * (unsigned)p.w_ld + (unsigned)k) : kBeyond), 0, 0));
+        const u32x4 v = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rw, (int)(m < M && k < K ? 4u * ((unsigned)m * (unsigned)ld + (unsigned)k) : kBeyond), 0, 0));
 #pragma unroll
         for (int e = 0; e < 4; ++e) w[e] = __uint_as_float(v[e]);
     } else {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const unsigned at = TRANS ? (unsigned)(k + e) * (unsigned)p.w_ld + (unsigned)m : (unsigned)m * (unsigned)p.w_ld + (unsigned)(k + e);
-            w[e] = __uint_as_float((unsigned)__builtin_amdgcn_raw_buffer_load_b32(rw, (int)(m < p.M && k + e < p.K ? 4u * at : kBeyond), 0, 0));
+            const unsigned at = TRANS ? (unsigned)(k + e) * (unsigned)ld + (unsigned)m : (unsigned)m * (unsigned)ld + (unsigned)(k + e);
+            w[e] = __uint_as_float((unsigned)__builtin_amdgcn_raw_buffer_load_b32(rw, (int)(m < M && k + e < K ? 4u * at : kBeyond), 0, 0));
         }
     }
 }
-__device__ __forceinline__ Rsrc weights_of(const ProductParams &p) { return resource(p.w, 4L * p.K * p.M); }
+
 
 // Which eighths of the grid the dies get: consecutive pieces on one die.
 __device__ __forceinline__ unsigned piece_of(unsigned block, unsigned blocks)
@@ -228,5 +229,19 @@ enum : int { kForwardF32, kForwardBf16, kSlopeF32, kSlopeBf16, kBackF32, kBackBf
 // Whether esc_product_strip.hip takes a product.
 __attribute__((visibility("hidden"))) bool strip_fits(int kind, const ProductParams &p, long N);
 __attribute__((visibility("hidden"))) hipError_t launch_strip(int kind, const ProductParams &p, long N, hipStream_t s);
+
+// grad_x of a product with an activation, gp on the way: gp = grad_out act'(b + w x), fp32, kept where gp is not nullptr, and grad_x = W^T gp.
+struct BackParams {
+    const void *x, *grad_out;
+    float *gp;
+    void *grad_x;
+    long x_stride, g_stride, gp_stride, gx_stride;  // elements
+    const float *w, *b;
+    int K, M, act;
+    long P;
+    unsigned tiles_of_image;
+};
+__attribute__((visibility("hidden"))) bool back_fits(bool f32, int K, int M, long P, long N);
+__attribute__((visibility("hidden"))) hipError_t launch_back(bool f32, const BackParams &p, long N, hipStream_t s);
 
 }  // namespace esc

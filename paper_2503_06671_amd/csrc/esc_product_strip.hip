@@ -45,7 +45,7 @@ __global__ __launch_bounds__(kThreads, 2) void strip_kernel(const StripParams p)
     const unsigned pxc = px + NT <= P ? px : P - NT;
 
     // ---- weights ----
-    const Rsrc rw = weights_of(p);
+    const Rsrc rw = resource(p.w, 4L * K * M);
     const bool four = (K & 3) == 0;
     float wr[kEach][4];
     float br = 0.f;
@@ -60,7 +60,7 @@ __global__ __launch_bounds__(kThreads, 2) void strip_kernel(const StripParams p)
         for (int i = 0; i < kEach; ++i) {
             int row, k4;
             run_of(i, row, k4);
-            load_weights<TRANS>(rw, p, four, 32 * chunk + row, 4 * k4, wr[i]);
+            load_weights<TRANS>(rw, M, K, p.w_ld, four, 32 * chunk + row, 4 * k4, wr[i]);
         }
     };
     auto wput = [&](int buffer) {
@@ -194,6 +194,230 @@ __global__ __launch_bounds__(kThreads, 2) void strip_kernel(const StripParams p)
     }
 }
 
+// ---- grad_x = W^T ( grad_out act'(b + W x) ) ----
+//
+// A chunk's 32 outputs gp of a wavefront's pixels, as the first product leaves them in a lane (rows 8 g + 4 half + r of its pixel), are the right operand of
+// the second as they lie there, the channels of W^T staged in that order; its sums, grad_x of all K channels, stay in registers over the chunks.  gp never has to
+// be read back for it.
+template <int KC, int TF, int TB>
+struct BackLds {
+    static constexpr int kBuffers = KC <= 4 ? 2 : 1;
+    static constexpr int kRows = 16 * KC, kPitchT = kRows + 1;
+    static constexpr int kForwardUnits = KC * TF * 2 * kPitch, kUnits = kForwardUnits + 2 * TB * 2 * kPitchT;
+    static constexpr size_t kBytes = (size_t)kBuffers * (kUnits * 16 + 32 * 4);
+};
+
+// TX, TF: terms of x and W in the first product; TG, TB: of gp and W in the second.
+template <typename T, int TX, int TF, int TG, int TB, int KC, int NT>
+__global__ __launch_bounds__(kThreads, 2) void strip_back_kernel(const BackParams p)
+{
+    typedef BackLds<KC, TF, TB> L;
+    constexpr int kTopF = TX > TF ? TX : TF, kTopB = TG > TB ? TG : TB, KT = KC / 2;
+    constexpr int kEach = 128 * KC / kThreads;                                  // runs of four weights of a chunk, of a thread
+    constexpr int kUnitsT = L::kRows * 4, kEachT = (kUnitsT + kThreads - 1) / kThreads;  // eights of outputs of a channel, of a thread
+    const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int l32 = lane & 31, half = lane >> 5;
+    const int K = p.K, M = p.M, chunks = (M + 31) / 32;
+    const unsigned P = (unsigned)p.P;
+    const unsigned tile = piece_of(blockIdx.x, gridDim.x), n = tile / p.tiles_of_image;
+    const unsigned px = (tile - n * p.tiles_of_image) * (128u * NT) + 32u * NT * (unsigned)wave + NT * (unsigned)l32;
+    const unsigned pxc = px + NT <= P ? px : P - NT;
+
+    const Rsrc rw = resource(p.w, 4L * K * M);
+    const bool four = (K & 3) == 0;
+    float wr[kEach][4], tr[kEachT][8], br = 0.f;
+    auto wfetch = [&](int chunk) {
+        br = p.b != nullptr && tid < 32 && 32 * chunk + tid < M ? p.b[32 * chunk + tid] : 0.f;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int u = tid + i * kThreads;
+            load_weights<false>(rw, M, K, K, four, 32 * chunk + u / (4 * KC), 4 * (u % (4 * KC)), wr[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < kEachT; ++i) {
+            const int u = tid + i * kThreads, row = u % L::kRows, part = u / L::kRows;   // part: sixteen 2, half of it
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int m = 32 * chunk + 16 * (part >> 1) + 8 * (j >> 2) + 4 * (part & 1) + (j & 3);
+                tr[i][j] = __uint_as_float((unsigned)__builtin_amdgcn_raw_buffer_load_b32(rw, (int)(m < M && row < K && part < 4 ? 4u * ((unsigned)m * (unsigned)K + (unsigned)row) : kBeyond), 0, 0));
+            }
+        }
+    };
+    auto wput = [&](int buffer) {
+        u32x4 *const base = strip_lds + buffer * L::kUnits;
+        u32x2 *ws = reinterpret_cast<u32x2 *>(base);
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int u = tid + i * kThreads, row = u / (4 * KC), k4 = u % (4 * KC);
+            uint32_t t[2][TF];
+            terms_of<TF>(wr[i][0], wr[i][1], t[0]);
+            terms_of<TF>(wr[i][2], wr[i][3], t[1]);
+#pragma unroll
+            for (int q = 0; q < TF; ++q) ws[2 * ((((k4 >> 2) * TF + q) * 2 + (k4 >> 1 & 1)) * kPitch + row) + (k4 & 1)] = u32x2{t[0][q], t[1][q]};
+        }
+        u32x4 *const ts = base + L::kForwardUnits;
+#pragma unroll
+        for (int i = 0; i < kEachT; ++i) {
+            const int u = tid + i * kThreads, row = u % L::kRows, part = u / L::kRows;
+            if (kUnitsT % kThreads != 0 && u >= kUnitsT) break;
+            uint32_t t[4][TB];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) terms_of<TB>(tr[i][2 * e], tr[i][2 * e + 1], t[e]);
+#pragma unroll
+            for (int q = 0; q < TB; ++q) ts[(((part >> 1) * TB + q) * 2 + (part & 1)) * L::kPitchT + row] = u32x4{t[0][q], t[1][q], t[2][q], t[3][q]};
+        }
+        if (tid < 32) reinterpret_cast<float *>(strip_lds + L::kBuffers * L::kUnits)[32 * buffer + tid] = br;
+    };
+    wfetch(0);
+
+    const unsigned ib = P * (unsigned)sizeof(T), fb = P * 4u;
+    const unsigned first = pxc * (unsigned)sizeof(T);
+    u32x4 b[KC][NT][TX];
+    {
+        const Rsrc rx = resource(static_cast<const T *>(p.x) + (size_t)n * p.x_stride, (long)K * ib);
+        const unsigned in_off = 8u * (unsigned)half * ib + first;
+        Raw<T, NT> r[KC][8];
+#pragma unroll
+        for (int c = 0; c < KC; ++c)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) r[c][j] = load<T, NT>(rx, 16 * c + 8 * half + j < K ? in_off : kBeyond, 16 * c + j < K ? (unsigned)(16 * c + j) * ib : 0u);
+        wput(0);
+#pragma unroll
+        for (int c = 0; c < KC; ++c)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    if constexpr (TX == 1) {
+                        b[c][t][0][e] = __builtin_amdgcn_perm(r[c][2 * e + 1].w[0], r[c][2 * e].w[0], t == 0 ? 0x05040100u : 0x07060302u);
+                    } else {
+                        uint32_t q[TX];
+                        terms_of<TX>(r[c][2 * e].value(t), r[c][2 * e + 1].value(t), q);
+#pragma unroll
+                        for (int i = 0; i < TX; ++i) b[c][t][i][e] = q[i];
+                    }
+                }
+    }
+    __syncthreads();
+
+    const Rsrc rg = resource(static_cast<const T *>(p.grad_out) + (size_t)n * p.g_stride, (long)M * ib);
+    const Rsrc rp = resource(p.gp != nullptr ? p.gp + (size_t)n * p.gp_stride : nullptr, p.gp != nullptr ? (long)M * fb : 0);
+    auto row_of = [](int i) { return 8 * (i >> 2) + (i & 3); };
+    f32x16 gx[KT][NT];
+#pragma unroll
+    for (int k = 0; k < KT; ++k)
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) gx[k][t][i] = 0.f;
+    for (int chunk = 0; chunk < chunks; ++chunk) {
+        const int buffer = L::kBuffers == 2 ? chunk & 1 : 0, left = M - 32 * chunk - 4 * half;
+        if (chunk + 1 < chunks) wfetch(chunk + 1);
+        Raw<T, NT> ex[16];
+        {
+            const unsigned off = (unsigned)(32 * chunk + 4 * half) * ib + first;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) ex[i] = load<T, NT>(rg, row_of(i) < left ? off : kBeyond, (unsigned)row_of(i) * ib);
+        }
+        f32x16 acc[NT];
+        const float *bias = reinterpret_cast<const float *>(strip_lds + L::kBuffers * L::kUnits) + 32 * buffer;
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const f32x4 v = *reinterpret_cast<const f32x4 *>(bias + 8 * g + 4 * half);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int t = 0; t < NT; ++t) acc[t][4 * g + e] = v[e];
+        }
+        const u32x4 *ws = strip_lds + buffer * L::kUnits + half * kPitch + l32;
+        u32x4 next[TF];
+#pragma unroll
+        for (int q = 0; q < TF; ++q) next[q] = ws[q * 2 * kPitch];
+#pragma unroll
+        for (int c = 0; c < KC; ++c) {
+            u32x4 a[TF];
+#pragma unroll
+            for (int q = 0; q < TF; ++q) a[q] = next[q];
+            if (c + 1 < KC) {
+#pragma unroll
+                for (int q = 0; q < TF; ++q) next[q] = ws[((c + 1) * TF + q) * 2 * kPitch];
+            }
+#pragma unroll
+            for (int qw = TF - 1; qw >= 0; --qw)
+#pragma unroll
+                for (int qx = TX - 1; qx >= 0; --qx) {
+                    if (qw + qx >= kTopF) continue;
+#pragma unroll
+                    for (int t = 0; t < NT; ++t)
+                        acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a[qw]), __builtin_bit_cast(bf16x8, b[c][t][qx]), acc[t], 0, 0, 0);
+                }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        settle();
+        float v[NT * 16];
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) v[16 * t + i] = acc[t][i];
+        slopes(p.act, v);
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) v[16 * t + i] *= ex[i].value(t);
+        if (p.gp != nullptr) {
+            const unsigned off = (unsigned)(32 * chunk + 4 * half) * fb + pxc * 4u;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) store<float, NT>(rp, row_of(i) < left ? off : kBeyond, (unsigned)row_of(i) * fb, v[i], v[16 * (NT - 1) + i]);
+        }
+        const u32x4 *ts = strip_lds + buffer * L::kUnits + L::kForwardUnits + half * L::kPitchT + l32;
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            u32x4 g[NT][TG];
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    uint32_t q[TG];
+                    terms_of<TG>(v[16 * t + 8 * c + 2 * e], v[16 * t + 8 * c + 2 * e + 1], q);
+#pragma unroll
+                    for (int i = 0; i < TG; ++i) g[t][i][e] = q[i];
+                }
+#pragma unroll
+            for (int k = 0; k < KT; ++k) {
+                u32x4 a[TB];
+#pragma unroll
+                for (int q = 0; q < TB; ++q) a[q] = ts[(c * TB + q) * 2 * L::kPitchT + 32 * k];
+#pragma unroll
+                for (int qw = TB - 1; qw >= 0; --qw)
+#pragma unroll
+                    for (int qg = TG - 1; qg >= 0; --qg) {
+                        if (qw + qg >= kTopB) continue;
+#pragma unroll
+                        for (int t = 0; t < NT; ++t)
+                            gx[k][t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a[qw]), __builtin_bit_cast(bf16x8, g[t][qg]), gx[k][t], 0, 0, 0);
+                    }
+            }
+        }
+        if (chunk + 1 < chunks) {
+            if constexpr (L::kBuffers == 1) __syncthreads();   // everyone has finished with this chunk's weights
+            wput(L::kBuffers == 2 ? buffer ^ 1 : 0);
+        }
+        __syncthreads();
+    }
+    settle();
+    const Rsrc ro = resource(static_cast<T *>(p.grad_x) + (size_t)n * p.gx_stride, (long)K * ib);
+#pragma unroll
+    for (int k = 0; k < KT; ++k) {
+        const int left = K - 32 * k - 4 * half;
+        const unsigned off = (unsigned)(32 * k + 4 * half) * ib + first;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const float v0 = gx[k][0][i], v1 = gx[k][NT - 1][i];
+            store<T, NT>(ro, row_of(i) < left ? off : kBeyond, (unsigned)row_of(i) * ib, v0, v1);
+        }
+    }
+}
+
 template <typename TI, typename TO, typename TE, int TX, int TW, int KC, int NT, bool TRANS, int MODE>
 hipError_t launch_as(const ProductParams &q, long N, hipStream_t s)
 {
@@ -240,7 +464,41 @@ hipError_t launch_kc(const ProductParams &p, long N, hipStream_t s)
     return launch_nt<TI, TO, TE, TX, TW, 12, TRANS, MODE>(p, N, s);
 }
 
+template <typename T, int TX, int TF, int TG, int TB, int KC, int NT>
+hipError_t launch_back_as(BackParams p, long N, hipStream_t s)
+{
+    p.tiles_of_image = (unsigned)((p.P + 128 * NT - 1) / (128 * NT));
+    const long grid = p.tiles_of_image * N;
+    if (grid >= (1L << 31)) return hipErrorInvalidValue;
+    constexpr size_t lds = BackLds<KC, TF, TB>::kBytes;
+    static_assert(lds <= 64 * 1024, "");
+    hipLaunchKernelGGL((strip_back_kernel<T, TX, TF, TG, TB, KC, NT>), dim3((unsigned)grid), dim3(kThreads), lds, s, p);
+    return hipGetLastError();
+}
+constexpr int kBackMostK[2] = {128, 96};  // bf16, fp32: what the registers hold
+
 }  // namespace
+
+bool back_fits(bool f32, int K, int M, long P, long N)
+{
+    if (K > kBackMostK[f32] || (size_t)std::max(K, M) * P * 4 >= kMostImage || !(N == 1 || P >= 96)) return false;
+    // (a block goes through all outputs: few pixels are better shared out over two launches.  5 x 50 x 61, 96 to 45, fp32: 15.7 us, two launches 14.0)
+    return N * ((P + 127) / 128) >= kCus;
+}
+
+hipError_t launch_back(bool f32, const BackParams &p, long N, hipStream_t s)
+{
+    const int k = (p.K + 15) / 16;
+    if (f32) {
+        if (k <= 2) return launch_back_as<float, 3, 3, 3, 3, 2, 1>(p, N, s);
+        if (k <= 4) return launch_back_as<float, 3, 3, 3, 3, 4, 1>(p, N, s);
+        return launch_back_as<float, 3, 3, 3, 3, 6, 1>(p, N, s);
+    }
+    const bool two = p.P >= 2 && N * ((p.P + 255) / 256) >= 2 * kCus;
+    if (k <= 2) return two ? launch_back_as<bf16s, 1, 3, 2, 2, 2, 2>(p, N, s) : launch_back_as<bf16s, 1, 3, 2, 2, 2, 1>(p, N, s);
+    if (k <= 4) return two ? launch_back_as<bf16s, 1, 3, 2, 2, 4, 2>(p, N, s) : launch_back_as<bf16s, 1, 3, 2, 2, 4, 1>(p, N, s);
+    return launch_back_as<bf16s, 1, 3, 2, 2, 8, 1>(p, N, s);
+}
 
 bool strip_fits(int kind, const ProductParams &p, long N)
 {
