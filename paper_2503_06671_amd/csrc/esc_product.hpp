@@ -135,8 +135,8 @@ __device__ __forceinline__ void slopes(int act, float (&v)[N])
         for (int i = 0; i < N; ++i) v[i] = slope(kSilu, v[i]);
     }
 }
-// kForward: out = act(pre) + extra.  kSlope: out = extra act'(pre), fp32.
-enum : int { kForward = 0, kSlope = 1 };
+// kForward: out = act(pre).  kResidual: out = act(pre) + extra.  kSlope: out = extra act'(pre), fp32.
+enum : int { kForward = 0, kSlope = 1, kResidual = 2 };
 
 // ---- accesses to an image's planes by 32-bit offsets ----
 
@@ -146,6 +146,7 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kRawBuffer = 0x00020000;     // raw buffer (no stride, no swizzle), 32-bit data format
 constexpr unsigned kBeyond = 0x80000000u;  // an offset beyond every resource (an image of a tensor is < 2 GiB)
+constexpr int kSchedNoVmem = 0x38f;        // a scheduling barrier for accesses to memory alone
 constexpr int kSchedNoVmemNoMfma = 0x386;  // a scheduling barrier for accesses to memory and matrix instructions
 constexpr size_t kMostImage = (size_t)1 << 31;
 

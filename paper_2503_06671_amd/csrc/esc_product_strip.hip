@@ -12,8 +12,8 @@
 namespace esc {
 namespace {
 
-// Weights of a chunk in LDS: units of eight consecutive channels of one output, [channels / 16][term][half of the sixteen][output], halves a unit
-// further apart than outputs take (other banks for a thread's neighbours, who write other eighths of the same output).
+// Weights of a chunk in LDS: units of eight consecutive channels of one output, [term][eighth][output], eighths a unit further apart than outputs
+// take (other banks for a thread's neighbours, who write other eighths of the same output).
 constexpr int kPitch = 33;
 
 template <int KC, int TW>
@@ -23,14 +23,67 @@ struct StripLds {
 };
 extern __shared__ __align__(16) u32x4 strip_lds[];
 
+// A wavefront's pixels as right operands: channel 16 c + 8 half + j of its lanes' NT pixels, whose first channel's place (of this half) is `off`.  Four
+// sixteens are on their way while the four before them are split; `meanwhile` is done behind the first.
+template <typename T, int TX, int KC, int NT, typename F>
+__device__ __forceinline__ void load_operands(Rsrc rx, unsigned off, unsigned plane, int K, u32x4 (&b)[KC][NT][TX], F meanwhile)
+{
+    constexpr int kGroup = KC < 4 ? KC : 4;
+    const int half = ((int)threadIdx.x & 63) >> 5;
+    Raw<T, NT> r[2][kGroup][8];
+    auto ask = [&](int g) {
+#pragma unroll
+        for (int c = 0; c < kGroup; ++c)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int k = 16 * (kGroup * g + c) + j;
+                if (kGroup * g + c < KC) r[g & 1][c][j] = load<T, NT>(rx, k + 8 * half < K ? off : kBeyond, k < K ? (unsigned)k * plane : 0u);
+            }
+        __builtin_amdgcn_sched_barrier(kSchedNoVmem);
+    };
+    auto split = [&](int g) {
+#pragma unroll
+        for (int c = 0; c < kGroup; ++c) {
+            if (kGroup * g + c >= KC) break;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    const Raw<T, NT> &v0 = r[g & 1][c][2 * e], &v1 = r[g & 1][c][2 * e + 1];
+                    u32x4 (&to)[TX] = b[kGroup * g + c][t];
+                    if constexpr (!kWide<T> && TX == 1) {
+                        to[0][e] = __builtin_amdgcn_perm(v1.w[0], v0.w[0], t == 0 ? 0x05040100u : 0x07060302u);
+                    } else {
+                        uint32_t q[TX];
+                        terms_of<TX>(v0.value(t), v1.value(t), q);
+#pragma unroll
+                        for (int i = 0; i < TX; ++i) to[i][e] = q[i];
+                    }
+                }
+        }
+    };
+    constexpr int kAll = (KC + kGroup - 1) / kGroup;
+    ask(0);
+    if constexpr (kAll > 1) ask(1);
+    meanwhile();
+#pragma unroll
+    for (int g = 0; g < kAll; ++g) {
+        split(g);
+        if (g + 2 < kAll) ask(g + 2);
+    }
+}
+
 struct StripParams : ProductParams {
     int each;   // chunks of 32 outputs a block
     unsigned parts;
     unsigned tiles_of_image;
 };
 
+// blocks of a compute unit, by what the operands leave of the registers
+constexpr int strip_blocks(int words, bool more) { return words <= 32 && !more ? 4 : words < 48 ? 3 : 2; }
+
 template <typename TI, typename TO, typename TE, int TX, int TW, int KC, int NT, bool TRANS, int MODE>
-__global__ __launch_bounds__(kThreads, 2) void strip_kernel(const StripParams p)
+__global__ __launch_bounds__(kThreads, strip_blocks(4 * KC * NT * TX, MODE != kForward || TRANS)) void strip_kernel(const StripParams p)
 {
     constexpr int kTop = TX > TW ? TX : TW;      // products of terms whose orders add up to less
     constexpr int kRuns = 128 * KC, kEach = kRuns / kThreads;  // runs of four weights of a chunk, of a thread
@@ -73,7 +126,7 @@ __global__ __launch_bounds__(kThreads, 2) void strip_kernel(const StripParams p)
             terms_of<TW>(wr[i][0], wr[i][1], t[0]);
             terms_of<TW>(wr[i][2], wr[i][3], t[1]);
 #pragma unroll
-            for (int q = 0; q < TW; ++q) ws[2 * ((((k4 >> 2) * TW + q) * 2 + (k4 >> 1 & 1)) * kPitch + row) + (k4 & 1)] = u32x2{t[0][q], t[1][q]};
+            for (int q = 0; q < TW; ++q) ws[2 * ((q * 2 * KC + (k4 >> 1)) * kPitch + row) + (k4 & 1)] = u32x2{t[0][q], t[1][q]};
         }
         float *bias = reinterpret_cast<float *>(strip_lds + 2 * StripLds<KC, TW>::kUnits) + 32 * buffer;
         if (tid < 32) bias[tid] = br;
@@ -85,46 +138,19 @@ __global__ __launch_bounds__(kThreads, 2) void strip_kernel(const StripParams p)
     const Rsrc rx = resource(static_cast<const TI *>(p.x) + (size_t)n * p.x_stride, (long)K * ib);
     const unsigned in_off = 8u * (unsigned)half * ib + pxc * (unsigned)sizeof(TI);
     u32x4 b[KC][NT][TX];
-    {
-        Raw<TI, NT> r[KC][8];
-#pragma unroll
-        for (int c = 0; c < KC; ++c)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const bool in = 16 * c + 8 * half + j < K;
-                r[c][j] = load<TI, NT>(rx, in ? in_off : kBeyond, 16 * c + j < K ? (unsigned)(16 * c + j) * ib : 0u);
-            }
-        wput(0);
-#pragma unroll
-        for (int c = 0; c < KC; ++c)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                if constexpr (!kWide<TI> && TX == 1) {
-                    b[c][0][0][e] = __builtin_amdgcn_perm(r[c][2 * e + 1].w[0], r[c][2 * e].w[0], 0x05040100u);
-                    if constexpr (NT == 2) b[c][1][0][e] = __builtin_amdgcn_perm(r[c][2 * e + 1].w[0], r[c][2 * e].w[0], 0x07060302u);
-                } else {
-#pragma unroll
-                    for (int t = 0; t < NT; ++t) {
-                        uint32_t q[TX];
-                        terms_of<TX>(r[c][2 * e].value(t), r[c][2 * e + 1].value(t), q);
-#pragma unroll
-                        for (int i = 0; i < TX; ++i) b[c][t][i][e] = q[i];
-                    }
-                }
-            }
-    }
+    load_operands<TI, TX, KC, NT>(rx, in_off, ib, K, b, [&] { wput(0); });
     __syncthreads();
 
     const unsigned ob = P * (unsigned)sizeof(TO), eb = P * (unsigned)sizeof(TE);
     const Rsrc ro = resource(static_cast<TO *>(p.out) + (size_t)n * p.out_stride, (long)M * ob);
-    const Rsrc re = resource(p.extra != nullptr ? static_cast<const TE *>(p.extra) + (size_t)n * p.extra_stride : nullptr, p.extra != nullptr ? (long)M * eb : 0);
+    const Rsrc re = resource(MODE != kForward ? static_cast<const TE *>(p.extra) + (size_t)n * p.extra_stride : nullptr, MODE != kForward ? (long)M * eb : 0);
     // lane l has outputs 32 chunk + 8 (i / 4) + 4 half + i % 4 in element i of its pixels' sums
     auto row_of = [](int i) { return 8 * (i >> 2) + (i & 3); };
     for (int chunk = c0; chunk < c1; ++chunk) {
         const int buffer = (chunk - c0) & 1, left = M - 32 * chunk - 4 * half;
         if (chunk + 1 < c1) wfetch(chunk + 1);
         Raw<TE, NT> ex[16];
-        if (p.extra != nullptr) {
+        if constexpr (MODE != kForward) {
             const unsigned off = (unsigned)(32 * chunk + 4 * half) * eb + pxc * (unsigned)sizeof(TE);
 #pragma unroll
             for (int i = 0; i < 16; ++i) ex[i] = load<TE, NT>(re, row_of(i) < left ? off : kBeyond, (unsigned)row_of(i) * eb);
@@ -143,7 +169,7 @@ __global__ __launch_bounds__(kThreads, 2) void strip_kernel(const StripParams p)
         // (the next sixteen channels' weights are asked for ahead of these ones' products, and no others: they would take registers)
         u32x4 next[TW];
 #pragma unroll
-        for (int q = 0; q < TW; ++q) next[q] = ws[q * 2 * kPitch];
+        for (int q = 0; q < TW; ++q) next[q] = ws[q * 2 * KC * kPitch];
 #pragma unroll
         for (int c = 0; c < KC; ++c) {
             u32x4 a[TW];
@@ -151,7 +177,7 @@ __global__ __launch_bounds__(kThreads, 2) void strip_kernel(const StripParams p)
             for (int q = 0; q < TW; ++q) a[q] = next[q];
             if (c + 1 < KC) {
 #pragma unroll
-                for (int q = 0; q < TW; ++q) next[q] = ws[((c + 1) * TW + q) * 2 * kPitch];
+                for (int q = 0; q < TW; ++q) next[q] = ws[(q * 2 * KC + 2 * (c + 1)) * kPitch];
             }
             // small terms first; neighbouring instructions on different sums
 #pragma unroll
@@ -179,7 +205,7 @@ __global__ __launch_bounds__(kThreads, 2) void strip_kernel(const StripParams p)
                 for (int i = 0; i < 16; ++i) v[16 * t + i] *= ex[i].value(t);
         } else {
             activate(p.act, v);
-            if (p.extra != nullptr) {
+            if constexpr (MODE == kResidual) {
 #pragma unroll
                 for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -253,7 +279,7 @@ __global__ __launch_bounds__(kThreads, 2) void strip_back_kernel(const BackParam
             terms_of<TF>(wr[i][0], wr[i][1], t[0]);
             terms_of<TF>(wr[i][2], wr[i][3], t[1]);
 #pragma unroll
-            for (int q = 0; q < TF; ++q) ws[2 * ((((k4 >> 2) * TF + q) * 2 + (k4 >> 1 & 1)) * kPitch + row) + (k4 & 1)] = u32x2{t[0][q], t[1][q]};
+            for (int q = 0; q < TF; ++q) ws[2 * ((q * 2 * KC + (k4 >> 1)) * kPitch + row) + (k4 & 1)] = u32x2{t[0][q], t[1][q]};
         }
         u32x4 *const ts = base + L::kForwardUnits;
 #pragma unroll
@@ -275,28 +301,7 @@ __global__ __launch_bounds__(kThreads, 2) void strip_back_kernel(const BackParam
     u32x4 b[KC][NT][TX];
     {
         const Rsrc rx = resource(static_cast<const T *>(p.x) + (size_t)n * p.x_stride, (long)K * ib);
-        const unsigned in_off = 8u * (unsigned)half * ib + first;
-        Raw<T, NT> r[KC][8];
-#pragma unroll
-        for (int c = 0; c < KC; ++c)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) r[c][j] = load<T, NT>(rx, 16 * c + 8 * half + j < K ? in_off : kBeyond, 16 * c + j < K ? (unsigned)(16 * c + j) * ib : 0u);
-        wput(0);
-#pragma unroll
-        for (int c = 0; c < KC; ++c)
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-#pragma unroll
-                for (int t = 0; t < NT; ++t) {
-                    if constexpr (TX == 1) {
-                        b[c][t][0][e] = __builtin_amdgcn_perm(r[c][2 * e + 1].w[0], r[c][2 * e].w[0], t == 0 ? 0x05040100u : 0x07060302u);
-                    } else {
-                        uint32_t q[TX];
-                        terms_of<TX>(r[c][2 * e].value(t), r[c][2 * e + 1].value(t), q);
-#pragma unroll
-                        for (int i = 0; i < TX; ++i) b[c][t][i][e] = q[i];
-                    }
-                }
+        load_operands<T, TX, KC, NT>(rx, 8u * (unsigned)half * ib + first, ib, K, b, [&] { wput(0); });
     }
     __syncthreads();
 
@@ -332,7 +337,7 @@ __global__ __launch_bounds__(kThreads, 2) void strip_back_kernel(const BackParam
         const u32x4 *ws = strip_lds + buffer * L::kUnits + half * kPitch + l32;
         u32x4 next[TF];
 #pragma unroll
-        for (int q = 0; q < TF; ++q) next[q] = ws[q * 2 * kPitch];
+        for (int q = 0; q < TF; ++q) next[q] = ws[q * 2 * KC * kPitch];
 #pragma unroll
         for (int c = 0; c < KC; ++c) {
             u32x4 a[TF];
@@ -340,7 +345,7 @@ __global__ __launch_bounds__(kThreads, 2) void strip_back_kernel(const BackParam
             for (int q = 0; q < TF; ++q) a[q] = next[q];
             if (c + 1 < KC) {
 #pragma unroll
-                for (int q = 0; q < TF; ++q) next[q] = ws[((c + 1) * TF + q) * 2 * kPitch];
+                for (int q = 0; q < TF; ++q) next[q] = ws[(q * 2 * KC + 2 * (c + 1)) * kPitch];
             }
 #pragma unroll
             for (int qw = TF - 1; qw >= 0; --qw)
@@ -423,11 +428,12 @@ hipError_t launch_as(const ProductParams &q, long N, hipStream_t s)
 {
     const long tiles = (q.P + 128 * NT - 1) / (128 * NT), all = tiles * N;
     const int chunks = (q.M + 31) / 32;
-    // The outputs are shared out over blocks where pixels alone leave compute units without two blocks, or the last round of blocks short:
+    // The outputs are shared out over blocks where pixels alone leave compute units without the blocks they hold, or the last round of blocks short:
     // the fewest chunks on the longest way, a block's beginning and its reading of x counted as two.
+    constexpr long kPlaces = kCus * strip_blocks(4 * KC * NT * TX, MODE != kForward || TRANS);
     long parts = 1, best = 0;
     for (int k = 1; k <= chunks; ++k) {
-        const long way = (all * k + 2 * kCus - 1) / (2 * kCus) * ((chunks + k - 1) / k + 2);
+        const long way = (all * k + kPlaces - 1) / kPlaces * ((chunks + k - 1) / k + 2);
         if (best == 0 || way < best) parts = k, best = way;
     }
     StripParams p;
@@ -450,7 +456,7 @@ hipError_t launch_as(const ProductParams &q, long N, hipStream_t s)
 template <typename TI, typename TO, typename TE, int TX, int TW, int KC, bool TRANS, int MODE>
 hipError_t launch_nt(const ProductParams &p, long N, hipStream_t s)
 {
-    if constexpr (KC * TX <= 16)
+    if constexpr (KC * TX <= 12 && !(KC == 12 && MODE == kResidual))
         if (p.P >= 2 && N * ((p.P + 255) / 256) * std::min(3, (p.M + 31) / 32) >= 2 * kCus) return launch_as<TI, TO, TE, TX, TW, KC, 2, TRANS, MODE>(p, N, s);
     return launch_as<TI, TO, TE, TX, TW, KC, 1, TRANS, MODE>(p, N, s);
 }
@@ -461,7 +467,7 @@ hipError_t launch_kc(const ProductParams &p, long N, hipStream_t s)
     if (k <= 2) return launch_nt<TI, TO, TE, TX, TW, 2, TRANS, MODE>(p, N, s);
     if (k <= 4) return launch_nt<TI, TO, TE, TX, TW, 4, TRANS, MODE>(p, N, s);
     if (k <= 8) return launch_nt<TI, TO, TE, TX, TW, 8, TRANS, MODE>(p, N, s);
-    return launch_nt<TI, TO, TE, TX, TW, 12, TRANS, MODE>(p, N, s);
+    return launch_nt<TI, TO, TE, TX, TW, TX == 3 ? 10 : 12, TRANS, MODE>(p, N, s);
 }
 
 template <typename T, int TX, int TF, int TG, int TB, int KC, int NT>
@@ -475,14 +481,15 @@ hipError_t launch_back_as(BackParams p, long N, hipStream_t s)
     hipLaunchKernelGGL((strip_back_kernel<T, TX, TF, TG, TB, KC, NT>), dim3((unsigned)grid), dim3(kThreads), lds, s, p);
     return hipGetLastError();
 }
-constexpr int kBackMostK[2] = {128, 96};  // bf16, fp32: what the registers hold
+// what the registers hold, with bf16 storage and with fp32
+constexpr int kMostK[2] = {192, 160}, kBackMostK[2] = {128, 64};
 
 }  // namespace
 
 bool back_fits(bool f32, int K, int M, long P, long N)
 {
     if (K > kBackMostK[f32] || (size_t)std::max(K, M) * P * 4 >= kMostImage || !(N == 1 || P >= 96)) return false;
-    // (a block goes through all outputs: few pixels are better shared out over two launches.  5 x 50 x 61, 96 to 45, fp32: 15.7 us, two launches 14.0)
+    // (a block goes through all outputs: few pixels are better shared out over two launches.  5 x 50 x 61, 96 to 45, fp32: two launches 14.0 us, one 15.7)
     return N * ((P + 127) / 128) >= kCus;
 }
 
@@ -491,8 +498,7 @@ hipError_t launch_back(bool f32, const BackParams &p, long N, hipStream_t s)
     const int k = (p.K + 15) / 16;
     if (f32) {
         if (k <= 2) return launch_back_as<float, 3, 3, 3, 3, 2, 1>(p, N, s);
-        if (k <= 4) return launch_back_as<float, 3, 3, 3, 3, 4, 1>(p, N, s);
-        return launch_back_as<float, 3, 3, 3, 3, 6, 1>(p, N, s);
+        return launch_back_as<float, 3, 3, 3, 3, 4, 1>(p, N, s);
     }
     const bool two = p.P >= 2 && N * ((p.P + 255) / 256) >= 2 * kCus;
     if (k <= 2) return two ? launch_back_as<bf16s, 1, 3, 2, 2, 2, 2>(p, N, s) : launch_back_as<bf16s, 1, 3, 2, 2, 2, 1>(p, N, s);
@@ -504,7 +510,7 @@ bool strip_fits(int kind, const ProductParams &p, long N)
 {
     const size_t in = kind == kForwardBf16 || kind == kSlopeBf16 || kind == kBackBf16 ? 2 : 4, out = kind == kForwardBf16 || kind == kBackBf16 || kind == kBackGp ? 2 : 4;
     // (the slope's other input is no wider than what it writes)
-    if (p.K > 192 || (size_t)p.K * p.P * in >= kMostImage || (size_t)p.M * p.P * out >= kMostImage) return false;
+    if (p.K > kMostK[kind == kForwardF32 || kind == kSlopeF32 || kind == kBackF32] || (size_t)p.K * p.P * in >= kMostImage || (size_t)p.M * p.P * out >= kMostImage) return false;
     // small images fill too little of a block's pixels
     return N == 1 || p.P >= 96;
 }
@@ -512,8 +518,8 @@ bool strip_fits(int kind, const ProductParams &p, long N)
 hipError_t launch_strip(int kind, const ProductParams &p, long N, hipStream_t s)
 {
     switch (kind) {
-    case kForwardF32: return launch_kc<float, float, float, 3, 3, false, kForward>(p, N, s);
-    case kForwardBf16: return launch_kc<bf16s, bf16s, bf16s, 1, 2, false, kForward>(p, N, s);
+    case kForwardF32: return p.extra != nullptr ? launch_kc<float, float, float, 3, 3, false, kResidual>(p, N, s) : launch_kc<float, float, float, 3, 3, false, kForward>(p, N, s);
+    case kForwardBf16: return p.extra != nullptr ? launch_kc<bf16s, bf16s, bf16s, 1, 2, false, kResidual>(p, N, s) : launch_kc<bf16s, bf16s, bf16s, 1, 2, false, kForward>(p, N, s);
     case kSlopeF32: return launch_kc<float, float, float, 3, 3, false, kSlope>(p, N, s);
     case kSlopeBf16: return launch_kc<bf16s, float, bf16s, 1, 3, false, kSlope>(p, N, s);
     case kBackF32: return launch_kc<float, float, float, 3, 3, true, kForward>(p, N, s);
