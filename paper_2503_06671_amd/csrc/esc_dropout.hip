@@ -66,49 +66,115 @@ __device__ __forceinline__ uint32_t draw_at(const Words &w, uint32_t j)
     return (j & 1) ? v >> 16 : v & 0xffffu;
 }
 
-// Eight neighbouring elements at any address their type allows.
-template <typename E>
-struct __attribute__((packed, aligned(sizeof(E)))) Eight {
-    E e[kChunk];
-};
-template <typename E>
-__device__ __forceinline__ void load8(const E *p, int first, int last, float (&v)[kChunk])
-{
-    Eight<E> r;
-    if (first == 0 && last == kChunk) {
-        r = *reinterpret_cast<const Eight<E> *>(p);
-    } else {
-#pragma unroll
-        for (int j = 0; j < kChunk; ++j) r.e[j] = j >= first && j < last ? p[j] : E(0);
-    }
-#pragma unroll
-    for (int j = 0; j < kChunk; ++j) {
-        if constexpr (sizeof(E) == 4) v[j] = r.e[j];
-        else v[j] = __uint_as_float((uint32_t)r.e[j] << 16);
-    }
-}
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+typedef u32x4 Loose4 __attribute__((aligned(4)));
+typedef u32x4 Loose2 __attribute__((aligned(2)));
+
+// Eight neighbouring elements at any address their type allows: all of them (WHOLE), or those from `first` to `last`.
 template <typename E>
-__device__ __forceinline__ void store8(E *p, int first, int last, const float (&v)[kChunk])
-{
-    Eight<E> r;
-    if constexpr (sizeof(E) == 4) {
+struct Eight {
+    static constexpr int kWords = kChunk * (int)sizeof(E) / 16;
+    typedef typename std::conditional<sizeof(E) == 4, Loose4, Loose2>::type Loose;
+    u32x4 w[kWords];
+    template <bool WHOLE>
+    __device__ __forceinline__ void load(const E *p, int first, int last)
+    {
+        if constexpr (WHOLE) {
 #pragma unroll
-        for (int j = 0; j < kChunk; ++j) r.e[j] = v[j];
-    } else {
+            for (int i = 0; i < kWords; ++i) w[i] = reinterpret_cast<const Loose *>(p)[i];
+        } else {
+            E e[kChunk];
 #pragma unroll
-        for (int j = 0; j < kChunk; j += 2) {
-            const uint32_t two = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{v[j], v[j + 1]}, bf16x2));
-            r.e[j] = (uint16_t)two, r.e[j + 1] = (uint16_t)(two >> 16);
+            for (int j = 0; j < kChunk; ++j) e[j] = j >= first && j < last ? p[j] : E(0);
+            __builtin_memcpy(w, e, sizeof(w));
         }
     }
-    if (first == 0 && last == kChunk) {
-        *reinterpret_cast<Eight<E> *>(p) = r;
-    } else {
+    template <bool WHOLE>
+    __device__ __forceinline__ void store(E *p, int first, int last) const
+    {
+        if constexpr (WHOLE) {
 #pragma unroll
-        for (int j = 0; j < kChunk; ++j)
-            if (j >= first && j < last) p[j] = r.e[j];
+            for (int i = 0; i < kWords; ++i) reinterpret_cast<Loose *>(p)[i] = w[i];
+        } else {
+            E e[kChunk];
+            __builtin_memcpy(e, w, sizeof(w));
+#pragma unroll
+            for (int j = 0; j < kChunk; ++j)
+                if (j >= first && j < last) p[j] = e[j];
+        }
+    }
+    __device__ __forceinline__ float value(int j) const
+    {
+        if constexpr (sizeof(E) == 4) return __uint_as_float(w[j >> 2][j & 3]);
+        else return __uint_as_float((j & 1) ? w[0][j >> 1] & 0xffff0000u : w[0][j >> 1] << 16);
+    }
+    __device__ __forceinline__ void set(const float (&v)[kChunk])
+    {
+#pragma unroll
+        for (int j = 0; j < kChunk; ++j) {
+            if constexpr (sizeof(E) == 4) w[j >> 2][j & 3] = __float_as_uint(v[j]);
+            else if ((j & 1) == 0) w[0][j >> 1] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{v[j], v[j + 1]}, bf16x2));
+        }
+    }
+};
+
+// A block's part of a span: kUnroll chunks a thread.  WHOLE: all of them lie in the span.
+template <typename E, int KIND, bool RES, bool WHOLE>
+__device__ __forceinline__ void part_of_span(const DropParams &p, uint64_t offset, long span, long part, const E *x, const E *res, E *out, int shift)
+{
+    const long base = span * p.span / kChunk;
+    bool all = true;
+    if constexpr (KIND == kPerSpan) {
+        if (p.q != 0) all = draw_at(philox((uint64_t)span >> 3, offset, p.seed), (uint32_t)span & 7) >= p.q;
+    }
+    Eight<E> v[kUnroll], r[kUnroll];
+    int first[kUnroll], last[kUnroll];
+    long at[kUnroll];
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+        at[u] = (part * kPart + u * kThreads + (long)threadIdx.x) * kChunk - shift;
+        first[u] = at[u] < 0 ? (int)-at[u] : 0;
+        last[u] = (int)(at[u] >= p.span ? 0 : p.span - at[u] < kChunk ? p.span - at[u] : kChunk);
+        if (!WHOLE && last[u] <= 0) continue;
+        if (KIND != kPerSpan || all) v[u].template load<WHOLE>(x + at[u], first[u], last[u]);
+        if constexpr (RES) r[u].template load<WHOLE>(res + at[u], first[u], last[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+        if (!WHOLE && last[u] <= 0) continue;
+        bool keep[kChunk];
+        if constexpr (KIND == kPerElement) {
+            const Words w = philox((uint64_t)(base + (at[u] + shift) / kChunk), offset, p.seed);
+#pragma unroll
+            for (int j = 0; j < kChunk; ++j) keep[j] = draw_of(w, j) >= p.q;
+        } else if constexpr (KIND == kPerSpan) {
+#pragma unroll
+            for (int j = 0; j < kChunk; ++j) keep[j] = all;
+        } else {
+            // (a span is an image of fewer than 2^31 elements)
+            uint64_t held = ~(uint64_t)0;
+            Words w{};
+            uint32_t plane = (uint32_t)at[u] / p.plane, left = p.plane - ((uint32_t)at[u] - plane * p.plane);
+#pragma unroll
+            for (int j = 0; j < kChunk; ++j) {
+                const uint64_t unit = (uint64_t)span * (uint64_t)p.units_of_span + plane;
+                if (unit >> 3 != held) held = unit >> 3, w = philox(held, offset, p.seed);
+                keep[j] = draw_at(w, (uint32_t)unit & 7) >= p.q;
+                if (--left == 0) ++plane, left = p.plane;
+            }
+        }
+        float o[kChunk];
+#pragma unroll
+        for (int j = 0; j < kChunk; ++j) {
+            o[j] = keep[j] ? v[u].value(j) * p.scale : 0.f;
+            if constexpr (RES) o[j] = o[j] + r[u].value(j);
+        }
+        Eight<E> to;
+        to.set(o);
+        to.template store<WHOLE>(out + at[u], first[u], last[u]);
     }
 }
 
@@ -124,57 +190,10 @@ __global__ __launch_bounds__(kThreads) void dropout_kernel(const DropParams p)
         const E *res = RES ? static_cast<const E *>(p.residual) + image * p.residual_stride + inside : nullptr;
         E *out = static_cast<E *>(p.out) + image * p.out_stride + inside;
         // chunks begin at multiples of eight of the elements' numbers where these are the draws' too
-        const long g0 = span * p.span;
-        const int shift = KIND == kPerElement ? (int)(g0 & (kChunk - 1)) : 0;
-        const long base = g0 / kChunk;
-        bool all = true;
-        if constexpr (KIND == kPerSpan) {
-            if (p.q != 0) all = draw_at(philox((uint64_t)span >> 3, offset, p.seed), (uint32_t)span & 7) >= p.q;
-        }
-        float v[kUnroll][kChunk], r[kUnroll][kChunk];
-        int first[kUnroll], last[kUnroll];
-        long at[kUnroll];
-#pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
-            at[u] = (part * kPart + u * kThreads + (long)threadIdx.x) * kChunk - shift;
-            first[u] = at[u] < 0 ? (int)-at[u] : 0;
-            last[u] = (int)(at[u] >= p.span ? 0 : p.span - at[u] < kChunk ? p.span - at[u] : kChunk);
-            if (last[u] <= 0) continue;
-            if (KIND != kPerSpan || all) load8<E>(x + at[u], first[u], last[u], v[u]);
-            if constexpr (RES) load8<E>(res + at[u], first[u], last[u], r[u]);
-        }
-#pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
-            if (last[u] <= 0) continue;
-            bool keep[kChunk];
-            if constexpr (KIND == kPerElement) {
-                const Words w = philox((uint64_t)(base + (at[u] + shift) / kChunk), offset, p.seed);
-#pragma unroll
-                for (int j = 0; j < kChunk; ++j) keep[j] = draw_of(w, j) >= p.q;
-            } else if constexpr (KIND == kPerSpan) {
-#pragma unroll
-                for (int j = 0; j < kChunk; ++j) keep[j] = all;
-            } else {
-                // (a span is an image of fewer than 2^31 elements)
-                uint64_t held = ~(uint64_t)0;
-                Words w{};
-                uint32_t plane = (uint32_t)at[u] / p.plane, left = p.plane - ((uint32_t)at[u] - plane * p.plane);
-#pragma unroll
-                for (int j = 0; j < kChunk; ++j) {
-                    const uint64_t unit = (uint64_t)span * (uint64_t)p.units_of_span + plane;
-                    if (unit >> 3 != held) held = unit >> 3, w = philox(held, offset, p.seed);
-                    keep[j] = draw_at(w, (uint32_t)unit & 7) >= p.q;
-                    if (--left == 0) ++plane, left = p.plane;
-                }
-            }
-            float o[kChunk];
-#pragma unroll
-            for (int j = 0; j < kChunk; ++j) {
-                o[j] = keep[j] ? v[u][j] * p.scale : 0.f;
-                if constexpr (RES) o[j] = o[j] + r[u][j];
-            }
-            store8<E>(out + at[u], first[u], last[u], o);
-        }
+        const int shift = KIND == kPerElement ? (int)(span * p.span & (kChunk - 1)) : 0;
+        const long begin = part * kPart * kChunk - shift;
+        if (begin >= 0 && begin + kPart * kChunk <= p.span) part_of_span<E, KIND, RES, true>(p, offset, span, part, x, res, out, shift);
+        else part_of_span<E, KIND, RES, false>(p, offset, span, part, x, res, out, shift);
     }
 }
 
