@@ -344,16 +344,25 @@ struct Staged {
         for (int i = 0; i < kEach; ++i)
             r[i] = *reinterpret_cast<const R *>(image + (long)min(first + row_of(i), rows - 1) * P + at + R::kCount * run_of(i));
     }
-    // The same of a stage that begins with pixel q of all images' and lies where it likes: pixel by pixel, zeros beyond the last.
-    __device__ __forceinline__ void scattered(const T *base, long stride, long P, long pixels, long q, int first, int rows)
+    // The same of a stage that begins with pixel `at` of image n and passes the image's border or, `left` pixels on, the last image's: pixel by pixel,
+    // zeros beyond the last.
+    __device__ __forceinline__ void scattered(const T *base, long stride, long P, long left, long n, long at, int first, int rows)
     {
+        static_assert(kThreads % kRunsOfRow == 0, "a thread's runs are of the same pixels");
+        const int mine = R::kCount * run_of(0);
+        long pn = n, pat = at + mine;
+        while (pat >= P) pat -= P, ++pn;
 #pragma unroll
-        for (int i = 0; i < kEach; ++i)
+        for (int j = 0; j < R::kCount; ++j) {
+            const bool in = mine + j < left;
+            const T *const pixel = base + (in ? pn * stride + pat : n * stride + at);
 #pragma unroll
-            for (int j = 0; j < R::kCount; ++j) {
-                const long mine = q + R::kCount * run_of(i) + j, one = min(mine, pixels - 1), n = one / P;
-                r[i].e[j] = mine < pixels ? base[n * stride + (long)min(first + row_of(i), rows - 1) * P + one - n * P] : T{};
+            for (int i = 0; i < kEach; ++i) {
+                const T v = pixel[(long)min(first + row_of(i), rows - 1) * P];
+                r[i].e[j] = in ? v : T{};
             }
+            if (++pat == P) pat = 0, ++pn;
+        }
     }
     __device__ __forceinline__ void put(u32x4 *lds, float *sums) const
     {
@@ -398,14 +407,20 @@ __global__ __launch_bounds__(kThreads, 2) void product_weights_kernel(const Weig
     const TI *const xp = static_cast<const TI *>(p.x);
     G g;
     X x;
-    auto fetch = [&](long st) {
-        const long q = st * kPixels, n = q / p.P, at = q - n * p.P;
+    // the stage that is fetched next: its first pixel, of all images' and of its image
+    long q = first * kPixels, n = q / p.P, at = q - n * p.P;
+    auto fetch = [&] {
         if (at + kPixels <= p.P) {  // (the same for the block)
             g.whole(gp + n * p.g_stride, p.P, at, m0, p.M);
             x.whole(xp + n * p.x_stride, p.P, at, k0, p.K);
         } else {
-            g.scattered(gp, p.g_stride, p.P, p.pixels, q, m0, p.M);
-            x.scattered(xp, p.x_stride, p.P, p.pixels, q, k0, p.K);
+            g.scattered(gp, p.g_stride, p.P, p.pixels - q, n, at, m0, p.M);
+            x.scattered(xp, p.x_stride, p.P, p.pixels - q, n, at, k0, p.K);
+        }
+        q += kPixels, at += kPixels;
+        if (at >= p.P) {
+            const long images = at / p.P;
+            n += images, at -= images * p.P;
         }
     };
     const bool has_b = p.has_b && k0 == 0;
@@ -426,13 +441,13 @@ __global__ __launch_bounds__(kThreads, 2) void product_weights_kernel(const Weig
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
     if (first < end) {
-        fetch(first);
+        fetch();
         put(0);
     }
     __syncthreads();
     for (long st = first; st < end; ++st) {
         const int buffer = (int)(st - first) & 1;
-        if (st + 1 < end) fetch(st + 1);
+        if (st + 1 < end) fetch();
         const u32x4 *gs = s[buffer] + 32 * MT * wm + l32, *xs = s[buffer] + G::kUnits + 32 * KT * wk + l32;
 #pragma unroll
         for (int c = 0; c < kPixels / 16; ++c) {
