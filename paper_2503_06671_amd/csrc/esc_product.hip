@@ -108,21 +108,19 @@ __global__ __launch_bounds__(kThreads, 2) void product_kernel(const ProductParam
         for (int i = 0; i < kEach; ++i) {
             int row, k4;
             run_of(i, row, k4);
-            load_weights<TRANS>(rw, M, K, p.w_ld, four, m0 + row, 32 * st + 4 * k4, wr[i]);
+            if constexpr (TRANS) load_weights_across(rw, M, K, p.w_ld, m0 + row, 32 * st + 4 * __builtin_amdgcn_readfirstlane(k4), 0, wr[i]);
+            else load_weights(rw, M, K, p.w_ld, four, m0 + row, 32 * st + 4 * k4, wr[i]);
         }
     };
-    auto wput = [&](int st) {
+    auto wput = [&](int i, int st) {   // the i-th run
         u32x2 *ws = reinterpret_cast<u32x2 *>(product_lds + (st & 1) * C::kBuffer);
+        int row, k4;
+        run_of(i, row, k4);
+        uint32_t t[2][TW];
+        terms_of<TW>(wr[i][0], wr[i][1], t[0]);
+        terms_of<TW>(wr[i][2], wr[i][3], t[1]);
 #pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-            int row, k4;
-            run_of(i, row, k4);
-            uint32_t t[2][TW];
-            terms_of<TW>(wr[i][0], wr[i][1], t[0]);
-            terms_of<TW>(wr[i][2], wr[i][3], t[1]);
-#pragma unroll
-            for (int q = 0; q < TW; ++q) ws[2 * ((q * 4 + (k4 >> 1)) * C::kPitch + row) + (k4 & 1)] = u32x2{t[0][q], t[1][q]};
-        }
+        for (int q = 0; q < TW; ++q) ws[2 * ((q * 4 + (k4 >> 1)) * C::kPitch + row) + (k4 & 1)] = u32x2{t[0][q], t[1][q]};
     };
 
     // what is asked for stays in the order it is written in, and in front of the products that follow: at a wait for some of it the rest stays under way
@@ -139,7 +137,8 @@ __global__ __launch_bounds__(kThreads, 2) void product_kernel(const ProductParam
         }
     float *bias = reinterpret_cast<float *>(product_lds + 2 * C::kBuffer);
     if (tid < 32 * MT) bias[tid] = p.b != nullptr && m0 + tid < M ? p.b[m0 + tid] : 0.f;
-    wput(0);
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) wput(i, 0);
     f32x16 acc[MT][NT];
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
@@ -149,51 +148,70 @@ __global__ __launch_bounds__(kThreads, 2) void product_kernel(const ProductParam
             for (int i = 0; i < 16; ++i) acc[mt][t][i] = 0.f;
     __syncthreads();
 
-    auto body = [&](int st, X (&raw)[2][8][kLoads]) {
-        wfetch(st + 1);
-        order();
-        const u32x4 *ws = product_lds + (st & 1) * C::kBuffer + half * C::kPitch + l32;
+    // a quarter of the right operand of sixteen channels: the terms of two of each lane's eight
+    auto split = [&](const X (&raw)[8][kLoads], int e, u32x4 (&to)[NT][TX]) {
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
-            u32x4 b[NT][TX];
+        for (int t = 0; t < NT; ++t) {
+            constexpr bool one = kLoads > 1;
+            const X &v0 = raw[2 * e][one ? t : 0], &v1 = raw[2 * e + 1][one ? t : 0];
+            if constexpr (!kWide<TI> && TX == 1 && !ACROSS) {
+                to[t][0][e] = __builtin_amdgcn_perm(v1.w[0], v0.w[0], t == 0 ? 0x05040100u : 0x07060302u);
+            } else {
+                uint32_t q[TX];
+                terms_of<TX>(v0.value(one ? 0 : t), v1.value(one ? 0 : t), q);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                if constexpr (!kWide<TI> && TX == 1 && !ACROSS) {
-                    b[0][0][e] = __builtin_amdgcn_perm(raw[c][2 * e + 1][0].w[0], raw[c][2 * e][0].w[0], 0x05040100u);
-                    if constexpr (NT == 2) b[NT - 1][0][e] = __builtin_amdgcn_perm(raw[c][2 * e + 1][0].w[0], raw[c][2 * e][0].w[0], 0x07060302u);
-                } else {
-#pragma unroll
-                    for (int t = 0; t < NT; ++t) {
-                        constexpr bool one = kLoads > 1;
-                        uint32_t q[TX];
-                        terms_of<TX>(raw[c][2 * e][one ? t : 0].value(one ? 0 : t), raw[c][2 * e + 1][one ? t : 0].value(one ? 0 : t), q);
-#pragma unroll
-                        for (int i = 0; i < TX; ++i) b[t][i][e] = q[i];
-                    }
-                }
-            }
-            order();
-            xfetch(st + kAhead, c, raw[c]);
-            order();
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {
-                u32x4 a[TW];
-#pragma unroll
-                for (int q = 0; q < TW; ++q) a[q] = ws[(q * 4 + 2 * c) * C::kPitch + 32 * mt];
-                // small terms first; neighbouring instructions on different sums
-#pragma unroll
-                for (int qw = TW - 1; qw >= 0; --qw)
-#pragma unroll
-                    for (int qx = TX - 1; qx >= 0; --qx) {
-                        if (qw + qx >= kTop) continue;
-#pragma unroll
-                        for (int t = 0; t < NT; ++t)
-                            acc[mt][t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a[qw]), __builtin_bit_cast(bf16x8, b[t][qx]),
-                                                                                 acc[mt][t], 0, 0, 0);
-                    }
+                for (int i = 0; i < TX; ++i) to[t][i][e] = q[i];
             }
         }
-        wput(st + 1);
+    };
+    // A stage's products in steps of 32 outputs and sixteen channels, each with the next one's weights asked for ahead and, between its matrix instructions, a
+    // share of what is to be split: the second sixteen channels in the first MT steps, the next stage's weights in the others.
+    auto body = [&](int st, X (&raw)[2][8][kLoads]) {
+        static_assert(kEach == MT, "a run for each of the second sixteen channels' steps");
+        const u32x4 *ws = product_lds + (st & 1) * C::kBuffer + half * C::kPitch + l32;
+        auto weights_of = [&](int step, u32x4 (&a)[TW]) {
+#pragma unroll
+            for (int q = 0; q < TW; ++q) a[q] = ws[(q * 4 + 2 * (step / MT)) * C::kPitch + 32 * (step % MT)];
+        };
+        u32x4 b[2][NT][TX], next[TW];
+        weights_of(0, next);
+        wfetch(st + 1);
+        order();
+#pragma unroll
+        for (int e = 0; e < 4; ++e) split(raw[0], e, b[0]);
+        order();
+        xfetch(st + kAhead, 0, raw[0]);
+        order();
+#pragma unroll
+        for (int step = 0; step < 2 * MT; ++step) {
+            const int c = step / MT, mt = step % MT;
+            u32x4 a[TW];
+#pragma unroll
+            for (int q = 0; q < TW; ++q) a[q] = next[q];
+            if (step + 1 < 2 * MT) weights_of(step + 1, next);
+            // small terms first; neighbouring instructions on different sums
+#pragma unroll
+            for (int qw = TW - 1; qw >= 0; --qw)
+#pragma unroll
+                for (int qx = TX - 1; qx >= 0; --qx) {
+                    if (qw + qx >= kTop) continue;
+#pragma unroll
+                    for (int t = 0; t < NT; ++t)
+                        acc[mt][t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a[qw]), __builtin_bit_cast(bf16x8, b[c][t][qx]), acc[mt][t], 0, 0, 0);
+                }
+            if (c == 0) {
+#pragma unroll
+                for (int e = 4 * mt / MT; e < 4 * (mt + 1) / MT; ++e) split(raw[1], e, b[1]);
+            } else {
+                wput(mt, st + 1);
+            }
+            interleave<NT * (kTop == 1 ? 1 : TX == 1 || TW == 1 ? kTop : kTop * (kTop + 1) / 2)>();
+            __builtin_amdgcn_sched_barrier(0);
+            if (step == MT - 1) {
+                xfetch(st + kAhead, 1, raw[1]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
         __syncthreads();
     };
     // (beyond the last stage loads bring nothing, and zeros are put)
@@ -286,8 +304,9 @@ hipError_t launch_product(const ProductParams &p, long N, hipStream_t s)
     const size_t widest = std::max(std::max(p.K * sizeof(TI), p.M * sizeof(TO)), p.M * sizeof(TE)) * (size_t)p.P;
     if (widest >= kMostImage || p.P < 2 || (N > 1 && p.P < 96)) return launch_as<TI, TO, TE, TX, TW, 2, 1, TRANS, MODE, true>(p, N, s);
     const auto blocks = [&](int mt, int nt) { return N * ((p.P + 128 * nt - 1) / (128 * nt)) * ((p.M + 32 * mt - 1) / (32 * mt)); };
-    // as much for a wavefront as leaves every compute unit two blocks
-    if (p.M > 64 && blocks(4, 2) >= 2 * kCus) return launch_as<TI, TO, TE, TX, TW, 4, 2, TRANS, MODE, false>(p, N, s);
+    // as much for a wavefront as leaves every compute unit two blocks (and, with three terms of both, registers)
+    if constexpr (TX != 3)
+        if (p.M > 64 && blocks(4, 2) >= 2 * kCus) return launch_as<TI, TO, TE, TX, TW, 4, 2, TRANS, MODE, false>(p, N, s);
     if (blocks(2, 2) >= 2 * kCus) return launch_as<TI, TO, TE, TX, TW, 2, 2, TRANS, MODE, false>(p, N, s);
     return launch_as<TI, TO, TE, TX, TW, 2, 1, TRANS, MODE, false>(p, N, s);
 }

@@ -195,25 +195,40 @@ __device__ __forceinline__ void store(Rsrc r, unsigned voff, unsigned soff, floa
     }
 }
 
+// N matrix instructions, with ordinary ones between them: a wavefront's next instruction waits for the matrix unit only if it is one for it.
+template <int N>
+__device__ __forceinline__ void interleave()
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x002, 6, 0);
+    }
+}
+
 // ---- weights: runs of four channels of one output, zeros beyond K and M ----
 
-// Four weights of output m from channel k on (TRANS: w's rows are the channels).  FOUR: K is a multiple of four, a run is inside or outside as a whole.
-template <bool TRANS>
+// Four weights of output m from channel k on.  `four`: K is a multiple of four, a run is inside or outside as a whole.
 __device__ __forceinline__ void load_weights(Rsrc rw, int M, int K, int ld, bool four, int m, int k, float (&w)[4])
 {
-    if (!TRANS && four) {
+    if (four) {
         const u32x4 v = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rw, (int)(m < M && k < K ? 4u * ((unsigned)m * (unsigned)ld + (unsigned)k) : kBeyond), 0, 0));
 #pragma unroll
         for (int e = 0; e < 4; ++e) w[e] = __uint_as_float(v[e]);
     } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const unsigned at = TRANS ? (unsigned)(k + e) * (unsigned)ld + (unsigned)m : (unsigned)m * (unsigned)ld + (unsigned)(k + e);
-            w[e] = __uint_as_float((unsigned)__builtin_amdgcn_raw_buffer_load_b32(rw, (int)(m < M && k + e < K ? 4u * at : kBeyond), 0, 0));
-        }
+        for (int e = 0; e < 4; ++e)
+            w[e] = __uint_as_float((unsigned)__builtin_amdgcn_raw_buffer_load_b32(rw, (int)(m < M && k + e < K ? 4u * ((unsigned)m * (unsigned)ld + (unsigned)(k + e)) : kBeyond), 0, 0));
     }
 }
-
+// The same where w's rows are the channels.  K0 of k is the wavefront's, the rest a lane's.
+__device__ __forceinline__ void load_weights_across(Rsrc rw, int M, int K, int ld, int m, int k0, int k1, float (&w)[4])
+{
+    const unsigned at = m < M ? 4u * ((unsigned)k1 * (unsigned)ld + (unsigned)m) : kBeyond;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        w[e] = __uint_as_float((unsigned)__builtin_amdgcn_raw_buffer_load_b32(rw, (int)(k0 + k1 + e < K ? at : kBeyond), (int)(k0 + e < K ? 4u * ((unsigned)(k0 + e) * (unsigned)ld) : 0u), 0));
+}
 
 // Which eighths of the grid the dies get: consecutive pieces on one die.
 __device__ __forceinline__ unsigned piece_of(unsigned block, unsigned blocks)

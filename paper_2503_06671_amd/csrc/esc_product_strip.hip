@@ -113,7 +113,8 @@ __global__ __launch_bounds__(kThreads, strip_blocks(4 * KC * NT * TX, MODE != kF
         for (int i = 0; i < kEach; ++i) {
             int row, k4;
             run_of(i, row, k4);
-            load_weights<TRANS>(rw, M, K, p.w_ld, four, 32 * chunk + row, 4 * k4, wr[i]);
+            if constexpr (TRANS) load_weights_across(rw, M, K, p.w_ld, 32 * chunk + row, 8 * (__builtin_amdgcn_readfirstlane(k4) >> 1), 4 * (k4 & 1), wr[i]);
+            else load_weights(rw, M, K, p.w_ld, four, 32 * chunk + row, 4 * k4, wr[i]);
         }
     };
     auto wput = [&](int buffer) {
@@ -257,7 +258,7 @@ __global__ __launch_bounds__(kThreads, 2) void strip_back_kernel(const BackParam
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
             const int u = tid + i * kThreads;
-            load_weights<false>(rw, M, K, K, four, 32 * chunk + u / (4 * KC), 4 * (u % (4 * KC)), wr[i]);
+            load_weights(rw, M, K, K, four, 32 * chunk + u / (4 * KC), 4 * (u % (4 * KC)), wr[i]);
         }
 #pragma unroll
         for (int i = 0; i < kEachT; ++i) {
