@@ -19,7 +19,6 @@ using namespace esc;
 
 constexpr size_t kAlign = 256;
 constexpr int kThreads = 256;
-constexpr int kLanes = 64, kGroups = kThreads / kLanes;  // of a block: pixels, and groups of channels
 constexpr int kMaxSplits = 64;
 constexpr int kRun = 1024;  // pixels that a block of the weights' sums takes at a time
 
@@ -50,73 +49,105 @@ __device__ __forceinline__ void put(E *p, float v)
     else *p = __builtin_bit_cast(uint16_t, (__bf16)v);
 }
 
-// The sum over the block's groups of channels of each pixel's value.
-__device__ __forceinline__ float over_groups(float v, float (&s)[kGroups][kLanes])
+// ---- any number of channels: a block's 1024 threads are LANES pixels of 1024 / LANES groups of channels, and read x as often as they need it ----
+
+constexpr int kAnyThreads = 1024, kAnyAhead = 8;  // (values under way at a time)
+
+// The sums over the block's groups of channels of each pixel's values.
+template <int LANES, int Q>
+__device__ __forceinline__ void over_groups(float (&v)[Q], float (*s)[kAnyThreads / LANES][LANES])
 {
-    const int lane = threadIdx.x & 63, group = threadIdx.x >> 6;
+    const int lane = threadIdx.x % LANES, group = threadIdx.x / LANES;
     __syncthreads();
-    s[group][lane] = v;
-    __syncthreads();
-    float t = 0.f;
 #pragma unroll
-    for (int g = 0; g < kGroups; ++g) t += s[g][lane];
-    return t;
+    for (int q = 0; q < Q; ++q) s[q][group][lane] = v[q];
+#pragma unroll
+    for (int half = kAnyThreads / LANES / 2; half > 0; half /= 2) {
+        __syncthreads();
+        if (group < half) {
+#pragma unroll
+            for (int q = 0; q < Q; ++q) s[q][group][lane] += s[q][group + half][lane];
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < Q; ++q) v[q] = s[q][0][lane];
 }
 
-// Any number of channels: x is read three times.
-template <typename E>
-__global__ __launch_bounds__(kThreads) void norm_any_kernel(const NormParams p)
+// f(c, values of N tensors at channel c) for the channels group, group + GROUPS, ...: kAnyAhead of each are asked for at a time.
+template <int GROUPS, int N, typename E, typename F>
+__device__ __forceinline__ void over_rows(const E *const (&from)[N], int group, int C, long P, F f)
 {
-    __shared__ float s[kGroups][kLanes];
-    const int lane = threadIdx.x & 63, group = threadIdx.x >> 6;
-    const long tiles = (p.P + kLanes - 1) / kLanes, all = tiles * p.N;
-    for (long tile = blockIdx.x; tile < all; tile += gridDim.x) {
-        const long n = tile / tiles, px = (tile - n * tiles) * kLanes + lane, pc = px < p.P ? px : p.P - 1;
-        const E *x = static_cast<const E *>(p.x) + n * p.x_stride + pc;
-        E *out = static_cast<E *>(p.out) + n * p.out_stride + pc;
-        float sum = 0.f;
-        for (int c = group; c < p.C; c += kGroups) sum += value(x + c * p.P);
-        const float mean = over_groups(sum, s) * p.inv_c;
-        sum = 0.f;
-        for (int c = group; c < p.C; c += kGroups) {
-            const float d = value(x + c * p.P) - mean;
-            sum += d * d;
+    for (int c0 = group; c0 < C; c0 += kAnyAhead * GROUPS) {
+        E v[N][kAnyAhead];
+#pragma unroll
+        for (int u = 0; u < kAnyAhead; ++u)
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i][u] = from[i][(long)min(c0 + u * GROUPS, C - 1) * P];
+#pragma unroll
+        for (int u = 0; u < kAnyAhead; ++u) {
+            float w[N];
+#pragma unroll
+            for (int i = 0; i < N; ++i) w[i] = widen(v[i][u]);
+            if (c0 + u * GROUPS < C) f(c0 + u * GROUPS, w);
         }
-        const float r = 1.f / sqrtf(over_groups(sum, s) * p.inv_c + p.eps);
+    }
+}
+
+template <typename E, int LANES>
+__global__ __launch_bounds__(kAnyThreads) void norm_any_kernel(const NormParams p)
+{
+    constexpr int kGroups = kAnyThreads / LANES;
+    __shared__ float s[1][kGroups][LANES];
+    const int lane = threadIdx.x % LANES, group = threadIdx.x / LANES;
+    const long tiles = (p.P + LANES - 1) / LANES, all = tiles * p.N;
+    for (long tile = blockIdx.x; tile < all; tile += gridDim.x) {
+        const long n = tile / tiles, px = (tile - n * tiles) * LANES + lane, pc = px < p.P ? px : p.P - 1;
+        const E *const x[1] = {static_cast<const E *>(p.x) + n * p.x_stride + pc};
+        E *out = static_cast<E *>(p.out) + n * p.out_stride + pc;
+        float sum[1] = {0.f};
+        over_rows<kGroups>(x, group, p.C, p.P, [&](int, const float (&v)[1]) { sum[0] += v[0]; });
+        over_groups<LANES>(sum, s);
+        const float mean = sum[0] * p.inv_c;
+        sum[0] = 0.f;
+        over_rows<kGroups>(x, group, p.C, p.P, [&](int, const float (&v)[1]) { sum[0] += (v[0] - mean) * (v[0] - mean); });
+        over_groups<LANES>(sum, s);
+        const float r = 1.f / sqrtf(sum[0] * p.inv_c + p.eps);
         if (px < p.P) {
-            for (int c = group; c < p.C; c += kGroups) {
-                const float u = (value(x + c * p.P) - mean) * r;
-                put(out + c * p.P, p.weight != nullptr ? u * p.weight[c] + (p.bias != nullptr ? p.bias[c] : 0.f) : p.bias != nullptr ? u + p.bias[c] : u);
-            }
+            over_rows<kGroups>(x, group, p.C, p.P, [&](int c, const float (&v)[1]) {
+                put(out + c * p.P, ((v[0] - mean) * r) * (p.weight != nullptr ? p.weight[c] : 1.f) + (p.bias != nullptr ? p.bias[c] : 0.f));
+            });
             if (p.mean != nullptr && group == 0) p.mean[n * p.P + px] = mean, p.rstd[n * p.P + px] = r;
         }
     }
 }
 
-template <typename E>
-__global__ __launch_bounds__(kThreads) void norm_back_any_kernel(const NormParams p)
+template <typename E, int LANES>
+__global__ __launch_bounds__(kAnyThreads) void norm_back_any_kernel(const NormParams p)
 {
-    __shared__ float s[kGroups][kLanes];
-    const int lane = threadIdx.x & 63, group = threadIdx.x >> 6;
-    const long tiles = (p.P + kLanes - 1) / kLanes, all = tiles * p.N;
+    constexpr int kGroups = kAnyThreads / LANES;
+    __shared__ float s[2][kGroups][LANES];
+    const int lane = threadIdx.x % LANES, group = threadIdx.x / LANES;
+    const long tiles = (p.P + LANES - 1) / LANES, all = tiles * p.N;
     for (long tile = blockIdx.x; tile < all; tile += gridDim.x) {
-        const long n = tile / tiles, px = (tile - n * tiles) * kLanes + lane, pc = px < p.P ? px : p.P - 1;
-        const E *x = static_cast<const E *>(p.x) + n * p.x_stride + pc, *g = static_cast<const E *>(p.grad_out) + n * p.out_stride + pc;
+        const long n = tile / tiles, px = (tile - n * tiles) * LANES + lane, pc = px < p.P ? px : p.P - 1;
+        const E *const xg[2] = {static_cast<const E *>(p.x) + n * p.x_stride + pc, static_cast<const E *>(p.grad_out) + n * p.out_stride + pc};
         const E *skip = p.skip != nullptr ? static_cast<const E *>(p.skip) + n * p.skip_stride + pc : nullptr;
         E *gx = static_cast<E *>(p.grad_x) + n * p.gx_stride + pc;
         const float mean = p.mean[n * p.P + pc], r = p.rstd[n * p.P + pc];
-        float sa = 0.f, sau = 0.f;
-        for (int c = group; c < p.C; c += kGroups) {
-            const float a = value(g + c * p.P) * (p.weight != nullptr ? p.weight[c] : 1.f), u = (value(x + c * p.P) - mean) * r;
-            sa += a, sau += a * u;
-        }
-        sa = over_groups(sa, s) * p.inv_c, sau = over_groups(sau, s) * p.inv_c;
+        float sum[2] = {0.f, 0.f};
+        over_rows<kGroups>(xg, group, p.C, p.P, [&](int c, const float (&v)[2]) {
+            const float a = v[1] * (p.weight != nullptr ? p.weight[c] : 1.f);
+            sum[0] += a, sum[1] += a * ((v[0] - mean) * r);
+        });
+        over_groups<LANES>(sum, s);
+        const float sa = sum[0] * p.inv_c, sau = sum[1] * p.inv_c;
         if (px >= p.P) continue;
-        for (int c = group; c < p.C; c += kGroups) {
-            const float a = value(g + c * p.P) * (p.weight != nullptr ? p.weight[c] : 1.f), u = (value(x + c * p.P) - mean) * r;
-            const float v = r * (a - sa - u * sau);
-            put(gx + c * p.P, skip != nullptr ? v + value(skip + c * p.P) : v);
-        }
+        over_rows<kGroups>(xg, group, p.C, p.P, [&](int c, const float (&v)[2]) {
+            const float a = v[1] * (p.weight != nullptr ? p.weight[c] : 1.f), u = (v[0] - mean) * r;
+            const float o = r * (a - sa - u * sau);
+            put(gx + c * p.P, skip != nullptr ? o + value(skip + c * p.P) : o);
+        });
     }
 }
 
@@ -468,6 +499,25 @@ int lanes_pixels(long N, long P, Split k)
 }
 long sets_of(Split k) { return k.ws < 4 ? 4 / k.ws : 1; }
 
+// Sixteen pixels of a block where 64 would leave compute units without a tile.
+template <bool BACK>
+hipError_t launch_any(const NormParams &p, bool f32, hipStream_t s)
+{
+    const long few = (p.P + 63) / 64 * p.N;
+    const dim3 block(kAnyThreads), grid((unsigned)std::min<long>(few < kCus ? (p.P + 15) / 16 * p.N : few, 1 << 20));
+    const auto launch = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, grid, block, 0, s, p);
+        return hipGetLastError();
+    };
+    if constexpr (BACK) {
+        if (few < kCus) return f32 ? launch(norm_back_any_kernel<float, 16>) : launch(norm_back_any_kernel<uint16_t, 16>);
+        return f32 ? launch(norm_back_any_kernel<float, 64>) : launch(norm_back_any_kernel<uint16_t, 64>);
+    } else {
+        if (few < kCus) return f32 ? launch(norm_any_kernel<float, 16>) : launch(norm_any_kernel<uint16_t, 16>);
+        return f32 ? launch(norm_any_kernel<float, 64>) : launch(norm_any_kernel<uint16_t, 64>);
+    }
+}
+
 esc_status shape(const esc_layernorm *a, long *P)
 {
     if (a == nullptr) return ESC_ERR_NULL;
@@ -534,10 +584,7 @@ esc_status esc_layernorm_forward(const void *x, esc_dtype dt, const esc_layernor
             return e == hipSuccess ? ESC_OK : ESC_ERR_HIP;
         }
     }
-    const dim3 grid((unsigned)std::min<long>((P + kLanes - 1) / kLanes * a->N, 1 << 20)), block(kThreads);
-    if (dt == ESC_F32) hipLaunchKernelGGL(norm_any_kernel<float>, grid, block, 0, s, p);
-    else hipLaunchKernelGGL(norm_any_kernel<uint16_t>, grid, block, 0, s, p);
-    return hipGetLastError() == hipSuccess ? ESC_OK : ESC_ERR_HIP;
+    return launch_any<false>(p, dt == ESC_F32, s) == hipSuccess ? ESC_OK : ESC_ERR_HIP;
 }
 
 esc_status esc_layernorm_backward(const void *x, const void *grad_out, const void *grad_skip, esc_dtype dt, const esc_layernorm *a, const void *saved,
@@ -593,10 +640,7 @@ esc_status esc_layernorm_backward(const void *x, const void *grad_out, const voi
         return !sums || add_parts(p.part, p.splits, a->C, g->weight, a->C, g->bias, accumulate, s) == hipSuccess ? ESC_OK : ESC_ERR_HIP;
     }
     if (g->x != nullptr) {
-        const dim3 grid((unsigned)std::min<long>((P + kLanes - 1) / kLanes * a->N, 1 << 20));
-        if (dt == ESC_F32) hipLaunchKernelGGL(norm_back_any_kernel<float>, grid, block, 0, s, p);
-        else hipLaunchKernelGGL(norm_back_any_kernel<uint16_t>, grid, block, 0, s, p);
-        if (hipGetLastError() != hipSuccess) return ESC_ERR_HIP;
+        if (launch_any<true>(p, dt == ESC_F32, s) != hipSuccess) return ESC_ERR_HIP;
     }
     if (sums) {
         const dim3 grid(a->C, p.splits);

@@ -307,12 +307,135 @@ hipError_t launch_product(const ProductParams &p, long N, hipStream_t s)
     // as much for a wavefront as leaves every compute unit two blocks (and, with three terms of both, registers)
     if constexpr (TX != 3)
         if (p.M > 64 && blocks(4, 2) >= 2 * kCus) return launch_as<TI, TO, TE, TX, TW, 4, 2, TRANS, MODE, false>(p, N, s);
+    if (p.M <= 32 && blocks(1, 2) >= 2 * kCus) return launch_as<TI, TO, TE, TX, TW, 1, 2, TRANS, MODE, false>(p, N, s);
     if (blocks(2, 2) >= 2 * kCus) return launch_as<TI, TO, TE, TX, TW, 2, 2, TRANS, MODE, false>(p, N, s);
     return launch_as<TI, TO, TE, TX, TW, 2, 1, TRANS, MODE, false>(p, N, s);
 }
 
+// ---- few pixels and outputs, many channels: a block's eight wavefronts share one tile of 32 outputs and 32 pixels and take every eighth sixteen of its channels
+// each, both operands straight from memory; their sums are added in LDS ----
+
+constexpr int kThinWaves = 8, kThinAhead = 4;   // sixteens that are under way at a time
+
+template <typename TI, typename TO, typename TE, int TX, int TW, bool TRANS, int MODE>
+__global__ __launch_bounds__(64 * kThinWaves) void product_thin_kernel(const ProductParams p)
+{
+    constexpr int kTop = TX > TW ? TX : TW;
+    __shared__ float sums[kThinWaves][16][64];
+    const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int l32 = lane & 31, half = lane >> 5, K = p.K, M = p.M, sixteens = (K + 15) / 16;
+    const unsigned groups = (unsigned)(M + 31) / 32u, piece = piece_of(blockIdx.x, gridDim.x), tile = piece / groups;
+    const int m0 = (int)(piece - tile * groups) * 32;
+    const long q = (long)tile * 32 + l32, in = min(q, p.pixels - 1), n = in / p.P, at = in - n * p.P;
+    const TI *const x = static_cast<const TI *>(p.x) + n * p.x_stride + at;
+    const Rsrc rw = resource(p.w, 4L * K * M);
+    const bool four = (K & 3) == 0;
+    f32x16 acc;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) acc[i] = 0.f;
+    for (int c0 = wave; c0 < sixteens; c0 += kThinWaves * kThinAhead) {
+        TI xr[kThinAhead][8];
+        float wr[kThinAhead][8];
+#pragma unroll
+        for (int u = 0; u < kThinAhead; ++u) {
+            // (a sixteen beyond the last brings zeros)
+            const int k = 16 * (c0 + kThinWaves * u) + 8 * half;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) xr[u][j] = x[(long)min(k + j, K - 1) * p.P];
+#pragma unroll
+            for (int j = 0; j < 8; j += 4) {
+                float w[4];
+                if constexpr (TRANS) load_weights_across(rw, M, K, p.w_ld, m0 + l32, 16 * (c0 + kThinWaves * u) + j, 8 * half, w);
+                else load_weights(rw, M, K, p.w_ld, four, m0 + l32, k + j, w);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) wr[u][j + e] = w[e];
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < kThinAhead; ++u) {
+            const int left = K - (16 * (c0 + kThinWaves * u) + 8 * half);
+            u32x4 a[TW], b[TX];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                uint32_t ta[TW], tb[TX];
+                terms_of<TW>(wr[u][2 * e], wr[u][2 * e + 1], ta);
+                terms_of<TX>(2 * e < left ? widen(xr[u][2 * e]) : 0.f, 2 * e + 1 < left ? widen(xr[u][2 * e + 1]) : 0.f, tb);
+#pragma unroll
+                for (int i = 0; i < TW; ++i) a[i][e] = ta[i];
+#pragma unroll
+                for (int i = 0; i < TX; ++i) b[i][e] = tb[i];
+            }
+#pragma unroll
+            for (int qw = TW - 1; qw >= 0; --qw)
+#pragma unroll
+                for (int qx = TX - 1; qx >= 0; --qx)
+                    if (qw + qx < kTop)
+                        acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a[qw]), __builtin_bit_cast(bf16x8, b[qx]), acc, 0, 0, 0);
+        }
+    }
+    settle();
+#pragma unroll
+    for (int i = 0; i < 16; ++i) sums[wave][i][lane] = acc[i];
+    __syncthreads();
+    const bool has = p.extra != nullptr;
+    constexpr int kMine = 16 / kThinWaves;
+    float v[kMine], e[kMine];
+    int row[kMine];
+#pragma unroll
+    for (int r = 0; r < kMine; ++r) {
+        const int i = kMine * wave + r;
+        row[r] = m0 + 8 * (i >> 2) + 4 * half + (i & 3);
+        e[r] = has ? widen(static_cast<const TE *>(p.extra)[n * p.extra_stride + (long)min(row[r], M - 1) * p.P + at]) : 0.f;
+        v[r] = p.b != nullptr ? p.b[min(row[r], M - 1)] : 0.f;
+        float t = 0.f;
+#pragma unroll
+        for (int w = 0; w < kThinWaves; ++w) t += sums[w][i][lane];
+        v[r] += t;
+    }
+    if constexpr (MODE == kSlope) {
+        slopes(p.act, v);
+#pragma unroll
+        for (int r = 0; r < kMine; ++r) v[r] *= e[r];
+    } else {
+        activate(p.act, v);
+#pragma unroll
+        for (int r = 0; r < kMine; ++r) v[r] += e[r];
+    }
+    if (q >= p.pixels) return;
+#pragma unroll
+    for (int r = 0; r < kMine; ++r)
+        if (row[r] < M) {
+            TO *to = static_cast<TO *>(p.out) + n * p.out_stride + (long)row[r] * p.P + at;
+            if constexpr (kWide<TO>) *to = v[r];
+            else to->bits = (uint16_t)pack2(v[r], 0.f);
+        }
+}
+
+template <typename TI, typename TO, typename TE, int TX, int TW, bool TRANS, int MODE>
+hipError_t launch_thin(const ProductParams &p, hipStream_t s)
+{
+    const long grid = (p.pixels + 31) / 32 * ((p.M + 31) / 32);
+    hipLaunchKernelGGL((product_thin_kernel<TI, TO, TE, TX, TW, TRANS, MODE>), dim3((unsigned)grid), dim3(64 * kThinWaves), 0, s, p);
+    return hipGetLastError();
+}
+
+// Where the other kernels would leave most compute units without a block, and a block with a long way through the channels.
+bool thin_fits(const ProductParams &p) { return p.K >= 128 && (p.pixels + 127) / 128 * ((p.M + 63) / 64) < kCus / 4; }
+
 hipError_t launch_any(int kind, const ProductParams &p, long N, hipStream_t s)
 {
+    if (thin_fits(p)) {
+        switch (kind) {
+        case kForwardF32: return launch_thin<float, float, float, 3, 3, false, kForward>(p, s);
+        case kForwardBf16: return launch_thin<bf16s, bf16s, bf16s, 1, 2, false, kForward>(p, s);
+        case kSlopeF32: return launch_thin<float, float, float, 3, 3, false, kSlope>(p, s);
+        case kSlopeBf16: return launch_thin<bf16s, float, bf16s, 1, 3, false, kSlope>(p, s);
+        case kBackF32: return launch_thin<float, float, float, 3, 3, true, kForward>(p, s);
+        case kBackBf16: return launch_thin<bf16s, bf16s, bf16s, 1, 2, true, kForward>(p, s);
+        case kBackGp: return launch_thin<float, bf16s, bf16s, 2, 2, true, kForward>(p, s);
+        default: return hipErrorInvalidValue;
+        }
+    }
     if (strip_fits(kind, p, N)) return launch_strip(kind, p, N, s);
     switch (kind) {
     case kForwardF32: return launch_product<float, float, float, 3, 3, false, kForward>(p, N, s);

@@ -14,7 +14,8 @@ TYPES = [torch.float32, torch.bfloat16]
 # N, K, M, H, W
 SHAPES = [(1, 1, 1, 1, 1), (1, 3, 5, 1, 1), (67, 9, 4, 1, 1), (1, 16, 32, 1, 2), (3, 17, 33, 1, 3), (2, 64, 64, 7, 9), (1, 64, 192, 16, 16), (2, 33, 65, 5, 27),
           (9, 48, 40, 3, 5), (1, 129, 70, 11, 13), (2, 200, 96, 8, 31), (1, 15, 257, 4, 130), (1, 640, 130, 5, 8), (5, 7, 300, 2, 2), (1, 500, 8, 33, 1),
-          (1, 64, 128, 64, 64), (40, 24, 24, 6, 7), (1, 1300, 20, 3, 3)]
+          (1, 64, 128, 64, 64), (40, 24, 24, 6, 7), (1, 1300, 20, 3, 3), (2, 201, 33, 1, 7), (5, 131, 40, 1, 1),
+          (1, 322, 30, 90, 900), (3, 196, 29, 150, 301), (2, 270, 66, 130, 255), (300, 35, 40, 3, 11)]
 
 
 def inputs(shape, dtype, seed=0, whole=False):
