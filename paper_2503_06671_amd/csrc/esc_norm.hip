@@ -446,7 +446,7 @@ struct Split {
     constexpr int places() const { return 4 * ws * kc; }
 };
 constexpr Split kForward[] = {{4, 1}, {8, 1}, {6, 2}, {8, 2}, {6, 4}, {8, 4}, {12, 4}, {16, 4}, {12, 8}, {16, 8}, {12, 16}, {16, 16}};
-constexpr Split kBackward[] = {{4, 1}, {4, 2}, {3, 4}, {4, 4}, {3, 8}, {4, 8}, {6, 8}, {8, 8}, {6, 16}, {8, 16}};
+constexpr Split kBackward[] = {{4, 1}, {4, 2}, {3, 4}, {4, 4}, {3, 8}, {4, 8}, {6, 8}, {8, 8}, {12, 8}, {16, 8}};
 template <bool BACK>
 constexpr const auto &splits()
 {
@@ -464,8 +464,8 @@ int split_of(int C)
     while (i < kSplitCount<BACK> && splits<BACK>()[i].places() < C) ++i;
     return i;
 }
-// pixels of a lane: fewer where sixteen wavefronts have 128 registers each
-constexpr int wide_of(bool back, int ws) { return ws < 16 ? kWide : back ? 1 : 2; }
+// pixels of a lane: fewer where sixteen wavefronts have 128 registers each, or a lane has many channels of two tensors
+constexpr int wide_of(bool back, Split k) { return (back ? k.kc > 8 : k.ws == 16) ? kWide / 2 : kWide; }
 
 template <typename E, bool BACK, int I = 0>
 hipError_t launch_held(const NormParams &p, int split, int v, long grid, hipStream_t s)
@@ -474,7 +474,7 @@ hipError_t launch_held(const NormParams &p, int split, int v, long grid, hipStre
         if (split != I) return launch_held<E, BACK, I + 1>(p, split, v, grid, s);
         constexpr Split k = splits<BACK>()[I];
         const dim3 blocks((unsigned)grid), block(kBlock<k.ws>);
-        constexpr int wide = wide_of(BACK, k.ws);
+        constexpr int wide = wide_of(BACK, k);
         if constexpr (BACK) {
             if (v == 1) hipLaunchKernelGGL((norm_back_kernel<E, 1, k.kc, k.ws>), blocks, block, 0, s, p);
             else hipLaunchKernelGGL((norm_back_kernel<E, wide, k.kc, k.ws>), blocks, block, 0, s, p);
@@ -494,7 +494,7 @@ long tiles_of(long N, long P, int v) { return N * ((P + 16 * v - 1) / (16 * v));
 template <bool BACK>
 int lanes_pixels(long N, long P, Split k)
 {
-    const int wide = wide_of(BACK, k.ws);
+    const int wide = wide_of(BACK, k);
     return P >= wide && tiles_of(N, P, wide) >= kCus ? wide : 1;
 }
 long sets_of(Split k) { return k.ws < 4 ? 4 / k.ws : 1; }

@@ -307,7 +307,7 @@ hipError_t launch_product(const ProductParams &p, long N, hipStream_t s)
     // as much for a wavefront as leaves every compute unit two blocks (and, with three terms of both, registers)
     if constexpr (TX != 3)
         if (p.M > 64 && blocks(4, 2) >= 2 * kCus) return launch_as<TI, TO, TE, TX, TW, 4, 2, TRANS, MODE, false>(p, N, s);
-    if (p.M <= 32 && blocks(1, 2) >= 2 * kCus) return launch_as<TI, TO, TE, TX, TW, 1, 2, TRANS, MODE, false>(p, N, s);
+    if (p.M <= 32) return blocks(1, 2) >= 2 * kCus ? launch_as<TI, TO, TE, TX, TW, 1, 2, TRANS, MODE, false>(p, N, s) : launch_as<TI, TO, TE, TX, TW, 1, 1, TRANS, MODE, false>(p, N, s);
     if (blocks(2, 2) >= 2 * kCus) return launch_as<TI, TO, TE, TX, TW, 2, 2, TRANS, MODE, false>(p, N, s);
     return launch_as<TI, TO, TE, TX, TW, 2, 1, TRANS, MODE, false>(p, N, s);
 }
@@ -420,7 +420,7 @@ hipError_t launch_thin(const ProductParams &p, hipStream_t s)
 }
 
 // Where the other kernels would leave most compute units without a block, and a block with a long way through the channels.
-bool thin_fits(const ProductParams &p) { return p.K >= 128 && (p.pixels + 127) / 128 * ((p.M + 63) / 64) < kCus / 4; }
+bool thin_fits(const ProductParams &p) { return p.K >= 128 && (p.pixels + 127) / 128 * ((p.M + 63) / 64) < kCus / 2; }
 
 hipError_t launch_any(int kind, const ProductParams &p, long N, hipStream_t s)
 {
