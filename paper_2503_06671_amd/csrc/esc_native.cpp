@@ -16,6 +16,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cmath>
+#include <initializer_list>
 #include <string>
 #include <vector>
 
@@ -871,6 +872,23 @@ Ws scratch_beside(PyObject *o, const Map &x, const char *name)
     return Ws{t.data_ptr(), (size_t)t.numel() * (size_t)t.element_size()};
 }
 
+// `need` is None or names gradients of these.
+void known(PyObject *need, std::initializer_list<const char *> names)
+{
+    if (!given(need)) return;
+    PyObject *all = PySequence_Fast(need, "need must be a sequence of gradients' names");
+    if (all == nullptr) throw PyError{};
+    bool ok = !PyUnicode_Check(need);
+    for (Py_ssize_t i = 0; ok && i < PySequence_Fast_GET_SIZE(all); ++i) {
+        PyObject *o = PySequence_Fast_GET_ITEM(all, i);
+        bool found = false;
+        for (const char *n : names) found = found || (PyUnicode_Check(o) && PyUnicode_CompareWithASCIIString(o, n) == 0);
+        ok = found;
+    }
+    Py_DECREF(all);
+    if (!ok) fail(PyExc_ValueError, "need must be a sequence of gradients' names, of " + std::string(*names.begin()) + " and its like");
+}
+
 // Which gradients are wanted: all that there are where `need` is None, else those that it names.
 bool wanted(PyObject *need, const char *name)
 {
@@ -938,6 +956,7 @@ PyObject *layernorm_backward(PyObject *const *a, Py_ssize_t n)
     Grads grads(a[8]);
     esc_layernorm_grads g{};
     bool brought_w = false, brought_b = false;
+    known(a[9], {"grad_x", "grad_weight", "grad_bias"});
     if (wanted(a[9], "grad_x")) g.x = grads.map("grad_x", x, &g.x_stride);
     if (l.weight != nullptr && wanted(a[9], "grad_weight")) g.weight = grads.weights("grad_weight", x, {x.C}, &brought_w);
     if (l.bias != nullptr && wanted(a[9], "grad_bias")) g.bias = grads.weights("grad_bias", x, {x.C}, &brought_b);
@@ -994,6 +1013,7 @@ PyObject *pointwise_backward(PyObject *const *a, Py_ssize_t n)
     Grads grads(a[7]);
     esc_pointwise_grads g{};
     bool brought_w = false, brought_b = false;
+    known(a[8], {"grad_x", "grad_w", "grad_b"});
     if (wanted(a[8], "grad_x")) g.x = grads.map("grad_x", x, &g.x_stride);
     if (wanted(a[8], "grad_w")) g.w = grads.weights("grad_w", x, {p.M, p.K}, &brought_w);
     if (p.b != nullptr && wanted(a[8], "grad_b")) g.b = grads.weights("grad_b", x, {p.M}, &brought_b);

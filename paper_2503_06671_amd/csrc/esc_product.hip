@@ -302,7 +302,7 @@ hipError_t launch_product(const ProductParams &p, long N, hipStream_t s)
 {
     // small images share tiles; their pixels, and those of images beyond 2 GiB, go one by one
     const size_t widest = std::max(std::max(p.K * sizeof(TI), p.M * sizeof(TO)), p.M * sizeof(TE)) * (size_t)p.P;
-    if (widest >= kMostImage || p.P < 2 || (N > 1 && p.P < 96)) return launch_as<TI, TO, TE, TX, TW, 2, 1, TRANS, MODE, true>(p, N, s);
+    if (widest >= kMostImage || p.P > kMostPlane || p.P < 2 || (N > 1 && p.P < 96)) return launch_as<TI, TO, TE, TX, TW, 2, 1, TRANS, MODE, true>(p, N, s);
     const auto blocks = [&](int mt, int nt) { return N * ((p.P + 128 * nt - 1) / (128 * nt)) * ((p.M + 32 * mt - 1) / (32 * mt)); };
     // as much for a wavefront as leaves every compute unit two blocks (and, with three terms of both, registers)
     if constexpr (TX != 3)
@@ -807,7 +807,7 @@ esc_status esc_pointwise_backward(const void *x, const void *grad_out, esc_dtype
         WeightParams p{};
         p.g = act ? mem : grad_out, p.x = x, p.g_stride = act ? (long)a->M * P : g_stride, p.x_stride = x_stride;
         p.part = reinterpret_cast<float *>(mem + sc.part), p.has_w = g->w != nullptr, p.has_b = g->b != nullptr;
-        p.K = a->K, p.M = a->M, p.splits = splits_of(a, P, f32), p.P = P, p.pixels = P * a->N;
+        p.K = p.has_w ? a->K : 1, p.M = a->M, p.splits = splits_of(a, P, f32), p.P = P, p.pixels = P * a->N;
         const hipError_t e = f32 ? launch_weights<float, float, 3, 3>(p, s) : act ? launch_weights<float, bf16s, 3, 1>(p, s) : launch_weights<bf16s, bf16s, 1, 1>(p, s);
         if (e != hipSuccess) return ESC_ERR_HIP;
         if (add_parts(p.part, p.splits, p.has_w ? (long)a->M * a->K : 0, g->w, p.has_b ? a->M : 0, g->b, accumulate, s) != hipSuccess) return ESC_ERR_HIP;

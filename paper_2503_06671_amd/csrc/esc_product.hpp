@@ -149,6 +149,7 @@ constexpr unsigned kBeyond = 0x80000000u;  // an offset beyond every resource (a
 constexpr int kSchedNoVmem = 0x38f;        // a scheduling barrier for accesses to memory alone
 constexpr int kSchedNoVmemNoMfma = 0x386;  // a scheduling barrier for accesses to memory and matrix instructions
 constexpr size_t kMostImage = (size_t)1 << 31;
+constexpr long kMostPlane = 1L << 24;      // pixels: 31 planes' offset beside kBeyond does not pass 32 bits
 
 __device__ __forceinline__ Rsrc resource(const void *at, long bytes)
 {

@@ -489,7 +489,7 @@ constexpr int kMostK[2] = {192, 160}, kBackMostK[2] = {128, 64};
 
 bool back_fits(bool f32, int K, int M, long P, long N)
 {
-    if (K > kBackMostK[f32] || (size_t)std::max(K, M) * P * 4 >= kMostImage || !(N == 1 || P >= 96)) return false;
+    if (K > kBackMostK[f32] || (size_t)std::max(K, M) * P * 4 >= kMostImage || P > kMostPlane || !(N == 1 || P >= 96)) return false;
     // (a block goes through all outputs: few pixels are better shared out over two launches.  5 x 50 x 61, 96 to 45, fp32: two launches 14.0 us, one 15.7)
     return N * ((P + 127) / 128) >= kCus;
 }
@@ -511,7 +511,7 @@ bool strip_fits(int kind, const ProductParams &p, long N)
 {
     const size_t in = kind == kForwardBf16 || kind == kSlopeBf16 || kind == kBackBf16 ? 2 : 4, out = kind == kForwardBf16 || kind == kBackBf16 || kind == kBackGp ? 2 : 4;
     // (the slope's other input is no wider than what it writes)
-    if (p.K > kMostK[kind == kForwardF32 || kind == kSlopeF32 || kind == kBackF32] || (size_t)p.K * p.P * in >= kMostImage || (size_t)p.M * p.P * out >= kMostImage) return false;
+    if (p.K > kMostK[kind == kForwardF32 || kind == kSlopeF32 || kind == kBackF32] || (size_t)p.K * p.P * in >= kMostImage || (size_t)p.M * p.P * out >= kMostImage || p.P > kMostPlane) return false;
     // small images fill too little of a block's pixels
     return N == 1 || p.P >= 96;
 }

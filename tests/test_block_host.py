@@ -81,7 +81,7 @@ def test_pointwise_forward_rejects(lib):
     for n in ("N", "K", "M", "H", "W"):
         assert fw(**{n: 0}) == fw(**{n: -1}) == E_SHAPE, n
     assert fw(act=3) == fw(act=-1) == E_SHAPE
-    assert fw(K=65537, x_stride=BIG) == fw(M=65537) == fw(H=65536, W=32768) == fw(N=1 << 20, H=1024, W=1024) == E_UNSUP
+    assert fw(K=65537, x_stride=BIG) == fw(M=65537) == fw(K=32768, M=16384, x_stride=BIG, out_stride=BIG, residual_stride=BIG) == fw(H=65536, W=32768) == fw(N=1 << 20, H=1024, W=1024) == E_UNSUP
     assert fw(x_stride=279) == fw(out_stride=209) == fw(residual_stride=0) == E_SHAPE
     assert fw(x=X + 2) == fw(res=SKIP + 2) == fw(out=OUT + 1) == fw(w=W + 2) == fw(b=B + 3) == E_SHAPE
     assert fw(out=X + 4) == fw(out=SKIP) == fw(w=OUT) == fw(b=OUT + 4 * 419) == fw(out=W + 4 * 47) == E_ALIAS

@@ -215,6 +215,8 @@ def test_binding_refuses():
         (TypeError, lambda: binding.layernorm_backward(x, go.bfloat16(), saved, ws)),
         (binding.EscError, lambda: binding.layernorm_backward(x, go, saved, ws[:0])),
         (binding.EscError, lambda: binding.layernorm_backward(x, go, saved, ws, need=())),
+        (ValueError, lambda: binding.layernorm_backward(x, go, saved, ws, need=("grad_y",))),
+        (ValueError, lambda: binding.layernorm_backward(x, go, saved, ws, need="grad_x")),
         (binding.EscError, lambda: binding.layernorm_backward(x, go, saved, ws, grads=dict(grad_x=go))),
     ]:
         with pytest.raises(error):

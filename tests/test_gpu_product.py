@@ -253,6 +253,8 @@ def test_binding_refuses():
         (binding.EscError, lambda: binding.pointwise_backward(x, go, w, ws[:128])),
         (binding.EscError, lambda: binding.pointwise_backward(x, go, w, ws, act="gelu")),  # (a workspace for none is too small)
         (binding.EscError, lambda: binding.pointwise_backward(x, go, w, ws, need=())),
+        (ValueError, lambda: binding.pointwise_backward(x, go, w, ws, need=("grad_y",))),
+        (ValueError, lambda: binding.pointwise_backward(x, go, w, ws, need="grad_x")),
         (ValueError, lambda: binding.pointwise_backward(x, go, w, ws, grads=dict(grad_w=b))),
         (TypeError, lambda: binding.pointwise_backward(x, go, w, ws, grads=dict(grad_w=w.double()))),
     ]:
