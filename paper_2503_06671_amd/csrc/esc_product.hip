@@ -140,13 +140,13 @@ __global__ __launch_bounds__(kThreads, 2) void product_kernel(const ProductParam
 #pragma unroll
     for (int i = 0; i < kEach; ++i) wput(i, 0);
     f32x16 acc[MT][NT];
+    __syncthreads();
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
+        for (int i = 0; i < 16; ++i)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) acc[mt][t][i] = 0.f;
-    __syncthreads();
+            for (int t = 0; t < NT; ++t) acc[mt][t][i] = bias[32 * mt + 4 * half + 8 * (i >> 2) + (i & 3)];
 
     // a quarter of the right operand of sixteen channels: the terms of two of each lane's eight
     auto split = [&](const X (&raw)[8][kLoads], int e, u32x4 (&to)[NT][TX]) {
@@ -226,45 +226,43 @@ __global__ __launch_bounds__(kThreads, 2) void product_kernel(const ProductParam
     // ---- lane l has outputs m0 + 32 mt + 8 (i / 4) + 4 half + i % 4 in element i of its pixels' sums ----
     auto row_of = [](int i) { return 8 * (i >> 2) + (i & 3); };
     const unsigned ob = (unsigned)p.P * (unsigned)sizeof(TO), eb = (unsigned)p.P * (unsigned)sizeof(TE);
-    const bool has = p.extra != nullptr;
+    constexpr bool has = MODE != kForward;
     const Rsrc ro = resource(static_cast<TO *>(p.out) + image * p.out_stride, ACROSS ? 0 : (long)M * ob);
     const Rsrc re = resource(has ? static_cast<const TE *>(p.extra) + image * p.extra_stride : nullptr, ACROSS || !has ? 0 : (long)M * eb);
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
         const int left = M - (m0 + 32 * mt) - 4 * half;
         float v[NT * 16], e[NT * 16];
+        if constexpr (has && ACROSS) {
 #pragma unroll
-        for (int i = 0; i < NT * 16; ++i) e[i] = 0.f;
-        if (has) {
-            if constexpr (ACROSS) {
+            for (int i = 0; i < 16; ++i)
 #pragma unroll
-                for (int i = 0; i < 16; ++i)
+                for (int t = 0; t < NT; ++t)
+                    e[16 * t + i] = widen(static_cast<const TE *>(p.extra)[pn[t] * p.extra_stride + (long)min(m0 + 32 * mt + 4 * half + row_of(i), M - 1) * p.P + pat[t]]);
+        } else if constexpr (has) {
+            const unsigned off = (unsigned)(m0 + 32 * mt + 4 * half) * eb + pxc * (unsigned)sizeof(TE);
+            Raw<TE, NT> ex[16];
 #pragma unroll
-                    for (int t = 0; t < NT; ++t)
-                        e[16 * t + i] = widen(static_cast<const TE *>(p.extra)[pn[t] * p.extra_stride + (long)min(m0 + 32 * mt + 4 * half + row_of(i), M - 1) * p.P + pat[t]]);
-            } else {
-                const unsigned off = (unsigned)(m0 + 32 * mt + 4 * half) * eb + pxc * (unsigned)sizeof(TE);
-                Raw<TE, NT> ex[16];
+            for (int i = 0; i < 16; ++i) ex[i] = load<TE, NT>(re, row_of(i) < left ? off : kBeyond, (unsigned)row_of(i) * eb);
 #pragma unroll
-                for (int i = 0; i < 16; ++i) ex[i] = load<TE, NT>(re, row_of(i) < left ? off : kBeyond, (unsigned)row_of(i) * eb);
+            for (int i = 0; i < 16; ++i)
 #pragma unroll
-                for (int i = 0; i < 16; ++i)
-#pragma unroll
-                    for (int t = 0; t < NT; ++t) e[16 * t + i] = ex[i].value(t);
-            }
+                for (int t = 0; t < NT; ++t) e[16 * t + i] = ex[i].value(t);
         }
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) v[16 * t + i] = acc[mt][t][i] + bias[32 * mt + 4 * half + row_of(i)];
+            for (int i = 0; i < 16; ++i) v[16 * t + i] = acc[mt][t][i];
         if constexpr (MODE == kSlope) {
             slopes(p.act, v);
 #pragma unroll
             for (int i = 0; i < NT * 16; ++i) v[i] *= e[i];
         } else {
             activate(p.act, v);
+            if constexpr (MODE == kResidual) {
 #pragma unroll
-            for (int i = 0; i < NT * 16; ++i) v[i] += e[i];
+                for (int i = 0; i < NT * 16; ++i) v[i] += e[i];
+            }
         }
         if constexpr (ACROSS) {
 #pragma unroll
@@ -438,8 +436,8 @@ hipError_t launch_any(int kind, const ProductParams &p, long N, hipStream_t s)
     }
     if (strip_fits(kind, p, N)) return launch_strip(kind, p, N, s);
     switch (kind) {
-    case kForwardF32: return launch_product<float, float, float, 3, 3, false, kForward>(p, N, s);
-    case kForwardBf16: return launch_product<bf16s, bf16s, bf16s, 1, 2, false, kForward>(p, N, s);
+    case kForwardF32: return p.extra != nullptr ? launch_product<float, float, float, 3, 3, false, kResidual>(p, N, s) : launch_product<float, float, float, 3, 3, false, kForward>(p, N, s);
+    case kForwardBf16: return p.extra != nullptr ? launch_product<bf16s, bf16s, bf16s, 1, 2, false, kResidual>(p, N, s) : launch_product<bf16s, bf16s, bf16s, 1, 2, false, kForward>(p, N, s);
     case kSlopeF32: return launch_product<float, float, float, 3, 3, false, kSlope>(p, N, s);
     // (weights in three terms with bf16 storage too: what is left of them goes into every pixel's gradient)
     case kSlopeBf16: return launch_product<bf16s, float, bf16s, 1, 3, false, kSlope>(p, N, s);
