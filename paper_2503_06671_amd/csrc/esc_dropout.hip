@@ -3,7 +3,12 @@
 //   out[i] = residual[i] + ( draw(unit(i)) >= q ? x[i] * 65536 / (65536 - q) : 0 )
 //
 // draw(u) is a 16-bit part of block u / 8 of Philox4x32 with ten rounds: eight draws a block, so that a thread that takes eight
-// consecutive elements runs the generator once.
+// consecutive elements runs the generator once (some 110 instructions for eight elements, a quarter of what the vector units could do in the time).  Whole planes
+// and images are spans of blocks of their own: one draw a block, and what is dropped is not read.
+//
+// What bounds it: memory.  One MI355X, 64 x 64 x 64 of 64 channels, bf16: elements with residual 16.8 us (101 MB, 6.0 TB/s: part of it from the last-level
+// cache), the gradient 12.7; 4 x 64 x 64 of 192, fp32, whole images 6.6.  (Loads of eight elements behind conditions, which the compiler took apart: 23.7,
+// 16.7 and 8.6.)
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>

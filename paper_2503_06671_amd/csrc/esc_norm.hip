@@ -2,6 +2,13 @@
 //
 //   u = (x - mean) r,  r = 1 / sqrt(mean of (x - mean)^2 + eps),  out = weight u + bias
 //   a = weight g,  grad_x = r (a - mean(a) - u mean(a u)) + skip,  grad_weight = sum over pixels of g u,  grad_bias = sum over pixels of g
+//
+// What bounds it: memory.  x is read once and out written once; the backward pass reads x, g and skip once and writes grad_x.  That takes a pixel's
+// channels out of registers: the mean first, then the squares of differences from it (no difference of large sums), then the result.  Planes of one
+// channel are contiguous, so neighbouring lanes are neighbouring pixels, four at a time where there are enough, and the channels are
+// spread over a wavefront's other lanes and over wavefronts.  One MI355X: 180 x 320 of 192 channels, bf16 10.4 us (44 MB, 4.2 TB/s; a kernel that
+// reads x three times 48); 64 x 64 x 64 of 64 channels, bf16 forward 13.9 (4.8 TB/s), backward with skip 26.2 (5.1 TB/s; a copy of 1 GiB 5.1) and 4.6 for the
+// parts of the weights' sums; 2 x 339 x 511 of 45, fp32 25.8 and 45; 64 x 64 of 64, fp32 4.4.
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>

@@ -4,6 +4,11 @@
 // eight consecutive channels of its pixel for each sixteen, as eight loads of channel rows bring them (32 lanes on a run of 32 NT pixels), split into
 // terms once.  The weights pass LDS in chunks of 32 outputs, two buffers, one barrier a chunk; behind a chunk's products stand its
 // activation, residual and stores, while other wavefronts multiply.  x is read once where one block takes all outputs.
+//
+// What bounds it: memory, for as many channels as the vector units' share (splitting, activation) hides behind.  One MI355X: 339 x 511, 64 to 64 channels
+// with residual, fp32 23.4 us (133 MB, 5.7 TB/s); 64 x 64 x 64, 64 to 128, gelu, bf16 forward 28.8 (101 MB, 3.5 TB/s: one round of blocks, whose reading and
+// writing do not overlap), gp and grad_x 59 (268 MB, 4.5 TB/s; as two kernels 84); 180 x 320, 192 to 576, bf16 33 (780 TFLOP/s of products of terms); a
+// kernel that stages both operands in LDS: 57, 97, 290 and 150.
 #include "esc_product.hpp"
 
 #include <algorithm>
