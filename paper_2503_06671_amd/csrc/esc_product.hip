@@ -114,7 +114,9 @@ __global__ __launch_bounds__(kThreads, 2) void product_kernel(const ProductParam
         for (int i = 0; i < kEach; ++i) {
             int row, k4;
             run_of(i, row, k4);
-            if constexpr (TRANS) load_weights_across(rw, M, K, p.w_ld, m0 + row, 32 * st + 4 * __builtin_amdgcn_readfirstlane(k4), 0, wr[i]);
+            // (64 outputs and more: a wavefront's threads have one run of channels; 32: two)
+            if constexpr (TRANS && MT == 1) load_weights_across(rw, M, K, p.w_ld, m0 + row, 32 * st + 8 * (__builtin_amdgcn_readfirstlane(k4) >> 1), 4 * (k4 & 1), wr[i]);
+            else if constexpr (TRANS) load_weights_across(rw, M, K, p.w_ld, m0 + row, 32 * st + 4 * __builtin_amdgcn_readfirstlane(k4), 0, wr[i]);
             else load_weights(rw, M, K, p.w_ld, four, m0 + row, 32 * st + 4 * k4, wr[i]);
         }
     };

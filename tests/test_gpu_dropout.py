@@ -33,7 +33,7 @@ def test_equal_to_the_definition(shape, dtype, over):
 
 @pytest.mark.parametrize("over", ["element", "plane", "image"])
 @pytest.mark.parametrize("dtype", TYPES, ids=["f32", "bf16"])
-@pytest.mark.parametrize("shape", [(3, 5, 3, 7), (4, 2, 30, 31), (5, 1, 1, 3)], ids=str)
+@pytest.mark.parametrize("shape", [(3, 5, 3, 7), (4, 2, 30, 31), (5, 1, 1, 3), (3, 5, 63, 45), (2, 45, 15, 15)], ids=str)
 def test_masks_do_not_depend_on_strides(shape, dtype, over):
     x, res, go = inputs(shape, dtype, 1)
     N, C, H, W = shape

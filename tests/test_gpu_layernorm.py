@@ -14,6 +14,9 @@ TYPES = [torch.float32, torch.bfloat16]
 SHAPES = [(1, 1, 1, 1), (1, 3, 1, 1), (70, 5, 1, 1), (2, 7, 3, 5), (1, 64, 16, 16), (3, 64, 9, 31), (2, 45, 33, 17), (1, 192, 20, 36), (5, 193, 3, 3),
           (1, 256, 1, 63), (1, 257, 8, 8), (2, 640, 5, 13), (1, 1025, 4, 4), (2, 2500, 1, 3), (1, 16, 130, 129), (33, 12, 7, 1), (1, 100, 1, 4097)]
 
+# enough pixels for four of a lane (or two): every number of channels that has code of its own
+LARGE = [(2, C, 93, 91) for C in (15, 32, 47, 64, 94, 128, 190, 256, 380, 512, 700, 1000)] + [(1, 1100, 128, 130)]
+
 
 def inputs(shape, dtype, seed=0, mean=0.5):
     g = torch.Generator(device="cuda").manual_seed(seed)
@@ -28,7 +31,7 @@ def inputs(shape, dtype, seed=0, mean=0.5):
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=["f32", "bf16"])
-@pytest.mark.parametrize("shape", SHAPES, ids=str)
+@pytest.mark.parametrize("shape", SHAPES + LARGE + [(3, C, 5, 7) for _, C, _, _ in LARGE], ids=str)
 def test_against_float64(shape, dtype):
     i = inputs(shape, dtype)
     N, C, H, W = shape

@@ -17,6 +17,11 @@ SHAPES = [(1, 1, 1, 1, 1), (1, 3, 5, 1, 1), (67, 9, 4, 1, 1), (1, 16, 32, 1, 2),
           (1, 64, 128, 64, 64), (40, 24, 24, 6, 7), (1, 1300, 20, 3, 3), (2, 201, 33, 1, 7), (5, 131, 40, 1, 1),
           (1, 322, 30, 90, 900), (3, 196, 29, 150, 301), (2, 270, 66, 130, 255), (300, 35, 40, 3, 11)]
 
+# many pixels: two a lane, wide tiles, and the backward pass in one launch (up to 128 channels, 64 with fp32); every number of channels that has code of its own
+LARGE = [(2, 30, 40, 301, 255), (2, 50, 100, 301, 255), (3, 64, 33, 150, 301), (2, 120, 70, 301, 255), (2, 155, 20, 301, 255), (2, 190, 100, 301, 255),
+         (2, 24, 300, 301, 255), (1, 24, 300, 130, 257), (2, 210, 260, 301, 255), (1, 300, 60, 130, 200), (2, 300, 60, 301, 255), (2, 260, 129, 160, 161),
+         (70, 100, 90, 31, 33), (45, 60, 130, 31, 33), (300, 140, 300, 8, 8)]
+
 
 def inputs(shape, dtype, seed=0, whole=False):
     N, K, M, H, W = shape
@@ -36,7 +41,7 @@ def workspace(shape, dtype, act="none"):
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=["f32", "bf16"])
-@pytest.mark.parametrize("shape", SHAPES, ids=str)
+@pytest.mark.parametrize("shape", SHAPES + LARGE, ids=str)
 def test_whole_numbers_are_exact(shape, dtype):
     # sums of products up to 16 stay below 2^24: every result is a whole number (rounded where its type is bf16)
     i = inputs(shape, dtype, whole=True)
@@ -51,9 +56,8 @@ def test_whole_numbers_are_exact(shape, dtype):
     assert torch.equal(got["grad_b"], go.sum((0, 2, 3)).float())
 
 
-@pytest.mark.parametrize("act", ["none", "gelu", "silu"])
+@pytest.mark.parametrize("shape, act", [(s, a) for s in SHAPES for a in ("none", "gelu", "silu")] + [(s, "gelu") for s in LARGE], ids=str)
 @pytest.mark.parametrize("dtype", TYPES, ids=["f32", "bf16"])
-@pytest.mark.parametrize("shape", SHAPES, ids=str)
 def test_against_float64(shape, dtype, act):
     i = inputs(shape, dtype, 1)
     want = ref.product(i["x"], i["w"], i["b"], act, i["residual"], i["grad_out"])
@@ -205,6 +209,19 @@ def test_an_image_beyond_32_bits():
     out = binding.pointwise_forward(x, w)
     for y, rows in ((0, 3), (4100, 2), (H - 2, 2)):
         ref.check(out[:, :, y:y + rows], ref.product(x[:, :, y:y + rows], w)["out"], "out")
+    # The gradients, of signs and zeros.  A share of the pixels (one of 512) has a whole sum far below 2^24, exact; shares are added 16 in a row and
+    # then in five halvings.  Where out follows x the shares' sums have one sign, up to 67 million in all: beyond 2^24 each of those 21 additions is off by
+    # 2^-24 of what it adds up at most; sums below 2^23 stay exact (their partial sums too, which have the same sign or are the few thousands of chance).
+    x.copy_(torch.sign(x) * (x.abs() > 0.4))
+    go = torch.sign(out) * (out.abs() > 0.5)
+    del out
+    got = binding.pointwise_backward(x, go, w, workspace((1, K, M, H, W), torch.bfloat16))
+    want = sum(go[0, :, y:y + 1024].reshape(M, -1).double() @ x[0, :, y:y + 1024].reshape(K, -1).double().t().contiguous() for y in range(0, H, 1024))
+    off, small = (got["grad_w"].double() - want).abs(), want.abs() < 2 ** 23
+    assert small.sum() > 300 and (off[small] == 0).all() and (off <= 21 * 2.0 ** -24 * H * W).all()
+    for y, rows in ((0, 3), (4100, 2), (H - 2, 2)):
+        part = ref.product(x[:, :, y:y + rows], w, None, "none", None, go[:, :, y:y + rows])
+        ref.check(got["grad_x"][:, :, y:y + rows], part["grad_x"], "grad_x")
 
 
 def test_streams_and_two_at_once():
