@@ -455,6 +455,10 @@ def window_attention_backward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
                                              kv_heads, accumulate, grads, stream)
 
 
+def _names(need):
+    return None if need is None else tuple(need)
+
+
 def new_layernorm_saved(N: int, H: int, W: int, device="cuda") -> torch.Tensor:
     """Allocate (with torch) what layernorm_forward keeps for the backward pass."""
     nbytes = int(load_library().esc_layernorm_saved_bytes(_LayerNorm(N=N, C=1, H=H, W=W)))
@@ -485,7 +489,7 @@ def layernorm_backward(x: torch.Tensor, grad_out: torch.Tensor, saved: torch.Ten
     """esc_layernorm_backward.  Returns a dict of device tensors: grad_x (with grad_skip, the gradient that reaches x around the norm, added) and, with
     a weight and a bias, grad_weight and grad_bias; `need` names those that are wanted (None: all).  `grads` may carry buffers to write into;
     accumulate=True adds the parameters' gradients to theirs."""
-    return _native.layernorm_backward(x, grad_out, saved, workspace, weight, bias, grad_skip, accumulate, grads, need, stream)
+    return _native.layernorm_backward(x, grad_out, saved, workspace, weight, bias, grad_skip, accumulate, grads, _names(need), stream)
 
 
 def _activation(act: str) -> int:
@@ -515,7 +519,7 @@ def pointwise_backward(x: torch.Tensor, grad_out: torch.Tensor, w: torch.Tensor,
                        act: str = "none", accumulate: bool = False, grads: Optional[dict] = None, need=None, stream=None) -> dict:
     """esc_pointwise_backward.  Returns a dict of device tensors: grad_x, grad_w and, with a bias, grad_b; `need` names those that are wanted (None:
     all).  (The residual's gradient is grad_out.)  `grads` may carry buffers to write into; accumulate=True adds the parameters' gradients to theirs."""
-    return _native.pointwise_backward(x, grad_out, w, workspace, b, _activation(act), accumulate, grads, need, stream)
+    return _native.pointwise_backward(x, grad_out, w, workspace, b, _activation(act), accumulate, grads, _names(need), stream)
 
 
 def _dropout_unit(over: str) -> int:

@@ -872,21 +872,17 @@ Ws scratch_beside(PyObject *o, const Map &x, const char *name)
     return Ws{t.data_ptr(), (size_t)t.numel() * (size_t)t.element_size()};
 }
 
-// `need` is None or names gradients of these.
+// `need` is None or a tuple that names gradients of these.
 void known(PyObject *need, std::initializer_list<const char *> names)
 {
     if (!given(need)) return;
-    PyObject *all = PySequence_Fast(need, "need must be a sequence of gradients' names");
-    if (all == nullptr) throw PyError{};
-    bool ok = !PyUnicode_Check(need);
-    for (Py_ssize_t i = 0; ok && i < PySequence_Fast_GET_SIZE(all); ++i) {
-        PyObject *o = PySequence_Fast_GET_ITEM(all, i);
+    if (!PyTuple_Check(need)) fail(PyExc_TypeError, "need must be a tuple");
+    for (Py_ssize_t i = 0; i < PyTuple_GET_SIZE(need); ++i) {
+        PyObject *o = PyTuple_GET_ITEM(need, i);
         bool found = false;
         for (const char *n : names) found = found || (PyUnicode_Check(o) && PyUnicode_CompareWithASCIIString(o, n) == 0);
-        ok = found;
+        if (!found) fail(PyExc_ValueError, "need must be a sequence of gradients' names, " + std::string(*names.begin()) + " and its like");
     }
-    Py_DECREF(all);
-    if (!ok) fail(PyExc_ValueError, "need must be a sequence of gradients' names, of " + std::string(*names.begin()) + " and its like");
 }
 
 // Which gradients are wanted: all that there are where `need` is None, else those that it names.

@@ -113,6 +113,21 @@ def test_slices_of_larger_tensors(shape, dtype, act):
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(1, 64, 40, 9, 17), (2, 60, 100, 301, 255), (1, 256, 72, 130, 257), (1, 512, 40, 3, 5), (1, 40, 256, 130, 257)], ids=str)
+def test_weights_at_odd_addresses(shape, dtype):
+    N, K, M, H, W = shape
+    i = inputs(shape, dtype, 11)
+    room, bias = torch.empty(M * K + 1, device="cuda"), torch.empty(M + 1, device="cuda")
+    w, b, gw, gb = room[1:].view(M, K), bias[1:], torch.empty(M * K + 3, device="cuda")[3:].view(M, K), torch.empty(M + 1, device="cuda")[1:]
+    w.copy_(i["w"]), b.copy_(i["b"])
+    ws = workspace(shape, dtype, "gelu")
+    assert torch.equal(binding.pointwise_forward(i["x"], w, b, "silu"), binding.pointwise_forward(i["x"], i["w"], i["b"], "silu"))
+    want = binding.pointwise_backward(i["x"], i["grad_out"], i["w"], ws, i["b"], "gelu")
+    got = binding.pointwise_backward(i["x"], i["grad_out"], w, ws, b, "gelu", grads=dict(grad_w=gw, grad_b=gb), need=(n for n in ("grad_x", "grad_w", "grad_b")))
+    assert got["grad_w"] is gw and got["grad_b"] is gb and all(torch.equal(got[n], want[n]) for n in want)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=["f32", "bf16"])
 def test_single_gradients_accumulation_and_buffers_full_of_nan(dtype):
     shape = (2, 40, 24, 13, 7)
     i = inputs(shape, dtype, 4)
