@@ -382,7 +382,8 @@ esc_status esc_window_attention_backward(const void *q, const void *k, const voi
  *   weight, bias device, fp32 [C], or NULL (ones, zeros)
  *   saved        mean and r of each pixel for the backward pass (fp32; esc_layernorm_saved_bytes, 256-byte aligned), or NULL
  * Means and sums are fp32, of differences from the mean (not of squares of x); out is rounded once.  A value that is not finite makes NaN of
- * its own pixel's outputs and of no other's (squares of differences have to lie in fp32's range).  Limits: C <= 65536, H W < 2^31, N H W < 2^40, 0 < eps < infinity.  One launch; no workspace.
+ * its own pixel's outputs and of no other's (squares of differences have to lie in fp32's range).  Limits: C <= 65536, H W < 2^31, N H W < 2^40, 0 < eps < infinity.  One launch
+ * (several where it would have 2^32 threads or more); no workspace.
  */
 typedef struct esc_layernorm {
     int N, C, H, W;
@@ -429,8 +430,9 @@ esc_status esc_layernorm_backward(const void *x, const void *grad_out, const voi
  * Accumulation is fp32, out is rounded once.  fp32 storage: values and weights as three bf16 terms each (exact down to 2^-110), six products of
  * terms on the matrix cores (what is left out lies below 2^-21 of a product).  bf16 storage: the stored values, weights as two bf16 terms (2^-16 left out at
  * most).  A value or weight that is not finite makes what its products reach not finite (NaN also where the definition has an infinity), and
- * nothing else (bf16 storage: a weight beyond the largest bf16 counts as infinite).  Limits: K, M <= 65536, K M < 2^29, H W < 2^31, N H W < 2^40;
- * ESC_ERR_UNSUPPORTED beyond.  One launch; no workspace.
+ * nothing else (bf16 storage: a weight beyond the largest bf16 counts as infinite).  Limits: K, M <= 65536, K M < 2^29, H W < 2^31, N H W < 2^40, and
+ * T ceil(max(K, M) / 32) < 2^31 for T = N ceil(H W / 128), or ceil(N H W / 128) where N > 1 and H W < 96 (400 GB of bf16 at least);
+ * ESC_ERR_UNSUPPORTED beyond.  One launch (several where it would have 2^32 threads or more); no workspace.
  */
 typedef enum { ESC_ACT_NONE = 0, ESC_ACT_GELU = 1, ESC_ACT_SILU = 2, ESC_ACT_INT_RANGE = 0x7fffffff } esc_activation;
 

@@ -1,5 +1,6 @@
 // Host-side helpers of the C ABI's translation units.
 #pragma once
+#include <hip/hip_runtime.h>
 #include <stddef.h>
 #include <stdint.h>
 
@@ -41,6 +42,19 @@ inline bool images_of(const void *at, long stride, int N, size_t elements, size_
     return true;
 }
 inline bool meets(const Images &a, const void *b, size_t bytes) { return b != nullptr && overlaps(a.at, a.extent(), b, bytes); }
+
+// `blocks` blocks of `threads` by launch(first block, number): in one launch, or in several where it would have 2^32 threads or more, which HIP
+// refuses.
+template <typename F>
+hipError_t in_launches(long blocks, int threads, F launch)
+{
+    const long most = 0xffffffffL / threads;
+    for (long first = 0; first < blocks; first += most) {
+        const hipError_t e = launch(first, (unsigned)(blocks - first < most ? blocks - first : most));
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
 
 }  // namespace
 }  // namespace esc

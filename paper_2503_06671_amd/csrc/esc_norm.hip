@@ -38,6 +38,7 @@ struct NormParams {
     float *part;         // [splits][2][C]
     int N, C, splits;
     long P;
+    long first;          // of a launch's blocks
     float eps, inv_c;
 };
 
@@ -299,7 +300,7 @@ __global__ __launch_bounds__(kBlock<WS>) void norm_kernel(const NormParams p)
     __shared__ float s[2][kSets<WS>][WS][1][V][16];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), set = wave / WS, share = wave % WS;
     const long tiles = (p.P + 16 * V - 1) / (16 * V), all = tiles * p.N;
-    const long mine = (long)blockIdx.x * kSets<WS> + set;
+    const long mine = (p.first + blockIdx.x) * kSets<WS> + set;
     const Place at = place<V, WS>(mine < all ? mine : all - 1, tiles, p.P, p.C, share);  // (a set beyond the last tile does that one again)
     const E *x = static_cast<const E *>(p.x) + at.n * p.x_stride + at.origin;
     E *out = static_cast<E *>(p.out) + at.n * p.out_stride + at.origin;
@@ -475,21 +476,25 @@ int split_of(int C)
 constexpr int wide_of(bool back, Split k) { return (back ? k.kc > 8 : k.ws == 16) ? kWide / 2 : kWide; }
 
 template <typename E, bool BACK, int I = 0>
-hipError_t launch_held(const NormParams &p, int split, int v, long grid, hipStream_t s)
+hipError_t launch_held(NormParams p, int split, int v, long grid, hipStream_t s)
 {
     if constexpr (I < kSplitCount<BACK>) {
         if (split != I) return launch_held<E, BACK, I + 1>(p, split, v, grid, s);
         constexpr Split k = splits<BACK>()[I];
-        const dim3 blocks((unsigned)grid), block(kBlock<k.ws>);
+        const dim3 block(kBlock<k.ws>);
         constexpr int wide = wide_of(BACK, k);
         if constexpr (BACK) {
-            if (v == 1) hipLaunchKernelGGL((norm_back_kernel<E, 1, k.kc, k.ws>), blocks, block, 0, s, p);
-            else hipLaunchKernelGGL((norm_back_kernel<E, wide, k.kc, k.ws>), blocks, block, 0, s, p);
+            if (v == 1) hipLaunchKernelGGL((norm_back_kernel<E, 1, k.kc, k.ws>), dim3((unsigned)grid), block, 0, s, p);
+            else hipLaunchKernelGGL((norm_back_kernel<E, wide, k.kc, k.ws>), dim3((unsigned)grid), block, 0, s, p);
+            return hipGetLastError();
         } else {
-            if (v == 1) hipLaunchKernelGGL((norm_kernel<E, 1, k.kc, k.ws>), blocks, block, 0, s, p);
-            else hipLaunchKernelGGL((norm_kernel<E, wide, k.kc, k.ws>), blocks, block, 0, s, p);
+            return in_launches(grid, kBlock<k.ws>, [&](long first, unsigned blocks) {
+                p.first = first;
+                if (v == 1) hipLaunchKernelGGL((norm_kernel<E, 1, k.kc, k.ws>), dim3(blocks), block, 0, s, p);
+                else hipLaunchKernelGGL((norm_kernel<E, wide, k.kc, k.ws>), dim3(blocks), block, 0, s, p);
+                return hipGetLastError();
+            });
         }
-        return hipGetLastError();
     } else {
         return hipErrorInvalidValue;
     }
@@ -586,10 +591,8 @@ esc_status esc_layernorm_forward(const void *x, esc_dtype dt, const esc_layernor
         const Split k = kForward[split];
         const int v = lanes_pixels<false>(a->N, P, k);
         const long blocks = (tiles_of(a->N, P, v) + sets_of(k) - 1) / sets_of(k);
-        if (blocks < (1L << 31)) {
-            const hipError_t e = dt == ESC_F32 ? launch_held<float, false>(p, split, v, blocks, s) : launch_held<uint16_t, false>(p, split, v, blocks, s);
-            return e == hipSuccess ? ESC_OK : ESC_ERR_HIP;
-        }
+        const hipError_t e = dt == ESC_F32 ? launch_held<float, false>(p, split, v, blocks, s) : launch_held<uint16_t, false>(p, split, v, blocks, s);
+        return e == hipSuccess ? ESC_OK : ESC_ERR_HIP;
     }
     return launch_any<false>(p, dt == ESC_F32, s) == hipSuccess ? ESC_OK : ESC_ERR_HIP;
 }

@@ -56,7 +56,7 @@ __global__ __launch_bounds__(kThreads, 2) void product_kernel(const ProductParam
     const int l32 = lane & 31, half = lane >> 5;
     const int K = p.K, M = p.M, stages = (K + 31) / 32;
     const unsigned groups = (unsigned)(M + 32 * MT - 1) / (32u * MT);
-    const unsigned piece = piece_of(blockIdx.x, gridDim.x), tile = piece / groups;
+    const unsigned piece = p.first + piece_of(blockIdx.x, gridDim.x), tile = piece / groups;
     const int m0 = (int)(piece - tile * groups) * 32 * MT;
     const unsigned mine = 32u * NT * (unsigned)wave + NT * (unsigned)l32;   // this lane's first pixel, of the tile
 
@@ -296,11 +296,13 @@ hipError_t launch_as(ProductParams p, long N, hipStream_t s)
     using C = Streamed<MT, TW>;
     p.tiles = ((ACROSS ? p.pixels : p.P) + 128 * NT - 1) / (128 * NT);
     const long grid = p.tiles * (ACROSS ? 1 : N) * ((p.M + 32 * MT - 1) / (32 * MT));
-    if (grid >= (1L << 31)) return hipErrorInvalidValue;
     const auto kernel = product_kernel<TI, TO, TE, TX, TW, MT, NT, TRANS, MODE, ACROSS>;
     static_assert(C::kLds <= 64 * 1024, "");
-    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(kThreads), C::kLds, s, p);
-    return hipGetLastError();
+    return in_launches(grid, kThreads, [&](long first, unsigned blocks) {
+        p.first = (unsigned)first;
+        hipLaunchKernelGGL(kernel, dim3(blocks), dim3(kThreads), C::kLds, s, p);
+        return hipGetLastError();
+    });
 }
 
 template <typename TI, typename TO, typename TE, int TX, int TW, bool TRANS, int MODE>
@@ -690,6 +692,9 @@ esc_status shape(const esc_pointwise *a, long *P)
     if (a->act != ESC_ACT_NONE && a->act != ESC_ACT_GELU && a->act != ESC_ACT_SILU) return ESC_ERR_SHAPE;
     *P = (long)a->H * a->W;
     if (a->K > 65536 || a->M > 65536 || (long)a->K * a->M >= (1L << 29) || *P >= (1L << 31) || (double)*P * a->N >= 0x1p40) return ESC_ERR_UNSUPPORTED;
+    // (the smallest pieces of either product, numbered in 32 bits: 128 pixels of an image, or of all images where these are small, and 32 channels)
+    const long tiles = a->N == 1 || *P >= 96 ? a->N * ((*P + 127) / 128) : (a->N * *P + 127) / 128;
+    if (tiles * ((std::max(a->K, a->M) + 31) / 32) >= (1L << 31)) return ESC_ERR_UNSUPPORTED;
     return ESC_OK;
 }
 

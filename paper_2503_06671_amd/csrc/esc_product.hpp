@@ -18,6 +18,7 @@ struct ProductParams {
     int K, M, w_ld, act;
     long P, pixels;        // of an image, of all
     long tiles;            // of pixels, of an image (or of all, where they pass images' borders)
+    unsigned first;        // a launch's first block
 };
 
 namespace {
@@ -231,7 +232,7 @@ __device__ __forceinline__ void load_weights_across(Rsrc rw, int M, int K, int l
         w[e] = __uint_as_float((unsigned)__builtin_amdgcn_raw_buffer_load_b32(rw, (int)(k0 + k1 + e < K ? at : kBeyond), (int)(k0 + e < K ? 4u * ((unsigned)(k0 + e) * (unsigned)ld) : 0u), 0));
 }
 
-// Which eighths of the grid the dies get: consecutive pieces on one die.
+// Which eighths of a launch the dies get: consecutive pieces on one die.
 __device__ __forceinline__ unsigned piece_of(unsigned block, unsigned blocks)
 {
     const unsigned each = blocks / 8u, rest = blocks % 8u, die = block % 8u;
@@ -257,6 +258,7 @@ struct BackParams {
     int K, M, act;
     long P;
     unsigned tiles_of_image;
+    unsigned first;        // a launch's first block
 };
 __attribute__((visibility("hidden"))) bool back_fits(bool f32, int K, int M, long P, long N);
 __attribute__((visibility("hidden"))) hipError_t launch_back(bool f32, const BackParams &p, long N, hipStream_t s);

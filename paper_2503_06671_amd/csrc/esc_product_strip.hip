@@ -9,6 +9,7 @@
 // with residual, fp32 23.4 us (133 MB, 5.7 TB/s); 64 x 64 x 64, 64 to 128, gelu, bf16 forward 28.8 (101 MB, 3.5 TB/s: one round of blocks, whose reading and
 // writing do not overlap), gp and grad_x 59 (268 MB, 4.5 TB/s; as two kernels 84); 180 x 320, 192 to 576, bf16 33 (780 TFLOP/s of products of terms); a
 // kernel that stages both operands in LDS: 57, 97, 290 and 150.
+#include "esc_host.hpp"
 #include "esc_product.hpp"
 
 #include <algorithm>
@@ -96,7 +97,7 @@ __global__ __launch_bounds__(kThreads, strip_blocks(4 * KC * NT * TX, MODE != kF
     const int l32 = lane & 31, half = lane >> 5;
     const int K = p.K, M = p.M;
     const unsigned P = (unsigned)p.P;
-    const unsigned piece = piece_of(blockIdx.x, gridDim.x), tile = piece / p.parts, n = tile / p.tiles_of_image;
+    const unsigned piece = p.first + piece_of(blockIdx.x, gridDim.x), tile = piece / p.parts, n = tile / p.tiles_of_image;
     const int c0 = (int)(piece - tile * p.parts) * p.each, c1 = min(c0 + p.each, (M + 31) / 32);
     const unsigned px = (tile - n * p.tiles_of_image) * (128u * NT) + 32u * NT * (unsigned)wave + NT * (unsigned)l32;
     // (a lane whose pixels reach beyond the plane takes the plane's last ones again: the same bits are stored)
@@ -251,7 +252,7 @@ __global__ __launch_bounds__(kThreads, 2) void strip_back_kernel(const BackParam
     const int l32 = lane & 31, half = lane >> 5;
     const int K = p.K, M = p.M, chunks = (M + 31) / 32;
     const unsigned P = (unsigned)p.P;
-    const unsigned tile = piece_of(blockIdx.x, gridDim.x), n = tile / p.tiles_of_image;
+    const unsigned tile = p.first + piece_of(blockIdx.x, gridDim.x), n = tile / p.tiles_of_image;
     const unsigned px = (tile - n * p.tiles_of_image) * (128u * NT) + 32u * NT * (unsigned)wave + NT * (unsigned)l32;
     const unsigned pxc = px + NT <= P ? px : P - NT;
 
@@ -447,15 +448,17 @@ hipError_t launch_as(const ProductParams &q, long N, hipStream_t s)
     p.each = (int)((chunks + parts - 1) / parts);
     p.parts = (unsigned)((chunks + p.each - 1) / p.each);
     p.tiles_of_image = (unsigned)tiles;
-    if (all * p.parts >= (1L << 31)) return hipErrorInvalidValue;
     const auto kernel = strip_kernel<TI, TO, TE, TX, TW, KC, NT, TRANS, MODE>;
     constexpr size_t lds = StripLds<KC, TW>::kBytes;
     if (lds > 64 * 1024) {
         const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
         if (e != hipSuccess) return e;
     }
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(all * p.parts)), dim3(kThreads), lds, s, p);
-    return hipGetLastError();
+    return in_launches(all * p.parts, kThreads, [&](long first, unsigned blocks) {
+        p.first = (unsigned)first;
+        hipLaunchKernelGGL(kernel, dim3(blocks), dim3(kThreads), lds, s, p);
+        return hipGetLastError();
+    });
 }
 
 // Two pixels a lane where the registers hold their channels and every compute unit has two blocks, of a third of the outputs at least.
@@ -480,12 +483,13 @@ template <typename T, int TX, int TF, int TG, int TB, int KC, int NT>
 hipError_t launch_back_as(BackParams p, long N, hipStream_t s)
 {
     p.tiles_of_image = (unsigned)((p.P + 128 * NT - 1) / (128 * NT));
-    const long grid = p.tiles_of_image * N;
-    if (grid >= (1L << 31)) return hipErrorInvalidValue;
     constexpr size_t lds = BackLds<KC, TF, TB>::kBytes;
     static_assert(lds <= 64 * 1024, "");
-    hipLaunchKernelGGL((strip_back_kernel<T, TX, TF, TG, TB, KC, NT>), dim3((unsigned)grid), dim3(kThreads), lds, s, p);
-    return hipGetLastError();
+    return in_launches(p.tiles_of_image * N, kThreads, [&](long first, unsigned blocks) {
+        p.first = (unsigned)first;
+        hipLaunchKernelGGL((strip_back_kernel<T, TX, TF, TG, TB, KC, NT>), dim3(blocks), dim3(kThreads), lds, s, p);
+        return hipGetLastError();
+    });
 }
 // what the registers hold, with bf16 storage and with fp32
 constexpr int kMostK[2] = {192, 160}, kBackMostK[2] = {128, 64};
