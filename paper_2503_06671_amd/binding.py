@@ -5,6 +5,10 @@ paper) runs in the HIP kernels.  torch supplies device memory and streams.  The 
 made once per pass check their tensors in native code (csrc/esc_native.cpp, built into
 _native.so); the workspace calls, made once, go through ctypes.
 There is no CPU fallback; a missing library raises.
+
+`stream` is a torch stream, or any object with `cuda_stream`; None is the current one.  What a call allocates (results, gradients, prepared workspaces)
+comes from the memory of the stream it runs on, as what torch itself allocates there does: ordered with that stream's work; used on another stream
+it is the caller's to order, and to keep until that use is over (record_stream).
 """
 from __future__ import annotations
 
@@ -229,6 +233,13 @@ def _stream(stream) -> Optional[int]:
     return stream.cuda_stream or None
 
 
+def _as_torch(stream, device):
+    """A stream (None, or any object with `cuda_stream`) as torch.cuda.stream() takes it."""
+    if stream is None or isinstance(stream, torch.cuda.Stream):
+        return stream
+    return torch.cuda.ExternalStream(stream.cuda_stream, device=device)
+
+
 def _dev_f32(t: Optional[torch.Tensor], name: str) -> Optional[torch.Tensor]:
     if t is None:
         return None
@@ -285,14 +296,20 @@ def workspace_errors(ws: torch.Tensor, stream=None) -> int:
     return int(v.value)
 
 
+def _prepared(nbytes: int, device, stream) -> torch.Tensor:
+    """A workspace of the pool of the stream that prepares it."""
+    if nbytes == 0:
+        raise ValueError("bad shape for a workspace")
+    with torch.cuda.stream(_as_torch(stream, device)):
+        ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
+    workspace_init(ws, stream)
+    return ws
+
+
 def new_workspace(N: int, Ca: int, H: int, W: int, device="cuda", stream=None) -> torch.Tensor:
     """Allocate (with torch) and prepare a workspace for this shape."""
     nbytes = workspace_bytes(N, Ca, H, W)
-    if nbytes == 0:
-        raise ValueError("bad shape for a workspace")
-    ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
-    workspace_init(ws, stream)
-    return ws
+    return _prepared(nbytes, device, stream)
 
 
 def dynkernel_gen(x: torch.Tensor, Ca: int, gen: GenParams, workspace: torch.Tensor,
@@ -320,11 +337,7 @@ def new_fused_workspace(N: int, Ca: int, H: int, W: int, dtype: torch.dtype, wit
                         stream=None) -> torch.Tensor:
     """Allocate (with torch) and prepare a workspace for esc_convattn_fused_forward."""
     nbytes = fused_workspace_bytes(N, Ca, H, W, dtype, with_lk_c)
-    if nbytes == 0:
-        raise ValueError("bad shape for a workspace")
-    ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
-    workspace_init(ws, stream)
-    return ws
+    return _prepared(nbytes, device, stream)
 
 
 def convattn_fused_forward(x: torch.Tensor, Ca: int, lk: torch.Tensor, w_fuse: torch.Tensor, workspace: torch.Tensor,
@@ -357,11 +370,7 @@ def new_residual_step_workspace(N: int, C: int, H: int, W: int, Ca: int, Ch: int
     """Allocate (with torch) and prepare a workspace for esc_residual_step_forward."""
     dt = ESC_F32 if dtype == torch.float32 else ESC_BF16
     nbytes = int(load_library().esc_residual_step_workspace_bytes(N, C, H, W, Ca, Ch, dt, int(bool(with_lk_c))))
-    if nbytes == 0:
-        raise ValueError("bad shape for a workspace")
-    ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
-    workspace_init(ws, stream)
-    return ws
+    return _prepared(nbytes, device, stream)
 
 
 def residual_step_forward(f_in: torch.Tensor, w1: torch.Tensor, k_dw: torch.Tensor, w2: torch.Tensor, Ca: int,
@@ -378,11 +387,7 @@ def residual_step_forward(f_in: torch.Tensor, w1: torch.Tensor, k_dw: torch.Tens
 def new_dense_workspace(N: int, Ca: int, H: int, W: int, Ks: int, device="cuda", stream=None) -> torch.Tensor:
     """Allocate (with torch) and prepare a workspace for esc_convattn_dense_forward."""
     nbytes = int(load_library().esc_dense_workspace_bytes(N, Ca, H, W, Ks))
-    if nbytes == 0:
-        raise ValueError("bad shape for a workspace")
-    ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
-    workspace_init(ws, stream)
-    return ws
+    return _prepared(nbytes, device, stream)
 
 
 def convattn_dense_forward(x: torch.Tensor, Ca: int, lk_dense: torch.Tensor, workspace: torch.Tensor,
@@ -395,11 +400,7 @@ def convattn_dense_forward(x: torch.Tensor, Ca: int, lk_dense: torch.Tensor, wor
 def new_backward_workspace(N: int, Ca: int, H: int, W: int, Ks: int, hidden: int, device="cuda", stream=None) -> torch.Tensor:
     """Allocate (with torch) and prepare a workspace for esc_convattn_backward."""
     nbytes = int(load_library().esc_backward_workspace_bytes(N, Ca, H, W, Ks, hidden))
-    if nbytes == 0:
-        raise ValueError("bad shape for a workspace")
-    ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
-    workspace_init(ws, stream)
-    return ws
+    return _prepared(nbytes, device, stream)
 
 
 def convattn_backward(x: torch.Tensor, grad_out: torch.Tensor, Ca: int, lk: torch.Tensor, workspace: torch.Tensor,
@@ -582,8 +583,7 @@ class AdamW:
             return tensors
 
         # (zeros and the plan on one stream: the first step, ordered behind the plan, is behind the zeros too)
-        if stream is not None and not isinstance(stream, torch.cuda.Stream):
-            stream = torch.cuda.ExternalStream(stream.cuda_stream, device=device)
+        stream = _as_torch(stream, device)
 
         def state(name, given, dtype, sizes):
             if given is None:

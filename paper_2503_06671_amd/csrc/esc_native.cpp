@@ -146,6 +146,23 @@ void *stream_of(PyObject *o)
     return p;
 }
 
+// The stream of a call on tensors of device `d`.  While this stands a stream that the caller gave is the current one there: what the call allocates is of
+// that stream's pool and ready for it (memory of another stream's pool may still be in use by what that stream has under way), and zeros are written on it.
+struct OnStream {
+    void *const raw;
+    const bool changed;
+    const c10::hip::HIPStream before;
+    OnStream(PyObject *o, const c10::Device &d) : raw(stream_of(o)), changed(given(o)), before(c10::hip::getCurrentHIPStream(d.index()))
+    {
+        if (changed) c10::hip::setCurrentHIPStream(c10::hip::getStreamFromExternal(static_cast<hipStream_t>(raw), d.index()));
+    }
+    OnStream(const OnStream &) = delete;
+    ~OnStream()
+    {
+        if (changed) c10::hip::setCurrentHIPStream(before);
+    }
+};
+
 struct Ws {
     void *ptr;
     size_t bytes;
@@ -301,15 +318,15 @@ PyObject *dynkernel_gen(PyObject *const *a, Py_ssize_t n)
     want_args(n, 6);  // x, Ca, gen, workspace, dk_out, stream
     const at::Tensor &x = tensor(a[0], "x");
     const Shape s = x_checked(x);
+    const OnStream on(a[5], x.device());
     const int Ca = integer(a[1]);
     const Gen *g = gen_of(a[2], Ca);
     const Ws ws = workspace(a[3]);
     at::Tensor dk = given(a[4]) ? dev_f32_required(a[4], "dk_out") : at::empty({s.N, Ca, 3, 3}, x.options().dtype(at::kFloat));
     if (dk.numel() != (int64_t)s.N * Ca * 9) fail(PyExc_ValueError, "dk_out must hold [N, Ca, 3, 3] values");
-    void *st = stream_of(a[5]);
     float *dkp = static_cast<float *>(dk.data_ptr());
     const void *xp = x.data_ptr();
-    check(unlocked([&] { return esc_dynkernel_gen(xp, s.dt, s.N, s.C, s.H, s.W, Ca, g != nullptr ? &g->p : nullptr, dkp, ws.ptr, ws.bytes, st); }));
+    check(unlocked([&] { return esc_dynkernel_gen(xp, s.dt, s.N, s.C, s.H, s.W, Ca, g != nullptr ? &g->p : nullptr, dkp, ws.ptr, ws.bytes, on.raw); }));
     return result(a[4], dk);
 }
 
@@ -318,21 +335,21 @@ PyObject *convattn_forward(PyObject *const *a, Py_ssize_t n)
     want_args(n, 10);  // x, Ca, lk, workspace, gen, dk_in, out, stream, ks, lk_channel_stride
     const at::Tensor &x = tensor(a[0], "x");
     const Shape s = x_checked(x);
+    const OnStream on(a[7], x.device());
     const int Ca = integer(a[1]);
     const Lk lk = lk_checked(a[2], Ca, a[8], a[9]);
     const Gen *g = gen_of(a[4], Ca);
     const at::Tensor out = out_or_new(a[6], x);
     const float *dk = ptr(dk_checked(a[5], s, Ca));
-    void *st = stream_of(a[7]);
     const esc_gen_params *gp = g != nullptr ? &g->p : nullptr;
     const void *xp = x.data_ptr();
     void *op = out.data_ptr();
     if (!given(a[3])) {  // the entry point that allocates nothing: the library's own scratch
-        check(unlocked([&] { return esc_convattn_forward_noalloc(xp, s.dt, s.N, s.C, s.H, s.W, Ca, lk.ptr, lk.Ks, lk.stride, gp, dk, op, st); }));
+        check(unlocked([&] { return esc_convattn_forward_noalloc(xp, s.dt, s.N, s.C, s.H, s.W, Ca, lk.ptr, lk.Ks, lk.stride, gp, dk, op, on.raw); }));
     } else {
         const Ws ws = workspace(a[3]);
         check(unlocked([&] {
-            return esc_convattn_forward(xp, s.dt, s.N, s.C, s.H, s.W, Ca, lk.ptr, lk.Ks, lk.stride, gp, dk, op, ws.ptr, ws.bytes, st);
+            return esc_convattn_forward(xp, s.dt, s.N, s.C, s.H, s.W, Ca, lk.ptr, lk.Ks, lk.stride, gp, dk, op, ws.ptr, ws.bytes, on.raw);
         }));
     }
     return result(a[6], out);
@@ -357,6 +374,7 @@ PyObject *convattn_fused_forward(PyObject *const *a, Py_ssize_t n)
     want_args(n, 12);  // x, Ca, lk, w_fuse, workspace, b_fuse, lk_c, residual, gen, dk_in, out, stream
     const at::Tensor &x = tensor(a[0], "x");
     const Shape s = x_checked(x);
+    const OnStream on(a[11], x.device());
     const int Ca = integer(a[1]);
     const Lk lk = lk_checked(a[2], Ca);
     const Gen *g = gen_of(a[8], Ca);
@@ -371,12 +389,11 @@ PyObject *convattn_fused_forward(PyObject *const *a, Py_ssize_t n)
     }
     const at::Tensor out = out_or_new(a[10], x);
     const Ws ws = workspace(a[4]);
-    void *st = stream_of(a[11]);
     const void *xp = x.data_ptr();
     void *op = out.data_ptr();
     check(unlocked([&] {
         return esc_convattn_fused_forward(xp, s.dt, s.N, s.C, s.H, s.W, Ca, f.lkc, lk.ptr, lk.Ks, lk.stride, g != nullptr ? &g->p : nullptr,
-                                          dk, f.w, f.b, res, op, ws.ptr, ws.bytes, st);
+                                          dk, f.w, f.b, res, op, ws.ptr, ws.bytes, on.raw);
     }));
     return result(a[10], out);
 }
@@ -386,14 +403,14 @@ PyObject *convffn_forward(PyObject *const *a, Py_ssize_t n)
     want_args(n, 10);  // x, w1, k_dw, w2, workspace, b1, b_dw, b2, out, stream
     const at::Tensor &x = tensor(a[0], "x");
     const Shape s = x_checked(x);
+    const OnStream on(a[9], x.device());
     const Ffn f = ffn_checked(s.C, a[1], a[2], a[3], a[5], a[6], a[7]);
     const at::Tensor out = out_or_new(a[8], x);
     const Ws ws = workspace(a[4]);
-    void *st = stream_of(a[9]);
     const void *xp = x.data_ptr();
     void *op = out.data_ptr();
     check(unlocked([&] {
-        return esc_convffn_forward(xp, s.dt, s.N, s.C, s.H, s.W, f.Ch, f.w1, f.b1, f.k, f.bk, f.w2, f.b2, op, ws.ptr, ws.bytes, st);
+        return esc_convffn_forward(xp, s.dt, s.N, s.C, s.H, s.W, f.Ch, f.w1, f.b1, f.k, f.bk, f.w2, f.b2, op, ws.ptr, ws.bytes, on.raw);
     }));
     return result(a[8], out);
 }
@@ -404,6 +421,7 @@ PyObject *residual_step_forward(PyObject *const *a, Py_ssize_t n)
     want_args(n, 16);
     const at::Tensor &x = tensor(a[0], "x");
     const Shape s = x_checked(x);
+    const OnStream on(a[15], x.device());
     const Ffn f = ffn_checked(s.C, a[1], a[2], a[3], a[8], a[9], a[10]);
     const int Ca = integer(a[4]);
     const Lk lk = lk_checked(a[5], Ca);
@@ -411,12 +429,11 @@ PyObject *residual_step_forward(PyObject *const *a, Py_ssize_t n)
     const Fuse fu = fuse_checked(s.C, Ca, a[6], a[13], a[11]);
     const at::Tensor out = out_or_new(a[14], x, "out must match f_in in dtype and shape and be contiguous");
     const Ws ws = workspace(a[7]);
-    void *st = stream_of(a[15]);
     const void *xp = x.data_ptr();
     void *op = out.data_ptr();
     check(unlocked([&] {
         return esc_residual_step_forward(xp, s.dt, s.N, s.C, s.H, s.W, f.Ch, f.w1, f.b1, f.k, f.bk, f.w2, f.b2, Ca, fu.lkc, lk.ptr, lk.Ks,
-                                         lk.stride, g != nullptr ? &g->p : nullptr, fu.w, fu.b, op, ws.ptr, ws.bytes, st);
+                                         lk.stride, g != nullptr ? &g->p : nullptr, fu.w, fu.b, op, ws.ptr, ws.bytes, on.raw);
     }));
     return result(a[14], out);
 }
@@ -426,6 +443,7 @@ PyObject *convattn_dense_forward(PyObject *const *a, Py_ssize_t n)
     want_args(n, 8);  // x, Ca, lk_dense, workspace, gen, dk_in, out, stream
     const at::Tensor &x = tensor(a[0], "x");
     const Shape s = x_checked(x);
+    const OnStream on(a[7], x.device());
     const int Ca = integer(a[1]);
     const at::Tensor &lk = dev_f32_required(a[2], "lk_dense");
     if (lk.dim() != 4 || lk.size(0) != Ca || lk.size(1) != Ca || lk.size(2) != lk.size(3))
@@ -435,12 +453,11 @@ PyObject *convattn_dense_forward(PyObject *const *a, Py_ssize_t n)
     const float *dk = ptr(dk_checked(a[5], s, Ca));
     const at::Tensor out = out_or_new(a[6], x);
     const Ws ws = workspace(a[3]);
-    void *st = stream_of(a[7]);
     const float *lp = ptr(&lk);
     const void *xp = x.data_ptr();
     void *op = out.data_ptr();
     check(unlocked([&] {
-        return esc_convattn_dense_forward(xp, s.dt, s.N, s.C, s.H, s.W, Ca, lp, Ks, g != nullptr ? &g->p : nullptr, dk, op, ws.ptr, ws.bytes, st);
+        return esc_convattn_dense_forward(xp, s.dt, s.N, s.C, s.H, s.W, Ca, lp, Ks, g != nullptr ? &g->p : nullptr, dk, op, ws.ptr, ws.bytes, on.raw);
     }));
     return result(a[6], out);
 }
@@ -457,6 +474,7 @@ PyObject *convattn_backward(PyObject *const *a, Py_ssize_t n)
     want_args(n, 10);  // x, grad_out, Ca, lk, workspace, gen, dk_in, accumulate, grads, stream
     const at::Tensor &x = tensor(a[0], "x");
     const Shape s = x_checked(x);
+    const OnStream on(a[9], x.device());
     const at::Tensor &go = tensor(a[1], "grad_out");
     if (!like(go, x) || !go.is_cuda()) fail(PyExc_TypeError, "grad_out must match x in dtype and shape and be a contiguous device tensor");
     const int Ca = integer(a[2]);
@@ -530,11 +548,10 @@ PyObject *convattn_backward(PyObject *const *a, Py_ssize_t n)
             dev_f32(val, name);
         }
     const Ws ws = workspace(a[4]);
-    void *st = stream_of(a[9]);
     const void *xp = x.data_ptr(), *gop = go.data_ptr();
     check(unlocked([&] {
         return esc_convattn_backward(xp, gop, s.dt, s.N, s.C, s.H, s.W, Ca, lk.ptr, lk.Ks, lk.stride, g != nullptr ? &g->p : nullptr, dk, gxp,
-                                     glk, g != nullptr ? &gg : nullptr, gdk, acc, ws.ptr, ws.bytes, st);
+                                     glk, g != nullptr ? &gg : nullptr, gdk, acc, ws.ptr, ws.bytes, on.raw);
     }));
     PyObject *r = grads.d;
     grads.d = nullptr;
@@ -663,6 +680,7 @@ PyObject *window_attention_forward(PyObject *const *a, Py_ssize_t n)
     at.a.edges = at.edges.data();
     const at::Tensor &q = *at.q;
     const c10::DeviceGuard guard(q.device());
+    const OnStream on(a[12], q.device());
     at::Tensor out;
     if (given(a[10])) {
         out = tensor(a[10], "out");
@@ -677,10 +695,9 @@ PyObject *window_attention_forward(PyObject *const *a, Py_ssize_t n)
         saved = workspace(a[11]);
         same_device(tensor(a[11], "saved"), q, "saved");
     }
-    void *st = stream_of(a[12]);
     const void *qp = q.data_ptr(), *kp = at.k->data_ptr(), *vp = at.v->data_ptr();
     void *op = out.data_ptr();
-    check(unlocked([&] { return esc_window_attention_forward(qp, kp, vp, at.dt, &at.a, op, saved.ptr, saved.bytes, st); }));
+    check(unlocked([&] { return esc_window_attention_forward(qp, kp, vp, at.dt, &at.a, op, saved.ptr, saved.bytes, on.raw); }));
     return result(a[10], out);
 }
 
@@ -704,6 +721,7 @@ PyObject *window_attention_backward(PyObject *const *a, Py_ssize_t n)
     int acc = PyObject_IsTrue(a[14]);
     if (acc < 0) throw PyError{};
     const c10::DeviceGuard guard(q.device());
+    const OnStream on(a[16], q.device());
     struct Dict {
         PyObject *d;
         ~Dict() { Py_XDECREF(d); }
@@ -750,10 +768,9 @@ PyObject *window_attention_backward(PyObject *const *a, Py_ssize_t n)
             g.bias = static_cast<float *>(t.data_ptr());
         }
     }
-    void *st = stream_of(a[16]);
     const void *qp = q.data_ptr(), *kp = at.k->data_ptr(), *vp = at.v->data_ptr(), *op = out.data_ptr(), *gop = go.data_ptr();
     check(unlocked([&] {
-        return esc_window_attention_backward(qp, kp, vp, at.dt, &at.a, op, gop, saved.ptr, saved.bytes, &g, acc, ws.ptr, ws.bytes, st);
+        return esc_window_attention_backward(qp, kp, vp, at.dt, &at.a, op, gop, saved.ptr, saved.bytes, &g, acc, ws.ptr, ws.bytes, on.raw);
     }));
     PyObject *r = grads.d;
     grads.d = nullptr;
@@ -921,13 +938,13 @@ PyObject *layernorm_forward(PyObject *const *a, Py_ssize_t n)
     l.N = x.N, l.C = x.C, l.H = x.H, l.W = x.W, l.eps = (float)number(a[3]), l.x_stride = x.stride;
     l.weight = weights_beside(a[1], x, {x.C}, "weight"), l.bias = weights_beside(a[2], x, {x.C}, "bias");
     const c10::DeviceGuard guard(x.t->device());
+    const OnStream on(a[6], x.t->device());
     const at::Tensor out = map_or_new(a[4], x, x.C, "out", &l.out_stride);
     Ws saved{nullptr, 0};
     if (given(a[5])) saved = scratch_beside(a[5], x, "saved");
-    void *st = stream_of(a[6]);
     const void *xp = x.t->data_ptr();
     void *op = out.data_ptr();
-    check(unlocked([&] { return esc_layernorm_forward(xp, x.dt, &l, op, saved.ptr, saved.bytes, st); }));
+    check(unlocked([&] { return esc_layernorm_forward(xp, x.dt, &l, op, saved.ptr, saved.bytes, on.raw); }));
     return result(a[4], out);
 }
 
@@ -949,6 +966,7 @@ PyObject *layernorm_backward(PyObject *const *a, Py_ssize_t n)
     }
     int acc = truth(a[7]);
     const c10::DeviceGuard guard(x.t->device());
+    const OnStream on(a[10], x.t->device());
     Grads grads(a[8]);
     esc_layernorm_grads g{};
     bool brought_w = false, brought_b = false;
@@ -957,9 +975,8 @@ PyObject *layernorm_backward(PyObject *const *a, Py_ssize_t n)
     if (l.weight != nullptr && wanted(a[9], "grad_weight")) g.weight = grads.weights("grad_weight", x, {x.C}, &brought_w);
     if (l.bias != nullptr && wanted(a[9], "grad_bias")) g.bias = grads.weights("grad_bias", x, {x.C}, &brought_b);
     acc = adds(acc, brought_w, brought_b, g.weight, g.bias, "grad_weight", "grad_bias");
-    void *st = stream_of(a[10]);
     const void *xp = x.t->data_ptr(), *gop = go.data_ptr();
-    check(unlocked([&] { return esc_layernorm_backward(xp, gop, skip, x.dt, &l, saved.ptr, saved.bytes, &g, acc, ws.ptr, ws.bytes, st); }));
+    check(unlocked([&] { return esc_layernorm_backward(xp, gop, skip, x.dt, &l, saved.ptr, saved.bytes, &g, acc, ws.ptr, ws.bytes, on.raw); }));
     return grads.release();
 }
 
@@ -988,11 +1005,11 @@ PyObject *pointwise_forward(PyObject *const *a, Py_ssize_t n)
         res = t.data_ptr();
     }
     const c10::DeviceGuard guard(x.t->device());
+    const OnStream on(a[6], x.t->device());
     const at::Tensor out = map_or_new(a[5], x, p.M, "out", &p.out_stride);
-    void *st = stream_of(a[6]);
     const void *xp = x.t->data_ptr();
     void *op = out.data_ptr();
-    check(unlocked([&] { return esc_pointwise_forward(xp, res, x.dt, &p, op, st); }));
+    check(unlocked([&] { return esc_pointwise_forward(xp, res, x.dt, &p, op, on.raw); }));
     return result(a[5], out);
 }
 
@@ -1006,6 +1023,7 @@ PyObject *pointwise_backward(PyObject *const *a, Py_ssize_t n)
     const Ws ws = scratch_beside(a[3], x, "workspace");
     int acc = truth(a[6]);
     const c10::DeviceGuard guard(x.t->device());
+    const OnStream on(a[9], x.t->device());
     Grads grads(a[7]);
     esc_pointwise_grads g{};
     bool brought_w = false, brought_b = false;
@@ -1014,9 +1032,8 @@ PyObject *pointwise_backward(PyObject *const *a, Py_ssize_t n)
     if (wanted(a[8], "grad_w")) g.w = grads.weights("grad_w", x, {p.M, p.K}, &brought_w);
     if (p.b != nullptr && wanted(a[8], "grad_b")) g.b = grads.weights("grad_b", x, {p.M}, &brought_b);
     acc = adds(acc, brought_w, brought_b, g.w, g.b, "grad_w", "grad_b");
-    void *st = stream_of(a[9]);
     const void *xp = x.t->data_ptr(), *gop = go.data_ptr();
-    check(unlocked([&] { return esc_pointwise_backward(xp, gop, x.dt, &p, &g, acc, ws.ptr, ws.bytes, st); }));
+    check(unlocked([&] { return esc_pointwise_backward(xp, gop, x.dt, &p, &g, acc, ws.ptr, ws.bytes, on.raw); }));
     return grads.release();
 }
 
@@ -1062,11 +1079,11 @@ PyObject *dropout_forward(PyObject *const *a, Py_ssize_t n)
         res = t.data_ptr();
     }
     const c10::DeviceGuard guard(x.t->device());
+    const OnStream on(a[8], x.t->device());
     const at::Tensor out = map_or_new(a[7], x, x.C, "out", &d.out_stride);
-    void *st = stream_of(a[8]);
     const void *xp = x.t->data_ptr();
     void *op = out.data_ptr();
-    check(unlocked([&] { return esc_dropout_forward(xp, res, x.dt, &d, op, st); }));
+    check(unlocked([&] { return esc_dropout_forward(xp, res, x.dt, &d, op, on.raw); }));
     return result(a[7], out);
 }
 
@@ -1077,11 +1094,11 @@ PyObject *dropout_backward(PyObject *const *a, Py_ssize_t n)
     esc_dropout d = dropout_checked(g, a[1], a[2], a[3], a[4], a[5]);
     d.out_stride = g.stride;
     const c10::DeviceGuard guard(g.t->device());
+    const OnStream on(a[7], g.t->device());
     const at::Tensor gx = map_or_new(a[6], g, g.C, "grad_x", &d.x_stride);
-    void *st = stream_of(a[7]);
     const void *gop = g.t->data_ptr();
     void *gxp = gx.data_ptr();
-    check(unlocked([&] { return esc_dropout_backward(gop, g.dt, &d, gxp, st); }));
+    check(unlocked([&] { return esc_dropout_backward(gop, g.dt, &d, gxp, on.raw); }));
     return result(a[6], gx);
 }
 

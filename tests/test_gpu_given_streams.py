@@ -1,0 +1,121 @@
+"""Calls that are given a stream and no buffers: what they allocate is of that stream's memory, and all of their work, zeros too, is on it."""
+import pytest
+import torch
+
+from paper_2503_06671_amd import binding
+
+pytestmark = pytest.mark.gpu
+
+N, C, CA, CH, KS, H, W = 2, 8, 4, 12, 3, 9, 10
+
+
+def calls():
+    """{name: call(stream), which gives the tensors that it allocated}; everything else is here before."""
+    g = torch.Generator(device="cuda").manual_seed(0)
+    r = lambda *s: torch.randn(*s, device="cuda", generator=g)  # noqa: E731
+    x, go, lk, gen = r(N, C, H, W), r(N, C, H, W), r(CA, KS, KS), binding.GenParams(r(9 * CA, CA), r(9 * CA))
+    w1, kd, w2, wf, w = r(CH, C), r(CH, 3, 3), r(C, CH), r(C, C), r(5, C)
+    ws, fws = binding.new_workspace(N, CA, H, W), binding.new_fused_workspace(N, CA, H, W, torch.float32, False)
+    cws = binding.new_convffn_workspace(N, CH, H, W, torch.float32)
+    rws = binding.new_residual_step_workspace(N, C, H, W, CA, CH, torch.float32, False)
+    dws, bws, dense = binding.new_dense_workspace(N, CA, H, W, KS), binding.new_backward_workspace(N, CA, H, W, KS, 0), r(CA, CA, KS, KS)
+    heads, win, bias = 2, (4, 5), r(2, 7, 9)
+    saved, aws = binding.new_window_attention_saved(N, heads, C // heads, H, W, torch.float32), binding.new_window_attention_backward_workspace(N, heads, C // heads, H, W, win)
+    att = binding.window_attention_forward(x, x, x, heads, win, bias=bias, saved=saved)
+    nsaved, nws, nw = binding.new_layernorm_saved(N, H, W), binding.new_layernorm_backward_workspace(N, C, H, W), r(C)
+    binding.layernorm_forward(x, nw, nw, saved=nsaved)
+    go5, pws = r(N, 5, H, W), binding.new_pointwise_backward_workspace(N, C, 5, H, W, torch.float32, act="gelu")
+    b5 = r(5)
+    return {
+        "dynkernel_gen": lambda s: [binding.dynkernel_gen(x, CA, gen, ws, stream=s)],
+        "convattn_forward": lambda s: [binding.convattn_forward(x, CA, lk, ws, gen=gen, stream=s)],
+        "convattn_fused_forward": lambda s: [binding.convattn_fused_forward(x, CA, lk, wf, fws, gen=gen, stream=s)],
+        "convffn_forward": lambda s: [binding.convffn_forward(x, w1, kd, w2, cws, stream=s)],
+        "residual_step_forward": lambda s: [binding.residual_step_forward(x, w1, kd, w2, CA, lk, wf, rws, gen=gen, stream=s)],
+        "convattn_dense_forward": lambda s: [binding.convattn_dense_forward(x, CA, dense, dws, gen=gen, stream=s)],
+        "convattn_backward": lambda s: list(binding.convattn_backward(x, go, CA, lk, bws, gen=gen, stream=s).values()),
+        "convattn_backward, adding to zeros": lambda s: list(binding.convattn_backward(x, go, CA, lk, bws, gen=gen, accumulate=True, stream=s).values()),
+        "window_attention_forward": lambda s: [binding.window_attention_forward(x, x, x, heads, win, bias=bias, stream=s)],
+        "window_attention_backward": lambda s: list(binding.window_attention_backward(x, x, x, att, go, saved, heads, win, aws, bias=bias, stream=s).values()),
+        "layernorm_forward": lambda s: [binding.layernorm_forward(x, nw, nw, stream=s)],
+        "layernorm_backward": lambda s: list(binding.layernorm_backward(x, go, nsaved, nws, nw, nw, stream=s).values()),
+        "pointwise_forward": lambda s: [binding.pointwise_forward(x, w, b5, "gelu", stream=s)],
+        "pointwise_backward": lambda s: list(binding.pointwise_backward(x, go5, w, pws, b5, "gelu", stream=s).values()),
+        "dropout_forward": lambda s: [binding.dropout_forward(x, 0.3, 7, stream=s)],
+        "dropout_backward": lambda s: [binding.dropout_backward(go, 0.3, 7, stream=s)],
+    }
+
+
+def pool_of(t):
+    """The stream whose memory a tensor's is."""
+    for seg in torch.cuda.memory_snapshot():
+        if seg["address"] <= t.data_ptr() < seg["address"] + seg["total_size"]:
+            return seg["stream"]
+
+
+class Handle:
+    def __init__(self, stream):
+        self.cuda_stream = stream.cuda_stream
+
+
+@pytest.mark.parametrize("kind", ["torch", "handle"])
+def test_results_are_of_the_streams_memory(kind):
+    # (a call's result in memory that the current stream freed could be written while that stream still works with it)
+    side = torch.cuda.Stream()
+    for name, call in calls().items():
+        print(f"[case] {name}", flush=True)
+        want = call(None)
+        here = torch.cuda.current_stream()
+        assert all(pool_of(t) == here.cuda_stream for t in want), name
+        torch.cuda.synchronize()
+        got = call(side if kind == "torch" else Handle(side))
+        assert torch.cuda.current_stream() == here, name
+        assert got and all(pool_of(t) == side.cuda_stream for t in got), name
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), name
+
+
+def test_all_work_is_on_the_stream():
+    # the current one is busy for some milliseconds: nothing that was asked of the other waits for it, or comes behind it
+    all_of = calls()
+    want = {n: call(None) for n, call in all_of.items()}
+    big, side = torch.randn(4096, 4096, device="cuda"), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    got = {}
+    for name, call in all_of.items():
+        for _ in range(10):
+            big = big @ big * 1e-4
+        end = torch.cuda.Event()
+        end.record()
+        got[name] = call(side)
+        side.synchronize()
+        busy = not end.query()
+        copies = []
+        with torch.cuda.stream(side):
+            copies = [t.clone() for t in got[name]]
+        side.synchronize()
+        assert busy and not end.query(), name
+        assert all(torch.equal(a, b) for a, b in zip(copies, want[name])), name
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got[name], want[name])), name
+
+
+def test_a_refused_call_leaves_the_current_stream():
+    x, here = torch.randn(1, 6, 3, 3, device="cuda"), torch.cuda.current_stream()
+    for error, call in [(binding.EscError, lambda s: binding.layernorm_forward(x, eps=-1.0, stream=s)), (ValueError, lambda s: binding.pointwise_forward(x, torch.ones(2, 5, device="cuda"), stream=s)),
+                        (binding.EscError, lambda s: binding.dropout_forward(x, 1.0, 1, stream=s))]:
+        with pytest.raises(error):
+            call(torch.cuda.Stream())
+        assert torch.cuda.current_stream() == here
+    with pytest.raises(AttributeError):
+        binding.layernorm_forward(x, stream=object())
+    assert torch.cuda.current_stream() == here
+
+
+def test_prepared_workspaces_are_of_the_streams_memory():
+    side = torch.cuda.Stream()
+    for s in (side, Handle(side)):
+        for ws in (binding.new_workspace(N, CA, H, W, stream=s), binding.new_fused_workspace(N, CA, H, W, torch.float32, True, stream=s),
+                   binding.new_residual_step_workspace(N, C, H, W, CA, CH, torch.float32, True, stream=s), binding.new_dense_workspace(N, CA, H, W, KS, stream=s),
+                   binding.new_backward_workspace(N, CA, H, W, KS, 0, stream=s)):
+            assert pool_of(ws) == side.cuda_stream and binding.workspace_errors(ws, s) == 0
