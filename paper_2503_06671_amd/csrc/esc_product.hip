@@ -315,7 +315,12 @@ hipError_t launch_product(const ProductParams &p, long N, hipStream_t s)
     // as much for a wavefront as leaves every compute unit two blocks (and, with three terms of both, registers)
     if constexpr (TX != 3)
         if (p.M > 64 && blocks(4, 2) >= 2 * kCus) return launch_as<TI, TO, TE, TX, TW, 4, 2, TRANS, MODE, false>(p, N, s);
-    if (p.M <= 32) return blocks(1, 2) >= 2 * kCus ? launch_as<TI, TO, TE, TX, TW, 1, 2, TRANS, MODE, false>(p, N, s) : launch_as<TI, TO, TE, TX, TW, 1, 1, TRANS, MODE, false>(p, N, s);
+    if (p.M <= 32) {
+        // (gp of that many pixels has its grad_x in the same launch: back_fits)
+        if constexpr (!(kWide<TI> && !kWide<TO>))
+            if (blocks(1, 2) >= 2 * kCus) return launch_as<TI, TO, TE, TX, TW, 1, 2, TRANS, MODE, false>(p, N, s);
+        return launch_as<TI, TO, TE, TX, TW, 1, 1, TRANS, MODE, false>(p, N, s);
+    }
     if (blocks(2, 2) >= 2 * kCus) return launch_as<TI, TO, TE, TX, TW, 2, 2, TRANS, MODE, false>(p, N, s);
     return launch_as<TI, TO, TE, TX, TW, 2, 1, TRANS, MODE, false>(p, N, s);
 }

@@ -1,7 +1,10 @@
 """Launches of layer norm, the point-wise product and dropout at sizes up to the documented limits: a launch has fewer than 2^32 threads a dimension."""
+import re
+
 import pytest
 
 from tests import launches
+from tests.test_abi_host import kernel_notes, lib  # noqa: F401
 
 OK, SHAPE, UNSUPPORTED = 0, 2, 4
 
@@ -30,6 +33,19 @@ def test_no_launch_has_more_threads_than_there_may_be(program, extent):
         assert status == OK and made or status in ((SHAPE, UNSUPPORTED) if far else (UNSUPPORTED,)) and not made, (call, status, made)
         for l in made:
             assert 0 < l.gx * l.block < 2 ** 32 and 0 < l.gy < 2 ** 16 and l.gz == 1, (call, l)
+
+
+def test_every_built_kernel_is_launched_at_some_size(program, lib):  # noqa: F811
+    built = {k[0] for k in kernel_notes() if re.search("(product|strip|norm|dropout|parts)_(thin_|weights_|back_|any_)*kernel", k[0])}
+    assert len(built) > 230
+    extents = [(1, 3, 3), (1, 30, 30), (1, 64, 64), (1, 100, 130), (1, 130, 257), (2, 301, 255), (3, 150, 301), (5, 50, 61), (20, 31, 33), (700, 8, 8), (3000, 1, 2)]
+    channels = [8, 16, 17, 30, 33, 49, 60, 70, 100, 129, 160, 190, 193, 260, 300, 385, 520, 770, 1100]
+    calls = [(name, dt, N, K, 1, H, W, 0, 0) for name in ("layernorm_forward", "layernorm_backward") for dt in (0, 1) for N, H, W in extents for K in channels]
+    calls += [("dropout_forward", dt, N, K, 1, H, W, over, flag) for dt in (0, 1) for N, H, W in extents for K in (5, 64) for over in (0, 1, 2) for flag in (0, 1)]
+    calls += [(name, dt, N, K, M, H, W, act, flag) for name in ("pointwise_forward", "pointwise_backward") for dt in (0, 1) for N, H, W in extents
+              for K in channels[:-4] for M in (8, 20, 33, 65, 130, 210, 300) for act in (0, 1) for flag in (0, 1)]
+    reached = {l.kernel for _, made in launches.ask(program, calls) for l in made}
+    assert built == reached, (built - reached, reached - built)
 
 
 def test_what_fits_a_card_is_taken(program):
