@@ -3,7 +3,7 @@ import re
 
 import pytest
 
-from tests import launches
+from tests import launches, product_limits
 from tests.test_abi_host import kernel_notes, lib  # noqa: F401
 
 OK, SHAPE, UNSUPPORTED = 0, 2, 4
@@ -55,3 +55,12 @@ def test_what_fits_a_card_is_taken(program):
     assert len(calls) > 200
     for call, (status, _) in zip(calls, launches.ask(program, calls)):
         assert status == OK, call
+
+
+def test_sizes_beyond_32_bit_offsets_go_by_addresses(program):
+    acts = {"none": 0, "gelu": 1, "silu": 2}
+    for dt, K, M, H, W, act, forward, backward in product_limits.CASES:
+        made = launches.ask(program, [(f"pointwise_{d}", dt, 1, K, M, H, W, acts[act], 0) for d in ("forward", "backward")])
+        for (status, all_of), kernels in zip(made, (forward, backward)):
+            names = [l.kernel for l in all_of if "weights" not in l.kernel and "parts" not in l.kernel]
+            assert status == OK and names and all(re.search(kernels, n) for n in names), (dt, K, M, H, W, act, names)

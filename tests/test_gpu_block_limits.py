@@ -1,9 +1,12 @@
 """Layer norm, the point-wise product and their gradients at sizes near the limits of a launch and of 32-bit offsets."""
+import math
+
 import pytest
 import torch
 
 from paper_2503_06671_amd import binding
 from tests import block_reference as ref
+from tests import product_limits
 
 pytestmark = pytest.mark.gpu
 
@@ -81,3 +84,37 @@ def test_products_of_more_blocks_than_a_launch_has(N, H, W, K, M, act):
                         off[m, k] += (e[:, m] * xs[:, k].abs()).sum()
     depth = (N * H * W / 512 / 16 + 64) * 2.0 ** -23
     assert ((got["grad_w"].double() - sums).abs() <= off + (2.0 ** -21 + depth) * size).all()
+
+
+@pytest.mark.parametrize("case", product_limits.CASES, ids=lambda c: "-".join(map(str, c[:6])))
+def test_products_on_either_side_of_32_bit_offsets(case):
+    dt, K, M, H, W, act, _, _ = case
+    dtype = torch.float32 if dt == product_limits.F32 else BF16
+    x, go, res = filled(1, K, H, W, dtype=dtype), filled(1, M, H, W, dtype=dtype, seed=1), filled(1, M, H, W, dtype=dtype, seed=2)
+    w, b = filled(M, K, dtype=torch.float32, seed=3) * K ** -0.5, filled(M, dtype=torch.float32, seed=4)
+    print(f"[case] product of {H} x {W} pixels, {K} to {M} channels, {act}, {dtype}", flush=True)
+    # (guards: nothing is written in front of a result or behind it)
+    room = {n: torch.full((c * H * W + 2048,), 7.0, device="cuda", dtype=dtype) for n, c in (("out", M), ("grad_x", K))}
+    out, gx = room["out"][1024:-1024].view(1, M, H, W), room["grad_x"][1024:-1024].view(1, K, H, W)
+    out.fill_(math.nan), gx.fill_(math.nan)
+    binding.pointwise_forward(x, w, b, act, res, out=out)
+    ws = binding.new_pointwise_backward_workspace(1, K, M, H, W, dtype, act=act)
+    got = binding.pointwise_backward(x, go, w, ws, b, act, grads=dict(grad_x=gx))
+    for n in room:
+        assert (room[n][:1024] == 7).all() and (room[n][-1024:] == 7).all() and torch.isfinite(room[n]).all(), n
+    for y in (0, H // 3, H // 2, H - 2):
+        rows = (slice(None), slice(None), slice(y, y + 2))
+        want = ref.product(x[rows], w, b, act, res[rows], go[rows])
+        ref.check(out[rows], want["out"], "out")
+        ref.check(gx[rows], want["grad_x"], "grad_x")
+    # the weights' gradients, by their 2-norm: terms and slope 2^-20, a share's additions (128 shares at least, six products of terms
+    # for sixteen pixels) and the shares'
+    sums = {"grad_w": 0.0, "grad_b": 0.0}
+    for y in range(0, H, 256):
+        xs, gp = x[0, :, y:y + 256].double().flatten(1), go[0, :, y:y + 256].double().flatten(1)
+        if act != "none":
+            gp = gp * ref.slope(act, w.double() @ xs + b.double()[:, None])
+        sums = {"grad_w": sums["grad_w"] + torch.stack([(gp * row).sum(1) for row in xs], 1), "grad_b": sums["grad_b"] + gp.sum(1)}
+    bar = 2.0 ** -20 + 2.0 ** -23 * math.sqrt(6 * H * W / 16 / 128 + 32)
+    for n, true in sums.items():
+        assert ((got[n].double() - true).norm() / true.norm()).item() < bar, n
