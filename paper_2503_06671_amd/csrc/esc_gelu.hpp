@@ -1,4 +1,4 @@
-// GELU of ConvFFN for gfx950 (MI355X).
+// GELU of ConvFFN and of the point-wise products for gfx950 (MI355X).
 #pragma once
 #include <hip/hip_runtime.h>
 
@@ -14,9 +14,8 @@ namespace esc {
 // A hidden element costs two of these, which is what the vector units of ConvFFN's kernels spend most of
 // their time on.  NaN stays NaN, +inf stays +inf and -inf gives NaN, as 0.5 v (1 + erf(v / sqrt 2)) does (the
 // form max(v, 0) - |v| e would save one instruction and give NaN for both).
-__device__ __forceinline__ float ffn_gelu(float v)
+__device__ __forceinline__ float erfc_root2(float t)   // erfc(t / sqrt 2), t >= 0
 {
-    const float t = fabsf(v);
     float q = fmaf(2.834909764715121e-06f, t, -3.937766086892225e-05f);
     q = fmaf(q, t, 0.0001861801283666864f);
     q = fmaf(q, t, 0.0001369366073049605f);
@@ -24,7 +23,11 @@ __device__ __forceinline__ float ffn_gelu(float v)
     q = fmaf(q, t, 0.052496179938316345f);
     q = fmaf(q, t, 0.4592081904411316f);
     q = fmaf(q, t, 1.1511051654815674f);
-    const float e = __builtin_amdgcn_exp2f(-q * t);
+    return __builtin_amdgcn_exp2f(-q * t);
+}
+__device__ __forceinline__ float ffn_gelu(float v)
+{
+    const float e = erfc_root2(fabsf(v));
     const float h = 0.5f * v;
     return fmaf(fabsf(h), 1.f - e, h);
 }

@@ -9,8 +9,8 @@
 // mantissa bits, the next eight, the rest: exact), a product of two such values the six products of terms whose orders add up to
 // two at most (the rest lies below 2^-21 of it).
 //
-// Which kernel: up to 192 input channels (fp32 160) strip_kernel and strip_back_kernel (esc_product_strip.hip), bound by memory; wider ones product_kernel, bound
-// by the matrix and vector units; few pixels and outputs with many channels product_thin_kernel, bound by latency; grad_w
+// Which kernel: up to 192 input channels (fp32 160) strip_kernel, and for gp and grad_x in one launch up to 128 (fp32 64) strip_back_kernel
+// (esc_product_strip.hip), bound by memory; wider ones product_kernel, bound by the matrix and vector units; few pixels and outputs with many channels product_thin_kernel, bound by latency; grad_w
 // product_weights_kernel.  One MI355X, 16 x 64 x 64, 640 to 1280 channels, gelu, bf16 (107 GFLOP a product): forward 260 us (two products of terms, 830 TFLOP/s
 // of those; 8192^3 in a library 1229), gp 350 (three, 920), grad_x 315 (three, 1020), grad_w 360 (three, 890).
 #include <hip/hip_runtime.h>

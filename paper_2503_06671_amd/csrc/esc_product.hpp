@@ -5,6 +5,7 @@
 #include <math.h>
 #include <stdint.h>
 
+#include "esc_gelu.hpp"
 #include "esc_terms.hpp"
 
 namespace esc {
@@ -69,41 +70,20 @@ __device__ __forceinline__ float widen(T v)
     if constexpr (kWide<T>) return v;
     else return __uint_as_float((uint32_t)v.bits << 16);
 }
-// Two neighbours at any address their type allows.
-template <typename T>
-struct __attribute__((packed, aligned(sizeof(T)))) Two {
-    T a, b;
-};
-
 enum : int { kNone = 0, kGelu = 1, kSilu = 2 };
 
-// e = erfc(|v| / sqrt 2) as 2^-(t P(t)), t = |v| (esc_gelu.hpp has the polynomial's derivation)
-__device__ __forceinline__ float erfc_of(float t)
-{
-    float q = fmaf(2.834909764715121e-06f, t, -3.937766086892225e-05f);
-    q = fmaf(q, t, 0.0001861801283666864f);
-    q = fmaf(q, t, 0.0001369366073049605f);
-    q = fmaf(q, t, -0.0070634204894304276f);
-    q = fmaf(q, t, 0.052496179938316345f);
-    q = fmaf(q, t, 0.4592081904411316f);
-    q = fmaf(q, t, 1.1511051654815674f);
-    return __builtin_amdgcn_exp2f(-q * t);
-}
 __device__ __forceinline__ float sigmoid(float v) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(v * -1.44269504f)); }
 
 __device__ __forceinline__ float activation(int act, float v)
 {
-    if (act == kGelu) {
-        const float h = 0.5f * v;
-        return fmaf(fabsf(h), 1.f - erfc_of(fabsf(v)), h);
-    }
+    if (act == kGelu) return ffn_gelu(v);
     return act == kSilu ? v * sigmoid(v) : v;
 }
 __device__ __forceinline__ float slope(int act, float v)
 {
     if (act == kGelu) {
         // Phi(v) + v phi(v)
-        const float e = 0.5f * erfc_of(fabsf(v));
+        const float e = 0.5f * erfc_root2(fabsf(v));
         return fmaf(v * 0.3989422804f, __builtin_amdgcn_exp2f(v * v * -0.7213475204f), v >= 0.f ? 1.f - e : e);
     }
     if (act == kSilu) {
