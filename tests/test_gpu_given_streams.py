@@ -75,6 +75,20 @@ def test_results_are_of_the_streams_memory(kind):
         assert all(torch.equal(a, b) for a, b in zip(got, want)), name
 
 
+def test_the_default_stream_given():
+    # (its handle is zero)
+    side = torch.cuda.Stream()
+    for name, call in calls().items():
+        want = call(None)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            got = call(torch.cuda.default_stream())
+            assert torch.cuda.current_stream() == side, name
+        assert all(pool_of(t) == 0 for t in got), name
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), name
+
+
 def test_all_work_is_on_the_stream():
     # the current one is busy for some milliseconds: nothing that was asked of the other waits for it, or comes behind it
     all_of = calls()
