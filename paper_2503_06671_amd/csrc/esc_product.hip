@@ -10,9 +10,10 @@
 // two at most (the rest lies below 2^-21 of it).
 //
 // Which kernel: up to 192 input channels (fp32 160) strip_kernel, and for gp and grad_x in one launch up to 128 (fp32 64) strip_back_kernel
-// (esc_product_strip.hip), bound by memory; wider ones product_kernel, bound by the matrix and vector units; few pixels and outputs with many channels product_thin_kernel, bound by latency; grad_w
-// product_weights_kernel.  One MI355X, 16 x 64 x 64, 640 to 1280 channels, gelu, bf16 (107 GFLOP a product): forward 260 us (two products of terms, 830 TFLOP/s
-// of those; 8192^3 in a library 1229), gp 350 (three, 920), grad_x 315 (three, 1020), grad_w 360 (three, 890).
+// (esc_product_strip.hip), bound by memory; wider ones product_kernel, bound by the matrix and vector units; few pixels and outputs with many channels
+// product_thin_kernel, bound by latency; grad_w product_weights_kernel.  One MI355X, 16 x 64 x 64, 640 to 1280 channels, gelu, bf16 (107 GFLOP a
+// product), medians of 80 calls in a row (the first ten of a process are a sixth slower): forward 250 us (two products of terms, 860 TFLOP/s of those;
+// 8192^3 in a library 1229), gp 343 (three, 940), grad_x 311 (three, 1040), grad_w 343 (three, 940).
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -545,9 +546,11 @@ struct Staged {
 
 // A block's tile of grad_w is 64 MT x 64 KT, a wavefront's 32 MT x 32 KT.
 //
-// Products of the first terms have sums of their own, `acc`, those of the others `low`: the matrix unit cuts off what lies far below the sum that it adds to,
-// always downwards, and over the thousands of additions of a long share that leans to one side.  (One sum for all, 31 x 3 gradients over 4096 x 4096 pixels, fp32, normal values: all of
-// them too low, 3.9e-5 of their 2-norm, now 1.3e-6; 1024 x 1024: 2.3e-6, now 3.0e-7.  The times are the same: 16 x 64 x 64 of 640 to 1280 channels 665 and 664 us, bf16 176 both.)
+// Products of the first terms have sums of their own, `acc`, those of the others `low`: the matrix unit cuts off what lies far below the sum that it
+// adds to, always downwards, and over the thousands of additions of a long share that leans to one side.  (One sum for all, 31 x 3 gradients over
+// 4096 x 4096 pixels, fp32, normal values: all of them too low, 3.9e-5 of their 2-norm, now 1.3e-6; 1024 x 1024: 2.3e-6, now 3.0e-7.  The times are the
+// same, both builds in turn: 16 x 64 x 64 of 640 to 1280 channels fp32 666 and 664 us; the whole backward pass of 64 to 128 channels, 64 x 64 x 64,
+// gelu, bf16 101 both.)
 template <typename TG, typename TI, int QG, int QX, int MT, int KT>
 __global__ __launch_bounds__(kThreads, 2) void product_weights_kernel(const WeightParams p)
 {
