@@ -7,8 +7,8 @@
 //
 // What bounds it: memory, for as many channels as the vector units' share (splitting, activation) hides behind.  MI355X, over several cards:
 // 339 x 511, 64 to 64 channels with residual, fp32 23.2 us where the last-level cache holds its inputs, 28 to 32 with others in each call (133 MB, 4.2
-// to 4.8 TB/s); 64 x 64 x 64, 64 to 128, gelu, bf16 forward 29 to 32 (101 MB: one round of blocks, whose reading and writing do not overlap), gp and
-// grad_x 60 to 67 (268 MB, 4.0 to 4.5 TB/s; as two kernels 84); 180 x 320, 192 to 576, bf16 30 to 35 (730 to 850 TFLOP/s of products of terms); a
+// to 4.8 TB/s); 64 x 64 x 64, 64 to 128, gelu, bf16 forward 29 to 34 (101 MB: one round of blocks, whose reading and writing do not overlap), gp and
+// grad_x 60 to 71 (268 MB, 3.8 to 4.5 TB/s; as two kernels 84); 180 x 320, 192 to 576, bf16 30 to 35 (730 to 850 TFLOP/s of products of terms); a
 // kernel that stages both operands in LDS: 57, 97, 290 and 150.
 #include "esc_host.hpp"
 #include "esc_product.hpp"
